@@ -318,6 +318,102 @@ fq_status fq_watchdog_selftest(uint64_t limit_ns, void* stream);
  * last call (and clears the record), else FQ_OK.  *detail (host, may be NULL) gets the raw word. */
 fq_status fq_device_status(uint32_t* detail);
 
+/* ==== operators between the projections of a layer ==================================================
+ * A layer runs  site qkv -> attention (float) -> site o.  The calls below are that middle: head norms with rotary
+ * positions on what the fused qkv projection wrote, a cache of 8-bit keys and values, attention over it, and attention
+ * to an encoder's states.  Forward only, like the rest of this library.  Head h of a row is its channels [h D, (h+1) D).
+ * Statistics, sums and softmax are binary32; one rounding at the store (except where stated).
+ *
+ * ---- rotary frequencies (host) ----------------------------------------------------------------
+ * frequencies host double[rotary_dim / 2], radians per position: f_i = base^(-2i/rotary_dim), then by `scaling`
+ *   FQ_ROPE_PLAIN   as it is;
+ *   FQ_ROPE_LINEAR  f_i / factor (positions interpolated);
+ *   FQ_ROPE_BASE    base * factor^(r/(r-2)) in place of base: the fastest pair keeps its frequency, the slowest is divided by factor;
+ *   FQ_ROPE_PARTS   f_i (k_i + (1 - k_i)/factor), k_i = clamp((turns_i - low_turns)/(high_turns - low_turns), 0, 1) with
+ *                   turns_i = f_i original_length / 2 pi: pairs that turn often within the trained length are kept, slow ones interpolated.
+ * Arguments that a scaling does not use are ignored. */
+typedef enum { FQ_ROPE_PLAIN = 0, FQ_ROPE_LINEAR = 1, FQ_ROPE_BASE = 2, FQ_ROPE_PARTS = 3 } fq_rope_scaling;
+typedef enum { FQ_ROPE_HALF = 0, FQ_ROPE_INTERLEAVED = 1 } fq_rope_layout;
+fq_status fq_rope_frequencies(int rotary_dim, double base, fq_rope_scaling scaling, double factor, double original_length,
+                              double low_turns, double high_turns, double* frequencies);
+
+/* ---- RMS norm of each query and key head, then rotary positions, in one pass --------------------------
+ * qkv device [M, >= (q_heads + k_heads) D] of dtype xt, leading dimension ldx: query heads, then key heads (what follows,
+ *   the value heads, is not read).
+ * q_gain, k_gain device float[D] or NULL: n = x / sqrt(mean(x^2) + eps) * gain; NULL leaves those heads unnormalised.
+ * positions device int32[M], frequencies device double[rotary_dim / 2] (fq_rope_frequencies copied to the device).  The
+ *   angle position * frequency is formed in binary64.  rotary_dim is even and <= D; channels from it on are not rotated.
+ * layout FQ_ROPE_HALF pairs channels (i, i + rotary_dim/2), FQ_ROPE_INTERLEAVED (2i, 2i + 1);
+ *   (a, b) -> amplitude (a cos - b sin, a sin + b cos); amplitude is 1 unless the scaling in use asks for another.
+ * q device [M, q_heads D], k device [M, k_heads D] of dtype yt; either may be the very memory of its heads in qkv (same
+ *   address, leading dimension and dtype), otherwise nothing may overlap.  D a multiple of 8, at most 256. */
+fq_status fq_qk_norm_rope(const void* qkv, fq_dtype xt, int64_t M, int64_t ldx, int q_heads, int k_heads, int head_dim,
+                          const float* q_gain, const float* k_gain, float eps, const int32_t* positions, const double* frequencies,
+                          int rotary_dim, fq_rope_layout layout, float amplitude, void* q, int64_t ldq, void* k, int64_t ldk,
+                          fq_dtype yt, void* stream);
+
+/* ---- paged cache of 8-bit keys and values, one scale for each (page of tokens, head) ----------------------
+ * All device memory is the caller's.  k int8 [pages][heads][page][D]; v int8 [pages][heads][D][page] (tokens innermost: the
+ * order in which the product with the probabilities takes them); k_scale, v_scale float [pages][heads].  A code stands for
+ * code * scale.  page in {16, 32, 64, 128}; D a multiple of 16, at most 256.  A page needs no initialisation.
+ * `table` device int32 [batch][table_width], leading dimension ld_table: the pages of each sequence in order.  An entry
+ * outside [0, pages) is no page: nothing is written there, and its keys are as masked ones.  No page may belong to two
+ * sequences that one call appends to (pages of a shared prefix that nobody appends to may).
+ *
+ * fq_kv8_append: rows offsets[b] .. offsets[b+1] of k and v ([tokens, heads D] of dtype xt) become tokens kv_len[b],
+ * kv_len[b] + 1, .. of sequence b.  offsets device int32[batch + 1], or NULL: tokens / batch each.  kv_len device int32[batch]:
+ * what each sequence held before (it is not changed).  max_new: no sequence gets more (0: unknown); a hint that sizes the launch.
+ * Tokens beyond table_width pages are not written.
+ * Per page, operand and head, with a = max |x| over the page's new tokens, c = a/127 (0 below FLT_MIN) and s the scale of what
+ * the page holds already (0 where the new tokens start it): the scale becomes s' = max(s, c), new codes are x 127/a where
+ * c >= s and else x/s, held codes become code s/s' where s' > s, each the exact quotient rounded to nearest even.  (A held
+ * code loses at most half a step each time its page's scale grows.)  Inputs must be finite. */
+typedef struct {
+    int8_t* k;
+    int8_t* v;
+    float* k_scale;
+    float* v_scale;
+    int64_t pages;
+    int heads;
+    int head_dim;
+    int page;
+} fq_kv8_cache;
+fq_status fq_kv8_append(const void* k, const void* v, fq_dtype xt, int64_t tokens, int64_t ldk, int64_t ldv, const fq_kv8_cache* cache,
+                        const int32_t* table, int64_t ld_table, int64_t table_width, int batch, const int32_t* kv_len,
+                        const int32_t* offsets, int64_t max_new, void* stream);
+
+/* ---- attention over that cache ------------------------------------------------------------------
+ * q device [q_rows, q_heads D] of dtype dt; y likewise, same dtype.  Rows q_offsets[b] .. q_offsets[b+1] are the queries of
+ * sequence b (device int32[batch + 1]; NULL: q_rows / batch each); rows that belong to none are left as they were.
+ * Query head h reads kv head h / (q_heads / heads).  kv_len device int32[batch]: keys of each sequence, those of this
+ * step's tokens included; cut to table_width pages and, where max_kv > 0, to max_kv (which sizes the launch and the workspace).
+ * causal: query i of n sees keys j <= kv_len - n + i, else all.  A query without a key gives zeros.
+ * o = sum_j p_j v_j / sum_j p_j, p_j = exp(scale (q . k_j) - max).  bf16 queries are multiplied as binary16 after
+ * a power of two per row has been taken out (exact but for channels 2^-14 below the row's largest), probabilities as binary16
+ * (11 bits), sums in binary32.  max_q: no sequence has more queries (0: unknown); a hint.
+ * workspace device, fq_attention_kv8_workspace_bytes(..) bytes (ragged: q_offsets is given), 256-byte aligned, scratch;
+ * NULL where that is 0. */
+fq_status fq_attention_kv8(const void* q, fq_dtype dt, int64_t q_rows, int64_t ldq, int q_heads, const fq_kv8_cache* cache,
+                           const int32_t* table, int64_t ld_table, int64_t table_width, int batch, const int32_t* kv_len,
+                           const int32_t* q_offsets, int64_t max_q, int64_t max_kv, int causal, float scale, void* y, int64_t ldy,
+                           void* workspace, size_t ws_bytes, void* stream);
+size_t fq_attention_kv8_workspace_bytes(fq_dtype dt, int64_t q_rows, int q_heads, const fq_kv8_cache* cache, int64_t table_width,
+                                        int batch, int ragged, int64_t max_q, int64_t max_kv);
+
+/* ---- cross attention: queries to an encoder's keys and values of another length -----------------------------
+ * q, y as above.  k, v device [kv_rows, kv_heads D] of dtype dt, leading dimensions ldk, ldv (halves of one fused projection
+ * will do).  Rows kv_offsets[b] .. kv_offsets[b+1] belong to sequence b (NULL: kv_rows / batch each: a padded batch); of them
+ * the first kv_len[b] are keys (NULL: all), and of those the ones whose key_mask byte is not 0 (device uint8[kv_rows], NULL:
+ * all).  What masked rows hold does not matter, infinities and NaN included.  A query without a key gives zeros.
+ * No causal order.  D a multiple of 16, at most 256.  max_q, max_kv: as above (0: unknown; sequences are cut to max_kv keys).
+ * bf16: the probabilities are rounded to bf16 ahead of the product with v; sums in binary32. */
+fq_status fq_cross_attention(const void* q, fq_dtype dt, int64_t q_rows, int64_t ldq, int q_heads, const void* k, const void* v,
+                             int64_t kv_rows, int64_t ldk, int64_t ldv, int kv_heads, int head_dim, int batch, const int32_t* q_offsets,
+                             const int32_t* kv_offsets, const int32_t* kv_len, const uint8_t* key_mask, int64_t max_q, int64_t max_kv,
+                             float scale, void* y, int64_t ldy, void* workspace, size_t ws_bytes, void* stream);
+size_t fq_cross_attention_workspace_bytes(fq_dtype dt, int64_t q_rows, int q_heads, int64_t kv_rows, int kv_heads, int head_dim,
+                                          int batch, int ragged_q, int ragged_kv, int64_t max_q, int64_t max_kv);
+
 #ifdef __cplusplus
 }
 #endif

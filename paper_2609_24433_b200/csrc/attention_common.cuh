@@ -1,0 +1,106 @@
+// What the attention kernels share: where a sequence's queries and keys are, how far a tile's rows see.
+#pragma once
+
+#include "fq_common.cuh"
+#include "layer_common.cuh"
+#include "ptx_sm100.cuh"
+
+namespace fq {
+
+inline int64_t row_tiles(const Attention& a) {
+    const int64_t n = (a.max_q * a.group + a.tile_rows - 1) / a.tile_rows;
+    return n < 1 ? 1 : n > 0x7fffffff ? 0x7fffffff : n;
+}
+cudaError_t launch_attention_simt(const Attention& a, cudaStream_t stream);
+cudaError_t launch_attention_join(const Attention& a, cudaStream_t stream);
+
+#ifdef __CUDACC__
+namespace {
+
+struct Sequence {
+    int64_t q0, queries;                // rows of its queries
+    int64_t k0, keys;                   // rows of its keys (cached: k0 unused)
+};
+__device__ __forceinline__ Sequence sequence_of(const Attention& a, int b) {
+    Sequence s;
+    sequence_rows(a.q_offsets, b, a.batch, a.q_rows, &s.q0, &s.queries);
+    s.k0 = 0;
+    s.keys = a.max_kv;
+    if (!a.cached) {
+        int64_t n;
+        sequence_rows(a.kv_offsets, b, a.batch, a.kv_rows, &s.k0, &n);
+        s.keys = min(s.keys, n);
+    }
+    if (a.kv_len) s.keys = min(s.keys, max((int64_t)a.kv_len[b], (int64_t)0));
+    return s;
+}
+// The last key that a row -- (token, head of the group) -- sees, -1 for none.
+__device__ __forceinline__ int64_t row_limit(const Attention& a, const Sequence& s, int64_t row) {
+    return a.causal ? s.keys - s.queries + row / a.group : s.keys - 1;
+}
+// Keys that the rows of a tile see, and the chunks that they lie in (at least one, which then writes the zeros).
+struct TileKeys {
+    int64_t end;
+    int chunks;
+};
+__device__ __forceinline__ TileKeys tile_keys(const Attention& a, const Sequence& s, int64_t tile, int tile_rows) {
+    TileKeys t;
+    const int64_t last = min((tile + 1) * tile_rows, s.queries * a.group) - 1;
+    t.end = max(min(s.keys, row_limit(a, s, last) + 1), (int64_t)0);
+    t.chunks = max((int)((t.end + a.chunk - 1) / a.chunk), 1);
+    return t;
+}
+
+struct KeyPlace {
+    bool valid;
+    int64_t row;                        // of the keys, or page * kv_heads + head
+    int offset;                         // in the page
+};
+// Key j of sequence b (j < end where it may be read at all).
+template <bool CACHED>
+__device__ __forceinline__ KeyPlace key_place(const Attention& a, const Sequence& s, int b, int hk, int64_t j, int64_t end) {
+    KeyPlace p;
+    p.valid = j < end;
+    p.row = 0;
+    p.offset = 0;
+    if (!p.valid) return p;
+    if (CACHED) {
+        const int64_t id = a.table[b * a.ld_table + j / a.cache.page];
+        p.valid = id >= 0 && id < a.cache.pages;
+        p.row = id * a.kv_heads + hk;
+        p.offset = (int)(j % a.cache.page);
+    } else {
+        p.row = s.k0 + j;
+        p.valid = !a.key_mask || a.key_mask[p.row] != 0;
+    }
+    return p;
+}
+
+__device__ __forceinline__ float4 load4(const float* p) { return ld_global_f4(p); }
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+    uint32_t x, y;
+    asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "l"(p));
+    return make_float4(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u), __uint_as_float(y << 16), __uint_as_float(y & 0xffff0000u));
+}
+__device__ __forceinline__ float load1(const float* p) { return ld_global_f32(p); }
+__device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __uint_as_float(ld_global_u16(p) << 16); }
+__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+template <typename T, bool CACHED>
+__device__ __forceinline__ float4 load_key4(const Attention& a, const KeyPlace& p, int hk, int d) {
+    if (!CACHED) return load4(static_cast<const T*>(a.k) + p.row * a.ldk + (int64_t)hk * a.head_dim + d);
+    const uint32_t w = ld_global_u32(a.cache.k + (p.row * a.cache.page + p.offset) * a.head_dim + d);
+    const float f = ld_global_f32(a.cache.k_scale + p.row);
+    return make_float4((float)(int8_t)w * f, (float)(int8_t)(w >> 8) * f, (float)(int8_t)(w >> 16) * f, (float)(int8_t)(w >> 24) * f);
+}
+template <typename T, bool CACHED>
+__device__ __forceinline__ float load_value(const Attention& a, const KeyPlace& p, int hk, int d) {
+    if (!CACHED) return load1(static_cast<const T*>(a.v) + p.row * a.ldv + (int64_t)hk * a.head_dim + d);
+    return (float)a.cache.v[(p.row * a.head_dim + d) * a.cache.page + p.offset] * ld_global_f32(a.cache.v_scale + p.row);
+}
+
+}  // namespace
+#endif
+
+}  // namespace fq

@@ -13,6 +13,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
@@ -304,9 +305,234 @@ PyObject* linear_w4a16(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- the operators between a layer's projections ----
+// A tensor that the kernels of the current device and stream read or write.
+const at::Tensor& on_device(const at::Tensor& t, const char* what) {
+    if (!t.is_cuda() || t.device().index() != c10::cuda::current_device()) {
+        PyErr_Format(PyExc_ValueError, "%s has to be on the current CUDA device", what);
+        throw Refused();
+    }
+    return t;
+}
+const at::Tensor& vector_of(PyObject* o, at::ScalarType type, int64_t size, const char* what) {
+    const at::Tensor& t = on_device(tensor(o), what);
+    if (t.scalar_type() != type || t.dim() != 1 || !t.is_contiguous() || t.size(0) != size) {
+        PyErr_Format(PyExc_ValueError, "%s has to be a contiguous %s tensor of %lld elements", what, at::toString(type), (long long)size);
+        throw Refused();
+    }
+    return t;
+}
+template <typename T>
+T* data_or_null(PyObject* o, at::ScalarType type, int64_t size, const char* what) {
+    return none(o) ? nullptr : static_cast<T*>(vector_of(o, type, size, what).data_ptr());
+}
+const at::Tensor& rows_of(PyObject* o, int64_t width, const char* what) {
+    const at::Tensor& t = on_device(rowmajor(o), what);
+    if (t.size(1) != width) {
+        PyErr_Format(PyExc_ValueError, "%s has to have %lld columns, got %lld", what, (long long)width, (long long)t.size(1));
+        throw Refused();
+    }
+    return t;
+}
+// (the stride between the rows of a matrix of one row is whatever a view left there)
+int64_t pitch(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : (t.size(1) + 7) / 8 * 8; }
+
+struct RowsOut {
+    at::Tensor t;
+    RowsOut(PyObject* given, int64_t rows, int64_t width, at::ScalarType type, const char* what) {
+        if (none(given)) return;
+        t = rows_of(given, width, what);
+        if (t.size(0) != rows || t.scalar_type() != type) {
+            PyErr_Format(PyExc_ValueError, "%s has to have %lld rows of %s", what, (long long)rows, at::toString(type));
+            throw Refused();
+        }
+    }
+    void make(int64_t rows, int64_t width, at::ScalarType type, const at::Tensor& like) {
+        if (!t.defined()) t = fresh({rows, width}, type, like);
+    }
+};
+
+// qk_norm_rope(qkv, q_heads, k_heads, head_dim, positions, frequencies, q_gain, k_gain, eps, layout, amplitude, out_dtype, q, k) -> (q, k)
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 14);
+        const at::Tensor& x = on_device(rowmajor(a[0]), "qkv");
+        const int64_t q_heads = integer(a[1]), k_heads = integer(a[2]), D = integer(a[3]), M = x.size(0);
+        if (q_heads < 0 || k_heads < 0 || D < 1 || q_heads > 32767 || k_heads > 32767 || D > 256) return status(q_heads < 0 || k_heads < 0 || D < 1 ? FQ_ERR_INVALID_ARG : FQ_ERR_UNSUPPORTED);
+        if (x.size(1) < (q_heads + k_heads) * D) return status(FQ_ERR_INVALID_ARG);
+        const int32_t* positions = static_cast<int32_t*>(vector_of(a[4], at::kInt, M, "positions").data_ptr());
+        const at::Tensor& freq = tensor(a[5]);
+        const int64_t half = freq.dim() == 1 ? freq.size(0) : 0;
+        const double* frequencies = static_cast<double*>(vector_of(a[5], at::kDouble, half, "frequencies").data_ptr());
+        const float* q_gain = data_or_null<float>(a[6], at::kFloat, D, "q_gain");
+        const float* k_gain = data_or_null<float>(a[7], at::kFloat, D, "k_gain");
+        const float eps = real(a[8]), amplitude = real(a[10]);
+        const long long layout = integer(a[9]);
+        if (layout != FQ_ROPE_HALF && layout != FQ_ROPE_INTERLEAVED) return status(FQ_ERR_INVALID_ARG);
+        const fq_dtype xt = dtype_of(x.scalar_type());
+        at::ScalarType type = x.scalar_type();
+        if (!none(a[11])) {
+            if (!THPDtype_Check(a[11])) {
+                PyErr_SetString(PyExc_TypeError, "out_dtype has to be a torch.dtype");
+                throw Refused();
+            }
+            type = reinterpret_cast<THPDtype*>(a[11])->scalar_type;
+        } else if (!none(a[12])) {
+            type = tensor(a[12]).scalar_type();
+        }
+        const fq_dtype yt = dtype_of(type);
+        RowsOut q(a[12], M, q_heads * D, type, "q"), k(a[13], M, k_heads * D, type, "k");
+        fq_status s;
+        {
+            const Unlocked nogil;
+            q.make(M, q_heads * D, type, x);
+            k.make(M, k_heads * D, type, x);
+            s = fq_qk_norm_rope(x.data_ptr(), xt, M, pitch(x), (int)q_heads, (int)k_heads, (int)D, q_gain, k_gain, eps, positions, frequencies,
+                                (int)(2 * half), static_cast<fq_rope_layout>(layout), amplitude, q.t.data_ptr(), pitch(q.t), k.t.data_ptr(), pitch(k.t),
+                                yt, stream());
+        }
+        return s == FQ_OK ? pair(std::move(q.t), std::move(k.t)) : status(s);
+    });
+}
+
+// The tensors of a cache, (k, v, k_scale, v_scale), checked when the Python object was made.
+fq_kv8_cache cache_of(PyObject* const* a) {
+    const at::Tensor &k = on_device(tensor(a[0]), "the cache"), &v = on_device(tensor(a[1]), "the cache");
+    const at::Tensor &ks = on_device(tensor(a[2]), "the cache"), &vs = on_device(tensor(a[3]), "the cache");
+    fq_kv8_cache c = {};
+    c.k = static_cast<int8_t*>(k.data_ptr());
+    c.v = static_cast<int8_t*>(v.data_ptr());
+    c.k_scale = static_cast<float*>(ks.data_ptr());
+    c.v_scale = static_cast<float*>(vs.data_ptr());
+    c.pages = k.size(0);
+    c.heads = (int)k.size(1);
+    c.page = (int)k.size(2);
+    c.head_dim = (int)k.size(3);
+    return c;
+}
+struct Table {
+    const int32_t* p;
+    int64_t ld, width;
+    int batch;
+    explicit Table(PyObject* o) {
+        const at::Tensor& t = on_device(rowmajor(o), "the page table");
+        if (t.scalar_type() != at::kInt || t.size(0) > 0x7fffffff) {
+            PyErr_SetString(PyExc_ValueError, "the page table has to be int32");
+            throw Refused();
+        }
+        p = static_cast<int32_t*>(t.data_ptr());
+        width = t.size(1);
+        ld = t.size(0) > 1 ? t.stride(0) : width;
+        batch = (int)t.size(0);
+    }
+};
+
+// kv8_append(k, v, cache k, v, k_scale, v_scale, table, kv_len, offsets, max_new) -> None
+PyObject* kv8_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 10);
+        const fq_kv8_cache cache = cache_of(a + 2);
+        const int64_t width = (int64_t)cache.heads * cache.head_dim;
+        const at::Tensor &k = rows_of(a[0], width, "k"), &v = rows_of(a[1], width, "v");
+        if (v.size(0) != k.size(0) || v.scalar_type() != k.scalar_type()) {
+            PyErr_SetString(PyExc_ValueError, "k and v have to have the same rows and dtype");
+            throw Refused();
+        }
+        const fq_dtype xt = dtype_of(k.scalar_type());
+        const Table t(a[6]);
+        const int32_t* kv_len = static_cast<int32_t*>(vector_of(a[7], at::kInt, t.batch, "kv_len").data_ptr());
+        const int32_t* offsets = data_or_null<int32_t>(a[8], at::kInt, (int64_t)t.batch + 1, "offsets");
+        const int64_t max_new = integer(a[9]);
+        fq_status s;
+        {
+            const Unlocked nogil;
+            s = fq_kv8_append(k.data_ptr(), v.data_ptr(), xt, k.size(0), pitch(k), pitch(v), &cache, t.p, t.ld, t.width, t.batch, kv_len, offsets, max_new, stream());
+        }
+        if (s != FQ_OK) return status(s);
+        Py_RETURN_NONE;
+    });
+}
+
+// attention_kv8(q, q_heads, cache k, v, k_scale, v_scale, table, kv_len, offsets, max_q, max_kv, causal, scale, y, workspace)
+PyObject* attention_kv8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 15);
+        const int64_t q_heads = integer(a[1]);
+        const fq_kv8_cache cache = cache_of(a + 2);
+        if (q_heads < 1 || q_heads > 65535) return status(q_heads < 1 ? FQ_ERR_INVALID_ARG : FQ_ERR_UNSUPPORTED);
+        const int64_t width = q_heads * cache.head_dim;
+        const at::Tensor& q = rows_of(a[0], width, "q");
+        const fq_dtype dt = dtype_of(q.scalar_type());
+        const Table t(a[6]);
+        const int32_t* kv_len = static_cast<int32_t*>(vector_of(a[7], at::kInt, t.batch, "kv_len").data_ptr());
+        const int32_t* offsets = data_or_null<int32_t>(a[8], at::kInt, (int64_t)t.batch + 1, "offsets");
+        const int64_t max_q = integer(a[9]), max_kv = integer(a[10]);
+        const int causal = integer(a[11]) != 0;
+        const float scale = real(a[12]);
+        RowsOut y(a[13], q.size(0), width, q.scalar_type(), "y");
+        if (!none(a[14])) on_device(tensor(a[14]), "the workspace");
+        Workspace ws(a[14]);
+        fq_status s;
+        {
+            const Unlocked nogil;
+            y.make(q.size(0), width, q.scalar_type(), q);
+            ws.make([&] { return fq_attention_kv8_workspace_bytes(dt, q.size(0), (int)q_heads, &cache, t.width, t.batch, offsets != nullptr, max_q, max_kv); }, q);
+            s = fq_attention_kv8(q.data_ptr(), dt, q.size(0), pitch(q), (int)q_heads, &cache, t.p, t.ld, t.width, t.batch, kv_len, offsets, max_q, max_kv,
+                                 causal, scale, y.t.data_ptr(), pitch(y.t), ws.p, ws.bytes, stream());
+        }
+        return s == FQ_OK ? THPVariable_Wrap(std::move(y.t)) : status(s);
+    });
+}
+
+// cross_attention(q, k, v, q_heads, kv_heads, batch, q_offsets, kv_offsets, kv_len, key_mask, max_q, max_kv, scale, y, workspace)
+PyObject* cross_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 15);
+        const int64_t q_heads = integer(a[3]), kv_heads = integer(a[4]), batch = integer(a[5]);
+        if (q_heads < 1 || kv_heads < 1 || batch < 0) return status(FQ_ERR_INVALID_ARG);
+        if (q_heads > 65535 || kv_heads > 65535 || batch > 65535) return status(FQ_ERR_UNSUPPORTED);
+        const at::Tensor& q = on_device(rowmajor(a[0]), "q");
+        const int64_t width = q.size(1), D = width / q_heads;
+        if (D * q_heads != width) return status(FQ_ERR_INVALID_ARG);
+        const at::Tensor &k = rows_of(a[1], kv_heads * D, "k"), &v = rows_of(a[2], kv_heads * D, "v");
+        if (v.size(0) != k.size(0) || k.scalar_type() != q.scalar_type() || v.scalar_type() != q.scalar_type()) {
+            PyErr_SetString(PyExc_ValueError, "k and v have to have the same rows, and the dtype of q");
+            throw Refused();
+        }
+        const fq_dtype dt = dtype_of(q.scalar_type());
+        const int32_t* q_offsets = data_or_null<int32_t>(a[6], at::kInt, batch + 1, "q_offsets");
+        const int32_t* kv_offsets = data_or_null<int32_t>(a[7], at::kInt, batch + 1, "kv_offsets");
+        const int32_t* kv_len = data_or_null<int32_t>(a[8], at::kInt, batch, "kv_len");
+        const uint8_t* mask = nullptr;
+        if (!none(a[9])) {
+            const at::Tensor& m = on_device(tensor(a[9]), "key_mask");
+            if ((m.scalar_type() != at::kBool && m.scalar_type() != at::kByte) || !m.is_contiguous() || m.numel() != k.size(0)) {
+                PyErr_SetString(PyExc_ValueError, "key_mask has to be a contiguous bool or uint8 tensor with an element for each row of k");
+                throw Refused();
+            }
+            mask = static_cast<const uint8_t*>(m.data_ptr());
+        }
+        const int64_t max_q = integer(a[10]), max_kv = integer(a[11]);
+        const float scale = real(a[12]);
+        RowsOut y(a[13], q.size(0), width, q.scalar_type(), "y");
+        if (!none(a[14])) on_device(tensor(a[14]), "the workspace");
+        Workspace ws(a[14]);
+        fq_status s;
+        {
+            const Unlocked nogil;
+            y.make(q.size(0), width, q.scalar_type(), q);
+            ws.make([&] { return fq_cross_attention_workspace_bytes(dt, q.size(0), (int)q_heads, k.size(0), (int)kv_heads, (int)D, (int)batch, q_offsets != nullptr, kv_offsets != nullptr, max_q, max_kv); }, q);
+            s = fq_cross_attention(q.data_ptr(), dt, q.size(0), pitch(q), (int)q_heads, k.data_ptr(), v.data_ptr(), k.size(0), pitch(k), pitch(v), (int)kv_heads,
+                                   (int)D, (int)batch, q_offsets, kv_offsets, kv_len, mask, max_q, max_kv, scale, y.t.data_ptr(), pitch(y.t), ws.p, ws.bytes, stream());
+        }
+        return s == FQ_OK ? THPVariable_Wrap(std::move(y.t)) : status(s);
+    });
+}
+
 #define FQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FQ_METHOD(linear), FQ_METHOD(linear_gated), FQ_METHOD(gemm), FQ_METHOD(quantize_act), FQ_METHOD(quantize_act_composite),
-                         FQ_METHOD(linear_w4a16), {nullptr, nullptr, 0, nullptr}};
+                         FQ_METHOD(linear_w4a16), FQ_METHOD(qk_norm_rope), FQ_METHOD(kv8_append),
+                         FQ_METHOD(attention_kv8), FQ_METHOD(cross_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -31,6 +31,8 @@ EXPORTS = [
     "fq_weights_set_multiplier", "fq_weights_scale_outputs", "fq_linear_w4a16",
     "fq_fold_weights_composite", "fq_quantize_act_composite", "fq_weights_composite", "fq_fold_weights_gptq",
     "fq_quantize_act_gated", "fq_linear_gated", "fq_watchdog_selftest",
+    "fq_rope_frequencies", "fq_qk_norm_rope", "fq_kv8_append", "fq_attention_kv8", "fq_attention_kv8_workspace_bytes",
+    "fq_cross_attention", "fq_cross_attention_workspace_bytes",
 ]
 
 _lib = None
@@ -61,6 +63,13 @@ def lib() -> ctypes.CDLL:
         L.fq_weights_composite.argtypes = [ctypes.c_void_p]
         L.fq_workspace_bytes.restype = ctypes.c_size_t
         L.fq_workspace_bytes.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int]
+        L.fq_attention_kv8_workspace_bytes.restype = ctypes.c_size_t
+        L.fq_attention_kv8_workspace_bytes.argtypes = [ctypes.c_int, ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_int64,
+                                                       ctypes.c_int, ctypes.c_int, ctypes.c_int64, ctypes.c_int64]
+        L.fq_cross_attention_workspace_bytes.restype = ctypes.c_size_t
+        L.fq_cross_attention_workspace_bytes.argtypes = [ctypes.c_int, ctypes.c_int64, ctypes.c_int, ctypes.c_int64, ctypes.c_int,
+                                                         ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int64,
+                                                         ctypes.c_int64]
         _lib = L
     return _lib
 
@@ -365,6 +374,87 @@ def linear_w4a16(x, W: Weights, out_dtype=torch.float32, y=None):
 def linear(x, W: Weights, clip_ratio: float = 1.0, out_dtype=torch.float32, y=None, workspace=None):
     """Dispatch on the handle's bit width (the two entry points differ in nothing else)."""
     return (linear_w4a4 if W.bits == 4 else linear_w8a8)(x, W, clip_ratio, out_dtype, y, workspace)
+
+
+# ---- the operators between the projections of a layer ------------------------------------------------
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_PARTS = 0, 1, 2, 3
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+
+
+def rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: int = ROPE_PLAIN, factor: float = 1.0,
+                     original_length: float = 0.0, low_turns: float = 1.0, high_turns: float = 4.0, device=None) -> torch.Tensor:
+    """Rotary frequencies, float64[rotary_dim / 2] in radians per position, computed on the host and put on ``device``
+    (None: the current CUDA device); ``scaling`` stretches them for contexts longer than the trained ones."""
+    out = torch.empty(max(0, rotary_dim) // 2, dtype=torch.float64)
+    d = ctypes.c_double
+    _check(lib().fq_rope_frequencies(ctypes.c_int(rotary_dim), d(base), ctypes.c_int(scaling), d(factor), d(original_length),
+                                     d(low_turns), d(high_turns), _ptr(out)), "fq_rope_frequencies")
+    return out.to(torch.device("cuda", torch.cuda.current_device()) if device is None else device)
+
+
+def qk_norm_rope(qkv: torch.Tensor, q_heads: int, k_heads: int, head_dim: int, positions: torch.Tensor, frequencies: torch.Tensor,
+                 q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 layout: int = ROPE_HALF, amplitude: float = 1.0, out_dtype=None, q=None, k=None):
+    """RMS norm of each query and key head (those with a gain), then rotary positions: (q, k) of the fused projection's output.
+    ``frequencies``: float64[rotary_dim / 2] on the device; channels from rotary_dim on are not rotated."""
+    return _result(_native().qk_norm_rope(qkv, q_heads, k_heads, head_dim, positions, frequencies, q_gain, k_gain, eps, layout,
+                                          amplitude, out_dtype, q, k), "fq_qk_norm_rope")
+
+
+class KV8Cache:
+    """Pages of 8-bit keys and values with one scale for each page and head: k int8 [pages, heads, page, head_dim],
+    v int8 [pages, heads, head_dim, page], k_scale and v_scale float32 [pages, heads], all contiguous on one device."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        if k.dim() != 4:
+            raise ValueError("k has to be [pages, heads, page, head_dim]")
+        self.pages, self.heads, self.page, self.head_dim = k.shape
+        for name, t, dtype, shape in (("k", k, torch.int8, k.shape),
+                                      ("v", v, torch.int8, (self.pages, self.heads, self.head_dim, self.page)),
+                                      ("k_scale", k_scale, torch.float32, (self.pages, self.heads)),
+                                      ("v_scale", v_scale, torch.float32, (self.pages, self.heads))):
+            if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != k.device:
+                raise ValueError(f"{name} has to be a contiguous {dtype} tensor of shape {tuple(shape)} on {k.device}")
+        self.tensors = (k, v, k_scale, v_scale)
+        self.k, self.v, self.k_scale, self.v_scale = self.tensors
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, head_dim: int, page: int = 64, device=None) -> "KV8Cache":
+        """A cache of new device memory, uninitialised: a page is written before it is read."""
+        dev = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+        return cls(torch.empty((pages, heads, page, head_dim), dtype=torch.int8, device=dev),
+                   torch.empty((pages, heads, head_dim, page), dtype=torch.int8, device=dev),
+                   torch.empty((pages, heads), dtype=torch.float32, device=dev),
+                   torch.empty((pages, heads), dtype=torch.float32, device=dev))
+
+
+def kv8_append(k: torch.Tensor, v: torch.Tensor, cache: KV8Cache, table: torch.Tensor, kv_len: torch.Tensor,
+               offsets: Optional[torch.Tensor] = None, max_new: int = 0) -> None:
+    """Write the rows of k and v behind what each sequence holds (``kv_len``, which stays as it is)."""
+    _result(_native().kv8_append(k, v, *cache.tensors, table, kv_len, offsets, max_new), "fq_kv8_append")
+
+
+def _scale(scale: Optional[float], head_dim: int) -> float:
+    return head_dim ** -0.5 if scale is None else scale
+
+
+def attention_kv8(q: torch.Tensor, q_heads: int, cache: KV8Cache, table: torch.Tensor, kv_len: torch.Tensor,
+                  offsets: Optional[torch.Tensor] = None, max_q: int = 0, max_kv: int = 0, causal: bool = True,
+                  scale: Optional[float] = None, y=None, workspace=None):
+    """Attention of the rows of q over the pages of their sequences; ``kv_len`` counts this step's tokens in."""
+    return _result(_native().attention_kv8(q, q_heads, *cache.tensors, table, kv_len, offsets, max_q, max_kv, 1 if causal else 0,
+                                           _scale(scale, cache.head_dim), y, workspace), "fq_attention_kv8")
+
+
+def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_heads: int, kv_heads: int, batch: int,
+                    q_offsets: Optional[torch.Tensor] = None, kv_offsets: Optional[torch.Tensor] = None,
+                    kv_len: Optional[torch.Tensor] = None, key_mask: Optional[torch.Tensor] = None, max_q: int = 0, max_kv: int = 0,
+                    scale: Optional[float] = None, y=None, workspace=None):
+    """Attention of the rows of q to an encoder's rows of k and v, padded to one length per sequence or packed by offsets."""
+    if q.dim() == 2 and q_heads > 0 and q.shape[1] >= q_heads:
+        scale = _scale(scale, q.shape[1] // q_heads)
+    return _result(_native().cross_attention(q, k, v, q_heads, kv_heads, batch, q_offsets, kv_offsets, kv_len, key_mask, max_q, max_kv,
+                                             1.0 if scale is None else scale, y, workspace), "fq_cross_attention")
 
 
 def gemm_acc_i32(a_codes, W: Weights, workspace=None) -> torch.Tensor:
