@@ -11,6 +11,7 @@ inline int64_t row_tiles(const Attention& a) {
     const int64_t n = (a.max_q * a.group + a.tile_rows - 1) / a.tile_rows;
     return n < 1 ? 1 : n > 0x7fffffff ? 0x7fffffff : n;
 }
+cudaError_t launch_attention_tokens(const Attention& a, cudaStream_t stream);
 cudaError_t launch_attention_simt(const Attention& a, cudaStream_t stream);
 cudaError_t launch_attention_join(const Attention& a, cudaStream_t stream);
 
@@ -86,6 +87,9 @@ __device__ __forceinline__ float load1(const float* p) { return ld_global_f32(p)
 __device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __uint_as_float(ld_global_u16(p) << 16); }
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+__device__ __forceinline__ void store4(float* p, float x, float y, float z, float w) { *reinterpret_cast<float4*>(p) = make_float4(x, y, z, w); }
+__device__ __forceinline__ void store4(__nv_bfloat16* p, float x, float y, float z, float w) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x, y), pack_bf16(z, w)); }
 
 template <typename T, bool CACHED>
 __device__ __forceinline__ float4 load_key4(const Attention& a, const KeyPlace& p, int hk, int d) {

@@ -1,0 +1,401 @@
+// Attention of a few queries -- at most 16 (token, head of a group) rows a kv head, a decoding step -- over the 8-bit cache.
+//
+// Bound by the cache's bytes, so everything serves the loads: no thread waits for another on the way from memory to the
+// matrix instructions.  Each lane copies (cp.async, 16 bytes) exactly the bytes that it will multiply into slots of its own,
+// three half tiles deep, and waits for nothing but its own copies: no barrier until the end of a chunk.
+//
+// The products run transposed, S^T = K Q^T and O^T = V^T P^T: the cache's operand then fills the 16 rows of a warp-level MMA
+// (m16n8k16, binary16 in, binary32 out) and the few queries its 8 columns, with no row idle at one query of a group of eight.
+// Codes become binary16 exactly: byte permutes put (code + 128) under the exponent of 1024, one packed subtraction takes
+// 1152 off.  The order in which an MMA walks channels (of S) and tokens (of O) is free as long as both operands use it, so a
+// lane's 16 contiguous bytes are four steps of it: k16 step i of a 64-wide line takes bytes 16 t + 4 i .. + 3 of thread t of
+// four.  Queries are divided by the power of two below their row's largest channel and rounded to binary16 (bf16 values
+// keep all their bits above 2^-14 of the row's largest channel; binary32 queries and probabilities go as a sum of two terms).
+//
+// With p = 2^(s - m): l = sum p, O = sum (p vs 2^(14 - e)) code, e the running exponent of the largest value scale vs.  The factor
+// 2^14 keeps probabilities down to 2^-28 among binary16's normal numbers.
+#include "attention_common.cuh"
+
+#include <cuda_fp16.h>
+
+namespace fq {
+namespace {
+
+constexpr int kTile = 64;               // tokens
+constexpr int kSlots = 3;
+
+template <int DP>
+struct Shape {
+    static constexpr int kWarps = DP == 256 ? 2 : 4;
+    static constexpr int kUnits = DP / 8;                       // 16-byte units per lane and half tile
+    static constexpr int kSlotBytes = kUnits * 512;             // per warp
+    static constexpr int kRing = kWarps * kSlots * kSlotBytes;
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {        // zeros where !ok
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ uint4 lds_v4(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+// Four int8 -> two pairs of binary16.
+__device__ __forceinline__ void widen(uint32_t w, uint32_t* lo, uint32_t* hi) {
+    const uint32_t u = w ^ 0x80808080u;
+    const __half2 base = __half2half2(__ushort_as_half(0x6480));
+    const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), base), y = __hsub2(*reinterpret_cast<const __half2*>(&b), base);
+    *lo = *reinterpret_cast<const uint32_t*>(&x);
+    *hi = *reinterpret_cast<const uint32_t*>(&y);
+}
+__device__ __forceinline__ void mma(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float2 unpack_half(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+__device__ __forceinline__ uint32_t transpose8(uint32_t w) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255) - 127; }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+
+template <typename T, int DP, int NQ>
+__global__ void __launch_bounds__(Shape<DP>::kWarps * 32) attention_tokens_kernel(const Attention a) {
+    using S = Shape<DP>;
+    constexpr int kTerms = sizeof(T) == 4 ? 2 : 1;              // binary16 terms of a query or probability
+    constexpr int kLines = DP / 64;                             // 64-channel lines of a key
+    constexpr int kRows = 8 * NQ;
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+    griddep_wait();
+    const int b = blockIdx.z / a.kv_heads, hk = blockIdx.z % a.kv_heads, chunk = blockIdx.y;
+    const Sequence s = sequence_of(a, b);
+    const int D = a.head_dim, P = a.cache.page;
+    const int32_t* table = a.table + b * a.ld_table;
+    const uint32_t ring = smem_u32(smem) + warp * (kSlots * S::kSlotBytes) + lane * 16;
+
+    for (int64_t tile = blockIdx.x; tile * kRows < s.queries * a.group; tile += gridDim.x) {
+        const TileKeys tk = tile_keys(a, s, tile, kRows);
+        const int64_t k0 = (int64_t)chunk * a.chunk;
+        if (chunk > 0 && k0 >= tk.end) continue;
+        const int64_t k1 = min(tk.end, k0 + a.chunk);
+        const int tiles = (int)((k1 - k0 + kTile - 1) / kTile);
+        const int mine = tiles > warp ? (tiles - warp + S::kWarps - 1) / S::kWarps : 0;
+
+        // ---- pages: a lane looks up the one of tokens 16 (lane % 4) .. of a tile, -1 where there is none
+        auto page_of = [&](int n) -> int32_t {
+            const int64_t j = k0 + (int64_t)(warp + n * S::kWarps) * kTile + 16 * t;
+            if (n >= mine || j >= k1) return -1;
+            const int32_t id = (int32_t)ld_global_u32(table + j / P);
+            return id >= 0 && id < a.cache.pages ? id : -1;
+        };
+        auto offset_of = [&](int n, int sub) { return (int)((k0 + (int64_t)(warp + n * S::kWarps) * kTile + 16 * sub) % P); };
+        auto copy_keys = [&](int n, int32_t id_t, int slot) {
+            const int32_t id = __shfl_sync(0xffffffffu, id_t, g >> 1);
+            const bool ok = id >= 0;
+            const int8_t* src = a.cache.k + (((int64_t)(ok ? id : 0) * a.kv_heads + hk) * P + offset_of(n, g >> 1) + (g & 1)) * D + 16 * t;
+            const uint32_t dst = ring + slot * S::kSlotBytes;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int j = 0; j < kLines; ++j)
+                        cp_async16(dst + ((i * 2 + r) * kLines + j) * 512, ok && 64 * j + 16 * t < D ? src + (4 * i + 2 * r) * D + 64 * j : a.cache.k, ok && 64 * j + 16 * t < D);
+            cp_commit();
+        };
+        auto copy_values = [&](int n, int32_t id, int slot) {
+            const bool ok = id >= 0;
+            const int8_t* src = a.cache.v + (((int64_t)(ok ? id : 0) * a.kv_heads + hk) * D + g) * P + offset_of(n, t);
+            const uint32_t dst = ring + slot * S::kSlotBytes;
+#pragma unroll
+            for (int j = 0; j < DP / 8; ++j) {                  // rows 8 j + g
+                const bool in = ok && 8 * j + g < D;
+                cp_async16(dst + j * 512, in ? src + (int64_t)(8 * j) * P : a.cache.v, in);
+            }
+            cp_commit();
+        };
+        // Scales of this lane's tokens, those of the 16 behind 16 (g / 2).
+        auto scales_of = [&](int32_t id_t, float* ks, float* vs) {
+            const int32_t id = __shfl_sync(0xffffffffu, id_t, g >> 1);
+            *ks = id >= 0 ? ld_global_f32(a.cache.k_scale + (int64_t)id * a.kv_heads + hk) : 0.0f;
+            *vs = id >= 0 ? ld_global_f32(a.cache.v_scale + (int64_t)id * a.kv_heads + hk) : 0.0f;
+        };
+
+        int32_t id0 = page_of(0), id1 = page_of(1), id2;
+        int slot = 0;
+        copy_keys(0, id0, 0);
+        copy_values(0, id0, 1);
+        copy_keys(1, id1, 2);
+        float ks, vs;
+        scales_of(id0, &ks, &vs);
+
+        // ---- queries: column g of the n-tiles, channels 64 j + 16 t .. + 15
+        uint32_t q[NQ][kTerms][kLines * 8];
+        float factor[NQ][2];                                    // of scores in columns 2 t, 2 t + 1, the scale of the keys apart
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+            const int64_t row = tile * kRows + 8 * nq + g;
+            const bool ok = row < s.queries * a.group;
+            const T* src = static_cast<const T*>(a.q) + (s.q0 + (ok ? row / a.group : 0)) * a.ldq + (int64_t)(hk * a.group + (ok ? row % a.group : 0)) * D + 16 * t;
+            float f[kLines * 16], top = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kLines; ++j)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    if (ok && 64 * j + 16 * t < D) v = load4(src + 64 * j + 4 * x);
+                    f[j * 16 + 4 * x] = v.x; f[j * 16 + 4 * x + 1] = v.y; f[j * 16 + 4 * x + 2] = v.z; f[j * 16 + 4 * x + 3] = v.w;
+                    top = fmaxf(fmaxf(fmaxf(top, fabsf(v.x)), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w)));
+                }
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            const int e = min(max(exponent_of(top), -100), 126);
+            const float down = power_of_two(-e);
+#pragma unroll
+            for (int x = 0; x < kLines * 8; ++x) {
+                const float lo = f[2 * x] * down, hi = f[2 * x + 1] * down;
+                q[nq][0][x] = pack_half(lo, hi);
+                if (kTerms == 2) {
+                    const float2 first = unpack_half(q[nq][0][x]);
+                    q[nq][kTerms - 1][x] = pack_half(lo - first.x, hi - first.y);
+                }
+            }
+            const float mul = a.scale_log2 * power_of_two(e);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) factor[nq][c] = __shfl_sync(0xffffffffu, mul, (2 * t + c) * 4);
+        }
+        int64_t limit[NQ][2];
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) limit[nq][c] = min(row_limit(a, s, tile * kRows + 8 * nq + 2 * t + c), k1 - 1);
+
+        float o[NQ][DP / 16][4], m[NQ][2], l[NQ][2];
+        int e = -127;                                           // O carries 2^(14 - e)
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) { m[nq][c] = -INFINITY; l[nq][c] = 0.0f; }
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[nq][d][x] = 0.0f;
+        }
+        for (int n = 0; n < mine; ++n) {
+            id2 = page_of(n + 2);
+            cp_wait<2>();
+            // ---- S^T: m-tile i holds tokens 16 (g/2) + 4 i + (g & 1), and those + 2
+            float sc[NQ][4][4];
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) sc[nq][i][x] = 0.0f;
+            const uint32_t ksrc = ring + slot * S::kSlotBytes;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < kLines; ++j) {
+                    const uint4 x = lds_v4(ksrc + ((i * 2) * kLines + j) * 512), y = lds_v4(ksrc + ((i * 2 + 1) * kLines + j) * 512);
+                    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int st = 0; st < 4; ++st) {
+                        uint32_t a0, a1, a2, a3;
+                        widen(xs[st], &a0, &a2);
+                        widen(ys[st], &a1, &a3);
+#pragma unroll
+                        for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                            for (int term = 0; term < kTerms; ++term)
+                                mma(sc[nq][i], a0, a1, a2, a3, q[nq][term][j * 8 + 2 * st], q[nq][term][j * 8 + 2 * st + 1]);
+                    }
+                }
+            copy_values(n + 1, id1, slot);
+            float ks1, vs1;
+            scales_of(id1, &ks1, &vs1);
+            // ---- softmax: columns 2 t, 2 t + 1; tokens over i, the two halves and g
+            const int64_t j0 = k0 + (int64_t)(warp + n * S::kWarps) * kTile + 16 * (g >> 1) + (g & 1);
+            const bool there = __shfl_sync(0xffffffffu, id0, g >> 1) >= 0;
+            int top_e = vs > 0.0f ? exponent_of(vs) + 1 : -127;
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) top_e = max(top_e, __shfl_xor_sync(0xffffffffu, top_e, x));
+            const int now_e = max(e, top_e);
+            // vs 2^(14 - e): in two steps, each a normal number
+            const float vf = vs * power_of_two(-now_e / 2) * power_of_two(14 - now_e + now_e / 2);
+            const float down = now_e == e ? 1.0f : (e <= -127 ? 0.0f : exp2f((float)(e - now_e)));
+            e = now_e;
+            uint32_t pb[NQ][kTerms][4][2];
+#pragma unroll
+            for (int nq = 0; nq < NQ; ++nq) {
+                float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const int c = x & 1;
+                        const bool seen = there && j0 + 4 * i + (x & 2) <= limit[nq][c];
+                        sc[nq][i][x] = seen ? sc[nq][i][x] * (factor[nq][c] * ks) : -INFINITY;
+                        top[c] = fmaxf(top[c], sc[nq][i][x]);
+                    }
+                float base[2], keep[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], x));
+                    const float now = fmaxf(m[nq][c], top[c]);
+                    base[c] = now == -INFINITY ? 0.0f : now;
+                    keep[c] = exp2f(m[nq][c] - base[c]);
+                    m[nq][c] = now;
+                    l[nq][c] *= keep[c];
+                    keep[c] *= down;
+                }
+                if (__any_sync(0xffffffffu, keep[0] != 1.0f || keep[1] != 1.0f)) {
+#pragma unroll
+                    for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x) o[nq][d][x] *= keep[x & 1];
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float p[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        p[x] = exp2f(sc[nq][i][x] - base[x & 1]);
+                        l[nq][x & 1] += p[x];
+                        p[x] *= vf;
+                    }
+                    // tokens on rows -> tokens along the step, as the second operand wants them
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t first = pack_half(p[2 * h], p[2 * h + 1]);
+                        pb[nq][0][i][h] = transpose8(first);
+                        if (kTerms == 2) {
+                            const float2 f = unpack_half(first);
+                            pb[nq][kTerms - 1][i][h] = transpose8(pack_half(p[2 * h] - f.x, p[2 * h + 1] - f.y));
+                        }
+                    }
+                }
+            }
+            // ---- O^T: rows 16 d + g and + 8, step i the tokens of m-tile i
+            cp_wait<2>();
+            const int vslot = slot == kSlots - 1 ? 0 : slot + 1;
+            const uint32_t vsrc = ring + vslot * S::kSlotBytes;
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) {
+                const uint4 x = lds_v4(vsrc + (2 * d) * 512), y = lds_v4(vsrc + (2 * d + 1) * 512);
+                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t a0, a1, a2, a3;
+                    widen(xs[i], &a0, &a2);
+                    widen(ys[i], &a1, &a3);
+#pragma unroll
+                    for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                        for (int term = 0; term < kTerms; ++term) mma(o[nq][d], a0, a1, a2, a3, pb[nq][term][i][0], pb[nq][term][i][1]);
+                }
+            }
+            copy_keys(n + 2, id2, vslot);
+            slot = vslot == kSlots - 1 ? 0 : vslot + 1;
+            id0 = id1;
+            id1 = id2;
+            ks = ks1;
+            vs = vs1;
+        }
+        // ---- the warps' results meet in the ring's memory: [warp][row][m, l, then O 2^(e - 14)]
+        cp_wait<0>();
+        __syncthreads();
+        constexpr int kPitch = DP + 4;
+        float* meet = reinterpret_cast<float*>(smem);
+        const float up_hi = power_of_two(e / 2), up_lo = power_of_two(e - e / 2 - 14);
+#pragma unroll
+        for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l[nq][c] += __shfl_xor_sync(0xffffffffu, l[nq][c], x);
+                float* to = meet + (warp * kRows + 8 * nq + 2 * t + c) * kPitch;
+                if (g == 0) { to[0] = m[nq][c]; to[1] = l[nq][c]; }
+#pragma unroll
+                for (int d = 0; d < DP / 16; ++d) {
+                    to[4 + 16 * d + g] = o[nq][d][c] * up_hi * up_lo;
+                    to[4 + 16 * d + 8 + g] = o[nq][d][2 + c] * up_hi * up_lo;
+                }
+            }
+        __syncthreads();
+        for (int e2 = threadIdx.x; e2 < kRows * (DP / 4); e2 += S::kWarps * 32) {
+            const int r = e2 / (DP / 4), d = (e2 % (DP / 4)) * 4;
+            const int64_t row = tile * kRows + r;
+            if (row >= s.queries * a.group || d >= D) continue;
+            float top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < S::kWarps; ++w) top = fmaxf(top, meet[(w * kRows + r) * kPitch]);
+            const float base = top == -INFINITY ? 0.0f : top;
+            float sum = 0.0f;
+            float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+            for (int w = 0; w < S::kWarps; ++w) {
+                const float* from = meet + (w * kRows + r) * kPitch;
+                const float f = exp2f(from[0] - base);
+                sum = fmaf(f, from[1], sum);
+                const float4 v = *reinterpret_cast<const float4*>(from + 4 + d);
+                acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
+            }
+            const int64_t token = s.q0 + row / a.group, head = hk * a.group + row % a.group;
+            if (tk.chunks <= 1) {
+                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+                store4(static_cast<T*>(a.y) + token * a.ldy + head * D + d, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+            } else {
+                const int64_t at = (token * a.q_heads + head) * a.chunks + chunk;
+                *reinterpret_cast<float4*>(a.part + at * D + d) = acc;
+                if (d == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(top, sum);
+            }
+        }
+        __syncthreads();
+    }
+}
+
+template <typename T, int DP, int NQ>
+cudaError_t launch(const Attention& a, dim3 grid, cudaStream_t stream) {
+    using S = Shape<DP>;
+    constexpr size_t meet = sizeof(float) * S::kWarps * 8 * NQ * (DP + 4);
+    constexpr size_t smem = S::kRing > meet ? S::kRing : meet;
+    auto* kern = attention_tokens_kernel<T, DP, NQ>;
+    const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
+    return e != cudaSuccess ? e : launch_pdl3(kern, grid, S::kWarps * 32, smem, stream, a);
+}
+template <typename T, int DP>
+cudaError_t by_rows(const Attention& a, dim3 grid, cudaStream_t stream) {
+    if (sizeof(T) == 4 || a.tile_rows <= 8) return launch<T, DP, 1>(a, grid, stream);
+    return launch<T, DP, sizeof(T) == 4 ? 1 : 2>(a, grid, stream);
+}
+template <typename T>
+cudaError_t by_width(const Attention& a, dim3 grid, cudaStream_t stream) {
+    if (a.head_dim <= 64) return by_rows<T, 64>(a, grid, stream);
+    if (a.head_dim <= 128) return by_rows<T, 128>(a, grid, stream);
+    return by_rows<T, 256>(a, grid, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_attention_tokens(const Attention& a, cudaStream_t stream) {
+    const dim3 grid((unsigned)row_tiles(a), (unsigned)a.chunks, (unsigned)(a.batch * a.kv_heads));
+    return a.dt == FQ_BF16 ? by_width<__nv_bfloat16>(a, grid, stream) : by_width<float>(a, grid, stream);
+}
+
+}  // namespace fq

@@ -13,16 +13,28 @@ namespace {
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Tile and chunk of a call.  Chunks are what fills the SMs where rows, heads and sequences are few.
-void plan(Attention& a) {
-    a.tile_rows = a.max_q * a.group <= 16 ? 16 : 64;
+enum class Route { Simt, Tokens };
+Route plan(Attention& a) {
+    const Route route = a.cached && a.max_q * a.group <= 16 ? Route::Tokens : Route::Simt;
+    int64_t least = 256, most = 1 << 30, wave = 2 * 148;
+    if (route == Route::Tokens) {
+        a.tile_rows = a.dt == FQ_F32 || a.max_q * a.group <= 8 ? 8 : 16;     // (two terms of sixteen rows pass the registers)
+        least = 256;
+        most = 4096;
+        wave = 4 * 148;
+    } else {
+        a.tile_rows = a.max_q * a.group <= 16 ? 16 : 64;
+    }
     const int64_t units = row_tiles(a) * a.batch * a.kv_heads;
-    int64_t splits = ceil_div(2 * 148, units > 0 ? units : 1);
-    int64_t chunk = ceil_div(ceil_div(a.max_kv, splits), 64) * 64;
-    if (chunk < 256) chunk = 256;
-    if (chunk > (1 << 30)) chunk = 1 << 30;
+    const int64_t splits = ceil_div(wave, units > 0 ? units : 1);
+    int64_t chunk = ceil_div(ceil_div(a.max_kv, splits), 256) * 256;
+    if (chunk < least) chunk = least;
+    if (chunk > most) chunk = most;
+    if (ceil_div(a.max_kv, chunk) > 65535) chunk = ceil_div(ceil_div(a.max_kv, 65535), 256) * 256;
     a.chunk = (int)chunk;
     const int64_t chunks = ceil_div(a.max_kv, chunk);
     a.chunks = (int)(chunks < 1 ? 1 : chunks);
+    return route;
 }
 size_t part_bytes(const Attention& a) {
     return a.chunks <= 1 ? 0 : align_up(sizeof(float) * (size_t)a.q_rows * a.q_heads * a.chunks * a.head_dim, 256);
@@ -39,7 +51,7 @@ size_t attention_workspace_bytes(const Attention& given) {
 }
 
 fq_status launch_attention(Attention& a, void* workspace, size_t ws_bytes, cudaStream_t stream) {
-    plan(a);
+    const Route route = plan(a);
     const size_t parts = part_bytes(a), need = parts + ml_bytes(a);
     if (need > 0) {
         if (!workspace) return FQ_ERR_INVALID_ARG;
@@ -48,7 +60,8 @@ fq_status launch_attention(Attention& a, void* workspace, size_t ws_bytes, cudaS
         a.part = static_cast<float*>(workspace);
         a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + parts);
     }
-    if (launch_attention_simt(a, stream) != cudaSuccess) return FQ_ERR_CUDA;
+    const cudaError_t e = route == Route::Tokens ? launch_attention_tokens(a, stream) : launch_attention_simt(a, stream);
+    if (e != cudaSuccess) return FQ_ERR_CUDA;
     if (a.chunks > 1 && launch_attention_join(a, stream) != cudaSuccess) return FQ_ERR_CUDA;
     return FQ_OK;
 }
