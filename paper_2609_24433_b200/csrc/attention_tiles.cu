@@ -1,0 +1,666 @@
+// Attention of many queries on the tcgen05 tensor cores: bf16 keys and values as rows (cross attention) or the 8-bit cache.
+//
+// A CTA takes one chunk of the keys of one kv head and NT tiles of 128 rows -- (token, head of a group) pairs, so that a group
+// reads its keys once.  Per tile of 128 keys: S = Q K^T into TMEM; one thread per row keeps the running maximum and sum and
+// writes the probabilities, 16 bits each, over S in TMEM; O += P V takes them from there as its first operand.
+//   warps 0-7   softmax, a warpgroup per row tile
+//   warps 8-11  keys and values into 128-byte-swizzled stages of 128 keys x 64 or 128 channels
+//   warp 12     issues the MMAs
+// With two row tiles (D <= 128) the tensor core works on one while the other's probabilities are computed; with one (D > 128,
+// or few rows) S is double-buffered instead.
+//
+// The maximum is followed lazily: O and l are rescaled only where a row's maximum has risen by more than 2^8 over the base they
+// were built with, so almost never behind the first tiles; probabilities then reach 256, which changes no relative rounding.
+//
+// Cache: codes are widened to binary16, exactly, on their way into the stages (values keep tokens innermost and need no turn).
+// The scale of a page's keys multiplies S per 16 columns; that of its values multiplies the probabilities, over 2^e with e the
+// running exponent of the largest one: P = p vs 2^(7 - e) <= 2^15.  Queries: binary16 behind a power of two per row.
+// Rows: bf16 operands; a masked key's bytes are not read but replaced by zeros (cp.async with no source bytes), since 0 times a
+// masked NaN would reach the sums.
+#include "attention_common.cuh"
+#include "tc_sm100.cuh"
+
+#include <cuda_fp16.h>
+
+namespace fq {
+namespace {
+
+constexpr int kThreads = 13 * 32;
+constexpr int kKeys = 128;
+constexpr int kMetas = 8;
+constexpr float kSlack = 8.0f;          // log2 of how far a row's maximum may rise over its base
+
+constexpr uint32_t kWdProducer = 0x800u, kWdMma = 0x1000u, kWdSoftmax = 0x2000u;
+
+template <int DP, int NT>
+struct Shape {
+    static constexpr int kParts = DP == 256 ? 2 : 1;            // stages per key or value tile
+    static constexpr int kCh = DP / kParts;                     // channels per stage
+    static constexpr int kStageBytes = kKeys * kCh * 2;
+    static constexpr int kStages = DP == 64 ? 8 : 5;
+    static constexpr int kQTile = 128 * DP * 2;
+    static constexpr int kSmem = 1024 + NT * kQTile + kStages * kStageBytes;
+    static constexpr int kOCol = 256;                           // S: columns 0 .. 255
+};
+
+struct __align__(16) KeyMeta {
+    float ks[8];                        // per 16 keys
+    float vf[8];
+    uint32_t valid[4];
+    int e;
+    int unused[3];
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {        // zeros where !ok
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void widen(uint32_t w, uint32_t* lo, uint32_t* hi) {     // four int8 -> two pairs of binary16
+    const uint32_t u = w ^ 0x80808080u;
+    const __half2 base = __half2half2(__ushort_as_half(0x6480));                    // 1024 + 128
+    const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), base), y = __hsub2(*reinterpret_cast<const __half2*>(&b), base);
+    *lo = *reinterpret_cast<const uint32_t*>(&x);
+    *hi = *reinterpret_cast<const uint32_t*>(&y);
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255) - 127; }
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// 16-bit operands (type 0: binary16, 1: bf16) -> binary32; A K-major, B K-major or, transposed, N-major; M = 128.
+__device__ __forceinline__ uint32_t instr_desc_16(int type, bool b_transposed, int n) {
+    return (1u << 4) | ((uint32_t)type << 7) | ((uint32_t)type << 10) | ((b_transposed ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+// N-major operand, 128-byte rows of 64 channels, 128B swizzle: 8-row groups (of keys) 1024 bytes apart, 64-channel blocks one
+// 16 KB plane apart.
+__device__ __forceinline__ uint64_t smem_desc_n_major(uint32_t addr) {
+    uint64_t d = smem_desc_sw128(addr);
+    d &= ~((uint64_t)0x3FFF << 16);
+    return d | (uint64_t)(16384 >> 4) << 16;
+}
+__device__ __forceinline__ void mbar_inval(uint32_t bar) { asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
+
+template <int DP, int NT, bool CACHED>
+__global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Attention a, uint32_t* watchdog) {
+    using S = Shape<DP, NT>;
+    constexpr int kCh = S::kCh, kParts = S::kParts, kStages = S::kStages, kPlanes = kCh / 64;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(16) KeyMeta metas[kMetas];
+    __shared__ __align__(8) uint64_t s_full_kv[kStages], s_empty_kv[kStages], s_meta[kMetas], s_s[2], s_p[2], s_o, s_q;
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort;
+    volatile int* abort_flag = &s_abort;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t q_smem = smem, ring = smem + NT * S::kQTile;
+    auto full_kv = [&](int n) { return smem_u32(&s_full_kv[n % kStages]); };
+    auto empty_kv = [&](int n) { return smem_u32(&s_empty_kv[n % kStages]); };
+    auto stage = [&](int n) { return ring + (uint32_t)(n % kStages) * S::kStageBytes; };
+
+    auto init_barriers = [&]() {
+        for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&s_full_kv[i]), 4); mbar_init(smem_u32(&s_empty_kv[i]), 1); }
+        for (int i = 0; i < kMetas; ++i) mbar_init(smem_u32(&s_meta[i]), 4);
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&s_s[i]), 1); mbar_init(smem_u32(&s_p[i]), 4); }
+        mbar_init(smem_u32(&s_o), 1);
+        mbar_init(smem_u32(&s_q), 4 * NT);
+        fence_mbarrier_init();
+    };
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        init_barriers();
+    }
+    if (warp == 12) tmem_alloc<1>(smem_u32(&s_tmem), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    griddep_wait();
+
+    const int b = blockIdx.z / a.kv_heads, hk = blockIdx.z % a.kv_heads, chunk = blockIdx.y;
+    const Sequence s = sequence_of(a, b);
+    const int D = a.head_dim, G = a.group;
+    const int64_t rows = s.queries * G;
+    constexpr int kRows = NT * 128;
+    bool ok = true, again = false;
+
+    // (the longest rows of a causal sequence, its last ones, begin first)
+    const int64_t tiles = (rows + kRows - 1) / kRows;
+    for (int64_t back = blockIdx.x; back < tiles && ok; back += gridDim.x) {
+        const int64_t tile = tiles - 1 - back;
+        const TileKeys tk = tile_keys(a, s, tile, kRows);
+        const int64_t k0 = (int64_t)chunk * a.chunk;
+        if (chunk > 0 && k0 >= tk.end) continue;
+        const int64_t k1 = min(tk.end, k0 + a.chunk);
+        const int n = (int)((k1 - k0 + kKeys - 1) / kKeys);
+        const int uses = n * 2 * kParts;                        // of stages: per key tile its keys, then its values
+        if (again) {                                            // every arrival of the last tile has been waited for
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                for (int i = 0; i < kStages; ++i) { mbar_inval(smem_u32(&s_full_kv[i])); mbar_inval(smem_u32(&s_empty_kv[i])); }
+                for (int i = 0; i < kMetas; ++i) mbar_inval(smem_u32(&s_meta[i]));
+                for (int i = 0; i < 2; ++i) { mbar_inval(smem_u32(&s_s[i])); mbar_inval(smem_u32(&s_p[i])); }
+                mbar_inval(smem_u32(&s_o));
+                mbar_inval(smem_u32(&s_q));
+                init_barriers();
+            }
+            __syncthreads();
+        }
+        again = true;
+
+        if (warp < 8) {
+            // ================================================================ softmax
+            const int mine = NT == 2 ? warp / 4 : 0;
+            const int r = threadIdx.x % 128;
+            const int64_t row = tile * kRows + mine * 128 + r;
+            const bool active = NT == 2 || warp < 4;
+            const bool there = active && row < rows;
+            const int64_t token = s.q0 + (there ? row / G : 0), head = hk * G + (there ? row % G : 0);
+            float factor = a.scale_log2;
+            if (active) {
+                // ---- this thread's row of Q
+                const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + token * a.ldq + head * D;
+                const uint32_t dst = q_smem + mine * S::kQTile + r * 128;
+                float down = 1.0f;
+                if (CACHED) {
+                    float top = 0.0f;
+                    for (int d = 0; d < D; d += 8) {
+                        const uint4 v = ld_global_v4(src + d, there);
+                        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
+                    }
+                    const int e = min(max(exponent_of(top), -100), 126);
+                    down = power_of_two(-e);
+                    factor = a.scale_log2 * power_of_two(e);
+                }
+#pragma unroll 4
+                for (int d = 0; d < DP; d += 8) {
+                    uint4 v = ld_global_v4(src + d, there && d < D);
+                    if (CACHED) {
+                        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = pack_half(__uint_as_float(w[i] << 16) * down, __uint_as_float(w[i] & 0xffff0000u) * down);
+                        v = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                    sts128(dst + (d / 64) * 16384 + ((((d % 64) / 8) ^ (r & 7)) * 16), v.x, v.y, v.z, v.w);
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&s_q));
+            }
+            if (active) {
+                const uint32_t lanes = tmem + ((uint32_t)(warp % 4) << 21);
+                const uint32_t o_addr = lanes + S::kOCol + (NT == 2 ? mine * DP : 0);
+                const int64_t limit64 = row_limit(a, s, row);
+                float base = -INFINITY, l = 0.0f;
+                int e = -127;
+                for (int j = 0; j < n && ok; ++j) {
+                    const int buf = NT == 2 ? mine : j & 1;
+                    const uint32_t phase = NT == 2 ? j & 1 : (j >> 1) & 1;
+                    ok = mbar_wait_all(smem_u32(&s_s[buf]), phase, abort_flag, watchdog, kWdSoftmax) &&
+                         mbar_wait_all(smem_u32(&s_meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdSoftmax);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const KeyMeta& meta = metas[j % kMetas];
+                    const uint32_t s_addr = lanes + 128 * buf;
+                    const int lim = (int)min(max(limit64 - (k0 + (int64_t)j * kKeys), (int64_t)-1), (int64_t)kKeys);
+                    uint32_t seen[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int x = lim - 32 * c;
+                        seen[c] = meta.valid[c] & (x < 0 ? 0u : x >= 31 ? ~0u : (2u << x) - 1u);
+                    }
+                    const bool masked = __any_sync(0xffffffffu, (seen[0] & seen[1] & seen[2] & seen[3]) != ~0u);
+                    uint32_t v[64];
+                    // ---- the largest score
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        tmem_ld32(s_addr + 64 * h, v);
+                        tmem_ld32(s_addr + 64 * h + 32, v + 32);
+                        tmem_ld_wait();
+                        if (masked) {
+#pragma unroll
+                            for (int i = 0; i < 64; ++i) v[i] = (seen[2 * h + i / 32] >> (i % 32)) & 1 ? v[i] : 0xff800000u;
+                        }
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            float x = -INFINITY;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) x = fmaxf(x, __uint_as_float(v[16 * g + i]));
+                            top = fmaxf(top, CACHED ? (x == -INFINITY ? x : x * (factor * meta.ks[4 * h + g])) : x);
+                        }
+                    }
+                    if (!CACHED) top = top == -INFINITY ? top : top * factor;
+                    // ---- a new base
+                    const int now_e = CACHED ? meta.e : e;
+                    const bool rise = top > base + kSlack || (base == -INFINITY && top > base);
+                    if (__any_sync(0xffffffffu, rise || now_e != e)) {
+                        const float now = rise ? top : base;
+                        const float keep = rise ? exp2f(base - now) : 1.0f;        // (from nothing: 0)
+                        base = now;
+                        l *= keep;
+                        if (j > 0) {
+                            if (NT == 1) {
+                                ok = mbar_wait_all(smem_u32(&s_o), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
+                                if (!ok) break;
+                                tc_fence_after();
+                            }
+                            const float f = CACHED ? keep * (e <= -127 ? 0.0f : exp2f((float)(e - now_e))) : keep;
+#pragma unroll
+                            for (int c = 0; c < DP; c += 32) {
+                                uint32_t o[32];
+                                tmem_ld32(o_addr + c, o);
+                                tmem_ld_wait();
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                tmem_st16(o_addr + c, o);
+                                tmem_st16(o_addr + c + 16, o + 16);
+                            }
+                        }
+                        e = now_e;
+                    }
+                    const float minus = base == -INFINITY ? 0.0f : -base;
+                    // ---- probabilities, over the scores that they come from
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        tmem_ld32(s_addr + 64 * h, v);
+                        tmem_ld32(s_addr + 64 * h + 32, v + 32);
+                        tmem_ld_wait();
+                        uint32_t p[32];
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) {
+                            const float f = CACHED ? factor * meta.ks[4 * h + g] : factor;
+                            const float vf = CACHED ? meta.vf[4 * h + g] : 1.0f;
+#pragma unroll
+                            for (int i = 0; i < 16; i += 2) {
+                                float x = ex2(fmaf(__uint_as_float(v[16 * g + i]), f, minus)), y = ex2(fmaf(__uint_as_float(v[16 * g + i + 1]), f, minus));
+                                if (masked) {
+                                    const uint32_t bits = seen[2 * h + g / 2] >> (16 * (g % 2) + i);
+                                    x = bits & 1 ? x : 0.0f;
+                                    y = bits & 2 ? y : 0.0f;
+                                }
+                                l += x;
+                                l += y;
+                                p[8 * g + i / 2] = CACHED ? pack_half(x * vf, y * vf) : pack_bf16(x, y);
+                            }
+                        }
+                        tmem_st16(s_addr + 32 * h, p);
+                        tmem_st16(s_addr + 32 * h + 16, p + 16);
+                    }
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&s_p[buf]));
+                }
+                // ---- the rows' results
+                if (ok && n > 0) {
+                    if (NT == 1 && n > 1) ok = mbar_wait_all(smem_u32(&s_o), (n - 2) & 1, abort_flag, watchdog, kWdSoftmax);
+                    ok = ok && mbar_wait_all(smem_u32(&s_o), NT == 1 ? (n - 1) & 1 : 0, abort_flag, watchdog, kWdSoftmax);
+                    tc_fence_after();
+                }
+                if (ok) {
+                    const bool direct = tk.chunks <= 1;
+                    const int64_t at = (token * a.q_heads + head) * a.chunks + chunk;
+                    const float whole = CACHED ? power_of_two(e / 2) : 1.0f, rest = CACHED ? power_of_two(e - e / 2 - 7) : 1.0f;
+                    const float inv = direct ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f;
+                    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y) + token * a.ldy + head * D;
+                    float* part = direct ? nullptr : a.part + at * D;
+#pragma unroll
+                    for (int c = 0; c < DP; c += 32) {
+                        uint32_t o[32];
+                        if (n > 0) {
+                            tmem_ld32(o_addr + c, o);
+                            tmem_ld_wait();
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = 0u;
+                        }
+                        float f[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) f[i] = l > 0.0f ? __uint_as_float(o[i]) * whole * rest * inv : 0.0f;
+#pragma unroll
+                        for (int x = 0; x < 32; x += 8) {
+                            if (!there || c + x >= D) continue;
+                            if (direct) {
+                                *reinterpret_cast<uint4*>(y + c + x) = make_uint4(pack_bf16(f[x], f[x + 1]), pack_bf16(f[x + 2], f[x + 3]),
+                                                                                  pack_bf16(f[x + 4], f[x + 5]), pack_bf16(f[x + 6], f[x + 7]));
+                            } else {
+                                *reinterpret_cast<float4*>(part + c + x) = make_float4(f[x], f[x + 1], f[x + 2], f[x + 3]);
+                                *reinterpret_cast<float4*>(part + c + x + 4) = make_float4(f[x + 4], f[x + 5], f[x + 6], f[x + 7]);
+                            }
+                        }
+                    }
+                    if (!direct && there) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(base, l);
+                    tc_fence_before();
+                }
+            }
+        } else if (warp < 12) {
+            // ================================================================ keys and values
+            const int w = warp - 8;
+            if (!CACHED) {
+                constexpr int kLook = kStages == 8 ? 4 : 2;      // copies in flight beyond the stage that is handed over
+                constexpr int kPerRow = kCh / 8;                 // 16-byte units
+                int done = 0, use = 0;
+                uint32_t word = 0;
+                for (int j = 0; j < n && ok; ++j) {
+                    const int64_t key = k0 + (int64_t)j * kKeys + 32 * w;
+#pragma unroll
+                    for (int u = 0; u < 2 * kParts; ++u, ++use) {
+                        const bool values = u >= kParts;
+                        const int part = u % kParts;
+                        if (use >= kStages) {
+                            const uint32_t phase = ((use / kStages) & 1) ^ 1;
+                            const bool free = __all_sync(0xffffffffu, mbar_test_wait(empty_kv(use), phase));
+                            // What frees a stage may be waiting for the copies in flight: they are handed over ahead of the wait.
+                            if (!free && done < use) {
+                                cp_wait<0>();
+                                fence_proxy_async_smem();
+                                __syncwarp();
+                                for (; done < use; ++done)
+                                    if (lane == 0) mbar_arrive(full_kv(done));
+                            }
+                            ok = mbar_wait_all_lazy(empty_kv(use), phase, abort_flag, watchdog, kWdProducer, free);
+                        }
+                        if (!ok) break;
+                        if (u == 0) {
+                            const KeyPlace p = key_place<false>(a, s, b, hk, key + lane, k1);
+                            word = __ballot_sync(0xffffffffu, p.valid);
+                            if (lane == 0) {
+                                metas[j % kMetas].valid[w] = word;
+                                mbar_arrive(smem_u32(&s_meta[j % kMetas]));
+                            }
+                        }
+                        const int64_t ld = values ? a.ldv : a.ldk;
+                        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(values ? a.v : a.k) + (s.k0 + key) * ld + (int64_t)hk * D + part * 128;
+                        const uint32_t dst = stage(use) + 32 * w * 128;
+                        const int c = lane % kPerRow;
+                        const bool in = part * 128 + c * 8 < D;
+#pragma unroll
+                        for (int it = 0; it < kPerRow; ++it) {
+                            const int x = it * (32 / kPerRow) + lane / kPerRow;        // row of the warp's 32
+                            const bool take = in && ((word >> x) & 1);
+                            cp_async16(dst + (c / 8) * 16384 + x * 128 + (((c % 8) ^ (x & 7)) * 16), take ? static_cast<const void*>(src + x * ld + c * 8) : a.k, take);
+                        }
+                        cp_commit();
+                        if (use - done >= kLook) {
+                            cp_wait<kLook>();
+                            fence_proxy_async_smem();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(full_kv(done));
+                            ++done;
+                        }
+                    }
+                }
+                cp_wait<0>();
+                fence_proxy_async_smem();
+                __syncwarp();
+                for (; ok && done < uses; ++done)
+                    if (lane == 0) mbar_arrive(full_kv(done));
+            } else {
+                constexpr int kUnits = kCh / 16;                 // 16-byte units of codes per lane and stage
+                const int P = a.cache.page;
+                const int32_t* table = a.table + b * a.ld_table;
+                auto page_of = [&](int j) -> int32_t {           // of keys 16 (lane % 8) .. of tile j
+                    const int64_t key = k0 + (int64_t)j * kKeys + 16 * (lane % 8);
+                    if (j >= n || key >= k1) return -1;
+                    const int32_t id = (int32_t)ld_global_u32(table + key / P);
+                    return id >= 0 && id < a.cache.pages ? id : -1;
+                };
+                uint4 codes[2][kUnits];
+                auto fetch = [&](int u, int32_t id, uint4* to) {
+                    const int part = u % kParts;
+                    if (u < kParts) {
+                        const int32_t ids[2] = {__shfl_sync(0xffffffffu, id, 2 * w), __shfl_sync(0xffffffffu, id, 2 * w + 1)};
+                        const int du = lane % kUnits;
+#pragma unroll
+                        for (int it = 0; it < kUnits; ++it) {
+                            const int x = it * (32 / kUnits) + lane / kUnits;          // token of the warp's 32
+                            const int32_t page = ids[it * 2 / kUnits];
+                            const bool take = page >= 0 && part * 128 + du * 16 < D;
+                            const int off = (16 * (2 * w + it * 2 / kUnits)) % P + x % 16;
+                            to[it] = ld_global_v4(a.cache.k + (((int64_t)(take ? page : 0) * a.kv_heads + hk) * P + off) * D + part * 128 + du * 16, take);
+                        }
+                    } else {
+                        const int off = (16 * (lane % 8)) % P;
+#pragma unroll
+                        for (int it = 0; it < kUnits; ++it) {
+                            const int d = part * 128 + w * (kCh / 4) + it * 4 + lane / 8;
+                            const bool take = id >= 0 && d < D;
+                            to[it] = ld_global_v4(a.cache.v + (((int64_t)(take ? id : 0) * a.kv_heads + hk) * D + d) * P + off, take);
+                        }
+                    }
+                };
+                int32_t id = page_of(0), id1 = page_of(1), id2;
+                float ks = 0.0f, vs = 0.0f;
+                auto scales_of = [&](int32_t page, float* k, float* v) {
+                    *k = page >= 0 ? ld_global_f32(a.cache.k_scale + (int64_t)page * a.kv_heads + hk) : 0.0f;
+                    *v = page >= 0 ? ld_global_f32(a.cache.v_scale + (int64_t)page * a.kv_heads + hk) : 0.0f;
+                };
+                int e = -127, use = 0;
+                if (n > 0) {
+                    scales_of(id, &ks, &vs);
+                    fetch(0, id, codes[0]);
+                }
+                for (int j = 0; j < n && ok; ++j) {
+                    id2 = page_of(j + 2);
+                    float ks1, vs1;
+                    scales_of(id1, &ks1, &vs1);
+#pragma unroll
+                    for (int u = 0; u < 2 * kParts; ++u, ++use) {
+                        if (u + 1 < 2 * kParts) fetch(u + 1, id, codes[(u + 1) & 1]);
+                        else fetch(0, id1, codes[0]);
+                        if (use >= kStages) ok = mbar_wait_all_lazy(empty_kv(use), ((use / kStages) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
+                        if (!ok) break;
+                        if (u == 0) {
+                            int top = vs > 0.0f ? exponent_of(vs) + 1 : -127;
+#pragma unroll
+                            for (int x = 1; x < 8; x <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, x));
+                            e = max(e, top);
+                            KeyMeta& meta = metas[j % kMetas];
+                            const int64_t key = k0 + (int64_t)j * kKeys + 32 * w + lane;
+                            const int32_t page = __shfl_sync(0xffffffffu, id, 2 * w + lane / 16);
+                            const uint32_t word = __ballot_sync(0xffffffffu, page >= 0 && key < k1);
+                            if (lane / 2 == w) {                 // lanes 2 w, 2 w + 1: the warp's two groups of 16 keys
+                                meta.ks[lane] = ks;
+                                meta.vf[lane] = vs * power_of_two(-e / 2) * power_of_two(7 - e + e / 2);
+                            }
+                            if (lane == 0) {
+                                meta.valid[w] = word;
+                                if (w == 0) meta.e = e;
+                            }
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(smem_u32(&s_meta[j % kMetas]));
+                        }
+                        // 16 codes -> 32 bytes.  Lanes of the second plane write their halves the other way round: eight
+                        // lanes' 16-byte stores then meet all banks.
+                        const uint32_t dst = stage(use);
+#pragma unroll
+                        for (int it = 0; it < kUnits; ++it) {
+                            const uint4 x = codes[u & 1][it];
+                            uint32_t h[8];
+                            widen(x.x, &h[0], &h[1]);
+                            widen(x.y, &h[2], &h[3]);
+                            widen(x.z, &h[4], &h[5]);
+                            widen(x.w, &h[6], &h[7]);
+                            int row, unit;
+                            uint32_t plane;
+                            if (u < kParts) {
+                                row = 32 * w + it * (32 / kUnits) + lane / kUnits;
+                                unit = lane % kUnits;
+                                plane = 16384;
+                            } else {
+                                row = w * (kCh / 4) + it * 4 + lane / 8;
+                                unit = lane % 8;
+                                plane = kCh * 128;
+                            }
+                            const int second = unit / 4, c = (unit % 4) * 2;
+                            const uint32_t at = dst + second * plane + row * 128;
+                            const uint32_t lo = at + ((c ^ (row & 7)) * 16), hi = at + (((c + 1) ^ (row & 7)) * 16);
+                            const bool swap = second != 0;
+                            sts128(swap ? hi : lo, swap ? h[4] : h[0], swap ? h[5] : h[1], swap ? h[6] : h[2], swap ? h[7] : h[3]);
+                            sts128(swap ? lo : hi, swap ? h[0] : h[4], swap ? h[1] : h[5], swap ? h[2] : h[6], swap ? h[3] : h[7]);
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(full_kv(use));
+                    }
+                    id = id1;
+                    id1 = id2;
+                    ks = ks1;
+                    vs = vs1;
+                }
+            }
+        } else if (n > 0) {
+            // ================================================================ MMA issue
+            const uint32_t idesc_s = instr_desc_16(CACHED ? 0 : 1, false, kKeys), idesc_o = instr_desc_16(CACHED ? 0 : 1, !CACHED, kCh);
+            auto wait_kv = [&](int use) { return mbar_wait_all(full_kv(use), (use / kStages) & 1, abort_flag, watchdog, kWdMma); };
+            auto scores = [&](int j, int i, int buf) {           // S[buf] = Q_i K_j^T
+                if (elect_one()) {
+#pragma unroll
+                    for (int p = 0; p < kParts; ++p)
+#pragma unroll
+                        for (int c = 0; c < kPlanes; ++c)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                mma_f16_ss(tmem + 128 * buf, smem_desc_sw128(q_smem + i * S::kQTile + (p * kPlanes + c) * 16384 + k * 32),
+                                           smem_desc_sw128(stage(2 * kParts * j + p) + c * 16384 + k * 32), idesc_s, p + c + k > 0);
+                    mma_commit(smem_u32(&s_s[buf]));
+                }
+                __syncwarp();
+            };
+            auto products = [&](int j, int i, int buf) {         // O_i += P V_j
+                if (elect_one()) {
+#pragma unroll
+                    for (int p = 0; p < kParts; ++p)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const uint32_t v = stage(2 * kParts * j + kParts + p);
+                            const uint64_t desc = CACHED ? smem_desc_sw128(v + (k / 4) * (kCh * 128) + (k % 4) * 32) : smem_desc_n_major(v + k * 2048);
+                            mma_f16_ts(tmem + S::kOCol + i * DP + p * 128, tmem + 128 * buf + 8 * k, desc, idesc_o, j > 0 || k > 0);
+                        }
+                }
+                __syncwarp();
+            };
+            auto release = [&](int first) {                      // stages of a key or value tile, where they are filled again
+                if (elect_one()) {
+#pragma unroll
+                    for (int p = 0; p < kParts; ++p)
+                        if (first + p + kStages < uses) mma_commit(empty_kv(first + p));
+                }
+                __syncwarp();
+            };
+            ok = mbar_wait_all(smem_u32(&s_q), 0, abort_flag, watchdog, kWdMma);
+            for (int p = 0; ok && p < kParts; ++p) ok = wait_kv(p);
+            if (ok) {
+                tc_fence_after();
+                for (int i = 0; i < NT; ++i) scores(0, i, i);
+                release(0);
+            }
+            for (int j = 0; j < n && ok; ++j) {
+                const int vuse = 2 * kParts * j + kParts, kuse = 2 * kParts * (j + 1);
+                if (NT == 1 && j + 1 < n) {
+                    for (int p = 0; ok && p < kParts; ++p) ok = wait_kv(kuse + p);
+                    if (!ok) break;
+                    scores(j + 1, 0, (j + 1) & 1);
+                    release(kuse);
+                }
+                for (int i = 0; i < NT && ok; ++i) {
+                    const int buf = NT == 2 ? i : j & 1;
+                    ok = mbar_wait_all(smem_u32(&s_p[buf]), NT == 2 ? j & 1 : (j >> 1) & 1, abort_flag, watchdog, kWdMma);
+                    for (int p = 0; ok && i == 0 && p < kParts; ++p) ok = wait_kv(vuse + p);
+                    if (!ok) break;
+                    tc_fence_after();
+                    products(j, i, buf);
+                    if (NT == 2 && j + 1 < n) {
+                        for (int p = 0; ok && i == 0 && p < kParts; ++p) ok = wait_kv(kuse + p);
+                        if (!ok) break;
+                        scores(j + 1, i, i);
+                    }
+                }
+                if (!ok) break;
+                if (NT == 1 || j + 1 == n) {
+                    if (elect_one()) mma_commit(smem_u32(&s_o));
+                    __syncwarp();
+                }
+                release(vuse);
+                if (NT == 2 && j + 1 < n) release(kuse);
+            }
+        }
+        __syncthreads();
+        ok = s_abort == 0;
+    }
+    if (!ok && warp == 12) drain_after_abort();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 12) tmem_dealloc<1>(tmem, 512);
+}
+
+template <int DP, int NT, bool CACHED>
+cudaError_t launch(const Attention& a, cudaStream_t stream) {
+    auto* kern = attention_tiles_kernel<DP, NT, CACHED>;
+    uint32_t* watchdog = watchdog_device_ptr();
+    if (!watchdog) return cudaErrorUnknown;
+    const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), Shape<DP, NT>::kSmem);
+    const dim3 grid((unsigned)row_tiles(a), (unsigned)a.chunks, (unsigned)(a.batch * a.kv_heads));
+    return e != cudaSuccess ? e : launch_pdl3(kern, grid, kThreads, Shape<DP, NT>::kSmem, stream, a, watchdog);
+}
+template <bool CACHED>
+cudaError_t by_width(const Attention& a, cudaStream_t stream) {
+    if (a.head_dim > 128) return launch<256, 1, CACHED>(a, stream);
+    if (a.head_dim > 64) return a.tile_rows == 256 ? launch<128, 2, CACHED>(a, stream) : launch<128, 1, CACHED>(a, stream);
+    return a.tile_rows == 256 ? launch<64, 2, CACHED>(a, stream) : launch<64, 1, CACHED>(a, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_attention_tiles(const Attention& a, cudaStream_t stream) {
+    return a.cached ? by_width<true>(a, stream) : by_width<false>(a, stream);
+}
+
+}  // namespace fq

@@ -13,15 +13,18 @@ namespace {
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Tile and chunk of a call.  Chunks are what fills the SMs where rows, heads and sequences are few.
-enum class Route { Simt, Tokens };
+enum class Route { Simt, Tokens, Tiles };
 Route plan(Attention& a) {
-    const Route route = a.cached && a.max_q * a.group <= 16 ? Route::Tokens : Route::Simt;
+    const Route route = a.cached && a.max_q * a.group <= 16 ? Route::Tokens : a.dt == FQ_BF16 ? Route::Tiles : Route::Simt;
     int64_t least = 256, most = 1 << 30, wave = 2 * 148;
     if (route == Route::Tokens) {
         a.tile_rows = a.dt == FQ_F32 || a.max_q * a.group <= 8 ? 8 : 16;     // (two terms of sixteen rows pass the registers)
         least = 256;
         most = 4096;
         wave = 4 * 148;
+    } else if (route == Route::Tiles) {
+        a.tile_rows = a.head_dim <= 128 && a.max_q * a.group > 128 ? 256 : 128;
+        wave = 148;
     } else {
         a.tile_rows = a.max_q * a.group <= 16 ? 16 : 64;
     }
@@ -60,7 +63,9 @@ fq_status launch_attention(Attention& a, void* workspace, size_t ws_bytes, cudaS
         a.part = static_cast<float*>(workspace);
         a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + parts);
     }
-    const cudaError_t e = route == Route::Tokens ? launch_attention_tokens(a, stream) : launch_attention_simt(a, stream);
+    const cudaError_t e = route == Route::Tokens  ? launch_attention_tokens(a, stream)
+                          : route == Route::Tiles ? launch_attention_tiles(a, stream)
+                                                  : launch_attention_simt(a, stream);
     if (e != cudaSuccess) return FQ_ERR_CUDA;
     if (a.chunks > 1 && launch_attention_join(a, stream) != cudaSuccess) return FQ_ERR_CUDA;
     return FQ_OK;

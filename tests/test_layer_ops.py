@@ -24,6 +24,14 @@ TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 gpu = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def _watchdog_clean(request):
+    yield
+    if "gpu" in request.keywords and torch.cuda.is_available():
+        st, word = fq.device_status()
+        assert st == fq.OK, f"device wait watchdog fired: {word:#x}"
+
+
 def rand(shape, seed, dtype=torch.float32, gain=1.0):
     g = torch.Generator(device="cuda").manual_seed(seed)
     return (torch.randn(shape, device="cuda", generator=g) * gain).to(dtype)
