@@ -5,7 +5,7 @@
 // writes the probabilities, 16 bits each, over S in TMEM; O += P V takes them from there as its first operand.
 //   warps 0-7   softmax, a warpgroup per row tile
 //   warps 8-11  keys and values into 128-byte-swizzled stages of 128 keys x 64 or 128 channels
-//   warp 12     issues the MMAs
+//   warp 12     issues the MMAs (13-15 complete its warpgroup, whose registers go to the softmax)
 // With two row tiles (D <= 128) the tensor core works on one while the other's probabilities are computed; with one (D > 128,
 // or few rows) S is double-buffered instead.
 //
@@ -17,15 +17,20 @@
 // running exponent of the largest one: P = p vs 2^(7 - e) <= 2^15.  Queries: binary16 behind a power of two per row.
 // Rows: bf16 operands; a masked key's bytes are not read but replaced by zeros (cp.async with no source bytes), since 0 times a
 // masked NaN would reach the sums.
+#include "act_common.cuh"
 #include "attention_common.cuh"
 #include "tc_sm100.cuh"
 
 #include <cuda_fp16.h>
+#include <float.h>
 
 namespace fq {
 namespace {
 
-constexpr int kThreads = 13 * 32;
+constexpr int kThreads = 16 * 32;
+// Registers: a softmax thread holds a row of 128 scores.  The launch's 512 x 128 are shared out as 256 x 176 + 256 x 80.
+constexpr int kRegsLaunch = 128, kRegsSoftmax = 176, kRegsOther = 80;
+static_assert(256 * kRegsSoftmax + 256 * kRegsOther <= kThreads * kRegsLaunch, "");
 constexpr int kKeys = 128;
 constexpr int kMetas = 8;
 constexpr float kSlack = 8.0f;          // log2 of how far a row's maximum may rise over its base
@@ -122,6 +127,31 @@ __device__ __forceinline__ uint64_t smem_desc_n_major(uint32_t addr) {
     d &= ~((uint64_t)0x3FFF << 16);
     return d | (uint64_t)(16384 >> 4) << 16;
 }
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// mbar_wait_all with the bounded loop in line: a kernel that calls a function keeps its launch's registers in every warp.
+__device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* watchdog, uint32_t code) {
+    bool ok = true;
+    if (!mbar_try_wait(bar, parity)) {
+        uint64_t t0 = 0;
+        for (uint32_t spin = 1; !mbar_try_wait(bar, parity); ++spin) {
+            if ((spin & 0xfff) == 0) {
+                if (*abort_flag) { ok = false; break; }
+                const uint64_t now = global_timer_ns();
+                if (t0 == 0) t0 = now;
+                if (now - t0 > kWaitLimitNs) {
+                    *abort_flag = 1;
+                    atomicOr(watchdog, code);
+                    ok = false;
+                    break;
+                }
+            }
+        }
+    }
+    return __all_sync(0xffffffffu, ok);
+}
 __device__ __forceinline__ void mbar_inval(uint32_t bar) { asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
 
 template <int DP, int NT, bool CACHED>
@@ -167,31 +197,37 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     constexpr int kRows = NT * 128;
     bool ok = true, again = false;
 
-    // (the longest rows of a causal sequence, its last ones, begin first)
+    // Every warp walks the row tiles of this CTA; the longest rows of a causal sequence, its last ones, come first.
     const int64_t tiles = (rows + kRows - 1) / kRows;
-    for (int64_t back = blockIdx.x; back < tiles && ok; back += gridDim.x) {
-        const int64_t tile = tiles - 1 - back;
-        const TileKeys tk = tile_keys(a, s, tile, kRows);
-        const int64_t k0 = (int64_t)chunk * a.chunk;
-        if (chunk > 0 && k0 >= tk.end) continue;
-        const int64_t k1 = min(tk.end, k0 + a.chunk);
-        const int n = (int)((k1 - k0 + kKeys - 1) / kKeys);
-        const int uses = n * 2 * kParts;                        // of stages: per key tile its keys, then its values
-        if (again) {                                            // every arrival of the last tile has been waited for
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                for (int i = 0; i < kStages; ++i) { mbar_inval(smem_u32(&s_full_kv[i])); mbar_inval(smem_u32(&s_empty_kv[i])); }
-                for (int i = 0; i < kMetas; ++i) mbar_inval(smem_u32(&s_meta[i]));
-                for (int i = 0; i < 2; ++i) { mbar_inval(smem_u32(&s_s[i])); mbar_inval(smem_u32(&s_p[i])); }
-                mbar_inval(smem_u32(&s_o));
-                mbar_inval(smem_u32(&s_q));
-                init_barriers();
+    auto for_tiles = [&](auto body) {
+        for (int64_t back = blockIdx.x; back < tiles && ok; back += gridDim.x) {
+            const int64_t tile = tiles - 1 - back;
+            const TileKeys tk = tile_keys(a, s, tile, kRows);
+            const int64_t k0 = (int64_t)chunk * a.chunk;
+            if (chunk > 0 && k0 >= tk.end) continue;
+            const int64_t k1 = min(tk.end, k0 + a.chunk);
+            if (again) {                                        // every arrival of the last tile has been waited for
+                __syncthreads();
+                if (threadIdx.x == 0) {
+                    for (int i = 0; i < kStages; ++i) { mbar_inval(smem_u32(&s_full_kv[i])); mbar_inval(smem_u32(&s_empty_kv[i])); }
+                    for (int i = 0; i < kMetas; ++i) mbar_inval(smem_u32(&s_meta[i]));
+                    for (int i = 0; i < 2; ++i) { mbar_inval(smem_u32(&s_s[i])); mbar_inval(smem_u32(&s_p[i])); }
+                    mbar_inval(smem_u32(&s_o));
+                    mbar_inval(smem_u32(&s_q));
+                    init_barriers();
+                }
+                __syncthreads();
             }
+            again = true;
+            body(tile, tk.chunks <= 1, k0, k1, (int)((k1 - k0 + kKeys - 1) / kKeys));
             __syncthreads();
+            ok = s_abort == 0;
         }
-        again = true;
+    };
 
-        if (warp < 8) {
+    if (warp < 8) {
+        more_registers<kRegsSoftmax>();
+        for_tiles([&](int64_t tile, bool direct, int64_t k0, int64_t k1, int n) {
             // ================================================================ softmax
             const int mine = NT == 2 ? warp / 4 : 0;
             const int r = threadIdx.x % 128;
@@ -241,8 +277,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 for (int j = 0; j < n && ok; ++j) {
                     const int buf = NT == 2 ? mine : j & 1;
                     const uint32_t phase = NT == 2 ? j & 1 : (j >> 1) & 1;
-                    ok = mbar_wait_all(smem_u32(&s_s[buf]), phase, abort_flag, watchdog, kWdSoftmax) &&
-                         mbar_wait_all(smem_u32(&s_meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdSoftmax);
+                    ok = wait_all(smem_u32(&s_s[buf]), phase, abort_flag, watchdog, kWdSoftmax) &&
+                         wait_all(smem_u32(&s_meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdSoftmax);
                     if (!ok) break;
                     tc_fence_after();
                     const KeyMeta& meta = metas[j % kMetas];
@@ -255,24 +291,34 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                         seen[c] = meta.valid[c] & (x < 0 ? 0u : x >= 31 ? ~0u : (2u << x) - 1u);
                     }
                     const bool masked = __any_sync(0xffffffffu, (seen[0] & seen[1] & seen[2] & seen[3]) != ~0u);
-                    uint32_t v[64];
+                    uint32_t v[128];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, v + 32 * c);
+                    tmem_ld_wait();
                     // ---- the largest score
                     float top = -INFINITY;
+                    if (masked) {                                // (its own code: selects on every score cost a third of the loop)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        tmem_ld32(s_addr + 64 * h, v);
-                        tmem_ld32(s_addr + 64 * h + 32, v + 32);
-                        tmem_ld_wait();
-                        if (masked) {
-#pragma unroll
-                            for (int i = 0; i < 64; ++i) v[i] = (seen[2 * h + i / 32] >> (i % 32)) & 1 ? v[i] : 0xff800000u;
-                        }
-#pragma unroll
-                        for (int g = 0; g < 4; ++g) {
+                        for (int g = 0; g < 8; ++g) {
                             float x = -INFINITY;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) x = fmaxf(x, __uint_as_float(v[16 * g + i]));
-                            top = fmaxf(top, CACHED ? (x == -INFINITY ? x : x * (factor * meta.ks[4 * h + g])) : x);
+                            for (int i = 0; i < 16; ++i) {
+                                if (!((seen[g / 2] >> (16 * (g % 2) + i)) & 1)) v[16 * g + i] = 0xff800000u;
+                                x = fmaxf(x, __uint_as_float(v[16 * g + i]));
+                            }
+                            top = fmaxf(top, CACHED ? (x == -INFINITY ? x : x * (factor * meta.ks[g])) : x);
+                        }
+                    } else {
+#pragma unroll
+                        for (int g = 0; g < 8; ++g) {
+                            float x = -INFINITY, y = -INFINITY;
+#pragma unroll
+                            for (int i = 0; i < 16; i += 2) {
+                                x = fmaxf(x, __uint_as_float(v[16 * g + i]));
+                                y = fmaxf(y, __uint_as_float(v[16 * g + i + 1]));
+                            }
+                            x = fmaxf(x, y);
+                            top = fmaxf(top, CACHED ? x * (factor * meta.ks[g]) : x);
                         }
                     }
                     if (!CACHED) top = top == -INFINITY ? top : top * factor;
@@ -286,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                         l *= keep;
                         if (j > 0) {
                             if (NT == 1) {
-                                ok = mbar_wait_all(smem_u32(&s_o), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
+                                ok = wait_all(smem_u32(&s_o), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
                                 if (!ok) break;
                                 tc_fence_after();
                             }
@@ -306,32 +352,30 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     }
                     const float minus = base == -INFINITY ? 0.0f : -base;
                     // ---- probabilities, over the scores that they come from
+                    float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        tmem_ld32(s_addr + 64 * h, v);
-                        tmem_ld32(s_addr + 64 * h + 32, v + 32);
-                        tmem_ld_wait();
-                        uint32_t p[32];
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t p[16];
 #pragma unroll
-                        for (int g = 0; g < 4; ++g) {
-                            const float f = CACHED ? factor * meta.ks[4 * h + g] : factor;
-                            const float vf = CACHED ? meta.vf[4 * h + g] : 1.0f;
+                        for (int g = 2 * c; g < 2 * c + 2; ++g) {
+                            // (a masked score, -inf, needs a factor that is not 0 to give 2^-inf)
+                            const float f = fmaxf(CACHED ? factor * meta.ks[g] : factor, FLT_MIN);
+                            const float vf = CACHED ? meta.vf[g] : 1.0f;
 #pragma unroll
                             for (int i = 0; i < 16; i += 2) {
-                                float x = ex2(fmaf(__uint_as_float(v[16 * g + i]), f, minus)), y = ex2(fmaf(__uint_as_float(v[16 * g + i + 1]), f, minus));
-                                if (masked) {
-                                    const uint32_t bits = seen[2 * h + g / 2] >> (16 * (g % 2) + i);
-                                    x = bits & 1 ? x : 0.0f;
-                                    y = bits & 2 ? y : 0.0f;
-                                }
-                                l += x;
-                                l += y;
-                                p[8 * g + i / 2] = CACHED ? pack_half(x * vf, y * vf) : pack_bf16(x, y);
+                                float2 x = f2_fma(make_float2(__uint_as_float(v[16 * g + i]), __uint_as_float(v[16 * g + i + 1])), make_float2(f, f), make_float2(minus, minus));
+                                x.x = ex2(x.x);
+                                x.y = ex2(x.y);
+                                if (i & 2) sum1 = f2_add(sum1, x);
+                                else sum0 = f2_add(sum0, x);
+                                if (CACHED) x = f2_mul(x, make_float2(vf, vf));
+                                p[8 * (g % 2) + i / 2] = CACHED ? pack_half(x.x, x.y) : pack_bf16(x.x, x.y);
                             }
                         }
-                        tmem_st16(s_addr + 32 * h, p);
-                        tmem_st16(s_addr + 32 * h + 16, p + 16);
+                        tmem_st16(s_addr + 16 * c, p);
                     }
+                    sum0 = f2_add(sum0, sum1);
+                    l += sum0.x + sum0.y;
                     tmem_st_wait();
                     tc_fence_before();
                     __syncwarp();
@@ -339,12 +383,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 }
                 // ---- the rows' results
                 if (ok && n > 0) {
-                    if (NT == 1 && n > 1) ok = mbar_wait_all(smem_u32(&s_o), (n - 2) & 1, abort_flag, watchdog, kWdSoftmax);
-                    ok = ok && mbar_wait_all(smem_u32(&s_o), NT == 1 ? (n - 1) & 1 : 0, abort_flag, watchdog, kWdSoftmax);
+                    if (NT == 1 && n > 1) ok = wait_all(smem_u32(&s_o), (n - 2) & 1, abort_flag, watchdog, kWdSoftmax);
+                    ok = ok && wait_all(smem_u32(&s_o), NT == 1 ? (n - 1) & 1 : 0, abort_flag, watchdog, kWdSoftmax);
                     tc_fence_after();
                 }
                 if (ok) {
-                    const bool direct = tk.chunks <= 1;
                     const int64_t at = (token * a.q_heads + head) * a.chunks + chunk;
                     const float whole = CACHED ? power_of_two(e / 2) : 1.0f, rest = CACHED ? power_of_two(e - e / 2 - 7) : 1.0f;
                     const float inv = direct ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f;
@@ -379,8 +422,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     tc_fence_before();
                 }
             }
-        } else if (warp < 12) {
+        });
+    } else if (warp < 12) {
+        fewer_registers<kRegsOther>();
+        for_tiles([&](int64_t, bool, int64_t k0, int64_t k1, int n) {
             // ================================================================ keys and values
+            const int uses = n * 2 * kParts;                    // of stages: per key tile its keys, then its values
             const int w = warp - 8;
             if (!CACHED) {
                 constexpr int kLook = kStages == 8 ? 4 : 2;      // copies in flight beyond the stage that is handed over
@@ -451,30 +498,47 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     const int32_t id = (int32_t)ld_global_u32(table + key / P);
                     return id >= 0 && id < a.cache.pages ? id : -1;
                 };
-                uint4 codes[2][kUnits];
-                auto fetch = [&](int u, int32_t id, uint4* to) {
+                // A warp fills 32 rows (tokens) of a stage of keys, kCh / 4 rows (channels) of a stage of values.  A lane's row in
+                // every group of eight is lane / 4 -- eight lanes then store to two neighbouring rows, whose swizzles differ in
+                // the lowest bit, and meet all banks -- and its 16 codes of a 64-wide plane are the (lane % 4)th.
+                constexpr int kGroups[2] = {4, kCh / 32};        // of eight rows: keys, values
+                const int r8 = lane / 4, u4 = lane % 4;
+                const uint32_t lo = r8 * 128 + (((2 * u4) ^ r8) * 16), hi = r8 * 128 + (((2 * u4 + 1) ^ r8) * 16);
+                // Where a lane's codes of a stage lie: [0], [1] are the two groups of 16 keys, or the two planes of keys.  Codes that
+                // no product needs (no page, channels from D on) are read from where there is something, never from beyond.
+                const int8_t* src[2];
+                int step = 0, plane1 = 0;                        // bytes to the next group of rows; keys: to the second plane
+                auto locate = [&](int u, int32_t id) {
                     const int part = u % kParts;
                     if (u < kParts) {
-                        const int32_t ids[2] = {__shfl_sync(0xffffffffu, id, 2 * w), __shfl_sync(0xffffffffu, id, 2 * w + 1)};
-                        const int du = lane % kUnits;
+                        const int c = part * 128 + 16 * u4;
+                        step = 8 * D;
+                        plane1 = c + 64 < D ? 64 : 0;
 #pragma unroll
-                        for (int it = 0; it < kUnits; ++it) {
-                            const int x = it * (32 / kUnits) + lane / kUnits;          // token of the warp's 32
-                            const int32_t page = ids[it * 2 / kUnits];
-                            const bool take = page >= 0 && part * 128 + du * 16 < D;
-                            const int off = (16 * (2 * w + it * 2 / kUnits)) % P + x % 16;
-                            to[it] = ld_global_v4(a.cache.k + (((int64_t)(take ? page : 0) * a.kv_heads + hk) * P + off) * D + part * 128 + du * 16, take);
+                        for (int x = 0; x < 2; ++x) {
+                            const int32_t page = max(__shfl_sync(0xffffffffu, id, 2 * w + x), 0);
+                            src[x] = a.cache.k + (((int64_t)page * a.kv_heads + hk) * P + (16 * (2 * w + x)) % P + r8) * D + (c < D ? c : 0);
                         }
                     } else {
-                        const int off = (16 * (lane % 8)) % P;
+                        const int d = part * 128 + w * (kCh / 4) + r8;
+                        step = 8 * P;
 #pragma unroll
-                        for (int it = 0; it < kUnits; ++it) {
-                            const int d = part * 128 + w * (kCh / 4) + it * 4 + lane / 8;
-                            const bool take = id >= 0 && d < D;
-                            to[it] = ld_global_v4(a.cache.v + (((int64_t)(take ? id : 0) * a.kv_heads + hk) * D + d) * P + off, take);
+                        for (int x = 0; x < 2; ++x) {
+                            const int32_t page = max(__shfl_sync(0xffffffffu, id, u4 + 4 * x), 0);
+                            src[x] = a.cache.v + ((int64_t)page * a.kv_heads + hk) * D * P + (int64_t)d * P + (16 * (u4 + 4 * x)) % P;
                         }
                     }
                 };
+                auto load = [&](int u, int it) -> uint4 {
+                    if (u < kParts) {
+                        const int rg = it % 4, plane = it / 4;
+                        return ld_global_v4(src[rg / 2] + (rg % 2) * step + plane * plane1);
+                    }
+                    const int rg = it % kGroups[1], plane = it / kGroups[1];
+                    const int d = (u % kParts) * 128 + w * (kCh / 4) + r8 + 8 * rg;
+                    return ld_global_v4(d < D ? src[plane] + rg * step : a.cache.v);
+                };
+                uint4 codes[kUnits];                             // of the next stage, each loaded as its forerunner is stored
                 int32_t id = page_of(0), id1 = page_of(1), id2;
                 float ks = 0.0f, vs = 0.0f;
                 auto scales_of = [&](int32_t page, float* k, float* v) {
@@ -484,7 +548,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 int e = -127, use = 0;
                 if (n > 0) {
                     scales_of(id, &ks, &vs);
-                    fetch(0, id, codes[0]);
+#pragma unroll
+                    for (int it = 0; it < kUnits; ++it) {
+                        if (it == 0) locate(0, id);
+                        codes[it] = load(0, it);
+                    }
                 }
                 for (int j = 0; j < n && ok; ++j) {
                     id2 = page_of(j + 2);
@@ -492,8 +560,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     scales_of(id1, &ks1, &vs1);
 #pragma unroll
                     for (int u = 0; u < 2 * kParts; ++u, ++use) {
-                        if (u + 1 < 2 * kParts) fetch(u + 1, id, codes[(u + 1) & 1]);
-                        else fetch(0, id1, codes[0]);
                         if (use >= kStages) ok = mbar_wait_all_lazy(empty_kv(use), ((use / kStages) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
                         if (!ok) break;
                         if (u == 0) {
@@ -516,34 +582,22 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                             __syncwarp();
                             if (lane == 0) mbar_arrive(smem_u32(&s_meta[j % kMetas]));
                         }
-                        // 16 codes -> 32 bytes.  Lanes of the second plane write their halves the other way round: eight
-                        // lanes' 16-byte stores then meet all banks.
-                        const uint32_t dst = stage(use);
+                        const int next = u + 1 < 2 * kParts ? u + 1 : 0;
+                        locate(next, next ? id : id1);
+                        const uint32_t dst = stage(use) + (u < kParts ? 32 * w * 128 : w * (kCh / 4) * 128);
 #pragma unroll
                         for (int it = 0; it < kUnits; ++it) {
-                            const uint4 x = codes[u & 1][it];
+                            const int groups = kGroups[u < kParts ? 0 : 1];
+                            const uint32_t at = dst + (it / groups) * (u < kParts ? 16384 : kCh * 128) + (it % groups) * 1024;
+                            const uint4 x = codes[it];
+                            codes[it] = load(next, it);
                             uint32_t h[8];
                             widen(x.x, &h[0], &h[1]);
                             widen(x.y, &h[2], &h[3]);
                             widen(x.z, &h[4], &h[5]);
                             widen(x.w, &h[6], &h[7]);
-                            int row, unit;
-                            uint32_t plane;
-                            if (u < kParts) {
-                                row = 32 * w + it * (32 / kUnits) + lane / kUnits;
-                                unit = lane % kUnits;
-                                plane = 16384;
-                            } else {
-                                row = w * (kCh / 4) + it * 4 + lane / 8;
-                                unit = lane % 8;
-                                plane = kCh * 128;
-                            }
-                            const int second = unit / 4, c = (unit % 4) * 2;
-                            const uint32_t at = dst + second * plane + row * 128;
-                            const uint32_t lo = at + ((c ^ (row & 7)) * 16), hi = at + (((c + 1) ^ (row & 7)) * 16);
-                            const bool swap = second != 0;
-                            sts128(swap ? hi : lo, swap ? h[4] : h[0], swap ? h[5] : h[1], swap ? h[6] : h[2], swap ? h[7] : h[3]);
-                            sts128(swap ? lo : hi, swap ? h[0] : h[4], swap ? h[1] : h[5], swap ? h[2] : h[6], swap ? h[3] : h[7]);
+                            sts128(at + lo, h[0], h[1], h[2], h[3]);
+                            sts128(at + hi, h[4], h[5], h[6], h[7]);
                         }
                         fence_proxy_async_smem();
                         __syncwarp();
@@ -555,10 +609,15 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     vs = vs1;
                 }
             }
-        } else if (n > 0) {
+        });
+    } else {
+        fewer_registers<kRegsOther>();
+        for_tiles([&](int64_t, bool, int64_t, int64_t, int n) {
             // ================================================================ MMA issue
+            if (warp != 12 || n == 0) return;
+            const int uses = n * 2 * kParts;
             const uint32_t idesc_s = instr_desc_16(CACHED ? 0 : 1, false, kKeys), idesc_o = instr_desc_16(CACHED ? 0 : 1, !CACHED, kCh);
-            auto wait_kv = [&](int use) { return mbar_wait_all(full_kv(use), (use / kStages) & 1, abort_flag, watchdog, kWdMma); };
+            auto wait_kv = [&](int use) { return wait_all(full_kv(use), (use / kStages) & 1, abort_flag, watchdog, kWdMma); };
             auto scores = [&](int j, int i, int buf) {           // S[buf] = Q_i K_j^T
                 if (elect_one()) {
 #pragma unroll
@@ -594,7 +653,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 }
                 __syncwarp();
             };
-            ok = mbar_wait_all(smem_u32(&s_q), 0, abort_flag, watchdog, kWdMma);
+            ok = wait_all(smem_u32(&s_q), 0, abort_flag, watchdog, kWdMma);
             for (int p = 0; ok && p < kParts; ++p) ok = wait_kv(p);
             if (ok) {
                 tc_fence_after();
@@ -611,7 +670,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 }
                 for (int i = 0; i < NT && ok; ++i) {
                     const int buf = NT == 2 ? i : j & 1;
-                    ok = mbar_wait_all(smem_u32(&s_p[buf]), NT == 2 ? j & 1 : (j >> 1) & 1, abort_flag, watchdog, kWdMma);
+                    ok = wait_all(smem_u32(&s_p[buf]), NT == 2 ? j & 1 : (j >> 1) & 1, abort_flag, watchdog, kWdMma);
                     for (int p = 0; ok && i == 0 && p < kParts; ++p) ok = wait_kv(vuse + p);
                     if (!ok) break;
                     tc_fence_after();
@@ -630,9 +689,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 release(vuse);
                 if (NT == 2 && j + 1 < n) release(kuse);
             }
-        }
-        __syncthreads();
-        ok = s_abort == 0;
+        });
     }
     if (!ok && warp == 12) drain_after_abort();
     tc_fence_before();
@@ -646,6 +703,12 @@ cudaError_t launch(const Attention& a, cudaStream_t stream) {
     auto* kern = attention_tiles_kernel<DP, NT, CACHED>;
     uint32_t* watchdog = watchdog_device_ptr();
     if (!watchdog) return cudaErrorUnknown;
+    // (the softmax would wait for ever for registers that the launch does not bring)
+    static const bool enough = [&] {
+        cudaFuncAttributes f;
+        return cudaFuncGetAttributes(&f, reinterpret_cast<const void*>(kern)) == cudaSuccess && f.numRegs == kRegsLaunch;
+    }();
+    if (!enough) return cudaErrorUnknown;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), Shape<DP, NT>::kSmem);
     const dim3 grid((unsigned)row_tiles(a), (unsigned)a.chunks, (unsigned)(a.batch * a.kv_heads));
     return e != cudaSuccess ? e : launch_pdl3(kern, grid, kThreads, Shape<DP, NT>::kSmem, stream, a, watchdog);

@@ -29,7 +29,7 @@ Route plan(Attention& a) {
         a.tile_rows = a.max_q * a.group <= 16 ? 16 : 64;
     }
     const int64_t units = row_tiles(a) * a.batch * a.kv_heads;
-    const int64_t splits = ceil_div(wave, units > 0 ? units : 1);
+    const int64_t splits = route == Route::Tiles ? (units < wave ? wave / (units > 0 ? units : 1) : 1) : ceil_div(wave, units > 0 ? units : 1);
     int64_t chunk = ceil_div(ceil_div(a.max_kv, splits), 256) * 256;
     if (chunk < least) chunk = least;
     if (chunk > most) chunk = most;
@@ -125,7 +125,7 @@ fq_status fill_kv8(Attention& a, fq_dtype dt, int64_t q_rows, int q_heads, const
     if (st != FQ_OK) return st;
     a.dt = dt; a.q_rows = q_rows; a.q_heads = q_heads; a.kv_heads = cache->heads; a.head_dim = cache->head_dim; a.batch = batch;
     a.q_offsets = q_offsets; a.max_q = max_q; a.cached = true; a.cache = *cache; a.table_width = (int)table_width;
-    a.max_kv = table_width * cache->page;
+    a.max_kv = cache->pages > 0 ? table_width * cache->page : 0;
     if (max_kv < 0) return FQ_ERR_INVALID_ARG;
     if (max_kv > 0 && max_kv < a.max_kv) a.max_kv = max_kv;
     return check_heads(a);
