@@ -4,8 +4,9 @@
 // reads its keys once.  Per tile of 128 keys: S = Q K^T into TMEM; one thread per row keeps the running maximum and sum and
 // writes the probabilities, 16 bits each, over S in TMEM; O += P V takes them from there as its first operand.
 //   warps 0-7   softmax, a warpgroup per row tile
-//   warps 8-11  keys and values into 128-byte-swizzled stages of 128 keys x 64 or 128 channels
-//   warp 12     issues the MMAs (13-15 complete its warpgroup, whose registers go to the softmax)
+//   warps 8-11  which keys of a tile there are; from the cache, its codes into 128-byte-swizzled stages of 128 keys x 64 or 128 channels
+//   warp 12     issues the MMAs
+//   warp 13     rows: copies keys and values into the stages by TMA (14, 15 complete the warpgroup, whose registers go to the softmax)
 // With two row tiles (D <= 128) the tensor core works on one while the other's probabilities are computed; with one (D > 128,
 // or few rows) S is double-buffered instead.
 //
@@ -15,8 +16,8 @@
 // Cache: codes are widened to binary16, exactly, on their way into the stages (values keep tokens innermost and need no turn).
 // The scale of a page's keys multiplies S per 16 columns; that of its values multiplies the probabilities, over 2^e with e the
 // running exponent of the largest one: P = p vs 2^(7 - e) <= 2^15.  Queries: binary16 behind a power of two per row.
-// Rows: bf16 operands; a masked key's bytes are not read but replaced by zeros (cp.async with no source bytes), since 0 times a
-// masked NaN would reach the sums.
+// Rows: bf16 operands.  The scores of masked keys are replaced; their values are zeroed in shared memory, in the tiles that have
+// any, ahead of the product: 0 times a masked NaN would reach the sums.
 #include "act_common.cuh"
 #include "attention_common.cuh"
 #include "tc_sm100.cuh"
@@ -46,22 +47,27 @@ struct Shape {
     static constexpr int kQTile = 128 * DP * 2;
     static constexpr int kSmem = 1024 + NT * kQTile + kStages * kStageBytes;
     static constexpr int kOCol = 256;                           // S: columns 0 .. 255
+    // Two tiles of 64 channels leave TMEM for probabilities of their own (columns 384 ..): the next scores are computed as soon
+    // as the last ones have been read.  Elsewhere probabilities lie over their scores.
+    static constexpr bool kEarly = NT == 2 && DP == 64;
+    static constexpr bool kPerTile = NT == 1 || kEarly;         // every product of a tile signals its end
 };
 
 struct __align__(16) KeyMeta {
     float ks[8];                        // per 16 keys
-    float vf[8];
+    float lvf[8];                       // log2 of vs 2^(7 - e)
+    float inv[8];                       // 2^-lvf
     uint32_t valid[4];
     int e;
     int unused[3];
 };
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {        // zeros where !ok
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(c2), "r"(bar)
+        : "memory");
 }
-__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
@@ -79,10 +85,33 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 }
 __device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255) - 127; }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+__device__ __forceinline__ float max3(float x, uint32_t y, uint32_t z) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(__uint_as_float(y)), "f"(__uint_as_float(z)));
+    return r;
+}
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// 2^x of two values on the FMA pipe: 2^n by the exponent bits, 2^f on [-1/2, 1/2] by a polynomial of degree 4 (Remez, relative
+// error 2.7e-6 in binary32).  The exponential unit gives 16 values per clock and SM, a tile of 128 x 128 scores needs 1024
+// clocks of it; kPolynomial of eight pairs go here instead.
+constexpr int kPolynomial = 2;
+__device__ __forceinline__ float2 ex2_polynomial(float2 x) {
+    x.x = fmaxf(x.x, -126.0f);
+    x.y = fmaxf(x.y, -126.0f);
+    const float2 magic = make_float2(12582912.0f, 12582912.0f);             // 1.5 2^23: the sum's low bits are round(x)
+    const float2 t = f2_add(x, magic);
+    const float2 n = f2_add(t, make_float2(-12582912.0f, -12582912.0f));
+    const float2 f = f2_fma(n, make_float2(-1.0f, -1.0f), x);
+    float2 p = make_float2(0.009570102207362652f, 0.009570102207362652f);
+    p = f2_fma(p, f, make_float2(0.05591785907745361f, 0.05591785907745361f));
+    p = f2_fma(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
+    p = f2_fma(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
+    p = f2_fma(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
+    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)), __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* r) {
     asm volatile(
@@ -154,13 +183,16 @@ __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile
 }
 __device__ __forceinline__ void mbar_inval(uint32_t bar) { asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
 
+__device__ __forceinline__ bool all_valid(const KeyMeta& m) { return (m.valid[0] & m.valid[1] & m.valid[2] & m.valid[3]) == ~0u; }
+
 template <int DP, int NT, bool CACHED>
-__global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Attention a, uint32_t* watchdog) {
+__global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Attention a, const __grid_constant__ CUtensorMap map_k,
+                                                                      const __grid_constant__ CUtensorMap map_v, uint32_t* watchdog) {
     using S = Shape<DP, NT>;
     constexpr int kCh = S::kCh, kParts = S::kParts, kStages = S::kStages, kPlanes = kCh / 64;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(16) KeyMeta metas[kMetas];
-    __shared__ __align__(8) uint64_t s_full_kv[kStages], s_empty_kv[kStages], s_meta[kMetas], s_s[2], s_p[2], s_o, s_q;
+    __shared__ __align__(8) uint64_t s_full_kv[kStages], s_empty_kv[kStages], s_meta[kMetas], s_used[kMetas], s_landed, s_fixed, s_s[2], s_p[2], s_o[2], s_free[2], s_q;
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     volatile int* abort_flag = &s_abort;
@@ -172,11 +204,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     auto stage = [&](int n) { return ring + (uint32_t)(n % kStages) * S::kStageBytes; };
 
     auto init_barriers = [&]() {
-        for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&s_full_kv[i]), 4); mbar_init(smem_u32(&s_empty_kv[i]), 1); }
-        for (int i = 0; i < kMetas; ++i) mbar_init(smem_u32(&s_meta[i]), 4);
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&s_s[i]), 1); mbar_init(smem_u32(&s_p[i]), 4); }
-        mbar_init(smem_u32(&s_o), 1);
+        for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&s_full_kv[i]), CACHED ? 4 : 1); mbar_init(smem_u32(&s_empty_kv[i]), 1); }
+        for (int i = 0; i < kMetas; ++i) { mbar_init(smem_u32(&s_meta[i]), 4); mbar_init(smem_u32(&s_used[i]), 4 * NT + (CACHED ? 0 : 1)); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&s_s[i]), 1); mbar_init(smem_u32(&s_p[i]), 4); mbar_init(smem_u32(&s_o[i]), 1); mbar_init(smem_u32(&s_free[i]), 4); }
         mbar_init(smem_u32(&s_q), 4 * NT);
+        mbar_init(smem_u32(&s_landed), 1);
+        mbar_init(smem_u32(&s_fixed), 4);
         fence_mbarrier_init();
     };
     if (threadIdx.x == 0) {
@@ -210,10 +243,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 __syncthreads();
                 if (threadIdx.x == 0) {
                     for (int i = 0; i < kStages; ++i) { mbar_inval(smem_u32(&s_full_kv[i])); mbar_inval(smem_u32(&s_empty_kv[i])); }
-                    for (int i = 0; i < kMetas; ++i) mbar_inval(smem_u32(&s_meta[i]));
-                    for (int i = 0; i < 2; ++i) { mbar_inval(smem_u32(&s_s[i])); mbar_inval(smem_u32(&s_p[i])); }
-                    mbar_inval(smem_u32(&s_o));
+                    for (int i = 0; i < kMetas; ++i) { mbar_inval(smem_u32(&s_meta[i])); mbar_inval(smem_u32(&s_used[i])); }
+                    for (int i = 0; i < 2; ++i) { mbar_inval(smem_u32(&s_s[i])); mbar_inval(smem_u32(&s_p[i])); mbar_inval(smem_u32(&s_o[i])); mbar_inval(smem_u32(&s_free[i])); }
                     mbar_inval(smem_u32(&s_q));
+                    mbar_inval(smem_u32(&s_landed));
+                    mbar_inval(smem_u32(&s_fixed));
                     init_barriers();
                 }
                 __syncthreads();
@@ -282,7 +316,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     if (!ok) break;
                     tc_fence_after();
                     const KeyMeta& meta = metas[j % kMetas];
-                    const uint32_t s_addr = lanes + 128 * buf;
+                    const uint32_t s_addr = lanes + 128 * buf, p_addr = S::kEarly ? lanes + 384 + 64 * mine : s_addr;
                     const int lim = (int)min(max(limit64 - (k0 + (int64_t)j * kKeys), (int64_t)-1), (int64_t)kKeys);
                     uint32_t seen[4];
 #pragma unroll
@@ -295,6 +329,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, v + 32 * c);
                     tmem_ld_wait();
+                    if (S::kEarly) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&s_free[mine]));
+                    }
                     // ---- the largest score
                     float top = -INFINITY;
                     if (masked) {                                // (its own code: selects on every score cost a third of the loop)
@@ -313,15 +352,20 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                         for (int g = 0; g < 8; ++g) {
                             float x = -INFINITY, y = -INFINITY;
 #pragma unroll
-                            for (int i = 0; i < 16; i += 2) {
-                                x = fmaxf(x, __uint_as_float(v[16 * g + i]));
-                                y = fmaxf(y, __uint_as_float(v[16 * g + i + 1]));
+                            for (int i = 0; i < 16; i += 4) {
+                                x = max3(x, v[16 * g + i], v[16 * g + i + 1]);
+                                y = max3(y, v[16 * g + i + 2], v[16 * g + i + 3]);
                             }
                             x = fmaxf(x, y);
                             top = fmaxf(top, CACHED ? x * (factor * meta.ks[g]) : x);
                         }
                     }
                     if (!CACHED) top = top == -INFINITY ? top : top * factor;
+                    if (S::kEarly && j > 0) {                    // the last product has read its probabilities
+                        ok = wait_all(smem_u32(&s_o[mine]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
+                        if (!ok) break;
+                        tc_fence_after();
+                    }
                     // ---- a new base
                     const int now_e = CACHED ? meta.e : e;
                     const bool rise = top > base + kSlack || (base == -INFINITY && top > base);
@@ -332,7 +376,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                         l *= keep;
                         if (j > 0) {
                             if (NT == 1) {
-                                ok = wait_all(smem_u32(&s_o), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
+                                ok = wait_all(smem_u32(&s_o[0]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
                                 if (!ok) break;
                                 tc_fence_after();
                             }
@@ -353,6 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     const float minus = base == -INFINITY ? 0.0f : -base;
                     // ---- probabilities, over the scores that they come from
                     float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
+                    float total = 0.0f;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         uint32_t p[16];
@@ -360,31 +405,45 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                         for (int g = 2 * c; g < 2 * c + 2; ++g) {
                             // (a masked score, -inf, needs a factor that is not 0 to give 2^-inf)
                             const float f = fmaxf(CACHED ? factor * meta.ks[g] : factor, FLT_MIN);
-                            const float vf = CACHED ? meta.vf[g] : 1.0f;
+                            const float z = CACHED ? minus + meta.lvf[g] : minus;
 #pragma unroll
                             for (int i = 0; i < 16; i += 2) {
-                                float2 x = f2_fma(make_float2(__uint_as_float(v[16 * g + i]), __uint_as_float(v[16 * g + i + 1])), make_float2(f, f), make_float2(minus, minus));
-                                x.x = ex2(x.x);
-                                x.y = ex2(x.y);
+                                float2 x = f2_fma(make_float2(__uint_as_float(v[16 * g + i]), __uint_as_float(v[16 * g + i + 1])), make_float2(f, f), make_float2(z, z));
+                                if ((i / 2) % 8 < kPolynomial) x = ex2_polynomial(x);
+                                else x = make_float2(ex2(x.x), ex2(x.y));
                                 if (i & 2) sum1 = f2_add(sum1, x);
                                 else sum0 = f2_add(sum0, x);
-                                if (CACHED) x = f2_mul(x, make_float2(vf, vf));
                                 p[8 * (g % 2) + i / 2] = CACHED ? pack_half(x.x, x.y) : pack_bf16(x.x, x.y);
                             }
+                            if (CACHED) {
+                                sum0 = f2_add(sum0, sum1);
+                                total = fmaf(sum0.x + sum0.y, meta.inv[g], total);
+                                sum0 = sum1 = make_float2(0.0f, 0.0f);
+                            }
                         }
-                        tmem_st16(s_addr + 16 * c, p);
+                        tmem_st16(p_addr + 16 * c, p);
                     }
-                    sum0 = f2_add(sum0, sum1);
-                    l += sum0.x + sum0.y;
+                    if (!CACHED) {
+                        sum0 = f2_add(sum0, sum1);
+                        total = sum0.x + sum0.y;
+                    }
+                    l += total;
                     tmem_st_wait();
+                    // Every phase of s_o is waited for, so that none can pass unseen: the next one needs this warp's arrival below.
+                    if (NT == 1 && j > 0) {
+                        ok = wait_all(smem_u32(&s_o[0]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
+                        if (!ok) break;
+                    }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&s_p[buf]));
+                    if (lane == 0) {
+                        mbar_arrive(smem_u32(&s_p[buf]));
+                        mbar_arrive(smem_u32(&s_used[j % kMetas]));
+                    }
                 }
                 // ---- the rows' results
                 if (ok && n > 0) {
-                    if (NT == 1 && n > 1) ok = wait_all(smem_u32(&s_o), (n - 2) & 1, abort_flag, watchdog, kWdSoftmax);
-                    ok = ok && wait_all(smem_u32(&s_o), NT == 1 ? (n - 1) & 1 : 0, abort_flag, watchdog, kWdSoftmax);
+                    ok = wait_all(smem_u32(&s_o[S::kPerTile ? mine : 0]), S::kPerTile ? (n - 1) & 1 : 0, abort_flag, watchdog, kWdSoftmax);
                     tc_fence_after();
                 }
                 if (ok) {
@@ -430,64 +489,36 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             const int uses = n * 2 * kParts;                    // of stages: per key tile its keys, then its values
             const int w = warp - 8;
             if (!CACHED) {
-                constexpr int kLook = kStages == 8 ? 4 : 2;      // copies in flight beyond the stage that is handed over
-                constexpr int kPerRow = kCh / 8;                 // 16-byte units
-                int done = 0, use = 0;
-                uint32_t word = 0;
+                int mends = 0;
                 for (int j = 0; j < n && ok; ++j) {
-                    const int64_t key = k0 + (int64_t)j * kKeys + 32 * w;
-#pragma unroll
-                    for (int u = 0; u < 2 * kParts; ++u, ++use) {
-                        const bool values = u >= kParts;
-                        const int part = u % kParts;
-                        if (use >= kStages) {
-                            const uint32_t phase = ((use / kStages) & 1) ^ 1;
-                            const bool free = __all_sync(0xffffffffu, mbar_test_wait(empty_kv(use), phase));
-                            // What frees a stage may be waiting for the copies in flight: they are handed over ahead of the wait.
-                            if (!free && done < use) {
-                                cp_wait<0>();
-                                fence_proxy_async_smem();
-                                __syncwarp();
-                                for (; done < use; ++done)
-                                    if (lane == 0) mbar_arrive(full_kv(done));
-                            }
-                            ok = mbar_wait_all_lazy(empty_kv(use), phase, abort_flag, watchdog, kWdProducer, free);
-                        }
-                        if (!ok) break;
-                        if (u == 0) {
-                            const KeyPlace p = key_place<false>(a, s, b, hk, key + lane, k1);
-                            word = __ballot_sync(0xffffffffu, p.valid);
-                            if (lane == 0) {
-                                metas[j % kMetas].valid[w] = word;
-                                mbar_arrive(smem_u32(&s_meta[j % kMetas]));
-                            }
-                        }
-                        const int64_t ld = values ? a.ldv : a.ldk;
-                        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(values ? a.v : a.k) + (s.k0 + key) * ld + (int64_t)hk * D + part * 128;
-                        const uint32_t dst = stage(use) + 32 * w * 128;
-                        const int c = lane % kPerRow;
-                        const bool in = part * 128 + c * 8 < D;
-#pragma unroll
-                        for (int it = 0; it < kPerRow; ++it) {
-                            const int x = it * (32 / kPerRow) + lane / kPerRow;        // row of the warp's 32
-                            const bool take = in && ((word >> x) & 1);
-                            cp_async16(dst + (c / 8) * 16384 + x * 128 + (((c % 8) ^ (x & 7)) * 16), take ? static_cast<const void*>(src + x * ld + c * 8) : a.k, take);
-                        }
-                        cp_commit();
-                        if (use - done >= kLook) {
-                            cp_wait<kLook>();
-                            fence_proxy_async_smem();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(full_kv(done));
-                            ++done;
-                        }
+                    KeyMeta& meta = metas[j % kMetas];
+                    if (j >= kMetas) ok = mbar_wait_all_lazy(smem_u32(&s_used[j % kMetas]), ((j / kMetas) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
+                    if (!ok) break;
+                    const KeyPlace p = key_place<false>(a, s, b, hk, k0 + (int64_t)j * kKeys + 32 * w + lane, k1);
+                    const uint32_t word = __ballot_sync(0xffffffffu, p.valid);
+                    if (lane == 0) {
+                        meta.valid[w] = word;
+                        mbar_arrive(smem_u32(&s_meta[j % kMetas]));
                     }
+                    ok = wait_all(smem_u32(&s_meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdProducer);
+                    if (!ok) break;
+                    if (all_valid(meta)) continue;
+                    // Zeros for the values of masked keys, the lanes across a row: the MMA warp, which sees the same words, says when
+                    // the values are there and waits for the mending.  (The stages' own barriers cannot say it to a warp that looks
+                    // at some of their phases only.)
+                    ok = wait_all(smem_u32(&s_landed), mends & 1, abort_flag, watchdog, kWdProducer);
+                    if (!ok) break;
+                    ++mends;
+                    for (int part = 0; part < kParts; ++part)
+                        for (uint32_t gone = ~word; gone; gone &= gone - 1) {
+                            const uint32_t row = stage(2 * kParts * j + kParts + part) + (32 * w + __ffs(gone) - 1) * 128;
+#pragma unroll
+                            for (int plane = 0; plane < kPlanes; ++plane) sts32(row + plane * 16384 + lane * 4, 0u);
+                        }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&s_fixed));
                 }
-                cp_wait<0>();
-                fence_proxy_async_smem();
-                __syncwarp();
-                for (; ok && done < uses; ++done)
-                    if (lane == 0) mbar_arrive(full_kv(done));
             } else {
                 constexpr int kUnits = kCh / 16;                 // 16-byte units of codes per lane and stage
                 const int P = a.cache.page;
@@ -563,6 +594,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                         if (use >= kStages) ok = mbar_wait_all_lazy(empty_kv(use), ((use / kStages) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
                         if (!ok) break;
                         if (u == 0) {
+                            if (j >= kMetas) ok = mbar_wait_all_lazy(smem_u32(&s_used[j % kMetas]), ((j / kMetas) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
+                            if (!ok) break;
                             int top = vs > 0.0f ? exponent_of(vs) + 1 : -127;
 #pragma unroll
                             for (int x = 1; x < 8; x <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, x));
@@ -573,7 +606,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                             const uint32_t word = __ballot_sync(0xffffffffu, page >= 0 && key < k1);
                             if (lane / 2 == w) {                 // lanes 2 w, 2 w + 1: the warp's two groups of 16 keys
                                 meta.ks[lane] = ks;
-                                meta.vf[lane] = vs * power_of_two(-e / 2) * power_of_two(7 - e + e / 2);
+                                // (values of scale 0 keep a probability, which the sum gets back by `inv` and binary16 rounds to 0)
+                                const float lvf = log2f(fmaxf(vs * power_of_two(-e / 2) * power_of_two(7 - e + e / 2), 0x1p-60f));
+                                meta.lvf[lane] = lvf;
+                                meta.inv[lane] = exp2f(-lvf);
                             }
                             if (lane == 0) {
                                 meta.valid[w] = word;
@@ -612,10 +648,30 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
         });
     } else {
         fewer_registers<kRegsOther>();
-        for_tiles([&](int64_t, bool, int64_t, int64_t, int n) {
+        for_tiles([&](int64_t, bool, int64_t k0, int64_t, int n) {
+            const int uses = n * 2 * kParts;
+            if (!CACHED && warp == 13) {
+                // ============================================================ TMA: keys, values, keys, ..
+                for (int use = 0; use < uses && ok; ++use) {
+                    if (use >= kStages) ok = mbar_wait_all_lazy(empty_kv(use), ((use / kStages) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
+                    if (!ok) break;
+                    const int j = use / (2 * kParts), u = use % (2 * kParts), part = u % kParts;
+                    const CUtensorMap* map = u < kParts ? &map_k : &map_v;
+                    const int row = (int)(s.k0 + k0 + (int64_t)j * kKeys);
+                    if (elect_one()) {
+                        mbar_arrive_expect_tx(full_kv(use), S::kStageBytes);
+#pragma unroll
+                        for (int plane = 0; plane < kPlanes; ++plane)
+                            tma_load_3d(stage(use) + plane * 16384, map, part * 128 + plane * 64, hk, row, full_kv(use));
+                    }
+                    __syncwarp();
+                }
+                if (!ok && lane == 0) drain_after_abort();
+                return;
+            }
             // ================================================================ MMA issue
             if (warp != 12 || n == 0) return;
-            const int uses = n * 2 * kParts;
+            int mends = 0;                                      // tiles with masked keys so far
             const uint32_t idesc_s = instr_desc_16(CACHED ? 0 : 1, false, kKeys), idesc_o = instr_desc_16(CACHED ? 0 : 1, !CACHED, kCh);
             auto wait_kv = [&](int use) { return wait_all(full_kv(use), (use / kStages) & 1, abort_flag, watchdog, kWdMma); };
             auto scores = [&](int j, int i, int buf) {           // S[buf] = Q_i K_j^T
@@ -640,7 +696,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                         for (int k = 0; k < 8; ++k) {
                             const uint32_t v = stage(2 * kParts * j + kParts + p);
                             const uint64_t desc = CACHED ? smem_desc_sw128(v + (k / 4) * (kCh * 128) + (k % 4) * 32) : smem_desc_n_major(v + k * 2048);
-                            mma_f16_ts(tmem + S::kOCol + i * DP + p * 128, tmem + 128 * buf + 8 * k, desc, idesc_o, j > 0 || k > 0);
+                            mma_f16_ts(tmem + S::kOCol + i * DP + p * 128, tmem + (S::kEarly ? 384 + 64 * i : 128 * buf) + 8 * k, desc, idesc_o, j > 0 || k > 0);
                         }
                 }
                 __syncwarp();
@@ -662,32 +718,48 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             }
             for (int j = 0; j < n && ok; ++j) {
                 const int vuse = 2 * kParts * j + kParts, kuse = 2 * kParts * (j + 1);
-                if (NT == 1 && j + 1 < n) {
+                if ((NT == 1 || S::kEarly) && j + 1 < n) {
                     for (int p = 0; ok && p < kParts; ++p) ok = wait_kv(kuse + p);
+                    for (int i = 0; i < NT && ok; ++i) {
+                        if (S::kEarly) ok = wait_all(smem_u32(&s_free[i]), j & 1, abort_flag, watchdog, kWdMma);
+                        if (!ok) break;
+                        tc_fence_after();
+                        scores(j + 1, i, NT == 1 ? (j + 1) & 1 : i);
+                    }
                     if (!ok) break;
-                    scores(j + 1, 0, (j + 1) & 1);
                     release(kuse);
                 }
                 for (int i = 0; i < NT && ok; ++i) {
                     const int buf = NT == 2 ? i : j & 1;
                     ok = wait_all(smem_u32(&s_p[buf]), NT == 2 ? j & 1 : (j >> 1) & 1, abort_flag, watchdog, kWdMma);
                     for (int p = 0; ok && i == 0 && p < kParts; ++p) ok = wait_kv(vuse + p);
+                    if (!CACHED && ok && i == 0) {
+                        ok = wait_all(smem_u32(&s_meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdMma);
+                        const bool clean = all_valid(metas[j % kMetas]);
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(&s_used[j % kMetas]));
+                        if (!clean && ok) {
+                            if (lane == 0) mbar_arrive(smem_u32(&s_landed));
+                            ok = wait_all(smem_u32(&s_fixed), mends & 1, abort_flag, watchdog, kWdMma);
+                            ++mends;
+                        }
+                    }
                     if (!ok) break;
                     tc_fence_after();
                     products(j, i, buf);
-                    if (NT == 2 && j + 1 < n) {
+                    if (S::kPerTile || (j + 1 == n && i + 1 == NT)) {
+                        if (elect_one()) mma_commit(smem_u32(&s_o[S::kPerTile ? i : 0]));
+                        __syncwarp();
+                    }
+                    if (NT == 2 && !S::kEarly && j + 1 < n) {
                         for (int p = 0; ok && i == 0 && p < kParts; ++p) ok = wait_kv(kuse + p);
                         if (!ok) break;
                         scores(j + 1, i, i);
                     }
                 }
                 if (!ok) break;
-                if (NT == 1 || j + 1 == n) {
-                    if (elect_one()) mma_commit(smem_u32(&s_o));
-                    __syncwarp();
-                }
                 release(vuse);
-                if (NT == 2 && j + 1 < n) release(kuse);
+                if (NT == 2 && !S::kEarly && j + 1 < n) release(kuse);
             }
         });
     }
@@ -710,8 +782,18 @@ cudaError_t launch(const Attention& a, cudaStream_t stream) {
     }();
     if (!enough) return cudaErrorUnknown;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), Shape<DP, NT>::kSmem);
+    if (e != cudaSuccess) return e;
+    CUtensorMap map_k = {}, map_v = {};
+    if (!CACHED && a.kv_rows > 0) {                             // channels of a head, heads, rows
+        const uint64_t dims[3] = {(uint64_t)a.head_dim, (uint64_t)a.kv_heads, (uint64_t)a.kv_rows};
+        const uint32_t box[3] = {64, 1, kKeys};
+        const uint64_t head = (uint64_t)a.head_dim * 2, sk[2] = {head, (uint64_t)a.ldk * 2}, sv[2] = {head, (uint64_t)a.ldv * 2};
+        if (!encode_tiled(&map_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, a.k, dims, sk, box, CU_TENSOR_MAP_SWIZZLE_128B) ||
+            !encode_tiled(&map_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, a.v, dims, sv, box, CU_TENSOR_MAP_SWIZZLE_128B))
+            return cudaErrorUnknown;
+    }
     const dim3 grid((unsigned)row_tiles(a), (unsigned)a.chunks, (unsigned)(a.batch * a.kv_heads));
-    return e != cudaSuccess ? e : launch_pdl3(kern, grid, kThreads, Shape<DP, NT>::kSmem, stream, a, watchdog);
+    return launch_pdl3(kern, grid, kThreads, Shape<DP, NT>::kSmem, stream, a, map_k, map_v, watchdog);
 }
 template <bool CACHED>
 cudaError_t by_width(const Attention& a, cudaStream_t stream) {

@@ -5,8 +5,8 @@ Bounds (u = 2^-24, the half step of binary32; h = half a step of the output's ty
   rope       sum of squares, root, gain, angle, sine, product: at most 32 roundings of u on a pair's |a| + |b|, then h |y|
   append     codes equal (each is the rounding of an exact quotient), scales within u
   attention  a score is off by at most (D + 8) u A, A = scale max_j sum_d |q_d k_jd|, which scales a probability by e^(that);
-             numerator and denominator each: 2 ((D + 8) u A) + (L + 16) u; rounded probabilities add 2^-8 (bf16) or 2^-11
-             (binary16) of W = sum_j p_j |v_j|; then h |y|.  A probability beside the largest, 1, may underflow: each of L
+             numerator and denominator each: 2 ((D + 8) u A) + (L + 16) u; bf16 calls may take the exponential to 2^-18,
+             and their rounded probabilities add 2^-8 (bf16) or 2^-11 (binary16) of W = sum_j p_j |v_j|; then h |y|.  A probability beside the largest, 1, may underflow: each of L
              terms loses at most 2^-25 (binary16, whose numbers below 2^-14 are multiples of 2^-24) or 2^-126 of V = max_j |v_j|
 """
 import math
@@ -300,7 +300,7 @@ def attention_reference(q, k, v, scale, seen):
 
 def assert_attention(got, want, A, W, V, L, rounded):
     D = want.shape[-1]
-    bound = (2 * (2 * (D + 8) * U * A + (L + 16) * U) + rounded) * W + HALF[got.dtype] * want.abs()
+    bound = (2 * (2 * (D + 8) * U * A + (L + 16) * U + (2.0 ** -18 if rounded else 0.0)) + rounded) * W + HALF[got.dtype] * want.abs()
     bound = bound + L * (2.0 ** -25 if rounded == 2.0 ** -11 else 2.0 ** -126) * V
     off = (got.double().view_as(want) - want).abs()
     assert torch.isfinite(got).all()
