@@ -1,8 +1,8 @@
 // Attention of a few queries -- at most 16 (token, head of a group) rows a kv head, a decoding step -- over the 8-bit cache.
 //
 // Bound by the cache's bytes, so everything serves the loads: no thread waits for another on the way from memory to the
-// matrix instructions.  Each lane copies (cp.async, 16 bytes) exactly the bytes that it will multiply into slots of its own,
-// three half tiles deep, and waits for nothing but its own copies: no barrier until the end of a chunk.
+// matrix instructions.  Each lane copies (cp.async, 16 bytes) exactly the bytes that it will multiply into slots of its own, in
+// pieces of 64 tokens x 64 channels four ahead, and waits for nothing but its own copies: no barrier until the end of a chunk.
 //
 // The products run transposed, S^T = K Q^T and O^T = V^T P^T: the cache's operand then fills the 16 rows of a warp-level MMA
 // (m16n8k16, binary16 in, binary32 out) and the few queries its 8 columns, with no row idle at one query of a group of eight.
@@ -12,8 +12,8 @@
 // four.  Queries are divided by the power of two below their row's largest channel and rounded to binary16 (bf16 values
 // keep all their bits above 2^-14 of the row's largest channel; binary32 queries and probabilities go as a sum of two terms).
 //
-// With p = 2^(s - m): l = sum p, O = sum (p vs 2^(14 - e)) code, e the running exponent of the largest value scale vs.  The factor
-// 2^14 keeps probabilities down to 2^-28 among binary16's normal numbers.
+// With p = 2^(s - m): l = sum p, O = sum (p vs 2^(7 - e)) code, e the running exponent of the largest value scale vs.  m follows the
+// maximum lazily, when it has risen by more than 2^8: probabilities stay below 2^15 and, down to 2^-21, normal in binary16.
 #include "attention_common.cuh"
 
 #include <cuda_fp16.h>
@@ -22,15 +22,10 @@ namespace fq {
 namespace {
 
 constexpr int kTile = 64;               // tokens
-constexpr int kSlots = 3;
-
-template <int DP>
-struct Shape {
-    static constexpr int kWarps = DP == 256 ? 2 : 4;
-    static constexpr int kUnits = DP / 8;                       // 16-byte units per lane and half tile
-    static constexpr int kSlotBytes = kUnits * 512;             // per warp
-    static constexpr int kRing = kWarps * kSlots * kSlotBytes;
-};
+constexpr int kSlots = 4;
+constexpr int kPiece = 4096;            // 64 tokens x 64 channels: eight 16-byte units per lane
+constexpr int kWarps = 4;
+constexpr float kSlack = 8.0f;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {        // zeros where !ok
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
@@ -69,80 +64,73 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t w) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(w));
     return r;
 }
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 __device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255) - 127; }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
 
-template <typename T, int DP, int NQ>
-__global__ void __launch_bounds__(Shape<DP>::kWarps * 32) attention_tokens_kernel(const Attention a) {
-    using S = Shape<DP>;
+template <typename T, int DP, int NQ, bool EXACT>
+__global__ void __launch_bounds__(kWarps * 32, NQ == 1 && sizeof(T) == 2 && DP <= 128 ? 3 : 2) attention_tokens_kernel(const Attention a) {
     constexpr int kTerms = sizeof(T) == 4 ? 2 : 1;              // binary16 terms of a query or probability
-    constexpr int kLines = DP / 64;                             // 64-channel lines of a key
+    constexpr int kLines = DP / 64;                             // 64-channel lines of a key, and of values
     constexpr int kRows = 8 * NQ;
     extern __shared__ __align__(128) uint8_t smem[];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
     griddep_wait();
     const int b = blockIdx.z / a.kv_heads, hk = blockIdx.z % a.kv_heads, chunk = blockIdx.y;
     const Sequence s = sequence_of(a, b);
-    const int D = a.head_dim, P = a.cache.page;
+    const int D = EXACT ? DP : a.head_dim, P = a.cache.page, shift = 31 - __clz(P);
+    const int page_bytes = P * D, pages = (int)min(a.cache.pages, (int64_t)0x7fffffff);
     const int32_t* table = a.table + b * a.ld_table;
-    const uint32_t ring = smem_u32(smem) + warp * (kSlots * S::kSlotBytes) + lane * 16;
+    const uint32_t ring = smem_u32(smem) + warp * (kSlots * kPiece) + lane * 16;
 
     for (int64_t tile = blockIdx.x; tile * kRows < s.queries * a.group; tile += gridDim.x) {
         const TileKeys tk = tile_keys(a, s, tile, kRows);
-        const int64_t k0 = (int64_t)chunk * a.chunk;
-        if (chunk > 0 && k0 >= tk.end) continue;
-        const int64_t k1 = min(tk.end, k0 + a.chunk);
-        const int tiles = (int)((k1 - k0 + kTile - 1) / kTile);
-        const int mine = tiles > warp ? (tiles - warp + S::kWarps - 1) / S::kWarps : 0;
+        if (chunk > 0 && (int64_t)chunk * a.chunk >= tk.end) continue;
+        // (a sequence has fewer than 2^31 keys)
+        const int k0 = chunk * a.chunk, k1 = (int)min(tk.end, (int64_t)k0 + a.chunk);
+        const int tiles = (k1 - k0 + kTile - 1) / kTile;
+        const int mine = tiles > warp ? (tiles - warp + kWarps - 1) / kWarps : 0;
+        auto first_key = [&](int n) { return k0 + (warp + n * kWarps) * kTile; };
 
-        // ---- pages: a lane looks up the one of tokens 16 (lane % 4) .. of a tile, -1 where there is none
-        auto page_of = [&](int n) -> int32_t {
-            const int64_t j = k0 + (int64_t)(warp + n * S::kWarps) * kTile + 16 * t;
+        // ---- pages: a lane looks up (page, head) of keys 16 (lane % 4) .. of a tile, -1 where there is none
+        auto page_of = [&](int n) -> int {
+            const int j = first_key(n) + 16 * t;
             if (n >= mine || j >= k1) return -1;
-            const int32_t id = (int32_t)ld_global_u32(table + j / P);
-            return id >= 0 && id < a.cache.pages ? id : -1;
+            const int id = (int)ld_global_u32(table + (j >> shift));
+            return id >= 0 && id < pages ? id * a.kv_heads + hk : -1;
         };
-        auto offset_of = [&](int n, int sub) { return (int)((k0 + (int64_t)(warp + n * S::kWarps) * kTile + 16 * sub) % P); };
-        auto copy_keys = [&](int n, int32_t id_t, int slot) {
-            const int32_t id = __shfl_sync(0xffffffffu, id_t, g >> 1);
-            const bool ok = id >= 0;
-            const int8_t* src = a.cache.k + (((int64_t)(ok ? id : 0) * a.kv_heads + hk) * P + offset_of(n, g >> 1) + (g & 1)) * D + 16 * t;
-            const uint32_t dst = ring + slot * S::kSlotBytes;
+        // Copies of piece u of tile n: lines of keys, rows 16 (g / 2) + (g & 1) + 0, 2, 4, .. 14, then 64 rows of values.
+        auto copy = [&](int u, int n, int at_t, int slot) {
+            const uint32_t dst = ring + slot * kPiece;
+            if (u < kLines) {
+                const int at = __shfl_sync(0xffffffffu, at_t, g >> 1);
+                const bool ok = at >= 0 && (EXACT || 64 * u + 16 * t < D);
+                const int8_t* src = a.cache.k + (int64_t)at * page_bytes + ((first_key(n) + 16 * (g >> 1)) & (P - 1)) * D + (g & 1) * D + 16 * t + 64 * u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                for (int x = 0; x < 8; ++x) cp_async16(dst + x * 512, ok ? src + 2 * x * D : a.cache.k, ok);
+            } else {
+                const int d = 64 * (u - kLines) + g;
+                const int8_t* src = a.cache.v + (int64_t)at_t * page_bytes + d * P + ((first_key(n) + 16 * t) & (P - 1));
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
-#pragma unroll
-                    for (int j = 0; j < kLines; ++j)
-                        cp_async16(dst + ((i * 2 + r) * kLines + j) * 512, ok && 64 * j + 16 * t < D ? src + (4 * i + 2 * r) * D + 64 * j : a.cache.k, ok && 64 * j + 16 * t < D);
-            cp_commit();
-        };
-        auto copy_values = [&](int n, int32_t id, int slot) {
-            const bool ok = id >= 0;
-            const int8_t* src = a.cache.v + (((int64_t)(ok ? id : 0) * a.kv_heads + hk) * D + g) * P + offset_of(n, t);
-            const uint32_t dst = ring + slot * S::kSlotBytes;
-#pragma unroll
-            for (int j = 0; j < DP / 8; ++j) {                  // rows 8 j + g
-                const bool in = ok && 8 * j + g < D;
-                cp_async16(dst + j * 512, in ? src + (int64_t)(8 * j) * P : a.cache.v, in);
+                for (int x = 0; x < 8; ++x) {
+                    const bool ok = at_t >= 0 && (EXACT || d + 8 * x < D);
+                    cp_async16(dst + x * 512, ok ? src + 8 * x * P : a.cache.v, ok);
+                }
             }
             cp_commit();
         };
         // Scales of this lane's tokens, those of the 16 behind 16 (g / 2).
-        auto scales_of = [&](int32_t id_t, float* ks, float* vs) {
-            const int32_t id = __shfl_sync(0xffffffffu, id_t, g >> 1);
-            *ks = id >= 0 ? ld_global_f32(a.cache.k_scale + (int64_t)id * a.kv_heads + hk) : 0.0f;
-            *vs = id >= 0 ? ld_global_f32(a.cache.v_scale + (int64_t)id * a.kv_heads + hk) : 0.0f;
+        auto scales_of = [&](int at_t, float* ks, float* vs) {
+            const int at = __shfl_sync(0xffffffffu, at_t, g >> 1);
+            *ks = at >= 0 ? ld_global_f32(a.cache.k_scale + at) : 0.0f;
+            *vs = at >= 0 ? ld_global_f32(a.cache.v_scale + at) : 0.0f;
         };
 
-        int32_t id0 = page_of(0), id1 = page_of(1), id2;
-        int slot = 0;
-        copy_keys(0, id0, 0);
-        copy_values(0, id0, 1);
-        copy_keys(1, id1, 2);
-        float ks, vs;
-        scales_of(id0, &ks, &vs);
-
+        int at0 = page_of(0), at1 = page_of(1), at2 = page_of(2);
         // ---- queries: column g of the n-tiles, channels 64 j + 16 t .. + 15
         uint32_t q[NQ][kTerms][kLines * 8];
         float factor[NQ][2];                                    // of scores in columns 2 t, 2 t + 1, the scale of the keys apart
@@ -159,8 +147,13 @@ __global__ void __launch_bounds__(Shape<DP>::kWarps * 32) attention_tokens_kerne
                     float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                     if (ok && 64 * j + 16 * t < D) v = load4(src + 64 * j + 4 * x);
                     f[j * 16 + 4 * x] = v.x; f[j * 16 + 4 * x + 1] = v.y; f[j * 16 + 4 * x + 2] = v.z; f[j * 16 + 4 * x + 3] = v.w;
-                    top = fmaxf(fmaxf(fmaxf(top, fabsf(v.x)), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w)));
                 }
+            if (nq == 0) {                                      // (behind the first queries' loads)
+#pragma unroll
+                for (int u = 0; u < kSlots; ++u) copy(u % (2 * kLines), u / (2 * kLines), u < 2 * kLines ? at0 : at1, u);
+            }
+#pragma unroll
+            for (int x = 0; x < kLines * 16; ++x) top = fmaxf(top, fabsf(f[x]));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const int e = min(max(exponent_of(top), -100), 126);
@@ -178,14 +171,20 @@ __global__ void __launch_bounds__(Shape<DP>::kWarps * 32) attention_tokens_kerne
 #pragma unroll
             for (int c = 0; c < 2; ++c) factor[nq][c] = __shfl_sync(0xffffffffu, mul, (2 * t + c) * 4);
         }
-        int64_t limit[NQ][2];
+        float ks, vs;
+        scales_of(at0, &ks, &vs);
+        int limit[NQ][2], least = k1 - 1;                       // last keys that the columns see
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) limit[nq][c] = min(row_limit(a, s, tile * kRows + 8 * nq + 2 * t + c), k1 - 1);
+            for (int c = 0; c < 2; ++c) {
+                limit[nq][c] = (int)min(max(row_limit(a, s, tile * kRows + 8 * nq + 2 * t + c), (int64_t)-1), (int64_t)k1 - 1);
+                least = min(least, limit[nq][c]);
+            }
+        least = __reduce_min_sync(0xffffffffu, least);
 
         float o[NQ][DP / 16][4], m[NQ][2], l[NQ][2];
-        int e = -127;                                           // O carries 2^(14 - e)
+        int e = -127;                                           // O carries 2^(7 - e)
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq) {
 #pragma unroll
@@ -195,9 +194,17 @@ __global__ void __launch_bounds__(Shape<DP>::kWarps * 32) attention_tokens_kerne
 #pragma unroll
                 for (int x = 0; x < 4; ++x) o[nq][d][x] = 0.0f;
         }
+        int piece = 0;
+#pragma unroll 1
         for (int n = 0; n < mine; ++n) {
-            id2 = page_of(n + 2);
-            cp_wait<2>();
+            const int at3 = page_of(n + 3);
+            float ks1, vs1;
+            scales_of(at1, &ks1, &vs1);
+            // The slot of piece u is free: it takes the piece four behind.
+            auto refill = [&](int u, int slot) {
+                const int v = (u + kSlots) % (2 * kLines), ahead = (u + kSlots) / (2 * kLines);
+                copy(v, n + ahead, ahead == 0 ? at0 : ahead == 1 ? at1 : at2, slot);
+            };
             // ---- S^T: m-tile i holds tokens 16 (g/2) + 4 i + (g & 1), and those + 2
             float sc[NQ][4][4];
 #pragma unroll
@@ -206,12 +213,14 @@ __global__ void __launch_bounds__(Shape<DP>::kWarps * 32) attention_tokens_kerne
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int x = 0; x < 4; ++x) sc[nq][i][x] = 0.0f;
-            const uint32_t ksrc = ring + slot * S::kSlotBytes;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int j = 0; j < kLines; ++j) {
+                cp_wait<kSlots - 1>();
+                const int slot = kLines == 1 ? piece & (kSlots - 1) : j % kSlots;
+                const uint32_t src = ring + slot * kPiece;
 #pragma unroll
-                for (int j = 0; j < kLines; ++j) {
-                    const uint4 x = lds_v4(ksrc + ((i * 2) * kLines + j) * 512), y = lds_v4(ksrc + ((i * 2 + 1) * kLines + j) * 512);
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 x = lds_v4(src + (2 * i) * 512), y = lds_v4(src + (2 * i + 1) * 512);
                     const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                     for (int st = 0; st < 4; ++st) {
@@ -225,46 +234,56 @@ __global__ void __launch_bounds__(Shape<DP>::kWarps * 32) attention_tokens_kerne
                                 mma(sc[nq][i], a0, a1, a2, a3, q[nq][term][j * 8 + 2 * st], q[nq][term][j * 8 + 2 * st + 1]);
                     }
                 }
-            copy_values(n + 1, id1, slot);
-            float ks1, vs1;
-            scales_of(id1, &ks1, &vs1);
+                refill(j, slot);
+                ++piece;
+            }
             // ---- softmax: columns 2 t, 2 t + 1; tokens over i, the two halves and g
-            const int64_t j0 = k0 + (int64_t)(warp + n * S::kWarps) * kTile + 16 * (g >> 1) + (g & 1);
-            const bool there = __shfl_sync(0xffffffffu, id0, g >> 1) >= 0;
-            int top_e = vs > 0.0f ? exponent_of(vs) + 1 : -127;
-#pragma unroll
-            for (int x = 4; x < 32; x <<= 1) top_e = max(top_e, __shfl_xor_sync(0xffffffffu, top_e, x));
-            const int now_e = max(e, top_e);
-            // vs 2^(14 - e): in two steps, each a normal number
-            const float vf = vs * power_of_two(-now_e / 2) * power_of_two(14 - now_e + now_e / 2);
+            const int j0 = first_key(n);
+            const bool there = __shfl_sync(0xffffffffu, at0, g >> 1) >= 0;
+            const bool clean = __all_sync(0xffffffffu, there) && j0 + kTile - 1 <= least;
+            const int now_e = max(e, __reduce_max_sync(0xffffffffu, vs > 0.0f ? exponent_of(vs) + 1 : -127));
+            // vs 2^(7 - e): in two steps, each a normal number
+            const float vf = vs * power_of_two(-now_e / 2) * power_of_two(7 - now_e + now_e / 2);
             const float down = now_e == e ? 1.0f : (e <= -127 ? 0.0f : exp2f((float)(e - now_e)));
+            const bool grown = now_e != e;
             e = now_e;
             uint32_t pb[NQ][kTerms][4][2];
 #pragma unroll
             for (int nq = 0; nq < NQ; ++nq) {
+                const float f[2] = {factor[nq][0] * ks, factor[nq][1] * ks};
                 float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const int c = x & 1;
-                        const bool seen = there && j0 + 4 * i + (x & 2) <= limit[nq][c];
-                        sc[nq][i][x] = seen ? sc[nq][i][x] * (factor[nq][c] * ks) : -INFINITY;
-                        top[c] = fmaxf(top[c], sc[nq][i][x]);
-                    }
+                    for (int x = 0; x < 4; ++x) sc[nq][i][x] *= f[x & 1];
+                if (!clean) {
+                    const int from = j0 + 16 * (g >> 1) + (g & 1);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            if (!(there && from + 4 * i + (x & 2) <= limit[nq][x & 1])) sc[nq][i][x] = -INFINITY;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) top[x & 1] = fmaxf(top[x & 1], sc[nq][i][x]);
                 float base[2], keep[2];
+                bool rise = grown;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
 #pragma unroll
                     for (int x = 4; x < 32; x <<= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], x));
-                    const float now = fmaxf(m[nq][c], top[c]);
-                    base[c] = now == -INFINITY ? 0.0f : now;
-                    keep[c] = exp2f(m[nq][c] - base[c]);
+                    const bool up = top[c] > m[nq][c] + kSlack || (m[nq][c] == -INFINITY && top[c] > m[nq][c]);
+                    const float now = up ? top[c] : m[nq][c];
+                    keep[c] = up ? ex2(m[nq][c] - now) : 1.0f;          // (from nothing: 0)
+                    rise = rise || up;
                     m[nq][c] = now;
-                    l[nq][c] *= keep[c];
-                    keep[c] *= down;
+                    base[c] = now == -INFINITY ? 0.0f : now;
                 }
-                if (__any_sync(0xffffffffu, keep[0] != 1.0f || keep[1] != 1.0f)) {
+                if (__any_sync(0xffffffffu, rise)) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) { l[nq][c] *= keep[c]; keep[c] *= down; }
 #pragma unroll
                     for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
@@ -275,7 +294,7 @@ __global__ void __launch_bounds__(Shape<DP>::kWarps * 32) attention_tokens_kerne
                     float p[4];
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        p[x] = exp2f(sc[nq][i][x] - base[x & 1]);
+                        p[x] = ex2(sc[nq][i][x] - base[x & 1]);
                         l[nq][x & 1] += p[x];
                         p[x] *= vf;
                     }
@@ -292,37 +311,41 @@ __global__ void __launch_bounds__(Shape<DP>::kWarps * 32) attention_tokens_kerne
                 }
             }
             // ---- O^T: rows 16 d + g and + 8, step i the tokens of m-tile i
-            cp_wait<2>();
-            const int vslot = slot == kSlots - 1 ? 0 : slot + 1;
-            const uint32_t vsrc = ring + vslot * S::kSlotBytes;
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d) {
-                const uint4 x = lds_v4(vsrc + (2 * d) * 512), y = lds_v4(vsrc + (2 * d + 1) * 512);
-                const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+            for (int j = 0; j < kLines; ++j) {
+                cp_wait<kSlots - 1>();
+                const int slot = kLines == 1 ? piece & (kSlots - 1) : (kLines + j) % kSlots;
+                const uint32_t src = ring + slot * kPiece;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t a0, a1, a2, a3;
-                    widen(xs[i], &a0, &a2);
-                    widen(ys[i], &a1, &a3);
+                for (int d = 4 * j; d < 4 * j + 4; ++d) {
+                    const uint4 x = lds_v4(src + (2 * (d % 4)) * 512), y = lds_v4(src + (2 * (d % 4) + 1) * 512);
+                    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-                    for (int nq = 0; nq < NQ; ++nq)
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t a0, a1, a2, a3;
+                        widen(xs[i], &a0, &a2);
+                        widen(ys[i], &a1, &a3);
 #pragma unroll
-                        for (int term = 0; term < kTerms; ++term) mma(o[nq][d], a0, a1, a2, a3, pb[nq][term][i][0], pb[nq][term][i][1]);
+                        for (int nq = 0; nq < NQ; ++nq)
+#pragma unroll
+                            for (int term = 0; term < kTerms; ++term) mma(o[nq][d], a0, a1, a2, a3, pb[nq][term][i][0], pb[nq][term][i][1]);
+                    }
                 }
+                refill(kLines + j, slot);
+                ++piece;
             }
-            copy_keys(n + 2, id2, vslot);
-            slot = vslot == kSlots - 1 ? 0 : vslot + 1;
-            id0 = id1;
-            id1 = id2;
+            at0 = at1;
+            at1 = at2;
+            at2 = at3;
             ks = ks1;
             vs = vs1;
         }
-        // ---- the warps' results meet in the ring's memory: [warp][row][m, l, then O 2^(e - 14)]
+        // ---- the warps' results meet in the ring's memory: [warp][row][m, l, then O 2^(e - 7)]
         cp_wait<0>();
         __syncthreads();
         constexpr int kPitch = DP + 4;
         float* meet = reinterpret_cast<float*>(smem);
-        const float up_hi = power_of_two(e / 2), up_lo = power_of_two(e - e / 2 - 14);
+        const float up_hi = power_of_two(e / 2), up_lo = power_of_two(e - e / 2 - 7);
 #pragma unroll
         for (int nq = 0; nq < NQ; ++nq)
 #pragma unroll
@@ -338,18 +361,18 @@ __global__ void __launch_bounds__(Shape<DP>::kWarps * 32) attention_tokens_kerne
                 }
             }
         __syncthreads();
-        for (int e2 = threadIdx.x; e2 < kRows * (DP / 4); e2 += S::kWarps * 32) {
+        for (int e2 = threadIdx.x; e2 < kRows * (DP / 4); e2 += kWarps * 32) {
             const int r = e2 / (DP / 4), d = (e2 % (DP / 4)) * 4;
             const int64_t row = tile * kRows + r;
             if (row >= s.queries * a.group || d >= D) continue;
             float top = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < S::kWarps; ++w) top = fmaxf(top, meet[(w * kRows + r) * kPitch]);
+            for (int w = 0; w < kWarps; ++w) top = fmaxf(top, meet[(w * kRows + r) * kPitch]);
             const float base = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f;
             float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-            for (int w = 0; w < S::kWarps; ++w) {
+            for (int w = 0; w < kWarps; ++w) {
                 const float* from = meet + (w * kRows + r) * kPitch;
                 const float f = exp2f(from[0] - base);
                 sum = fmaf(f, from[1], sum);
@@ -370,19 +393,19 @@ __global__ void __launch_bounds__(Shape<DP>::kWarps * 32) attention_tokens_kerne
     }
 }
 
-template <typename T, int DP, int NQ>
+template <typename T, int DP, int NQ, bool EXACT>
 cudaError_t launch(const Attention& a, dim3 grid, cudaStream_t stream) {
-    using S = Shape<DP>;
-    constexpr size_t meet = sizeof(float) * S::kWarps * 8 * NQ * (DP + 4);
-    constexpr size_t smem = S::kRing > meet ? S::kRing : meet;
-    auto* kern = attention_tokens_kernel<T, DP, NQ>;
+    constexpr size_t ring = kWarps * kSlots * kPiece, meet = sizeof(float) * kWarps * 8 * NQ * (DP + 4);
+    constexpr size_t smem = ring > meet ? ring : meet;
+    auto* kern = attention_tokens_kernel<T, DP, NQ, EXACT>;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
-    return e != cudaSuccess ? e : launch_pdl3(kern, grid, S::kWarps * 32, smem, stream, a);
+    return e != cudaSuccess ? e : launch_pdl3(kern, grid, kWarps * 32, smem, stream, a);
 }
 template <typename T, int DP>
 cudaError_t by_rows(const Attention& a, dim3 grid, cudaStream_t stream) {
-    if (sizeof(T) == 4 || a.tile_rows <= 8) return launch<T, DP, 1>(a, grid, stream);
-    return launch<T, DP, sizeof(T) == 4 ? 1 : 2>(a, grid, stream);
+    constexpr int kMost = sizeof(T) == 4 ? 1 : 2;
+    if (a.head_dim == DP) return a.tile_rows <= 8 ? launch<T, DP, 1, true>(a, grid, stream) : launch<T, DP, kMost, true>(a, grid, stream);
+    return a.tile_rows <= 8 ? launch<T, DP, 1, false>(a, grid, stream) : launch<T, DP, kMost, false>(a, grid, stream);
 }
 template <typename T>
 cudaError_t by_width(const Attention& a, dim3 grid, cudaStream_t stream) {
