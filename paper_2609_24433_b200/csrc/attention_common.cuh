@@ -11,6 +11,7 @@ inline int64_t row_tiles(const Attention& a) {
     const int64_t n = (a.max_q * a.group + a.tile_rows - 1) / a.tile_rows;
     return n < 1 ? 1 : n > 0x7fffffff ? 0x7fffffff : n;
 }
+cudaError_t launch_attention_widen(const Attention& a, cudaStream_t stream);
 cudaError_t launch_attention_tiles(const Attention& a, cudaStream_t stream);
 cudaError_t launch_attention_tokens(const Attention& a, cudaStream_t stream);
 cudaError_t launch_attention_simt(const Attention& a, cudaStream_t stream);

@@ -1,21 +1,25 @@
 // Attention of many queries on the tcgen05 tensor cores: bf16 keys and values as rows (cross attention) or the 8-bit cache.
 //
 // A CTA takes one chunk of the keys of one kv head and NT tiles of 128 rows -- (token, head of a group) pairs, so that a group
-// reads its keys once.  Per tile of 128 keys: S = Q K^T into TMEM; one thread per row keeps the running maximum and sum and
-// writes the probabilities, 16 bits each, over S in TMEM; O += P V takes them from there as its first operand.
-//   warps 0-7   softmax, a warpgroup per row tile
-//   warps 8-11  which keys of a tile there are; from the cache, its codes into 128-byte-swizzled stages of 128 keys x 64 or 128 channels
-//   warp 12     issues the MMAs
-//   warp 13     rows: copies keys and values into the stages by TMA (14, 15 complete the warpgroup, whose registers go to the softmax)
+// reads its keys once.  Per tile of 128 keys: S = Q K^T into TMEM; a thread per row (two where there is one row tile) keeps the
+// running maximum and sum and writes the probabilities, 16 bits each, over S in TMEM; O += P V takes them from there as its first
+// operand.
+//   warps 0-7    softmax: a warpgroup per row tile, or the two halves of a row
+//   warps 8-11   which keys of a tile there are, the scales of cached ones
+//   warp 12      issues the MMAs
+//   warp 13      copies keys and values by TMA into 128-byte-swizzled stages of 128 keys x 64 or 128 channels (14, 15 complete the
+//                warpgroup, whose registers go to the softmax)
 // With two row tiles (D <= 128) the tensor core works on one while the other's probabilities are computed; with one (D > 128,
 // or few rows) S is double-buffered instead.
 //
 // The maximum is followed lazily: O and l are rescaled only where a row's maximum has risen by more than 2^8 over the base they
 // were built with, so almost never behind the first tiles; probabilities then reach 256, which changes no relative rounding.
 //
-// Cache: codes are widened to binary16, exactly, on their way into the stages (values keep tokens innermost and need no turn).
-// The scale of a page's keys multiplies S per 16 columns; that of its values multiplies the probabilities, over 2^e with e the
-// running exponent of the largest one: P = p vs 2^(7 - e) <= 2^15.  Queries: binary16 behind a power of two per row.
+// Cache: the codes come widened to binary16, exactly, by a kernel ahead (attention_widen.cu): as many row tiles read a key as there
+// are, and widening it for each of them on its way into the stages bounded the kernel (4 warps at it: 32 x 50 queries x 8 heads of
+// 256 over 866 keys 49 us, 3 x 4096 tokens x 16 heads of 128 over 6656 keys 660).  The scale of a page's keys multiplies S per 16
+// columns; that of its values multiplies the probabilities, over 2^e with e the running exponent of the largest one:
+// P = p vs 2^(7 - e) <= 2^15.  Queries: binary16 behind a power of two per row.
 // Rows: bf16 operands.  The scores of masked keys are replaced; their values are zeroed in shared memory, in the tiles that have
 // any, ahead of the product: 0 times a masked NaN would reach the sums.
 #include "act_common.cuh"
@@ -25,33 +29,20 @@
 #include <cuda_fp16.h>
 #include <float.h>
 
+#include <type_traits>
+
 namespace fq {
 namespace {
 
-constexpr int kThreads = 16 * 32;
-// Registers: a softmax thread holds a row of 128 scores.  The launch's 512 x 128 are shared out as 256 x 176 + 256 x 80.
-constexpr int kRegsLaunch = 128, kRegsSoftmax = 176, kRegsOther = 80;
+constexpr int kThreads = 16 * 32, kSoftmaxWarps = 8, kLoadWarp = 8, kMmaWarp = 12, kTmaWarp = 13;
+// Registers: a softmax thread holds a row of 128 scores.  The launch's 512 x 128 are shared out as 256 x 200 + 256 x 56.
+constexpr int kRegsLaunch = 128, kRegsSoftmax = 200, kRegsOther = 56;
 static_assert(256 * kRegsSoftmax + 256 * kRegsOther <= kThreads * kRegsLaunch, "");
 constexpr int kKeys = 128;
-constexpr int kMetas = 8;
+constexpr int kMetas = 4;
 constexpr float kSlack = 8.0f;          // log2 of how far a row's maximum may rise over its base
 
 constexpr uint32_t kWdProducer = 0x800u, kWdMma = 0x1000u, kWdSoftmax = 0x2000u;
-
-template <int DP, int NT>
-struct Shape {
-    static constexpr int kParts = DP == 256 ? 2 : 1;            // stages per key or value tile
-    static constexpr int kCh = DP / kParts;                     // channels per stage
-    static constexpr int kStageBytes = kKeys * kCh * 2;
-    static constexpr int kStages = DP == 64 ? 8 : 5;
-    static constexpr int kQTile = 128 * DP * 2;
-    static constexpr int kSmem = 1024 + NT * kQTile + kStages * kStageBytes;
-    static constexpr int kOCol = 256;                           // S: columns 0 .. 255
-    // Two tiles of 64 channels leave TMEM for probabilities of their own (columns 384 ..): the next scores are computed as soon
-    // as the last ones have been read.  Elsewhere probabilities lie over their scores.
-    static constexpr bool kEarly = NT == 2 && DP == 64;
-    static constexpr bool kPerTile = NT == 1 || kEarly;         // every product of a tile signals its end
-};
 
 struct __align__(16) KeyMeta {
     float ks[8];                        // per 16 keys
@@ -60,6 +51,37 @@ struct __align__(16) KeyMeta {
     uint32_t valid[4];
     int e;
     int unused[3];
+};
+// What the roles share beside the tiles.
+template <int STAGES>
+struct __align__(16) Control {
+    float rows[256];                    // maxima, sums on their way between the threads of a row
+    KeyMeta metas[kMetas];
+    uint64_t full_kv[STAGES], empty_kv[STAGES], meta[kMetas], used[kMetas], landed, fixed, s[2], p[2], o[2], free[2], q;
+    uint32_t tmem;
+    int abort;
+};
+
+template <int DP, int NT>
+struct Shape {
+    static constexpr int kParts = DP == 256 ? 2 : 1;            // stages per key or value tile
+    static constexpr int kCh = DP / kParts;                     // channels per stage
+    static constexpr int kStageBytes = kKeys * kCh * 2;
+    static constexpr int kStages = DP == 64 ? 8 : 5;
+    static constexpr int kQTile = 128 * DP * 2;
+    static constexpr int kTiles = NT * kQTile + kStages * kStageBytes;
+    static constexpr int kSmem = kTiles + (int)sizeof(Control<kStages>);
+    static constexpr int kSplit = 2 / NT;                       // threads per row
+    static constexpr int kCols = 128 / kSplit;                  // ... and the columns of S of each
+    static constexpr int kOCol = 256;                           // S: columns 0 .. 255
+    // Two tiles of 64 channels leave TMEM for probabilities of their own (columns 384 ..): the next scores are computed as soon
+    // as the last ones have been read.  Elsewhere probabilities lie over their scores.
+    static constexpr bool kEarly = NT == 2 && DP == 64;
+    static constexpr bool kAhead = NT == 1 || kEarly;           // scores of tile j + 1 are issued ahead of the products of tile j
+    // Stages are filled in the order in which they are needed: K0 V0 K1 V1 .., or ahead: K0 K1 V0 K2 V1 ..  First use by the keys,
+    // by the values of tile j of n.
+    static __device__ __forceinline__ int keys(int j) { return kParts * (kAhead && j > 0 ? 2 * j - 1 : 2 * j); }
+    static __device__ __forceinline__ int values(int j, int n) { return kParts * (kAhead && j + 1 < n ? 2 * j + 2 : 2 * j + 1); }
 };
 
 __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, uint32_t bar) {
@@ -70,14 +92,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
 }
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
-}
-__device__ __forceinline__ void widen(uint32_t w, uint32_t* lo, uint32_t* hi) {     // four int8 -> two pairs of binary16
-    const uint32_t u = w ^ 0x80808080u;
-    const __half2 base = __half2half2(__ushort_as_half(0x6480));                    // 1024 + 128
-    const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
-    const __half2 x = __hsub2(*reinterpret_cast<const __half2*>(&a), base), y = __hsub2(*reinterpret_cast<const __half2*>(&b), base);
-    *lo = *reinterpret_cast<const uint32_t*>(&x);
-    *hi = *reinterpret_cast<const uint32_t*>(&y);
 }
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
@@ -98,7 +112,7 @@ __device__ __forceinline__ float ex2(float x) {
 // 2^x of two values on the FMA pipe: 2^n by the exponent bits, 2^f on [-1/2, 1/2] by a polynomial of degree 4 (Remez, relative
 // error 2.7e-6 in binary32).  The exponential unit gives 16 values per clock and SM, a tile of 128 x 128 scores needs 1024
 // clocks of it; kPolynomial of eight pairs go here instead.
-constexpr int kPolynomial = 2;
+constexpr int kPolynomial = 1;
 __device__ __forceinline__ float2 ex2_polynomial(float2 x) {
     x.x = fmaxf(x.x, -126.0f);
     x.y = fmaxf(x.y, -126.0f);
@@ -131,18 +145,24 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// The issuing thread is the bottleneck of a tile where it computes a descriptor for every MMA (124 cycles each were measured
+// against the tensor core's 64): low words advance by constants, high words and predicates are constant.
+template <bool ACCUMULATE>
+__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t high, uint32_t idesc) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 a, {%1, %3};\n\tmov.b64 b, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(high), "r"(idesc), "n"(ACCUMULATE ? 1 : 0)
         : "memory");
 }
-__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+template <bool ACCUMULATE>
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t high, uint32_t idesc) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+        "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+        "mov.b64 b, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b), "r"(high), "r"(idesc), "n"(ACCUMULATE ? 1 : 0)
         : "memory");
 }
 // 16-bit operands (type 0: binary16, 1: bf16) -> binary32; A K-major, B K-major or, transposed, N-major; M = 128.
@@ -190,40 +210,46 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                                                                       const __grid_constant__ CUtensorMap map_v, uint32_t* watchdog) {
     using S = Shape<DP, NT>;
     constexpr int kCh = S::kCh, kParts = S::kParts, kStages = S::kStages, kPlanes = kCh / 64;
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(16) KeyMeta metas[kMetas];
-    __shared__ __align__(8) uint64_t s_full_kv[kStages], s_empty_kv[kStages], s_meta[kMetas], s_used[kMetas], s_landed, s_fixed, s_s[2], s_p[2], s_o[2], s_free[2], s_q;
-    __shared__ uint32_t s_tmem;
-    __shared__ int s_abort;
-    volatile int* abort_flag = &s_abort;
+    constexpr int kSplit = S::kSplit, kCols = S::kCols;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    Control<kStages>& ctl = *reinterpret_cast<Control<kStages>*>(smem_raw + S::kTiles);
+    volatile int* abort_flag = &ctl.abort;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t q_smem = smem, ring = smem + NT * S::kQTile;
-    auto full_kv = [&](int n) { return smem_u32(&s_full_kv[n % kStages]); };
-    auto empty_kv = [&](int n) { return smem_u32(&s_empty_kv[n % kStages]); };
+    const uint32_t q_smem = smem_u32(smem_raw), ring = q_smem + NT * S::kQTile;
+    if (q_smem & 1023u) {                                       // (swizzled tiles start on 1024 bytes; nothing else is in shared memory)
+        if (threadIdx.x == 0) atomicOr(watchdog, kWdProducer);
+        return;
+    }
+    auto full_kv = [&](int n) { return smem_u32(&ctl.full_kv[n % kStages]); };
+    auto empty_kv = [&](int n) { return smem_u32(&ctl.empty_kv[n % kStages]); };
     auto stage = [&](int n) { return ring + (uint32_t)(n % kStages) * S::kStageBytes; };
 
     auto init_barriers = [&]() {
-        for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&s_full_kv[i]), CACHED ? 4 : 1); mbar_init(smem_u32(&s_empty_kv[i]), 1); }
-        for (int i = 0; i < kMetas; ++i) { mbar_init(smem_u32(&s_meta[i]), 4); mbar_init(smem_u32(&s_used[i]), 4 * NT + (CACHED ? 0 : 1)); }
-        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&s_s[i]), 1); mbar_init(smem_u32(&s_p[i]), 4); mbar_init(smem_u32(&s_o[i]), 1); mbar_init(smem_u32(&s_free[i]), 4); }
-        mbar_init(smem_u32(&s_q), 4 * NT);
-        mbar_init(smem_u32(&s_landed), 1);
-        mbar_init(smem_u32(&s_fixed), 4);
+        for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&ctl.full_kv[i]), 1); mbar_init(smem_u32(&ctl.empty_kv[i]), 1); }
+        for (int i = 0; i < kMetas; ++i) { mbar_init(smem_u32(&ctl.meta[i]), 4); mbar_init(smem_u32(&ctl.used[i]), kSoftmaxWarps + (CACHED ? 0 : 1)); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&ctl.s[i]), 1);
+            mbar_init(smem_u32(&ctl.p[i]), 4 * kSplit);
+            mbar_init(smem_u32(&ctl.o[i]), 1);
+            mbar_init(smem_u32(&ctl.free[i]), 4 * kSplit);
+        }
+        mbar_init(smem_u32(&ctl.q), kSoftmaxWarps);
+        mbar_init(smem_u32(&ctl.landed), 1);
+        mbar_init(smem_u32(&ctl.fixed), 4);
         fence_mbarrier_init();
     };
     if (threadIdx.x == 0) {
-        s_abort = 0;
+        ctl.abort = 0;
         init_barriers();
     }
-    if (warp == 12) tmem_alloc<1>(smem_u32(&s_tmem), 512);
+    if (warp == kMmaWarp) tmem_alloc<1>(smem_u32(&ctl.tmem), 512);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = s_tmem;
+    const uint32_t tmem = ctl.tmem;
     griddep_wait();
 
-    const int b = blockIdx.z / a.kv_heads, hk = blockIdx.z % a.kv_heads, chunk = blockIdx.y;
+    const int unit = a.first_unit + blockIdx.z, b = unit / a.kv_heads, hk = unit % a.kv_heads, chunk = blockIdx.y;
     const Sequence s = sequence_of(a, b);
     const int D = a.head_dim, G = a.group;
     const int64_t rows = s.queries * G;
@@ -242,12 +268,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             if (again) {                                        // every arrival of the last tile has been waited for
                 __syncthreads();
                 if (threadIdx.x == 0) {
-                    for (int i = 0; i < kStages; ++i) { mbar_inval(smem_u32(&s_full_kv[i])); mbar_inval(smem_u32(&s_empty_kv[i])); }
-                    for (int i = 0; i < kMetas; ++i) { mbar_inval(smem_u32(&s_meta[i])); mbar_inval(smem_u32(&s_used[i])); }
-                    for (int i = 0; i < 2; ++i) { mbar_inval(smem_u32(&s_s[i])); mbar_inval(smem_u32(&s_p[i])); mbar_inval(smem_u32(&s_o[i])); mbar_inval(smem_u32(&s_free[i])); }
-                    mbar_inval(smem_u32(&s_q));
-                    mbar_inval(smem_u32(&s_landed));
-                    mbar_inval(smem_u32(&s_fixed));
+                    for (uint64_t* bar = ctl.full_kv; bar <= &ctl.q; ++bar) mbar_inval(smem_u32(bar));
                     init_barriers();
                 }
                 __syncthreads();
@@ -255,25 +276,27 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             again = true;
             body(tile, tk.chunks <= 1, k0, k1, (int)((k1 - k0 + kKeys - 1) / kKeys));
             __syncthreads();
-            ok = s_abort == 0;
+            ok = ctl.abort == 0;
         }
     };
 
-    if (warp < 8) {
+    if (warp < kSoftmaxWarps) {
         more_registers<kRegsSoftmax>();
         for_tiles([&](int64_t tile, bool direct, int64_t k0, int64_t k1, int n) {
             // ================================================================ softmax
-            const int mine = NT == 2 ? warp / 4 : 0;
-            const int r = threadIdx.x % 128;
-            const int64_t row = tile * kRows + mine * 128 + r;
-            const bool active = NT == 2 || warp < 4;
-            const bool there = active && row < rows;
+            // Warps of equal warp % 4 see the same lanes of TMEM: row tile warp / 4 / kSplit, columns kCols split .. of it.
+            const int mine = warp / (4 * kSplit), split = warp / 4 % kSplit;
+            const int r = mine * 128 + (warp % 4) * 32 + lane;
+            const int64_t row = tile * kRows + r;
+            const bool there = row < rows;
             const int64_t token = s.q0 + (there ? row / G : 0), head = hk * G + (there ? row % G : 0);
+            float* const seat = ctl.rows + r;                    // this row's, NT * 128 apart by split
+            auto meet = [&]() { if (kSplit > 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + mine * 4 + warp % 4), "n"(32 * kSplit) : "memory"); };
             float factor = a.scale_log2;
-            if (active) {
-                // ---- this thread's row of Q
+            {
+                // ---- this thread's part of its row of Q
                 const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + token * a.ldq + head * D;
-                const uint32_t dst = q_smem + mine * S::kQTile + r * 128;
+                const uint32_t dst = q_smem + mine * S::kQTile + (r % 128) * 128;
                 float down = 1.0f;
                 if (CACHED) {
                     float top = 0.0f;
@@ -287,8 +310,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     down = power_of_two(-e);
                     factor = a.scale_log2 * power_of_two(e);
                 }
-#pragma unroll 4
-                for (int d = 0; d < DP; d += 8) {
+#pragma unroll 2
+                for (int x = 0; x < DP / kSplit; x += 8) {
+                    const int d = split * (DP / kSplit) + x;
                     uint4 v = ld_global_v4(src + d, there && d < D);
                     if (CACHED) {
                         uint32_t w[4] = {v.x, v.y, v.z, v.w};
@@ -300,345 +324,264 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&s_q));
+                if (lane == 0) mbar_arrive(smem_u32(&ctl.q));
             }
-            if (active) {
-                const uint32_t lanes = tmem + ((uint32_t)(warp % 4) << 21);
-                const uint32_t o_addr = lanes + S::kOCol + (NT == 2 ? mine * DP : 0);
-                const int64_t limit64 = row_limit(a, s, row);
-                float base = -INFINITY, l = 0.0f;
-                int e = -127;
-                for (int j = 0; j < n && ok; ++j) {
-                    const int buf = NT == 2 ? mine : j & 1;
-                    const uint32_t phase = NT == 2 ? j & 1 : (j >> 1) & 1;
-                    ok = wait_all(smem_u32(&s_s[buf]), phase, abort_flag, watchdog, kWdSoftmax) &&
-                         wait_all(smem_u32(&s_meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdSoftmax);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const KeyMeta& meta = metas[j % kMetas];
-                    const uint32_t s_addr = lanes + 128 * buf, p_addr = S::kEarly ? lanes + 384 + 64 * mine : s_addr;
-                    const int lim = (int)min(max(limit64 - (k0 + (int64_t)j * kKeys), (int64_t)-1), (int64_t)kKeys);
-                    uint32_t seen[4];
+            constexpr int kOCols = DP / kSplit;                  // columns of O that this warp rescales and stores
+            const uint32_t lanes = tmem + ((uint32_t)(warp % 4) << 21);
+            const uint32_t o_addr = lanes + S::kOCol + (NT == 2 ? mine * DP : 0) + split * kOCols;
+            const int64_t limit64 = row_limit(a, s, row);
+            float base = -INFINITY, l = 0.0f;
+            int e = -127;
+            // (Each warp comes to every meeting, also once a wait has run out: the others may be there already.)
+            for (int j = 0; j < n; ++j) {
+                const int buf = NT == 2 ? mine : j & 1;
+                const uint32_t phase = NT == 2 ? j & 1 : (j >> 1) & 1;
+                ok = ok && wait_all(smem_u32(&ctl.s[buf]), phase, abort_flag, watchdog, kWdSoftmax) &&
+                     wait_all(smem_u32(&ctl.meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdSoftmax);
+                if (!ok) {
+                    meet();
+                    meet();
+                    continue;
+                }
+                tc_fence_after();
+                const KeyMeta& meta = ctl.metas[j % kMetas];
+                const uint32_t s_addr = lanes + 128 * buf + split * kCols;
+                const uint32_t p_addr = (S::kEarly ? lanes + 384 + 64 * mine : lanes + 128 * buf) + split * (kCols / 2);
+                const int lim = (int)min(max(limit64 - (k0 + (int64_t)j * kKeys), (int64_t)-1), (int64_t)kKeys) - split * kCols;
+                uint32_t seen[kCols / 32];
+                bool partly = false;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const int x = lim - 32 * c;
-                        seen[c] = meta.valid[c] & (x < 0 ? 0u : x >= 31 ? ~0u : (2u << x) - 1u);
+                for (int c = 0; c < kCols / 32; ++c) {
+                    const int x = lim - 32 * c;
+                    seen[c] = meta.valid[split * (kCols / 32) + c] & (x < 0 ? 0u : x >= 31 ? ~0u : (2u << x) - 1u);
+                    partly = partly || seen[c] != ~0u;
+                }
+                const bool masked = __any_sync(0xffffffffu, partly);
+                const float* const ks = meta.ks + split * (kCols / 16);
+                uint32_t v[kCols];
+#pragma unroll
+                for (int c = 0; c < kCols / 32; ++c) tmem_ld32(s_addr + 32 * c, v + 32 * c);
+                tmem_ld_wait();
+                if (masked) {                                    // (a branch: selects on every score cost a third of the loop)
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i)
+                        if (!((seen[i / 32] >> (i % 32)) & 1)) v[i] = 0xff800000u;
+                }
+                // ---- the largest score.  (A masked one, -inf, needs a factor that is not 0 to stay it.)
+                float top = -INFINITY;
+#pragma unroll
+                for (int g = 0; g < kCols / 16; ++g) {
+                    float x = -INFINITY, y = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) {
+                        x = max3(x, v[16 * g + i], v[16 * g + i + 1]);
+                        y = max3(y, v[16 * g + i + 2], v[16 * g + i + 3]);
                     }
-                    const bool masked = __any_sync(0xffffffffu, (seen[0] & seen[1] & seen[2] & seen[3]) != ~0u);
-                    uint32_t v[128];
+                    top = fmaxf(top, fmaxf(x, y) * (CACHED ? fmaxf(factor * ks[g], FLT_MIN) : fmaxf(factor, FLT_MIN)));
+                }
+                if (kSplit > 1) {
+                    seat[split * NT * 128] = top;
+                    meet();                                      // (and all of them have read their scores)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + 32 * c, v + 32 * c);
-                    tmem_ld_wait();
-                    if (S::kEarly) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&s_free[mine]));
-                    }
-                    // ---- the largest score
-                    float top = -INFINITY;
-                    if (masked) {                                // (its own code: selects on every score cost a third of the loop)
-#pragma unroll
-                        for (int g = 0; g < 8; ++g) {
-                            float x = -INFINITY;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                if (!((seen[g / 2] >> (16 * (g % 2) + i)) & 1)) v[16 * g + i] = 0xff800000u;
-                                x = fmaxf(x, __uint_as_float(v[16 * g + i]));
-                            }
-                            top = fmaxf(top, CACHED ? (x == -INFINITY ? x : x * (factor * meta.ks[g])) : x);
-                        }
-                    } else {
-#pragma unroll
-                        for (int g = 0; g < 8; ++g) {
-                            float x = -INFINITY, y = -INFINITY;
-#pragma unroll
-                            for (int i = 0; i < 16; i += 4) {
-                                x = max3(x, v[16 * g + i], v[16 * g + i + 1]);
-                                y = max3(y, v[16 * g + i + 2], v[16 * g + i + 3]);
-                            }
-                            x = fmaxf(x, y);
-                            top = fmaxf(top, CACHED ? x * (factor * meta.ks[g]) : x);
-                        }
-                    }
-                    if (!CACHED) top = top == -INFINITY ? top : top * factor;
-                    if (S::kEarly && j > 0) {                    // the last product has read its probabilities
-                        ok = wait_all(smem_u32(&s_o[mine]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
-                        if (!ok) break;
-                        tc_fence_after();
-                    }
-                    // ---- a new base
-                    const int now_e = CACHED ? meta.e : e;
-                    const bool rise = top > base + kSlack || (base == -INFINITY && top > base);
-                    if (__any_sync(0xffffffffu, rise || now_e != e)) {
-                        const float now = rise ? top : base;
-                        const float keep = rise ? exp2f(base - now) : 1.0f;        // (from nothing: 0)
-                        base = now;
-                        l *= keep;
-                        if (j > 0) {
-                            if (NT == 1) {
-                                ok = wait_all(smem_u32(&s_o[0]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
-                                if (!ok) break;
-                                tc_fence_after();
-                            }
-                            const float f = CACHED ? keep * (e <= -127 ? 0.0f : exp2f((float)(e - now_e))) : keep;
-#pragma unroll
-                            for (int c = 0; c < DP; c += 32) {
-                                uint32_t o[32];
-                                tmem_ld32(o_addr + c, o);
-                                tmem_ld_wait();
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                                tmem_st16(o_addr + c, o);
-                                tmem_st16(o_addr + c + 16, o + 16);
-                            }
-                        }
-                        e = now_e;
-                    }
-                    const float minus = base == -INFINITY ? 0.0f : -base;
-                    // ---- probabilities, over the scores that they come from
-                    float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
-                    float total = 0.0f;
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t p[16];
-#pragma unroll
-                        for (int g = 2 * c; g < 2 * c + 2; ++g) {
-                            // (a masked score, -inf, needs a factor that is not 0 to give 2^-inf)
-                            const float f = fmaxf(CACHED ? factor * meta.ks[g] : factor, FLT_MIN);
-                            const float z = CACHED ? minus + meta.lvf[g] : minus;
-#pragma unroll
-                            for (int i = 0; i < 16; i += 2) {
-                                float2 x = f2_fma(make_float2(__uint_as_float(v[16 * g + i]), __uint_as_float(v[16 * g + i + 1])), make_float2(f, f), make_float2(z, z));
-                                if ((i / 2) % 8 < kPolynomial) x = ex2_polynomial(x);
-                                else x = make_float2(ex2(x.x), ex2(x.y));
-                                if (i & 2) sum1 = f2_add(sum1, x);
-                                else sum0 = f2_add(sum0, x);
-                                p[8 * (g % 2) + i / 2] = CACHED ? pack_half(x.x, x.y) : pack_bf16(x.x, x.y);
-                            }
-                            if (CACHED) {
-                                sum0 = f2_add(sum0, sum1);
-                                total = fmaf(sum0.x + sum0.y, meta.inv[g], total);
-                                sum0 = sum1 = make_float2(0.0f, 0.0f);
-                            }
-                        }
-                        tmem_st16(p_addr + 16 * c, p);
-                    }
-                    if (!CACHED) {
-                        sum0 = f2_add(sum0, sum1);
-                        total = sum0.x + sum0.y;
-                    }
-                    l += total;
-                    tmem_st_wait();
-                    // Every phase of s_o is waited for, so that none can pass unseen: the next one needs this warp's arrival below.
-                    if (NT == 1 && j > 0) {
-                        ok = wait_all(smem_u32(&s_o[0]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
-                        if (!ok) break;
-                    }
+                    for (int i = 0; i < kSplit; ++i) top = fmaxf(top, seat[i * NT * 128]);
+                    meet();                                      // (the next maxima may come)
+                }
+                if (S::kEarly) {
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) {
-                        mbar_arrive(smem_u32(&s_p[buf]));
-                        mbar_arrive(smem_u32(&s_used[j % kMetas]));
+                    if (lane == 0) mbar_arrive(smem_u32(&ctl.free[mine]));
+                    if (j > 0) {                                 // the last product has read its probabilities
+                        ok = wait_all(smem_u32(&ctl.o[mine]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
+                        if (!ok) continue;
+                        tc_fence_after();
                     }
                 }
-                // ---- the rows' results
-                if (ok && n > 0) {
-                    ok = wait_all(smem_u32(&s_o[S::kPerTile ? mine : 0]), S::kPerTile ? (n - 1) & 1 : 0, abort_flag, watchdog, kWdSoftmax);
-                    tc_fence_after();
-                }
-                if (ok) {
-                    const int64_t at = (token * a.q_heads + head) * a.chunks + chunk;
-                    const float whole = CACHED ? power_of_two(e / 2) : 1.0f, rest = CACHED ? power_of_two(e - e / 2 - 7) : 1.0f;
-                    const float inv = direct ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f;
-                    __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y) + token * a.ldy + head * D;
-                    float* part = direct ? nullptr : a.part + at * D;
-#pragma unroll
-                    for (int c = 0; c < DP; c += 32) {
-                        uint32_t o[32];
-                        if (n > 0) {
-                            tmem_ld32(o_addr + c, o);
+                // ---- a new base
+                const int now_e = CACHED ? meta.e : e;
+                const bool rise = top > base + kSlack || (base == -INFINITY && top > base);
+                if (__any_sync(0xffffffffu, rise || now_e != e)) {
+                    const float now = rise ? top : base;
+                    const float keep = rise ? exp2f(base - now) : 1.0f;                // (from nothing: 0)
+                    base = now;
+                    l *= keep;
+                    if (j > 0) {
+                        if (NT == 1) {
+                            ok = wait_all(smem_u32(&ctl.o[0]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
+                            if (!ok) continue;
+                            tc_fence_after();
+                        }
+                        const float f = CACHED ? keep * (e <= -127 ? 0.0f : exp2f((float)(e - now_e))) : keep;
+#pragma unroll 1
+                        for (int c = 0; c < kOCols; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(o_addr + c, o);
                             tmem_ld_wait();
-                        } else {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = 0u;
-                        }
-                        float f[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) f[i] = l > 0.0f ? __uint_as_float(o[i]) * whole * rest * inv : 0.0f;
-#pragma unroll
-                        for (int x = 0; x < 32; x += 8) {
-                            if (!there || c + x >= D) continue;
-                            if (direct) {
-                                *reinterpret_cast<uint4*>(y + c + x) = make_uint4(pack_bf16(f[x], f[x + 1]), pack_bf16(f[x + 2], f[x + 3]),
-                                                                                  pack_bf16(f[x + 4], f[x + 5]), pack_bf16(f[x + 6], f[x + 7]));
-                            } else {
-                                *reinterpret_cast<float4*>(part + c + x) = make_float4(f[x], f[x + 1], f[x + 2], f[x + 3]);
-                                *reinterpret_cast<float4*>(part + c + x + 4) = make_float4(f[x + 4], f[x + 5], f[x + 6], f[x + 7]);
-                            }
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st16(o_addr + c, o);
                         }
                     }
-                    if (!direct && there) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(base, l);
-                    tc_fence_before();
+                    e = now_e;
+                }
+                const float minus = base == -INFINITY ? 0.0f : -base;
+                // ---- probabilities, over the scores or beside them
+                float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
+                float total = 0.0f;
+#pragma unroll
+                for (int c = 0; c < kCols / 32; ++c) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int g = 2 * c; g < 2 * c + 2; ++g) {
+                        const float f = fmaxf(CACHED ? factor * ks[g] : factor, FLT_MIN);
+                        const float z = CACHED ? minus + meta.lvf[split * (kCols / 16) + g] : minus;
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            float2 x = f2_fma(make_float2(__uint_as_float(v[16 * g + i]), __uint_as_float(v[16 * g + i + 1])), make_float2(f, f), make_float2(z, z));
+                            if ((i / 2) % 8 < kPolynomial) x = ex2_polynomial(x);
+                            else x = make_float2(ex2(x.x), ex2(x.y));
+                            if (i & 2) sum1 = f2_add(sum1, x);
+                            else sum0 = f2_add(sum0, x);
+                            p[8 * (g % 2) + i / 2] = CACHED ? pack_half(x.x, x.y) : pack_bf16(x.x, x.y);
+                        }
+                        if (CACHED) {
+                            sum0 = f2_add(sum0, sum1);
+                            total = fmaf(sum0.x + sum0.y, meta.inv[split * (kCols / 16) + g], total);
+                            sum0 = sum1 = make_float2(0.0f, 0.0f);
+                        }
+                    }
+                    tmem_st16(p_addr + 16 * c, p);
+                }
+                if (!CACHED) {
+                    sum0 = f2_add(sum0, sum1);
+                    total = sum0.x + sum0.y;
+                }
+                l += total;
+                tmem_st_wait();
+                // Every phase of ctl.o is waited for, so that none can pass unseen: the next one needs this warp's arrival below.
+                if (NT == 1 && j > 0) {
+                    ok = wait_all(smem_u32(&ctl.o[0]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
+                    if (!ok) continue;
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&ctl.p[buf]));
+                    mbar_arrive(smem_u32(&ctl.used[j % kMetas]));
                 }
             }
+            // ---- the rows' results
+            if (ok && n > 0) {
+                ok = wait_all(smem_u32(&ctl.o[mine]), S::kAhead ? (n - 1) & 1 : 0, abort_flag, watchdog, kWdSoftmax);
+                tc_fence_after();
+            }
+            if (kSplit > 1) {
+                seat[split * NT * 128] = l;
+                meet();
+                l = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kSplit; ++i) l += seat[i * NT * 128];
+            }
+            if (ok) {
+                const int64_t at = (token * a.q_heads + head) * a.chunks + chunk;
+                const float whole = CACHED ? power_of_two(e / 2) : 1.0f, rest = CACHED ? power_of_two(e - e / 2 - 7) : 1.0f;
+                const float inv = direct ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f;
+                __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y) + token * a.ldy + head * D + split * kOCols;
+                float* part = direct ? nullptr : a.part + at * D + split * kOCols;
+#pragma unroll 1
+                for (int c = 0; c < kOCols; c += 16) {
+                    uint32_t o[16];
+                    if (n > 0) {
+                        tmem_ld16(o_addr + c, o);
+                        tmem_ld_wait();
+                    }
+                    float f[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) f[i] = n > 0 && l > 0.0f ? __uint_as_float(o[i]) * whole * rest * inv : 0.0f;
+                    if (!there || split * kOCols + c >= D) continue;           // (D is a multiple of 16)
+#pragma unroll
+                    for (int x = 0; x < 16; x += 8) {
+                        if (direct) {
+                            *reinterpret_cast<uint4*>(y + c + x) = make_uint4(pack_bf16(f[x], f[x + 1]), pack_bf16(f[x + 2], f[x + 3]),
+                                                                              pack_bf16(f[x + 4], f[x + 5]), pack_bf16(f[x + 6], f[x + 7]));
+                        } else {
+                            *reinterpret_cast<float4*>(part + c + x) = make_float4(f[x], f[x + 1], f[x + 2], f[x + 3]);
+                            *reinterpret_cast<float4*>(part + c + x + 4) = make_float4(f[x + 4], f[x + 5], f[x + 6], f[x + 7]);
+                        }
+                    }
+                }
+                if (!direct && there && split == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(base, l);
+                tc_fence_before();
+            }
         });
-    } else if (warp < 12) {
+    } else if (warp < kMmaWarp) {
         fewer_registers<kRegsOther>();
         for_tiles([&](int64_t, bool, int64_t k0, int64_t k1, int n) {
-            // ================================================================ keys and values
-            const int uses = n * 2 * kParts;                    // of stages: per key tile its keys, then its values
-            const int w = warp - 8;
+            // ================================================================ which keys there are
+            const int w = warp - kLoadWarp;
             if (!CACHED) {
                 int mends = 0;
                 for (int j = 0; j < n && ok; ++j) {
-                    KeyMeta& meta = metas[j % kMetas];
-                    if (j >= kMetas) ok = mbar_wait_all_lazy(smem_u32(&s_used[j % kMetas]), ((j / kMetas) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
+                    KeyMeta& meta = ctl.metas[j % kMetas];
+                    if (j >= kMetas) ok = mbar_wait_all_lazy(smem_u32(&ctl.used[j % kMetas]), ((j / kMetas) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
                     if (!ok) break;
                     const KeyPlace p = key_place<false>(a, s, b, hk, k0 + (int64_t)j * kKeys + 32 * w + lane, k1);
                     const uint32_t word = __ballot_sync(0xffffffffu, p.valid);
                     if (lane == 0) {
                         meta.valid[w] = word;
-                        mbar_arrive(smem_u32(&s_meta[j % kMetas]));
+                        mbar_arrive(smem_u32(&ctl.meta[j % kMetas]));
                     }
-                    ok = wait_all(smem_u32(&s_meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdProducer);
+                    ok = wait_all(smem_u32(&ctl.meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdProducer);
                     if (!ok) break;
                     if (all_valid(meta)) continue;
                     // Zeros for the values of masked keys, the lanes across a row: the MMA warp, which sees the same words, says when
                     // the values are there and waits for the mending.  (The stages' own barriers cannot say it to a warp that looks
                     // at some of their phases only.)
-                    ok = wait_all(smem_u32(&s_landed), mends & 1, abort_flag, watchdog, kWdProducer);
+                    ok = wait_all(smem_u32(&ctl.landed), mends & 1, abort_flag, watchdog, kWdProducer);
                     if (!ok) break;
                     ++mends;
                     for (int part = 0; part < kParts; ++part)
                         for (uint32_t gone = ~word; gone; gone &= gone - 1) {
-                            const uint32_t row = stage(2 * kParts * j + kParts + part) + (32 * w + __ffs(gone) - 1) * 128;
+                            const uint32_t row = stage(S::values(j, n) + part) + (32 * w + __ffs(gone) - 1) * 128;
 #pragma unroll
                             for (int plane = 0; plane < kPlanes; ++plane) sts32(row + plane * 16384 + lane * 4, 0u);
                         }
                     fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(smem_u32(&s_fixed));
+                    if (lane == 0) mbar_arrive(smem_u32(&ctl.fixed));
                 }
             } else {
-                constexpr int kUnits = kCh / 16;                 // 16-byte units of codes per lane and stage
-                const int P = a.cache.page;
                 const int32_t* table = a.table + b * a.ld_table;
-                auto page_of = [&](int j) -> int32_t {           // of keys 16 (lane % 8) .. of tile j
+                auto page_of = [&](int j) -> int32_t {           // (page, head) of keys 16 (lane % 8) .. of tile j, -1 where there is none
                     const int64_t key = k0 + (int64_t)j * kKeys + 16 * (lane % 8);
                     if (j >= n || key >= k1) return -1;
-                    const int32_t id = (int32_t)ld_global_u32(table + key / P);
-                    return id >= 0 && id < a.cache.pages ? id : -1;
+                    const int32_t id = (int32_t)ld_global_u32(table + key / a.cache.page);
+                    return id >= 0 && id < a.cache.pages ? id * a.kv_heads + hk : -1;
                 };
-                // A warp fills 32 rows (tokens) of a stage of keys, kCh / 4 rows (channels) of a stage of values.  A lane's row in
-                // every group of eight is lane / 4 -- eight lanes then store to two neighbouring rows, whose swizzles differ in
-                // the lowest bit, and meet all banks -- and its 16 codes of a 64-wide plane are the (lane % 4)th.
-                constexpr int kGroups[2] = {4, kCh / 32};        // of eight rows: keys, values
-                const int r8 = lane / 4, u4 = lane % 4;
-                const uint32_t lo = r8 * 128 + (((2 * u4) ^ r8) * 16), hi = r8 * 128 + (((2 * u4 + 1) ^ r8) * 16);
-                // Where a lane's codes of a stage lie: [0], [1] are the two groups of 16 keys, or the two planes of keys.  Codes that
-                // no product needs (no page, channels from D on) are read from where there is something, never from beyond.
-                const int8_t* src[2];
-                int step = 0, plane1 = 0;                        // bytes to the next group of rows; keys: to the second plane
-                auto locate = [&](int u, int32_t id) {
-                    const int part = u % kParts;
-                    if (u < kParts) {
-                        const int c = part * 128 + 16 * u4;
-                        step = 8 * D;
-                        plane1 = c + 64 < D ? 64 : 0;
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const int32_t page = max(__shfl_sync(0xffffffffu, id, 2 * w + x), 0);
-                            src[x] = a.cache.k + (((int64_t)page * a.kv_heads + hk) * P + (16 * (2 * w + x)) % P + r8) * D + (c < D ? c : 0);
-                        }
-                    } else {
-                        const int d = part * 128 + w * (kCh / 4) + r8;
-                        step = 8 * P;
-#pragma unroll
-                        for (int x = 0; x < 2; ++x) {
-                            const int32_t page = max(__shfl_sync(0xffffffffu, id, u4 + 4 * x), 0);
-                            src[x] = a.cache.v + ((int64_t)page * a.kv_heads + hk) * D * P + (int64_t)d * P + (16 * (u4 + 4 * x)) % P;
-                        }
-                    }
-                };
-                auto load = [&](int u, int it) -> uint4 {
-                    if (u < kParts) {
-                        const int rg = it % 4, plane = it / 4;
-                        return ld_global_v4(src[rg / 2] + (rg % 2) * step + plane * plane1);
-                    }
-                    const int rg = it % kGroups[1], plane = it / kGroups[1];
-                    const int d = (u % kParts) * 128 + w * (kCh / 4) + r8 + 8 * rg;
-                    return ld_global_v4(d < D ? src[plane] + rg * step : a.cache.v);
-                };
-                uint4 codes[kUnits];                             // of the next stage, each loaded as its forerunner is stored
-                int32_t id = page_of(0), id1 = page_of(1), id2;
-                float ks = 0.0f, vs = 0.0f;
-                auto scales_of = [&](int32_t page, float* k, float* v) {
-                    *k = page >= 0 ? ld_global_f32(a.cache.k_scale + (int64_t)page * a.kv_heads + hk) : 0.0f;
-                    *v = page >= 0 ? ld_global_f32(a.cache.v_scale + (int64_t)page * a.kv_heads + hk) : 0.0f;
-                };
-                int e = -127, use = 0;
-                if (n > 0) {
-                    scales_of(id, &ks, &vs);
-#pragma unroll
-                    for (int it = 0; it < kUnits; ++it) {
-                        if (it == 0) locate(0, id);
-                        codes[it] = load(0, it);
-                    }
-                }
+                int32_t id = page_of(0), id1 = page_of(1);
+                float ks = id >= 0 ? ld_global_f32(a.cache.k_scale + id) : 0.0f, vs = id >= 0 ? ld_global_f32(a.cache.v_scale + id) : 0.0f;
+                int e = -127;
                 for (int j = 0; j < n && ok; ++j) {
-                    id2 = page_of(j + 2);
-                    float ks1, vs1;
-                    scales_of(id1, &ks1, &vs1);
-#pragma unroll
-                    for (int u = 0; u < 2 * kParts; ++u, ++use) {
-                        if (use >= kStages) ok = mbar_wait_all_lazy(empty_kv(use), ((use / kStages) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
-                        if (!ok) break;
-                        if (u == 0) {
-                            if (j >= kMetas) ok = mbar_wait_all_lazy(smem_u32(&s_used[j % kMetas]), ((j / kMetas) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
-                            if (!ok) break;
-                            int top = vs > 0.0f ? exponent_of(vs) + 1 : -127;
-#pragma unroll
-                            for (int x = 1; x < 8; x <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, x));
-                            e = max(e, top);
-                            KeyMeta& meta = metas[j % kMetas];
-                            const int64_t key = k0 + (int64_t)j * kKeys + 32 * w + lane;
-                            const int32_t page = __shfl_sync(0xffffffffu, id, 2 * w + lane / 16);
-                            const uint32_t word = __ballot_sync(0xffffffffu, page >= 0 && key < k1);
-                            if (lane / 2 == w) {                 // lanes 2 w, 2 w + 1: the warp's two groups of 16 keys
-                                meta.ks[lane] = ks;
-                                // (values of scale 0 keep a probability, which the sum gets back by `inv` and binary16 rounds to 0)
-                                const float lvf = log2f(fmaxf(vs * power_of_two(-e / 2) * power_of_two(7 - e + e / 2), 0x1p-60f));
-                                meta.lvf[lane] = lvf;
-                                meta.inv[lane] = exp2f(-lvf);
-                            }
-                            if (lane == 0) {
-                                meta.valid[w] = word;
-                                if (w == 0) meta.e = e;
-                            }
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(smem_u32(&s_meta[j % kMetas]));
-                        }
-                        const int next = u + 1 < 2 * kParts ? u + 1 : 0;
-                        locate(next, next ? id : id1);
-                        const uint32_t dst = stage(use) + (u < kParts ? 32 * w * 128 : w * (kCh / 4) * 128);
-#pragma unroll
-                        for (int it = 0; it < kUnits; ++it) {
-                            const int groups = kGroups[u < kParts ? 0 : 1];
-                            const uint32_t at = dst + (it / groups) * (u < kParts ? 16384 : kCh * 128) + (it % groups) * 1024;
-                            const uint4 x = codes[it];
-                            codes[it] = load(next, it);
-                            uint32_t h[8];
-                            widen(x.x, &h[0], &h[1]);
-                            widen(x.y, &h[2], &h[3]);
-                            widen(x.z, &h[4], &h[5]);
-                            widen(x.w, &h[6], &h[7]);
-                            sts128(at + lo, h[0], h[1], h[2], h[3]);
-                            sts128(at + hi, h[4], h[5], h[6], h[7]);
-                        }
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(full_kv(use));
+                    if (j >= kMetas) ok = mbar_wait_all_lazy(smem_u32(&ctl.used[j % kMetas]), ((j / kMetas) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
+                    if (!ok) break;
+                    const int32_t id2 = page_of(j + 2);
+                    const float ks1 = id1 >= 0 ? ld_global_f32(a.cache.k_scale + id1) : 0.0f, vs1 = id1 >= 0 ? ld_global_f32(a.cache.v_scale + id1) : 0.0f;
+                    e = max(e, __reduce_max_sync(0xffffffffu, vs > 0.0f ? exponent_of(vs) + 1 : -127));
+                    KeyMeta& meta = ctl.metas[j % kMetas];
+                    const int64_t key = k0 + (int64_t)j * kKeys + 32 * w + lane;
+                    const uint32_t word = __ballot_sync(0xffffffffu, __shfl_sync(0xffffffffu, id, 2 * w + lane / 16) >= 0 && key < k1);
+                    if (lane / 2 == w) {                         // lanes 2 w, 2 w + 1: the warp's two groups of 16 keys
+                        meta.ks[lane] = ks;
+                        // (values of scale 0 keep a probability, which the sum gets back by `inv` and binary16 rounds to 0)
+                        const float lvf = log2f(fmaxf(vs * power_of_two(-e / 2) * power_of_two(7 - e + e / 2), 0x1p-60f));
+                        meta.lvf[lane] = lvf;
+                        meta.inv[lane] = exp2f(-lvf);
                     }
+                    if (lane == 0) {
+                        meta.valid[w] = word;
+                        if (w == 0) meta.e = e;
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&ctl.meta[j % kMetas]));
                     id = id1;
                     id1 = id2;
                     ks = ks1;
@@ -650,54 +593,80 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
         fewer_registers<kRegsOther>();
         for_tiles([&](int64_t, bool, int64_t k0, int64_t, int n) {
             const int uses = n * 2 * kParts;
-            if (!CACHED && warp == 13) {
-                // ============================================================ TMA: keys, values, keys, ..
-                for (int use = 0; use < uses && ok; ++use) {
-                    if (use >= kStages) ok = mbar_wait_all_lazy(empty_kv(use), ((use / kStages) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
-                    if (!ok) break;
-                    const int j = use / (2 * kParts), u = use % (2 * kParts), part = u % kParts;
-                    const CUtensorMap* map = u < kParts ? &map_k : &map_v;
-                    const int row = (int)(s.k0 + k0 + (int64_t)j * kKeys);
-                    if (elect_one()) {
-                        mbar_arrive_expect_tx(full_kv(use), S::kStageBytes);
+            if (warp == kTmaWarp) {
+                // ============================================================ TMA
+                int use = 0;
+                auto copy = [&](bool keys, int j) {
+                    for (int part = 0; part < kParts && ok; ++part, ++use) {
+                        if (use >= kStages) ok = mbar_wait_all_lazy(empty_kv(use), ((use / kStages) & 1) ^ 1, abort_flag, watchdog, kWdProducer);
+                        if (ok && elect_one()) {
+                            const uint32_t bar = full_kv(use);
+                            const int key = (int)(k0 + (int64_t)j * kKeys);
+                            mbar_arrive_expect_tx(bar, S::kStageBytes);
+                            if (CACHED && !keys) {               // two planes of 64 keys, rows are channels
 #pragma unroll
-                        for (int plane = 0; plane < kPlanes; ++plane)
-                            tma_load_3d(stage(use) + plane * 16384, map, part * 128 + plane * 64, hk, row, full_kv(use));
+                                for (int plane = 0; plane < 2; ++plane)
+                                    tma_load_3d(stage(use) + plane * (kCh * 128), &map_v, key + 64 * plane, part * 128, (int)blockIdx.z, bar);
+                            } else {                             // planes of 64 channels, rows are keys
+#pragma unroll
+                                for (int plane = 0; plane < kPlanes; ++plane) {
+                                    if (CACHED) tma_load_3d(stage(use) + plane * 16384, &map_k, part * 128 + plane * 64, key, (int)blockIdx.z, bar);
+                                    else tma_load_3d(stage(use) + plane * 16384, keys ? &map_k : &map_v, part * 128 + plane * 64, hk, (int)s.k0 + key, bar);
+                                }
+                            }
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
+                };
+                for (int kt = 0, vt = 0; vt < n && ok;) {        // (in the order of S::keys and S::values)
+                    if (kt < n && kt <= vt + (S::kAhead ? 1 : 0)) copy(true, kt++);
+                    else copy(false, vt++);
                 }
                 if (!ok && lane == 0) drain_after_abort();
                 return;
             }
             // ================================================================ MMA issue
-            if (warp != 12 || n == 0) return;
+            // One warp serves both row tiles in turn, products and next scores of one back to back: they then work half a period apart,
+            // one at the exponentials, one at the tensor core.  (A warp for each let the MMAs of both mix, so that both ended
+            // together and met again: 1.4 times the time at D = 128.)
+            if (warp != kMmaWarp || n == 0) return;
             int mends = 0;                                      // tiles with masked keys so far
             const uint32_t idesc_s = instr_desc_16(CACHED ? 0 : 1, false, kKeys), idesc_o = instr_desc_16(CACHED ? 0 : 1, !CACHED, kCh);
-            auto wait_kv = [&](int use) { return wait_all(full_kv(use), (use / kStages) & 1, abort_flag, watchdog, kWdMma); };
-            auto scores = [&](int j, int i, int buf) {           // S[buf] = Q_i K_j^T
+            // (the high word of all descriptors: 8-row groups 1024 bytes apart, 128-byte swizzle)
+            const uint32_t high = (uint32_t)(smem_desc_sw128(0) >> 32);
+            const uint32_t q_low = (uint32_t)smem_desc_sw128(q_smem);
+            auto scores = [&](int j, int i) {                    // S = Q_i K_j^T
+                const int buf = NT == 2 ? i : j & 1;
                 if (elect_one()) {
 #pragma unroll
-                    for (int p = 0; p < kParts; ++p)
+                    for (int p = 0; p < kParts; ++p) {
+                        const uint32_t k_low = (uint32_t)smem_desc_sw128(stage(S::keys(j) + p));
+                        const uint32_t row = q_low + i * (S::kQTile / 16) + p * kPlanes * 1024, d = tmem + 128 * buf;
+                        if (p == 0) mma_f16_ss<false>(d, row, k_low, high, idesc_s);
 #pragma unroll
-                        for (int c = 0; c < kPlanes; ++c)
-#pragma unroll
-                            for (int k = 0; k < 4; ++k)
-                                mma_f16_ss(tmem + 128 * buf, smem_desc_sw128(q_smem + i * S::kQTile + (p * kPlanes + c) * 16384 + k * 32),
-                                           smem_desc_sw128(stage(2 * kParts * j + p) + c * 16384 + k * 32), idesc_s, p + c + k > 0);
-                    mma_commit(smem_u32(&s_s[buf]));
+                        for (int k = p == 0 ? 1 : 0; k < 4 * kPlanes; ++k) {
+                            const int at = (k / 4) * 1024 + (k % 4) * 2;           // 64-channel planes of 16 KB, steps of 32 bytes
+                            mma_f16_ss<true>(d, row + at, k_low + at, high, idesc_s);
+                        }
+                    }
+                    mma_commit(smem_u32(&ctl.s[buf]));
                 }
                 __syncwarp();
             };
-            auto products = [&](int j, int i, int buf) {         // O_i += P V_j
+            auto products = [&](int j, int i) {                  // O_i += P V_j
+                const int buf = NT == 2 ? i : j & 1;
                 if (elect_one()) {
+                    const uint32_t from = tmem + (S::kEarly ? 384 + 64 * i : 128 * buf);
 #pragma unroll
-                    for (int p = 0; p < kParts; ++p)
+                    for (int p = 0; p < kParts; ++p) {
+                        const uint32_t at = stage(S::values(j, n) + p), d = tmem + S::kOCol + i * DP + p * 128;
+                        const uint32_t v_low = (uint32_t)(CACHED ? smem_desc_sw128(at) : smem_desc_n_major(at));
+                        if (j > 0) mma_f16_ts<true>(d, from, v_low, high, idesc_o);
+                        else mma_f16_ts<false>(d, from, v_low, high, idesc_o);
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            const uint32_t v = stage(2 * kParts * j + kParts + p);
-                            const uint64_t desc = CACHED ? smem_desc_sw128(v + (k / 4) * (kCh * 128) + (k % 4) * 32) : smem_desc_n_major(v + k * 2048);
-                            mma_f16_ts(tmem + S::kOCol + i * DP + p * 128, tmem + (S::kEarly ? 384 + 64 * i : 128 * buf) + 8 * k, desc, idesc_o, j > 0 || k > 0);
-                        }
+                        for (int k = 1; k < 8; ++k)
+                            mma_f16_ts<true>(d, from + 8 * k, v_low + (CACHED ? (k / 4) * (kCh * 8) + (k % 4) * 2 : k * 128), high, idesc_o);
+                    }
                 }
                 __syncwarp();
             };
@@ -709,65 +678,66 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 }
                 __syncwarp();
             };
-            ok = wait_all(smem_u32(&s_q), 0, abort_flag, watchdog, kWdMma);
-            for (int p = 0; ok && p < kParts; ++p) ok = wait_kv(p);
-            if (ok) {
+            auto all_there = [&](int first) {
+                for (int p = 0; ok && p < kParts; ++p) ok = wait_all(full_kv(first + p), ((first + p) / kStages) & 1, abort_flag, watchdog, kWdMma);
+                return ok;
+            };
+            ok = wait_all(smem_u32(&ctl.q), 0, abort_flag, watchdog, kWdMma);
+            if (all_there(0)) {
                 tc_fence_after();
-                for (int i = 0; i < NT; ++i) scores(0, i, i);
+                for (int i = 0; i < NT; ++i) scores(0, i);
                 release(0);
             }
             for (int j = 0; j < n && ok; ++j) {
-                const int vuse = 2 * kParts * j + kParts, kuse = 2 * kParts * (j + 1);
-                if ((NT == 1 || S::kEarly) && j + 1 < n) {
-                    for (int p = 0; ok && p < kParts; ++p) ok = wait_kv(kuse + p);
+                const int vuse = S::values(j, n), kuse = S::keys(j + 1);
+                if (S::kAhead && j + 1 < n) {
+                    all_there(kuse);
                     for (int i = 0; i < NT && ok; ++i) {
-                        if (S::kEarly) ok = wait_all(smem_u32(&s_free[i]), j & 1, abort_flag, watchdog, kWdMma);
+                        if (S::kEarly) ok = wait_all(smem_u32(&ctl.free[i]), j & 1, abort_flag, watchdog, kWdMma);
                         if (!ok) break;
                         tc_fence_after();
-                        scores(j + 1, i, NT == 1 ? (j + 1) & 1 : i);
+                        scores(j + 1, i);
                     }
                     if (!ok) break;
                     release(kuse);
                 }
                 for (int i = 0; i < NT && ok; ++i) {
-                    const int buf = NT == 2 ? i : j & 1;
-                    ok = wait_all(smem_u32(&s_p[buf]), NT == 2 ? j & 1 : (j >> 1) & 1, abort_flag, watchdog, kWdMma);
-                    for (int p = 0; ok && i == 0 && p < kParts; ++p) ok = wait_kv(vuse + p);
-                    if (!CACHED && ok && i == 0) {
-                        ok = wait_all(smem_u32(&s_meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdMma);
-                        const bool clean = all_valid(metas[j % kMetas]);
+                    ok = wait_all(smem_u32(&ctl.p[NT == 2 ? i : j & 1]), NT == 2 ? j & 1 : (j >> 1) & 1, abort_flag, watchdog, kWdMma);
+                    if (i == 0 && all_there(vuse) && !CACHED) {
+                        ok = wait_all(smem_u32(&ctl.meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdMma);
+                        const bool clean = all_valid(ctl.metas[j % kMetas]);
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&s_used[j % kMetas]));
+                        if (lane == 0) mbar_arrive(smem_u32(&ctl.used[j % kMetas]));
                         if (!clean && ok) {
-                            if (lane == 0) mbar_arrive(smem_u32(&s_landed));
-                            ok = wait_all(smem_u32(&s_fixed), mends & 1, abort_flag, watchdog, kWdMma);
+                            if (lane == 0) mbar_arrive(smem_u32(&ctl.landed));
+                            ok = wait_all(smem_u32(&ctl.fixed), mends & 1, abort_flag, watchdog, kWdMma);
                             ++mends;
                         }
                     }
                     if (!ok) break;
                     tc_fence_after();
-                    products(j, i, buf);
-                    if (S::kPerTile || (j + 1 == n && i + 1 == NT)) {
-                        if (elect_one()) mma_commit(smem_u32(&s_o[S::kPerTile ? i : 0]));
+                    products(j, i);
+                    if (S::kAhead || j + 1 == n) {
+                        if (elect_one()) mma_commit(smem_u32(&ctl.o[i]));
                         __syncwarp();
                     }
-                    if (NT == 2 && !S::kEarly && j + 1 < n) {
-                        for (int p = 0; ok && i == 0 && p < kParts; ++p) ok = wait_kv(kuse + p);
-                        if (!ok) break;
-                        scores(j + 1, i, i);
+                    if (!S::kAhead && j + 1 < n) {
+                        if (i == 0 && !all_there(kuse)) break;
+                        tc_fence_after();
+                        scores(j + 1, i);
                     }
                 }
                 if (!ok) break;
                 release(vuse);
-                if (NT == 2 && !S::kEarly && j + 1 < n) release(kuse);
+                if (!S::kAhead && j + 1 < n) release(kuse);
             }
         });
     }
-    if (!ok && warp == 12) drain_after_abort();
+    if (!ok && warp == kMmaWarp) drain_after_abort();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 12) tmem_dealloc<1>(tmem, 512);
+    if (warp == kMmaWarp) tmem_dealloc<1>(tmem, 512);
 }
 
 template <int DP, int NT, bool CACHED>
@@ -784,15 +754,22 @@ cudaError_t launch(const Attention& a, cudaStream_t stream) {
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), Shape<DP, NT>::kSmem);
     if (e != cudaSuccess) return e;
     CUtensorMap map_k = {}, map_v = {};
-    if (!CACHED && a.kv_rows > 0) {                             // channels of a head, heads, rows
+    bool mapped = true;
+    if (CACHED && a.wide_keys > 0) {                            // widened: keys [unit][key][channel], values [unit][channel][key]
+        const uint64_t D = (uint64_t)a.head_dim, L = (uint64_t)a.wide_keys, dk[3] = {D, L, (uint64_t)a.units}, dv[3] = {L, D, (uint64_t)a.units};
+        const uint64_t sk[2] = {D * 2, L * D * 2}, sv[2] = {L * 2, L * D * 2};
+        const uint32_t bk[3] = {64, kKeys, 1}, bv[3] = {64, (uint32_t)Shape<DP, NT>::kCh, 1};
+        mapped = encode_tiled(&map_k, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, a.wide, dk, sk, bk, CU_TENSOR_MAP_SWIZZLE_128B) &&
+                 encode_tiled(&map_v, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, static_cast<const uint16_t*>(a.wide) + a.units * L * D, dv, sv, bv, CU_TENSOR_MAP_SWIZZLE_128B);
+    } else if (!CACHED && a.kv_rows > 0) {                      // channels of a head, heads, rows
         const uint64_t dims[3] = {(uint64_t)a.head_dim, (uint64_t)a.kv_heads, (uint64_t)a.kv_rows};
         const uint32_t box[3] = {64, 1, kKeys};
         const uint64_t head = (uint64_t)a.head_dim * 2, sk[2] = {head, (uint64_t)a.ldk * 2}, sv[2] = {head, (uint64_t)a.ldv * 2};
-        if (!encode_tiled(&map_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, a.k, dims, sk, box, CU_TENSOR_MAP_SWIZZLE_128B) ||
-            !encode_tiled(&map_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, a.v, dims, sv, box, CU_TENSOR_MAP_SWIZZLE_128B))
-            return cudaErrorUnknown;
+        mapped = encode_tiled(&map_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, a.k, dims, sk, box, CU_TENSOR_MAP_SWIZZLE_128B) &&
+                 encode_tiled(&map_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, a.v, dims, sv, box, CU_TENSOR_MAP_SWIZZLE_128B);
     }
-    const dim3 grid((unsigned)row_tiles(a), (unsigned)a.chunks, (unsigned)(a.batch * a.kv_heads));
+    if (!mapped) return cudaErrorUnknown;
+    const dim3 grid((unsigned)row_tiles(a), (unsigned)a.chunks, (unsigned)a.units);
     return launch_pdl3(kern, grid, kThreads, Shape<DP, NT>::kSmem, stream, a, map_k, map_v, watchdog);
 }
 template <bool CACHED>

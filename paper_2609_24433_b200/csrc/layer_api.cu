@@ -45,28 +45,50 @@ size_t part_bytes(const Attention& a) {
 size_t ml_bytes(const Attention& a) {
     return a.chunks <= 1 ? 0 : align_up(sizeof(float) * 2 * (size_t)a.q_rows * a.q_heads * a.chunks, 256);
 }
+// Widened codes: so many (sequence, kv head) pairs at a time as kWideBytes hold, one at least.
+constexpr size_t kWideBytes = 256ull << 20;
+size_t wide_bytes(Attention& a, Route route) {
+    a.first_unit = 0;
+    a.units = a.batch * a.kv_heads;
+    a.wide_keys = 0;
+    if (route != Route::Tiles || !a.cached) return 0;
+    a.wide_keys = ceil_div(a.max_kv, 128) * 128;
+    const size_t unit = (size_t)a.wide_keys * a.head_dim * 4;
+    if (unit == 0) return 0;
+    const int64_t fit = (int64_t)(kWideBytes / unit);
+    if (fit < a.units) a.units = fit > 1 ? (int)fit : 1;
+    return align_up(unit * a.units, 256);
+}
 }  // namespace
 
 size_t attention_workspace_bytes(const Attention& given) {
     Attention a = given;
-    plan(a);
-    return part_bytes(a) + ml_bytes(a);
+    const Route route = plan(a);
+    return part_bytes(a) + ml_bytes(a) + wide_bytes(a, route);
 }
 
 fq_status launch_attention(Attention& a, void* workspace, size_t ws_bytes, cudaStream_t stream) {
     const Route route = plan(a);
-    const size_t parts = part_bytes(a), need = parts + ml_bytes(a);
+    const size_t parts = part_bytes(a), mls = ml_bytes(a), need = parts + mls + wide_bytes(a, route);
     if (need > 0) {
         if (!workspace) return FQ_ERR_INVALID_ARG;
         if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return FQ_ERR_ALIGNMENT;
         if (ws_bytes < need) return FQ_ERR_NOMEM;
         a.part = static_cast<float*>(workspace);
         a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + parts);
+        a.wide = static_cast<uint8_t*>(workspace) + parts + mls;
     }
-    const cudaError_t e = route == Route::Tokens  ? launch_attention_tokens(a, stream)
-                          : route == Route::Tiles ? launch_attention_tiles(a, stream)
-                                                  : launch_attention_simt(a, stream);
-    if (e != cudaSuccess) return FQ_ERR_CUDA;
+    if (route == Route::Tiles) {
+        const int all = a.batch * a.kv_heads, step = a.units;
+        for (a.first_unit = 0; a.first_unit < all; a.first_unit += step) {
+            a.units = all - a.first_unit < step ? all - a.first_unit : step;
+            if (a.cached && launch_attention_widen(a, stream) != cudaSuccess) return FQ_ERR_CUDA;
+            if (launch_attention_tiles(a, stream) != cudaSuccess) return FQ_ERR_CUDA;
+        }
+    } else {
+        const cudaError_t e = route == Route::Tokens ? launch_attention_tokens(a, stream) : launch_attention_simt(a, stream);
+        if (e != cudaSuccess) return FQ_ERR_CUDA;
+    }
     if (a.chunks > 1 && launch_attention_join(a, stream) != cudaSuccess) return FQ_ERR_CUDA;
     return FQ_OK;
 }

@@ -89,6 +89,10 @@ struct Attention {
     int tile_rows;                  // (token, head of a group) rows per tile
     float* part;                    // [q_rows][q_heads][chunks][head_dim], then [..][2] maxima and sums
     float* part_ml;
+    // (sequence, kv head) pairs of a launch; of the cache's, the codes widened to binary16 (many queries)
+    int first_unit, units;
+    void* wide;
+    int64_t wide_keys;              // keys of a unit, a multiple of 128
 };
 fq_status launch_attention(Attention& a, void* workspace, size_t ws_bytes, cudaStream_t stream);
 size_t attention_workspace_bytes(const Attention& a);
