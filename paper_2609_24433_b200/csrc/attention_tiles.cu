@@ -6,9 +6,9 @@
 // operand.
 //   warps 0-7    softmax: a warpgroup per row tile, or the two halves of a row
 //   warps 8-11   which keys of a tile there are, the scales of cached ones
-//   warp 12      issues the MMAs
-//   warp 13      copies keys and values by TMA into 128-byte-swizzled stages of 128 keys x 64 or 128 channels (14, 15 complete the
-//                warpgroup, whose registers go to the softmax)
+//   warp 12      issues the MMAs (D = 64 and two row tiles: those of the first one, warp 14 those of the second)
+//   warp 13      copies keys and values by TMA into 128-byte-swizzled stages of 128 keys x 64 or 128 channels (the others up to 15
+//                complete the warpgroup, whose registers go to the softmax)
 // With two row tiles (D <= 128) the tensor core works on one while the other's probabilities are computed; with one (D > 128,
 // or few rows) S is double-buffered instead.
 //
@@ -34,7 +34,7 @@
 namespace fq {
 namespace {
 
-constexpr int kThreads = 16 * 32, kSoftmaxWarps = 8, kLoadWarp = 8, kMmaWarp = 12, kTmaWarp = 13;
+constexpr int kThreads = 16 * 32, kSoftmaxWarps = 8, kLoadWarp = 8, kMmaWarp = 12, kTmaWarp = 13, kSecondMmaWarp = 14;
 // Registers: a softmax thread holds a row of 128 scores.  The launch's 512 x 128 are shared out as 256 x 200 + 256 x 56.
 constexpr int kRegsLaunch = 128, kRegsSoftmax = 200, kRegsOther = 56;
 static_assert(256 * kRegsSoftmax + 256 * kRegsOther <= kThreads * kRegsLaunch, "");
@@ -57,7 +57,7 @@ template <int STAGES>
 struct __align__(16) Control {
     float rows[256];                    // maxima, sums on their way between the threads of a row
     KeyMeta metas[kMetas];
-    uint64_t full_kv[STAGES], empty_kv[STAGES], meta[kMetas], used[kMetas], landed, fixed, s[2], p[2], o[2], free[2], q;
+    uint64_t full_kv[STAGES], empty_kv[STAGES], meta[kMetas], used[kMetas], landed, fixed, s[2], p[2], o[2], free[2], turn[8], q;
     uint32_t tmem;
     int abort;
 };
@@ -77,6 +77,11 @@ struct Shape {
     // Two tiles of 64 channels leave TMEM for probabilities of their own (columns 384 ..): the next scores are computed as soon
     // as the last ones have been read.  Elsewhere probabilities lie over their scores.
     static constexpr bool kEarly = NT == 2 && DP == 64;
+    // The two row tiles then have an issuing warp each, and the two warps of a scheduler take turns at the exponentials (`turn`):
+    // left alone they meet there, wait for the unit together and leave it idle together at everything else.  (48 x 8 heads of 64,
+    // 1024 queries x 1500 keys: one warp 557 us, two 533, and turns 484; turns handed over a quarter early 527.  D = 128, where
+    // S cannot be freed early: turns 329 against 316.)
+    static constexpr int kIssuers = kEarly ? 2 : 1;
     static constexpr bool kAhead = NT == 1 || kEarly;           // scores of tile j + 1 are issued ahead of the products of tile j
     // Stages are filled in the order in which they are needed: K0 V0 K1 V1 .., or ahead: K0 K1 V0 K2 V1 ..  First use by the keys,
     // by the values of tile j of n.
@@ -215,6 +220,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     Control<kStages>& ctl = *reinterpret_cast<Control<kStages>*>(smem_raw + S::kTiles);
     volatile int* abort_flag = &ctl.abort;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const bool issues = warp == kMmaWarp || (S::kIssuers == 2 && warp == kSecondMmaWarp);
     const uint32_t q_smem = smem_u32(smem_raw), ring = q_smem + NT * S::kQTile;
     if (q_smem & 1023u) {                                       // (swizzled tiles start on 1024 bytes; nothing else is in shared memory)
         if (threadIdx.x == 0) atomicOr(watchdog, kWdProducer);
@@ -225,8 +231,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
     auto stage = [&](int n) { return ring + (uint32_t)(n % kStages) * S::kStageBytes; };
 
     auto init_barriers = [&]() {
-        for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&ctl.full_kv[i]), 1); mbar_init(smem_u32(&ctl.empty_kv[i]), 1); }
-        for (int i = 0; i < kMetas; ++i) { mbar_init(smem_u32(&ctl.meta[i]), 4); mbar_init(smem_u32(&ctl.used[i]), kSoftmaxWarps + (CACHED ? 0 : 1)); }
+        for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&ctl.full_kv[i]), 1); mbar_init(smem_u32(&ctl.empty_kv[i]), S::kIssuers); }
+        for (int i = 0; i < kMetas; ++i) { mbar_init(smem_u32(&ctl.meta[i]), 4); mbar_init(smem_u32(&ctl.used[i]), kSoftmaxWarps + (CACHED ? 0 : S::kIssuers)); }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&ctl.s[i]), 1);
             mbar_init(smem_u32(&ctl.p[i]), 4 * kSplit);
@@ -234,7 +240,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             mbar_init(smem_u32(&ctl.free[i]), 4 * kSplit);
         }
         mbar_init(smem_u32(&ctl.q), kSoftmaxWarps);
-        mbar_init(smem_u32(&ctl.landed), 1);
+        for (int i = 0; i < 8; ++i) mbar_init(smem_u32(&ctl.turn[i]), 1);
+        mbar_init(smem_u32(&ctl.landed), S::kIssuers);
         mbar_init(smem_u32(&ctl.fixed), 4);
         fence_mbarrier_init();
     };
@@ -377,8 +384,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                         x = max3(x, v[16 * g + i], v[16 * g + i + 1]);
                         y = max3(y, v[16 * g + i + 2], v[16 * g + i + 3]);
                     }
-                    top = fmaxf(top, fmaxf(x, y) * (CACHED ? fmaxf(factor * ks[g], FLT_MIN) : fmaxf(factor, FLT_MIN)));
+                    top = fmaxf(top, CACHED ? fmaxf(x, y) * fmaxf(factor * ks[g], FLT_MIN) : fmaxf(x, y));
                 }
+                if (!CACHED) top *= fmaxf(factor, FLT_MIN);
                 if (kSplit > 1) {
                     seat[split * NT * 128] = top;
                     meet();                                      // (and all of them have read their scores)
@@ -424,6 +432,10 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     e = now_e;
                 }
                 const float minus = base == -INFINITY ? 0.0f : -base;
+                if (S::kEarly && j + mine > 0) {                 // its turn at the exponentials
+                    ok = wait_all(smem_u32(&ctl.turn[warp]), (j - 1 + mine) & 1, abort_flag, watchdog, kWdSoftmax);
+                    if (!ok) continue;
+                }
                 // ---- probabilities, over the scores or beside them
                 float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
                 float total = 0.0f;
@@ -451,6 +463,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     }
                     tmem_st16(p_addr + 16 * c, p);
                 }
+                if (S::kEarly && lane == 0) mbar_arrive(smem_u32(&ctl.turn[warp ^ 4]));
                 if (!CACHED) {
                     sum0 = f2_add(sum0, sum1);
                     total = sum0.x + sum0.y;
@@ -626,10 +639,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 return;
             }
             // ================================================================ MMA issue
-            // One warp serves both row tiles in turn, products and next scores of one back to back: they then work half a period apart,
+            // With D = 128 one warp serves both row tiles in turn, products and next scores of one back to back: they then work half a period apart,
             // one at the exponentials, one at the tensor core.  (A warp for each let the MMAs of both mix, so that both ended
-            // together and met again: 1.4 times the time at D = 128.)
-            if (warp != kMmaWarp || n == 0) return;
+            // together and met again: 1.4 times the time.)
+            if (!issues || n == 0) return;
+            const int lo = warp == kMmaWarp ? 0 : 1, hi = S::kIssuers == 2 ? lo + 1 : NT;         // this warp's row tiles
             int mends = 0;                                      // tiles with masked keys so far
             const uint32_t idesc_s = instr_desc_16(CACHED ? 0 : 1, false, kKeys), idesc_o = instr_desc_16(CACHED ? 0 : 1, !CACHED, kCh);
             // (the high word of all descriptors: 8-row groups 1024 bytes apart, 128-byte swizzle)
@@ -685,14 +699,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             ok = wait_all(smem_u32(&ctl.q), 0, abort_flag, watchdog, kWdMma);
             if (all_there(0)) {
                 tc_fence_after();
-                for (int i = 0; i < NT; ++i) scores(0, i);
+                for (int i = lo; i < hi; ++i) scores(0, i);
                 release(0);
             }
             for (int j = 0; j < n && ok; ++j) {
                 const int vuse = S::values(j, n), kuse = S::keys(j + 1);
                 if (S::kAhead && j + 1 < n) {
                     all_there(kuse);
-                    for (int i = 0; i < NT && ok; ++i) {
+                    for (int i = lo; i < hi && ok; ++i) {
                         if (S::kEarly) ok = wait_all(smem_u32(&ctl.free[i]), j & 1, abort_flag, watchdog, kWdMma);
                         if (!ok) break;
                         tc_fence_after();
@@ -701,9 +715,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     if (!ok) break;
                     release(kuse);
                 }
-                for (int i = 0; i < NT && ok; ++i) {
+                for (int i = lo; i < hi && ok; ++i) {
                     ok = wait_all(smem_u32(&ctl.p[NT == 2 ? i : j & 1]), NT == 2 ? j & 1 : (j >> 1) & 1, abort_flag, watchdog, kWdMma);
-                    if (i == 0 && all_there(vuse) && !CACHED) {
+                    if (i == lo && all_there(vuse) && !CACHED) {
                         ok = wait_all(smem_u32(&ctl.meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdMma);
                         const bool clean = all_valid(ctl.metas[j % kMetas]);
                         __syncwarp();
@@ -733,7 +747,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             }
         });
     }
-    if (!ok && warp == kMmaWarp) drain_after_abort();
+    if (!ok && issues) drain_after_abort();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
