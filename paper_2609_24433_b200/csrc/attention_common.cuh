@@ -7,6 +7,8 @@
 
 namespace fq {
 
+constexpr int kTokensBlock = 256;       // keys of a block of work of the few-queries kernel
+
 inline int64_t row_tiles(const Attention& a) {
     const int64_t n = (a.max_q * a.group + a.tile_rows - 1) / a.tile_rows;
     return n < 1 ? 1 : n > 0x7fffffff ? 0x7fffffff : n;
@@ -15,6 +17,7 @@ cudaError_t launch_attention_widen(const Attention& a, cudaStream_t stream);
 cudaError_t launch_attention_tiles(const Attention& a, cudaStream_t stream);
 cudaError_t launch_attention_tokens(const Attention& a, cudaStream_t stream);
 cudaError_t launch_attention_simt(const Attention& a, cudaStream_t stream);
+int tokens_ctas(const Attention& a);             // of the few-queries kernel, resident at once
 cudaError_t launch_attention_join(const Attention& a, cudaStream_t stream);
 
 #ifdef __CUDACC__
@@ -104,6 +107,67 @@ template <typename T, bool CACHED>
 __device__ __forceinline__ float load_value(const Attention& a, const KeyPlace& p, int hk, int d) {
     if (!CACHED) return load1(static_cast<const T*>(a.v) + p.row * a.ldv + (int64_t)hk * a.head_dim + d);
     return (float)a.cache.v[(p.row * a.head_dim + d) * a.cache.page + p.offset] * ld_global_f32(a.cache.v_scale + p.row);
+}
+
+// Joins n partial results of a row, at(c) their places: o = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c.  WARPS warps (1, or
+// all 4 of the CTA) take them in turn, four at a time under way each: a lone sequence has few rows and many chunks (16384 keys,
+// 32 heads of 128 in 64 chunks: the whole call 51 us with one warp a row and one chunk at a time, 17 so).  Fixed order of sums.
+template <typename T, int WARPS, typename At>
+__device__ __forceinline__ void join_row(const Attention& a, int n, At at, T* y) {
+    __shared__ float4 seats[4][64];
+    __shared__ float sums[4];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, part = warp % WARPS;
+    float m = -INFINITY;
+    for (int c = lane; c < n; c += 32) m = fmaxf(m, ld_global_f32(a.part_ml + 2 * at(c)));
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+    const float base = m == -INFINITY ? 0.0f : m;
+    const bool low = 4 * lane < a.head_dim, high = 128 + 4 * lane < a.head_dim;
+    float l = 0.0f;
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f), p = o;       // channels 4 lane .., 128 + 4 lane ..
+    for (int c0 = part; c0 < n; c0 += 32 * WARPS) {              // (a lane looks up the weight of one of 32 chunks)
+        const int own = c0 + WARPS * lane;
+        const float mine = own < n ? exp2f(ld_global_f32(a.part_ml + 2 * at(own)) - base) : 0.0f;
+        if (own < n) l = fmaf(mine, ld_global_f32(a.part_ml + 2 * at(own) + 1), l);
+        for (int i = 0; i < 32 && c0 + WARPS * i < n; i += 4) {
+            float4 x[4], z[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int c = c0 + WARPS * (i + k);
+                const float* from = a.part + at(c) * a.head_dim + 4 * lane;
+                x[k] = c < n && low ? ld_global_f4(from) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                z[k] = c < n && high ? ld_global_f4(from + 128) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float w = __shfl_sync(0xffffffffu, mine, i + k);
+                o.x = fmaf(w, x[k].x, o.x); o.y = fmaf(w, x[k].y, o.y); o.z = fmaf(w, x[k].z, o.z); o.w = fmaf(w, x[k].w, o.w);
+                p.x = fmaf(w, z[k].x, p.x); p.y = fmaf(w, z[k].y, p.y); p.z = fmaf(w, z[k].z, p.z); p.w = fmaf(w, z[k].w, p.w);
+            }
+        }
+    }
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+    if (WARPS > 1) {
+        __syncthreads();                                         // (the last row's seats are read)
+        seats[warp][lane] = o;
+        seats[warp][32 + lane] = p;
+        if (lane == 0) sums[warp] = l;
+        __syncthreads();
+        if (part > 1) return;                                    // warp 0 has the low channels, warp 1 the high ones
+        l = 0.0f;
+        o = p = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) {
+            const float4 x = seats[w][32 * part + lane];
+            l += sums[w];
+            o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+        }
+        if (part == 1) p = o;
+    }
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    if (low && part == 0) store4(y + 4 * lane, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    if (high && part == (WARPS > 1 ? 1 : 0)) store4(y + 128 + 4 * lane, p.x * inv, p.y * inv, p.z * inv, p.w * inv);
 }
 
 }  // namespace

@@ -156,80 +156,23 @@ __global__ void __launch_bounds__(kThreads) attention_simt_kernel(const Attentio
     }
 }
 
-// Joins the chunks of a row: o = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c.  WARPS warps per row take its chunks in turn,
-// four at a time under way each: a lone sequence has few rows and many chunks (16384 keys, 32 heads in 64 chunks: the whole call
-// took 51 us with one warp and one chunk at a time).  Warps and chunks are summed in a fixed order.
+// Joins the chunks of the rows that have more than one, WARPS warps to a row.
 template <typename T, int WARPS>
 __global__ void __launch_bounds__(128) attention_join_kernel(const Attention a) {
-    __shared__ float4 seats[4][64];
-    __shared__ float sums[4];
     griddep_wait();
     const int b = blockIdx.y;
     const Sequence s = sequence_of(a, b);
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, part = warp % WARPS;
     const int64_t rows = s.queries * a.q_heads;
     constexpr int kRows = 4 / WARPS;
     for (int64_t r0 = (int64_t)blockIdx.x * kRows; r0 < rows; r0 += (int64_t)gridDim.x * kRows) {
-        const int64_t r = r0 + warp / WARPS;                     // (WARPS == 4: the same for the whole CTA)
+        const int64_t r = r0 + threadIdx.x / 32 / WARPS;         // (WARPS == 4: the same for the whole CTA)
         if (r >= rows) continue;
         const int64_t token = r / a.q_heads, head = r % a.q_heads;
         const int64_t tile = (token * a.group + head % a.group) / a.tile_rows;
         const int n = tile_keys(a, s, tile, a.tile_rows).chunks;
         if (n <= 1) continue;
         const int64_t at = ((s.q0 + token) * a.q_heads + head) * a.chunks;
-        const float* ml = a.part_ml + 2 * at;
-        const float* from = a.part + at * a.head_dim + 4 * lane;
-        float m = -INFINITY;
-        for (int c = lane; c < n; c += 32) m = fmaxf(m, ld_global_f32(ml + 2 * c));
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-        const float base = m == -INFINITY ? 0.0f : m;
-        const bool low = 4 * lane < a.head_dim, high = 128 + 4 * lane < a.head_dim;
-        float l = 0.0f;
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f), p = o;   // channels 4 lane .., 128 + 4 lane ..
-        for (int c0 = part; c0 < n; c0 += 32 * WARPS) {          // (a lane looks up the weight of one of 32 chunks)
-            const int own = c0 + WARPS * lane;
-            const float mine = own < n ? exp2f(ld_global_f32(ml + 2 * own) - base) : 0.0f;
-            if (own < n) l = fmaf(mine, ld_global_f32(ml + 2 * own + 1), l);
-            for (int i = 0; i < 32 && c0 + WARPS * i < n; i += 4) {
-                float4 x[4], y[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int c = c0 + WARPS * (i + k);
-                    x[k] = c < n && low ? ld_global_f4(from + (int64_t)c * a.head_dim) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    y[k] = c < n && high ? ld_global_f4(from + (int64_t)c * a.head_dim + 128) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float w = __shfl_sync(0xffffffffu, mine, i + k);
-                    o.x = fmaf(w, x[k].x, o.x); o.y = fmaf(w, x[k].y, o.y); o.z = fmaf(w, x[k].z, o.z); o.w = fmaf(w, x[k].w, o.w);
-                    p.x = fmaf(w, y[k].x, p.x); p.y = fmaf(w, y[k].y, p.y); p.z = fmaf(w, y[k].z, p.z); p.w = fmaf(w, y[k].w, p.w);
-                }
-            }
-        }
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-        if (WARPS > 1) {
-            __syncthreads();                                     // (the last row's seats are read)
-            seats[warp][lane] = o;
-            seats[warp][32 + lane] = p;
-            if (lane == 0) sums[warp] = l;
-            __syncthreads();
-            if (part > 1) continue;                              // warp 0 has the low channels, warp 1 the high ones
-            l = 0.0f;
-            o = p = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-            for (int w = 0; w < WARPS; ++w) {
-                const float4 x = seats[w][32 * part + lane];
-                l += sums[w];
-                o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
-            }
-            if (part == 1) p = o;
-        }
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-        T* y = static_cast<T*>(a.y) + (s.q0 + token) * a.ldy + head * a.head_dim + 4 * lane;
-        if (low && part == 0) store4(y, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-        if (high && part == (WARPS > 1 ? 1 : 0)) store4(y + 128, p.x * inv, p.y * inv, p.z * inv, p.w * inv);
+        join_row<T, WARPS>(a, n, [&](int c) { return at + c; }, static_cast<T*>(a.y) + (s.q0 + token) * a.ldy + head * a.head_dim);
     }
 }
 

@@ -12,6 +12,10 @@
 // four.  Queries are divided by the power of two below their row's largest channel and rounded to binary16 (bf16 values
 // keep all their bits above 2^-14 of the row's largest channel; binary32 queries and probabilities go as a sum of two terms).
 //
+// Every CTA takes an equal share of the call's blocks -- 256 keys of 8 or 16 rows of a kv head -- wherever that begins and ends: lengths
+// are known on the device only, and a ragged batch (48 sequences of up to 16384 keys) in chunks of 4096 ended 16 us behind its
+// bytes.  A tile of rows that several shares divide is joined by a second kernel; the others are written here.
+//
 // With p = 2^(s - m): l = sum p, O = sum (p vs 2^(7 - e)) code, e the running exponent of the largest value scale vs.  m follows the
 // maximum lazily, when it has risen by more than 2^8: probabilities stay below 2^15 and, down to 2^-21, normal in binary16.
 #include "attention_common.cuh"
@@ -72,27 +76,109 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255) - 127; }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
 
+// CTAs that an SM holds at once.
+constexpr int tokens_resident(bool bf16, int dp, int nq) { return nq == 1 && bf16 && dp <= 128 ? 3 : 2; }
+
+// Where a share leaves the result of its last tile (begins: block 0 is in this share), or else of its first.
+__device__ __forceinline__ int64_t tokens_seat(int cta, bool begins) { return 2 * (int64_t)cta + (begins ? 1 : 0); }
+
+// Blocks of work: of a sequence, per tile of its rows.
+struct Work {
+    int64_t units;                      // (tile of rows, kv head)
+    int per_unit;
+};
+__device__ __forceinline__ Work work_of(const Attention& a, const Sequence& s, int rows) {
+    Work w;
+    w.units = (s.queries * a.group + rows - 1) / rows * a.kv_heads;
+    w.per_unit = max((int)((s.keys + kTokensBlock - 1) / kTokensBlock), 1);
+    return w;
+}
+// The share of this CTA, blocks first .. last - 1 of all `total`, and the sequence with the first one.
+struct Share {
+    int64_t first, last, total, shares; // as many shares as CTAs, or as blocks
+    int64_t within;                     // blocks of the sequence ahead of the first one
+    int b;
+};
+__device__ __forceinline__ Share share_of(const Attention& a, int rows) {
+    __shared__ int64_t sums[kWarps];
+    __shared__ int64_t found[2];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, each = (a.batch + kWarps * 32 - 1) / (kWarps * 32);
+    const int b0 = min((int)threadIdx.x * each, a.batch), b1 = min(b0 + each, a.batch);
+    auto blocks = [&](int b) {
+        const Work w = work_of(a, sequence_of(a, b), rows);
+        return w.units * w.per_unit;
+    };
+    int64_t own = 0;
+    for (int b = b0; b < b1; ++b) own += blocks(b);
+    int64_t upto = own;                 // this thread's last
+#pragma unroll
+    for (int x = 1; x < 32; x <<= 1) {
+        const int64_t v = __shfl_up_sync(0xffffffffu, upto, x);
+        if (lane >= x) upto += v;
+    }
+    if (lane == 31) sums[warp] = upto;
+    __syncthreads();
+    Share r;
+    r.total = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) upto += sums[w];
+        r.total += sums[w];
+    }
+    r.shares = min((int64_t)gridDim.x, r.total);                // (none empty: the join goes through them without a gap)
+    r.first = r.shares > (int)blockIdx.x ? r.total * blockIdx.x / r.shares : r.total;
+    r.last = r.shares > (int)blockIdx.x ? r.total * (blockIdx.x + 1) / r.shares : r.total;
+    if (upto - own <= r.first && r.first < upto) {
+        int64_t ahead = r.first - (upto - own);
+        int b = b0;
+        for (int64_t n; b < b1 - 1 && ahead >= (n = blocks(b)); ++b) ahead -= n;
+        found[0] = b;
+        found[1] = ahead;
+    }
+    __syncthreads();
+    r.b = (int)found[0];                // (only read where first < last)
+    r.within = found[1];
+    return r;
+}
+
 template <typename T, int DP, int NQ, bool EXACT>
-__global__ void __launch_bounds__(kWarps * 32, NQ == 1 && sizeof(T) == 2 && DP <= 128 ? 3 : 2) attention_tokens_kernel(const Attention a) {
+__global__ void __launch_bounds__(kWarps * 32, tokens_resident(sizeof(T) == 2, DP, NQ)) attention_tokens_kernel(const Attention a) {
     constexpr int kTerms = sizeof(T) == 4 ? 2 : 1;              // binary16 terms of a query or probability
     constexpr int kLines = DP / 64;                             // 64-channel lines of a key, and of values
     constexpr int kRows = 8 * NQ;
     extern __shared__ __align__(128) uint8_t smem[];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
     griddep_wait();
-    const int b = blockIdx.z / a.kv_heads, hk = blockIdx.z % a.kv_heads, chunk = blockIdx.y;
-    const Sequence s = sequence_of(a, b);
+    const Share share = share_of(a, kRows);
+    if (a.splits && threadIdx.x == 0) a.splits[blockIdx.x] = make_int4(0, 0, 0, 0);
     const int D = EXACT ? DP : a.head_dim, P = a.cache.page, shift = 31 - __clz(P);
     const int page_bytes = P * D, pages = (int)min(a.cache.pages, (int64_t)0x7fffffff);
-    const int32_t* table = a.table + b * a.ld_table;
     const uint32_t ring = smem_u32(smem) + warp * (kSlots * kPiece) + lane * 16;
 
-    for (int64_t tile = blockIdx.x; tile * kRows < s.queries * a.group; tile += gridDim.x) {
-        const TileKeys tk = tile_keys(a, s, tile, kRows);
-        if (chunk > 0 && (int64_t)chunk * a.chunk >= tk.end) continue;
+    int b = share.b;
+    int64_t within = share.within;
+    for (int64_t at = share.first; at < share.last;) {
+        const Sequence s = sequence_of(a, b);
+        const Work work = work_of(a, s, kRows);
+        if (within >= work.units * work.per_unit) {              // on to the next sequence
+            ++b;
+            within = 0;
+            continue;
+        }
+        const int64_t unit = within / work.per_unit, tile = unit / a.kv_heads;
+        const int hk = (int)(unit % a.kv_heads), block = (int)(within % work.per_unit);
+        const int blocks = (int)min((int64_t)(work.per_unit - block), share.last - at);
+        within += blocks;
+        at += blocks;
+        const bool whole = blocks == work.per_unit;
+        if (!whole && block == 0 && threadIdx.x == 0) {          // ends in the share that holds the tile's last block
+            const int64_t end = at - blocks + work.per_unit;
+            a.splits[blockIdx.x] = make_int4((int)((end * share.shares - 1) / share.total), b, hk, (int)tile);
+        }
+        const int32_t* table = a.table + b * a.ld_table;
         // (a sequence has fewer than 2^31 keys)
-        const int k0 = chunk * a.chunk, k1 = (int)min(tk.end, (int64_t)k0 + a.chunk);
-        const int tiles = (k1 - k0 + kTile - 1) / kTile;
+        const int k0 = block * kTokensBlock, k1 = (int)min(tile_keys(a, s, tile, kRows).end, (int64_t)k0 + (int64_t)blocks * kTokensBlock);
+        const int tiles = max(k1 - k0 + kTile - 1, 0) / kTile;
         const int mine = tiles > warp ? (tiles - warp + kWarps - 1) / kWarps : 0;
         auto first_key = [&](int n) { return k0 + (warp + n * kWarps) * kTile; };
 
@@ -379,18 +465,33 @@ __global__ void __launch_bounds__(kWarps * 32, NQ == 1 && sizeof(T) == 2 && DP <
                 const float4 v = *reinterpret_cast<const float4*>(from + 4 + d);
                 acc.x = fmaf(f, v.x, acc.x); acc.y = fmaf(f, v.y, acc.y); acc.z = fmaf(f, v.z, acc.z); acc.w = fmaf(f, v.w, acc.w);
             }
-            const int64_t token = s.q0 + row / a.group, head = hk * a.group + row % a.group;
-            if (tk.chunks <= 1) {
+            if (whole) {
+                const int64_t token = s.q0 + row / a.group, head = hk * a.group + row % a.group;
                 const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
                 store4(static_cast<T*>(a.y) + token * a.ldy + head * D + d, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
             } else {
-                const int64_t at = (token * a.q_heads + head) * a.chunks + chunk;
-                *reinterpret_cast<float4*>(a.part + at * D + d) = acc;
-                if (d == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(top, sum);
+                const int64_t seat = tokens_seat(blockIdx.x, block == 0) * kRows + r;
+                *reinterpret_cast<float4*>(a.part + seat * D + d) = acc;
+                if (d == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * seat) = make_float2(top, sum);
             }
         }
         __syncthreads();
     }
+}
+
+// Joins row blockIdx.y of the tile, if there is one, that begins in share blockIdx.x and goes on behind it.
+template <typename T>
+__global__ void __launch_bounds__(128) attention_tokens_join_kernel(const Attention a) {
+    griddep_wait();
+    const int4 split = a.splits[blockIdx.x];
+    const int first = blockIdx.x, b = split.y, hk = split.z;
+    if (split.x <= first) return;
+    const Sequence s = sequence_of(a, b);
+    const int64_t row = (int64_t)split.w * a.tile_rows + blockIdx.y;
+    if (row >= s.queries * a.group) return;
+    const int64_t token = s.q0 + row / a.group, head = hk * a.group + row % a.group;
+    join_row<T, 4>(a, split.x - first + 1, [&](int c) { return tokens_seat(first + c, c == 0) * a.tile_rows + blockIdx.y; },
+                   static_cast<T*>(a.y) + token * a.ldy + head * a.head_dim);
 }
 
 template <typename T, int DP, int NQ, bool EXACT>
@@ -416,9 +517,15 @@ cudaError_t by_width(const Attention& a, dim3 grid, cudaStream_t stream) {
 
 }  // namespace
 
+int tokens_ctas(const Attention& a) { return 148 * tokens_resident(a.dt == FQ_BF16, a.head_dim, a.tile_rows / 8); }
+
 cudaError_t launch_attention_tokens(const Attention& a, cudaStream_t stream) {
-    const dim3 grid((unsigned)row_tiles(a), (unsigned)a.chunks, (unsigned)(a.batch * a.kv_heads));
-    return a.dt == FQ_BF16 ? by_width<__nv_bfloat16>(a, grid, stream) : by_width<float>(a, grid, stream);
+    const dim3 grid((unsigned)a.ctas);
+    const cudaError_t e = a.dt == FQ_BF16 ? by_width<__nv_bfloat16>(a, grid, stream) : by_width<float>(a, grid, stream);
+    if (e != cudaSuccess || !a.splits) return e;
+    const dim3 joins((unsigned)a.ctas, (unsigned)a.tile_rows);
+    return a.dt == FQ_BF16 ? launch_pdl3(attention_tokens_join_kernel<__nv_bfloat16>, joins, 128, 0, stream, a)
+                           : launch_pdl3(attention_tokens_join_kernel<float>, joins, 128, 0, stream, a);
 }
 
 }  // namespace fq

@@ -16,13 +16,17 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 enum class Route { Simt, Tokens, Tiles };
 Route plan(Attention& a) {
     const Route route = a.cached && a.max_q * a.group <= 16 ? Route::Tokens : a.dt == FQ_BF16 ? Route::Tiles : Route::Simt;
-    int64_t least = 256, most = 1 << 30, wave = 2 * 148;
+    int64_t wave = 2 * 148;
     if (route == Route::Tokens) {
         a.tile_rows = a.dt == FQ_F32 || a.max_q * a.group <= 8 ? 8 : 16;     // (two terms of sixteen rows pass the registers)
-        least = 256;
-        most = 4096;
-        wave = 4 * 148;
-    } else if (route == Route::Tiles) {
+        const int64_t blocks = (a.max_kv > 0 ? ceil_div(a.max_kv, kTokensBlock) : 1) * row_tiles(a) * a.batch * a.kv_heads;
+        a.ctas = blocks < tokens_ctas(a) ? (int)blocks : tokens_ctas(a);
+        if (a.ctas < 1) a.ctas = 1;
+        a.chunk = kTokensBlock;
+        a.chunks = 1;
+        return route;
+    }
+    if (route == Route::Tiles) {
         a.tile_rows = a.head_dim <= 128 && a.max_q * a.group > 128 ? 256 : 128;
         wave = 148;
     } else {
@@ -31,18 +35,20 @@ Route plan(Attention& a) {
     const int64_t units = row_tiles(a) * a.batch * a.kv_heads;
     const int64_t splits = route == Route::Tiles ? (units < wave ? wave / (units > 0 ? units : 1) : 1) : ceil_div(wave, units > 0 ? units : 1);
     int64_t chunk = ceil_div(ceil_div(a.max_kv, splits), 256) * 256;
-    if (chunk < least) chunk = least;
-    if (chunk > most) chunk = most;
+    if (chunk < 256) chunk = 256;
     if (ceil_div(a.max_kv, chunk) > 65535) chunk = ceil_div(ceil_div(a.max_kv, 65535), 256) * 256;
     a.chunk = (int)chunk;
     const int64_t chunks = ceil_div(a.max_kv, chunk);
     a.chunks = (int)(chunks < 1 ? 1 : chunks);
     return route;
 }
-size_t part_bytes(const Attention& a) {
+// (few queries: the first and the last tile of every share)
+size_t part_bytes(const Attention& a, Route route) {
+    if (route == Route::Tokens) return a.max_kv <= kTokensBlock ? 0 : align_up(sizeof(float) * 2 * (size_t)a.ctas * a.tile_rows * a.head_dim, 256);
     return a.chunks <= 1 ? 0 : align_up(sizeof(float) * (size_t)a.q_rows * a.q_heads * a.chunks * a.head_dim, 256);
 }
-size_t ml_bytes(const Attention& a) {
+size_t ml_bytes(const Attention& a, Route route) {
+    if (route == Route::Tokens) return a.max_kv <= kTokensBlock ? 0 : align_up(sizeof(float) * 4 * (size_t)a.ctas * a.tile_rows, 256) + align_up(sizeof(int4) * (size_t)a.ctas, 256);
     return a.chunks <= 1 ? 0 : align_up(sizeof(float) * 2 * (size_t)a.q_rows * a.q_heads * a.chunks, 256);
 }
 // Widened codes: so many (sequence, kv head) pairs at a time as kWideBytes hold, one at least.
@@ -64,12 +70,12 @@ size_t wide_bytes(Attention& a, Route route) {
 size_t attention_workspace_bytes(const Attention& given) {
     Attention a = given;
     const Route route = plan(a);
-    return part_bytes(a) + ml_bytes(a) + wide_bytes(a, route);
+    return part_bytes(a, route) + ml_bytes(a, route) + wide_bytes(a, route);
 }
 
 fq_status launch_attention(Attention& a, void* workspace, size_t ws_bytes, cudaStream_t stream) {
     const Route route = plan(a);
-    const size_t parts = part_bytes(a), mls = ml_bytes(a), need = parts + mls + wide_bytes(a, route);
+    const size_t parts = part_bytes(a, route), mls = ml_bytes(a, route), need = parts + mls + wide_bytes(a, route);
     if (need > 0) {
         if (!workspace) return FQ_ERR_INVALID_ARG;
         if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return FQ_ERR_ALIGNMENT;
@@ -77,6 +83,7 @@ fq_status launch_attention(Attention& a, void* workspace, size_t ws_bytes, cudaS
         a.part = static_cast<float*>(workspace);
         a.part_ml = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + parts);
         a.wide = static_cast<uint8_t*>(workspace) + parts + mls;
+        if (route == Route::Tokens) a.splits = reinterpret_cast<int4*>(static_cast<uint8_t*>(workspace) + parts + mls - align_up(sizeof(int4) * (size_t)a.ctas, 256));
     }
     if (route == Route::Tiles) {
         const int all = a.batch * a.kv_heads, step = a.units;

@@ -87,6 +87,9 @@ struct Attention {
     int chunk;                      // keys per chunk
     int chunks;                     // of max_kv keys
     int tile_rows;                  // (token, head of a group) rows per tile
+    // (few queries: equal shares of all the work instead, `ctas` of them; tiles that lie in several are listed in `splits`)
+    int ctas;
+    int4* splits;
     float* part;                    // [q_rows][q_heads][chunks][head_dim], then [..][2] maxima and sums
     float* part_ml;
     // (sequence, kv head) pairs of a launch; of the cache's, the codes widened to binary16 (many queries)

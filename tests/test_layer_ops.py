@@ -388,6 +388,33 @@ def test_attention_kv8_pages_that_are_none_and_cut_lengths(queries, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("Hq,Hk,D,P,dtype", [(4, 2, 64, 64, "bf16"), (16, 1, 128, 32, "bf16"), (8, 1, 256, 128, "bf16"), (3, 1, 128, 64, "f32")])
+def test_attention_kv8_few_queries_of_many_sequences(Hq, Hk, D, P, dtype):
+    """Equal shares of a ragged batch: tiles inside a share, across two, over many; sequences without keys or queries; more
+    sequences than a CTA has threads; hints of max_q that are too small."""
+    lens = [0, 1, 255, 256, 257, 511, 513, 90] * 37 + [9000, 0, 20]
+    queries = [1, 0, 2, 1, 1, 1, 1, 3] * 37 + [1, 0, 1]
+    rows = sum(queries)
+    cache = filled_cache(400, Hk, D, P, 61)
+    gen = torch.Generator().manual_seed(62)
+    table = torch.randint(0, 400, (len(lens), -(-9000 // P)), generator=gen).int().cuda()
+    check_cache_attention(cache, table, lens, queries, Hq, dtype, True, seed=63, max_q=3)
+    check_cache_attention(cache, table, lens, queries, Hq, dtype, True, seed=64, max_q=1)
+    q, offsets = rand((rows, Hq * D), 65, TYPES[dtype]), offsets_of(queries)
+    one, other = (fq.attention_kv8(q, Hq, cache, table, ints(lens), offsets, max_q=3) for _ in range(2))
+    assert torch.equal(one, other)
+
+
+@gpu
+@pytest.mark.parametrize("Hq,D,lens", [(8, 128, [16384]), (8, 256, [16384]), (1, 64, [0, 0, 16384, 0]), (8, 128, [100] * 500)])
+def test_attention_kv8_shares_of_one_long_or_many_short_sequences(Hq, D, lens):
+    cache = filled_cache(300, 1, D, 64, 66)
+    gen = torch.Generator().manual_seed(67)
+    table = torch.randint(0, 300, (len(lens), -(-max(lens) // 64)), generator=gen).int().cuda()
+    check_cache_attention(cache, table, lens, [1] * len(lens), Hq, "bf16", True, seed=68, max_q=1)
+
+
+@gpu
 def test_attention_kv8_peaked_scores_and_repeated_pages():
     """Scores far apart (the running maximum rises late, most terms vanish); a prefix page that two sequences share."""
     cache = filled_cache(70, 1, 128, 64, 31)
