@@ -4,8 +4,8 @@
 // start the page):  a = max|x|,  c = a/127 (0 below the smallest normal number),  s' = max(s, c),
 //   new codes  round(x 127 / a) where c >= s, else round(x / s);   held codes  round(code s / s') where s' > s.
 // Each is the rounding of the exact quotient, ties to even, so a code does not depend on how the division was done: the
-// kernel multiplies by a binary32 reciprocal, rounds by adding 1.5 2^23, and looks closer only where the product lies within
-// 2^-16 of a border: the reciprocal's error, 2^-24 of at most 127, is below 2^-17, and the distance itself comes from one fma.
+// kernel multiplies by binary32 reciprocals, rounds by adding 1.5 2^23, and looks closer only where one just above and one just
+// below the quotient give two codes.
 //
 // Bound by memory: D (e + 1) bytes per token, head and operand.  One CTA per (page, operand, head) copies its tokens into shared
 // memory (cp.async, all under way at once), where the maximum and then the codes read them: of keys eight channels a thread, of
@@ -15,6 +15,7 @@
 // (instructions: 75 % of the issue slots; the borders cost a third of them).
 #include <type_traits>
 
+#include "act_common.cuh"
 #include "fq_common.cuh"
 #include "layer_common.cuh"
 #include "ptx_sm100.cuh"
@@ -87,28 +88,38 @@ struct Largest<__nv_bfloat16> {
 __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {       // their low bytes
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
-// N codes, in the low bytes of t.  (1.5 2^23 + r ends in the two's complement of c = round(r).)  Half the page's largest value is
-// a border, 63.5, so that values next to one are nothing rare, and none is settled by a division.  SHORT, bf16 values over their
-// own maximum: r = 127 X / A 2^k with X and A of 8 bits, so r in [2^j, 2^(j+1)) that is no border lies 2^(j-17) from one, 64
-// times the error: whatever is nearer is one, and goes to the even side.  Else by 2 |x num - c den| against den, which binary64
-// holds exactly (c and num take 7 bits, x and den 24).
+// N codes, in the low bytes of t.  (1.5 2^23 + r ends in the two's complement of c = round(r).)  The exact quotient lies between
+// the products with a factor two steps above the rounded one and with one two steps below it: where both give the same code, it
+// is the code.  Half the page's largest value is a border, 63.5, so that borders are nothing rare, and none is settled by a
+// division.  SHORT, bf16 values over their own maximum: r = 127 X / A 2^k with X and A of 8 bits, so r in [2^j, 2^(j+1)) that is no
+// border lies 2^(j-17) from one, ten times as far as the products: two codes mean a border, and the even one is it.  Else by
+// 2 |x num - c den| against den, which binary64 holds exactly (c and num take 7 bits, x and den 24).
+struct Factors {
+    float above, below;
+};
+__device__ __forceinline__ Factors around(float f) {    // (0: nothing is larger than what binary32 holds of a page's scale)
+    const uint32_t w = __float_as_uint(f);
+    return w < 2 ? Factors{f, f} : Factors{__uint_as_float(w + 2), __uint_as_float(w - 2)};
+}
 template <int N, bool SHORT>
-__device__ __forceinline__ void codes(const float* f, float inv, float num, float den, uint32_t* t) {
-    constexpr float kMagic = 12582912.0f, kNear = 0.5f - 0x1p-16f;
-    float far = 0.0f;
+__device__ __forceinline__ void codes(const float* f, Factors by, float num, float den, uint32_t* t) {
+    constexpr float kMagic = 12582912.0f;
+    const float2 above = make_float2(by.above, by.above), below = make_float2(by.below, by.below), magic = make_float2(kMagic, kMagic);
+    uint32_t differ = 0, other[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float s = fmaf(f[i], inv, kMagic);
-        far = fmaxf(far, fabsf(fmaf(f[i], inv, kMagic - s)));
-        t[i] = __float_as_uint(s);
+    for (int i = 0; i < N; i += 2) {
+        const float2 x = make_float2(f[i], f[i + 1]), hi = f2_fma(x, above, magic), lo = f2_fma(x, below, magic);
+        t[i] = __float_as_uint(hi.x); t[i + 1] = __float_as_uint(hi.y);
+        other[i] = __float_as_uint(lo.x); other[i + 1] = __float_as_uint(lo.y);
+        differ |= (t[i] ^ other[i]) | (t[i + 1] ^ other[i + 1]);
     }
-    if (far > kNear) {
+    if (differ) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float c = __uint_as_float(t[i]) - kMagic, off = fmaf(f[i], inv, -c);
             if (SHORT) {
-                if (fabsf(off) > 0.5f - fmaxf(fabsf(c), 0.5f) * 0x1p-20f && (t[i] & 1)) t[i] += off > 0.0f ? 1u : ~0u;
-            } else if (fabsf(off) > kNear) {
+                if (t[i] & 1) t[i] = other[i];          // (the same, or the even one)
+            } else if (t[i] != other[i]) {
+                const float c = __uint_as_float(t[i]) - kMagic;
                 const double exact = fma((double)f[i], (double)num, -(double)c * (double)den), twice = 2.0 * fabs(exact);
                 if (twice > (double)den || (twice == (double)den && (t[i] & 1))) t[i] += exact > 0.0 ? 1u : ~0u;
             }
@@ -116,7 +127,7 @@ __device__ __forceinline__ void codes(const float* f, float inv, float num, floa
     }
 }
 // Four held codes, of a scale `was`, in the scale `now`.
-__device__ __forceinline__ uint32_t requantize4(uint32_t w, float ratio, float was, float now) {
+__device__ __forceinline__ uint32_t requantize4(uint32_t w, Factors ratio, float was, float now) {
     float f[4];
     uint32_t t[4];
 #pragma unroll
@@ -186,8 +197,7 @@ __global__ void __launch_bounds__(kMaxThreads, 4) kv8_append_kernel(const Append
         const float now = fmaxf(was, cand);
         const bool sets = cand >= was, grown = first > 0 && now > was;
         const float num = sets ? 127.0f : 1.0f, den = sets ? most : was;
-        const float inv = now > 0.0f ? __fdiv_rn(num, den) : 0.0f;
-        const float ratio = grown ? __fdiv_rn(was, now) : 1.0f;
+        const Factors inv = around(now > 0.0f ? __fdiv_rn(num, den) : 0.0f), ratio = around(grown ? __fdiv_rn(was, now) : 1.0f);
         int8_t* page = a.codes[which] + (id * a.heads + head) * (int64_t)P * D;
         // ---- the codes
         uint32_t* w = reinterpret_cast<uint32_t*>(page);
