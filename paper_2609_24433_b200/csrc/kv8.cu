@@ -11,8 +11,8 @@
 // memory (cp.async, all under way at once), where the maximum and then the codes read them: of keys eight channels a thread, of
 // values, whose pages keep tokens innermost, four tokens by four channels.  The loops stay rolled: with the tokens in registers,
 // eight units a thread, their code was long enough to wait for itself.  52224 tokens, one head of 256, bf16 (12.4 us at the
-// measured copy rate): 60 us with two passes of loads and bytes turned one by one, 39 with the tokens in registers, 30 now
-// (instructions: 75 % of the issue slots; the borders cost a third of them).
+// measured copy rate): 60 us with two passes of loads and bytes turned one by one, 39 with the tokens in registers, 30 with borders looked for by their distance, 27 now
+// (instructions: two thirds of the issue slots).
 #include <type_traits>
 
 #include "act_common.cuh"
@@ -137,7 +137,7 @@ __device__ __forceinline__ uint32_t requantize4(uint32_t w, Factors ratio, float
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kMaxThreads, 4) kv8_append_kernel(const AppendArgs a) {
+__global__ void __launch_bounds__(kMaxThreads, 5) kv8_append_kernel(const AppendArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];     // the page's new tokens, rows of head_dim T and 16 bytes
     __shared__ float warp_max[kMaxThreads / 32];
     const int kThreads = blockDim.x;
@@ -224,12 +224,14 @@ __global__ void __launch_bounds__(kMaxThreads, 4) kv8_append_kernel(const Append
             if (grown)
                 for (int e = threadIdx.x; e < first * D / 4; e += kThreads) w[e] = requantize4(w[e], ratio, was, now);
         } else {
-            // Words of four tokens, from the first that changes; eight of them (a sector) to four blocks of four channels a warp.
-            const int w0 = grown ? 0 : first / 4, groups = ((last + 3) / 4 - w0 + 7) / 8, words = P / 4, blocks = D / 16;
-            const int lane = threadIdx.x % 32, k8 = lane % 8, c16 = lane / 8;
+            // Words of four tokens, from the first that changes; a warp takes eight of them (a sector; pages of 16 tokens: all four)
+            // of four (eight) blocks of four channels.
+            const int w0 = grown ? 0 : first / 4, words = P / 4, in_run = words < 8 ? 4 : 8, runs = 32 / in_run;
+            const int groups = ((last + 3) / 4 - w0 + in_run - 1) / in_run, blocks = (D / 4 + runs - 1) / runs;
+            const int lane = threadIdx.x % 32, kr = lane & (in_run - 1), cr = in_run == 4 ? lane / 4 : lane / 8;
             for (int e = threadIdx.x / 32; e < groups * blocks; e += kThreads / 32) {
-                const int block = e / groups, k = w0 + (e - block * groups) * 8 + k8, t = 4 * k, c = block * 16 + c16 * 4;
-                if (t >= last) continue;
+                const int block = e / groups, k = w0 + (e - block * groups) * in_run + kr, t = 4 * k, c = (block * runs + cr) * 4;
+                if (t >= last || c >= D) continue;
                 uint32_t out[4][4];                     // [token][channel]
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
