@@ -307,8 +307,9 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 float down = 1.0f;
                 if (CACHED) {
                     float top = 0.0f;
-                    for (int d = 0; d < D; d += 8) {
-                        const uint4 v = ld_global_v4(src + d, there);
+#pragma unroll 8
+                    for (int d = 0; d < DP; d += 8) {            // (eight loads under way: one by one: 50 queries of 16 heads of 64 over 816 keys 13.6 us for 11.3)
+                        const uint4 v = ld_global_v4(src + d, there && d < D);
                         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                         for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     down = power_of_two(-e);
                     factor = a.scale_log2 * power_of_two(e);
                 }
-#pragma unroll 2
+#pragma unroll 8
                 for (int x = 0; x < DP / kSplit; x += 8) {
                     const int d = split * (DP / kSplit) + x;
                     uint4 v = ld_global_v4(src + d, there && d < D);

@@ -51,15 +51,24 @@ __global__ void __launch_bounds__(kThreads) attention_widen_kernel(const Attenti
         }
         __syncthreads();
         const int units = kKeys * D / 16, per_key = D / 16;
-        for (int e = threadIdx.x; e < units; e += kThreads) {           // keys: 16 channels
-            const int key = e / per_key, c = (e - key * per_key) * 16, page = at[key / 16];
-            const uint4 v = ld_global_v4(a.cache.k + (page >= 0 ? ((int64_t)page * P + (key & (P - 1))) * D + c : 0), page >= 0);
-            store16(keys + (j0 + key) * D + c, v);
-        }
-        for (int e = threadIdx.x; e < units; e += kThreads) {           // values: 16 keys of a channel
-            const int d = e / (kKeys / 16), x = e % (kKeys / 16), page = at[x];
-            const uint4 v = ld_global_v4(a.cache.v + (page >= 0 ? ((int64_t)page * D + d) * P + ((16 * x) & (P - 1)) : 0), page >= 0);
-            store16(values + d * L + j0 + 16 * x, v);
+        for (int e0 = threadIdx.x; e0 < units; e0 += 4 * kThreads) {    // four loads under way
+            uint4 v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = e0 + i * kThreads;
+                if (blockIdx.z == 0) {                                  // keys: 16 channels
+                    const int key = e / per_key, c = (e - key * per_key) * 16, page = e < units ? at[key / 16] : -1;
+                    v[i] = ld_global_v4(a.cache.k + (page >= 0 ? ((int64_t)page * P + (key & (P - 1))) * D + c : 0), page >= 0);
+                } else {                                                // values: 16 keys of a channel
+                    const int d = e / (kKeys / 16), x = e % (kKeys / 16), page = e < units ? at[x] : -1;
+                    v[i] = ld_global_v4(a.cache.v + (page >= 0 ? ((int64_t)page * D + d) * P + ((16 * x) & (P - 1)) : 0), page >= 0);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = e0 + i * kThreads;
+                if (e < units) store16(blockIdx.z == 0 ? keys + j0 * D + e * 16 : values + (int64_t)(e / (kKeys / 16)) * L + j0 + 16 * (e % (kKeys / 16)), v[i]);
+            }
         }
     }
 }
@@ -70,7 +79,7 @@ cudaError_t launch_attention_widen(const Attention& a, cudaStream_t stream) {
     int64_t tiles = a.wide_keys / kKeys;
     if (tiles < 1) return cudaSuccess;
     if (tiles > 65535) tiles = 65535;
-    return launch_pdl3(attention_widen_kernel, dim3((unsigned)tiles, (unsigned)a.units), kThreads, 0, stream, a);
+    return launch_pdl3(attention_widen_kernel, dim3((unsigned)tiles, (unsigned)a.units, 2), kThreads, 0, stream, a);
 }
 
 }  // namespace fq
