@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 if (CACHED) {
                     float top = 0.0f;
 #pragma unroll 8
-                    for (int d = 0; d < DP; d += 8) {            // (eight loads under way: one by one: 50 queries of 16 heads of 64 over 816 keys 13.6 us for 11.3)
+                    for (int d = 0; d < DP; d += 8) {            // (eight loads under way; one by one, 50 queries of 16 heads of 64 over 816 keys took 13.6 us for 11.3)
                         const uint4 v = ld_global_v4(src + d, there && d < D);
                         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
