@@ -390,9 +390,9 @@ fq_status fq_kv8_append(const void* k, const void* v, fq_dtype xt, int64_t token
  * causal: query i of n sees keys j <= kv_len - n + i, else all.  A query without a key gives zeros.
  * o = sum_j p_j v_j / sum_j p_j, p_j = exp(scale (q . k_j) - max).  bf16 queries are multiplied as binary16 after
  * a power of two per row has been taken out (exact but for channels 2^-14 below the row's largest), probabilities as binary16
- * (11 bits), sums in binary32.  max_q: no sequence has more queries (0: unknown); a hint.
- * workspace device, fq_attention_kv8_workspace_bytes(..) bytes (ragged: q_offsets is given), 256-byte aligned, scratch;
- * NULL where that is 0. */
+ * (11 bits), their exponentials to 2^-18, sums in binary32.  max_q: no sequence has more queries (0: unknown); a hint.
+ * workspace device, fq_attention_kv8_workspace_bytes(..) bytes (ragged: q_offsets is given), 256-byte aligned, scratch (many
+ * queries: up to 256 MiB of it hold codes as binary16, more only where one sequence's head does not fit); NULL where that is 0. */
 fq_status fq_attention_kv8(const void* q, fq_dtype dt, int64_t q_rows, int64_t ldq, int q_heads, const fq_kv8_cache* cache,
                            const int32_t* table, int64_t ld_table, int64_t table_width, int batch, const int32_t* kv_len,
                            const int32_t* q_offsets, int64_t max_q, int64_t max_kv, int causal, float scale, void* y, int64_t ldy,
@@ -406,7 +406,7 @@ size_t fq_attention_kv8_workspace_bytes(fq_dtype dt, int64_t q_rows, int q_heads
  * the first kv_len[b] are keys (NULL: all), and of those the ones whose key_mask byte is not 0 (device uint8[kv_rows], NULL:
  * all).  What masked rows hold does not matter, infinities and NaN included.  A query without a key gives zeros.
  * No causal order.  D a multiple of 16, at most 256.  max_q, max_kv: as above (0: unknown; sequences are cut to max_kv keys).
- * bf16: the probabilities are rounded to bf16 ahead of the product with v; sums in binary32. */
+ * bf16: the probabilities, exponentials to 2^-18, are rounded to bf16 ahead of the product with v; sums in binary32. */
 fq_status fq_cross_attention(const void* q, fq_dtype dt, int64_t q_rows, int64_t ldq, int q_heads, const void* k, const void* v,
                              int64_t kv_rows, int64_t ldk, int64_t ldv, int kv_heads, int head_dim, int batch, const int32_t* q_offsets,
                              const int32_t* kv_offsets, const int32_t* kv_len, const uint8_t* key_mask, int64_t max_q, int64_t max_kv,
