@@ -357,8 +357,8 @@ fq_status fq_qk_norm_rope(const void* qkv, fq_dtype xt, int64_t M, int64_t ldx, 
  * order in which the product with the probabilities takes them); k_scale, v_scale float [pages][heads].  A code stands for
  * code * scale.  page in {16, 32, 64, 128}; D a multiple of 16, at most 256.  A page needs no initialisation.
  * `table` device int32 [batch][table_width], leading dimension ld_table: the pages of each sequence in order.  An entry
- * outside [0, pages) is no page: nothing is written there, and its keys are as masked ones.  No page may belong to two
- * sequences that one call appends to (pages of a shared prefix that nobody appends to may).
+ * outside [0, pages) is no page: nothing is written there, and its keys are as masked ones.  No page may be listed twice among
+ * those that one call appends to (pages of a shared prefix that nobody appends to may).
  *
  * fq_kv8_append: rows offsets[b] .. offsets[b+1] of k and v ([tokens, heads D] of dtype xt) become tokens kv_len[b],
  * kv_len[b] + 1, .. of sequence b.  offsets device int32[batch + 1], or NULL: tokens / batch each.  kv_len device int32[batch]:

@@ -261,7 +261,7 @@ fq_status fq_attention_kv8(const void* q, fq_dtype dt, int64_t q_rows, int64_t l
     Attention a = {};
     st = fill_kv8(a, dt, q_rows, q_heads, cache, table_width, batch, q_offsets, max_q, max_kv);
     if (st != FQ_OK) return st;
-    if (!(scale >= 0.0f) || isinf(scale)) return FQ_ERR_INVALID_ARG;
+    if (!(scale >= 0.0f) || isinf(scale * 1.44269504088896341f)) return FQ_ERR_INVALID_ARG;
     if (q_rows == 0 || batch == 0) return FQ_OK;
     if (!kv_len) return FQ_ERR_INVALID_ARG;
     st = check_rows(q, ldq, y, ldy, (int64_t)q_heads * a.head_dim);
@@ -288,7 +288,7 @@ fq_status fq_cross_attention(const void* q, fq_dtype dt, int64_t q_rows, int64_t
     Attention a = {};
     fq_status st = fill_cross(a, dt, q_rows, q_heads, kv_rows, kv_heads, head_dim, batch, q_offsets, kv_offsets, max_q, max_kv);
     if (st != FQ_OK) return st;
-    if (!(scale >= 0.0f) || isinf(scale)) return FQ_ERR_INVALID_ARG;
+    if (!(scale >= 0.0f) || isinf(scale * 1.44269504088896341f)) return FQ_ERR_INVALID_ARG;
     if (q_rows == 0 || batch == 0) return FQ_OK;
     st = check_rows(q, ldq, y, ldy, (int64_t)q_heads * head_dim);
     if (st != FQ_OK) return st;

@@ -10,7 +10,10 @@ Bounds (u = 2^-24, the half step of binary32; h = half a step of the output's ty
              terms loses at most 2^-25 (binary16, whose numbers below 2^-14 are multiples of 2^-24) or 2^-126 of V = max_j |v_j|
 """
 import math
+import os
 import random
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -18,6 +21,7 @@ import torch
 
 from paper_2609_24433_b200 import fq
 
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 U = 2.0 ** -24
 HALF = {torch.float32: U, torch.bfloat16: 2.0 ** -8}
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
@@ -415,6 +419,30 @@ def test_attention_kv8_shares_of_one_long_or_many_short_sequences(Hq, D, lens):
 
 
 @gpu
+@pytest.mark.parametrize("Hq,Hk,D,P,queries", [(2, 1, 16, 16, [300, 70]), (4, 2, 48, 32, [200, 5]), (2, 2, 64, 64, [300, 129]), (4, 1, 128, 64, [300, 40]),
+                                               (8, 1, 256, 128, [50, 50])])
+def test_attention_kv8_many_queries_of_every_width(Hq, Hk, D, P, queries):
+    lens = [2100, 300]
+    width = -(-2100 // P)
+    cache = filled_cache(2 * width, Hk, D, P, 69)
+    table = table_of(2 * width, 2, width, 70)
+    table[0, 400 // P] = -1                             # a page that is none
+    check_cache_attention(cache, table, lens, queries, Hq, "bf16", True, seed=71, max_q=max(queries))
+    check_cache_attention(cache, table, lens, queries, Hq, "bf16", False, seed=72)
+
+
+@gpu
+def test_attention_kv8_widens_in_several_passes():
+    """More (sequence, head) pairs than the widened codes of one pass hold."""
+    cache = filled_cache(60, 4, 256, 128, 73)
+    gen = torch.Generator().manual_seed(74)
+    table = torch.randint(0, 60, (3, 260), generator=gen).int().cuda()
+    lens, queries = [33000, 40, 300], [20, 17, 33]
+    assert 12 * 33280 * 256 * 4 > 256 << 20
+    check_cache_attention(cache, table, lens, queries, 4, "bf16", True, seed=75, max_q=33)
+
+
+@gpu
 def test_attention_kv8_peaked_scores_and_repeated_pages():
     """Scores far apart (the running maximum rises late, most terms vanish); a prefix page that two sequences share."""
     cache = filled_cache(70, 1, 128, 64, 31)
@@ -521,6 +549,16 @@ def test_cross_attention_against_64_bits(Hq, Hk, D, queries, keys, dtype):
     mask = torch.rand(sum(keys), device="cuda", generator=g) > 0.4
     lens = [max(0, n - 7 * b - 3) for b, n in enumerate(keys)]
     check_cross(Hq, Hk, D, queries, keys, dtype, lens=lens, mask=mask, padded=True, seed=63)
+
+
+@gpu
+@pytest.mark.parametrize("D,queries", [(16, 300), (48, 300), (64, 300), (64, 40), (128, 300), (128, 40), (256, 300)])
+def test_cross_attention_masks_over_many_tiles(D, queries):
+    """Tiles of keys that are whole, that miss a few keys, that are all masked, in no regular order; more of them than stages."""
+    mask = torch.ones(3 * 2100, dtype=torch.bool, device="cuda")
+    mask[130:390], mask[700:701], mask[1023:1025], mask[1400:2099], mask[2100:2300], mask[3000:3512] = False, False, False, False, False, False
+    mask[4200:6300:7] = False
+    check_cross(4, 2, D, [queries] * 3, [2100] * 3, "bf16", mask=mask, padded=True, seed=74)
 
 
 @gpu
@@ -653,3 +691,33 @@ def test_attention_returns_the_same_bits_every_time():
     first = fq.cross_attention(q, k, v, 16, 16, 2)
     for _ in range(50):
         assert torch.equal(fq.cross_attention(q, k, v, 16, 16, 2), first)
+
+
+@gpu
+def test_first_calls_inside_a_capture():
+    """A process whose first call of each operator is captured: nothing is set up behind the capture's back."""
+    code = """
+import torch
+from paper_2609_24433_b200 import fq
+bf = torch.bfloat16
+for T in (1, 40):
+    x = torch.randn(2 * T, 6 * 64, device="cuda").to(bf)
+    cache = fq.KV8Cache.empty(40, 1, 64, 16)
+    table = torch.arange(40, device="cuda", dtype=torch.int32).view(2, 20)
+    held = torch.zeros(2, dtype=torch.int32, device="cuda")
+    lens, pos, f = held + T, torch.arange(2 * T, device="cuda", dtype=torch.int32), fq.rope_frequencies(64)
+    def run():
+        q, k = fq.qk_norm_rope(x, 4, 1, 64, pos, f)
+        fq.kv8_append(k, x[:, 320:], cache, table, held)
+        return fq.attention_kv8(q, 4, cache, table, lens), fq.cross_attention(q, k, k, 4, 1, 2), fq.cross_attention(q.float(), k.float(), k.float(), 4, 1, 2)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = run()
+    g.replay()
+    for a, b in zip(out, run()):
+        assert torch.equal(a, b)
+assert fq.device_status()[0] == fq.OK
+print("fine")
+"""
+    got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=ROOT)
+    assert got.returncode == 0 and "fine" in got.stdout, got.stderr[-2000:]

@@ -81,7 +81,7 @@ def attend(lib, c, rows=4, hq=4, q=ONE, ldq=256, table=ONE, ld=8, width=8, batch
 def test_attention_kv8_refusals(lib):
     assert attend(lib, cache(), rows=0) == fq.OK and attend(lib, cache(), rows=0, batch=0) == fq.OK
     for bad in (dict(rows=-1), dict(rows=5), dict(hq=0), dict(hq=3), dict(q=NULL), dict(ldq=248), dict(table=NULL), dict(ld=7), dict(lens=NULL),
-                dict(max_q=-1), dict(max_kv=-1), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(y=NULL), dict(dt=2)):
+                dict(max_q=-1), dict(max_kv=-1), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=3e38), dict(y=NULL), dict(dt=2)):
         assert attend(lib, cache(), **bad) == fq.ERR_INVALID_ARG, bad
     assert attend(lib, None) == fq.ERR_INVALID_ARG
     for c in (cache(head_dim=24), cache(head_dim=512), cache(page=100)):
