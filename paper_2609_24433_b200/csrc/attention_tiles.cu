@@ -185,12 +185,14 @@ template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-// mbar_wait_all with the bounded loop in line: a kernel that calls a function keeps its launch's registers in every warp.
-__device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* watchdog, uint32_t code) {
+// mbar_wait_all for two barriers, which are looked at together, with the bounded loop in line: a kernel that calls a function keeps
+// its launch's registers in every warp.
+__device__ __forceinline__ bool wait_all(uint32_t first, uint32_t first_parity, uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* watchdog, uint32_t code) {
     bool ok = true;
-    if (!mbar_try_wait(bar, parity)) {
+    const bool one = mbar_try_wait(first, first_parity), other = bar == first || mbar_try_wait(bar, parity);
+    if (!(one && other)) {
         uint64_t t0 = 0;
-        for (uint32_t spin = 1; !mbar_try_wait(bar, parity); ++spin) {
+        for (uint32_t spin = 1; !(mbar_try_wait(first, first_parity) && (bar == first || mbar_try_wait(bar, parity))); ++spin) {
             if ((spin & 0xfff) == 0) {
                 if (*abort_flag) { ok = false; break; }
                 const uint64_t now = global_timer_ns();
@@ -205,6 +207,9 @@ __device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile
         }
     }
     return __all_sync(0xffffffffu, ok);
+}
+__device__ __forceinline__ bool wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* watchdog, uint32_t code) {
+    return wait_all(bar, parity, bar, parity, abort_flag, watchdog, code);
 }
 __device__ __forceinline__ void mbar_inval(uint32_t bar) { asm volatile("mbarrier.inval.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
 
@@ -344,8 +349,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
             for (int j = 0; j < n; ++j) {
                 const int buf = NT == 2 ? mine : j & 1;
                 const uint32_t phase = NT == 2 ? j & 1 : (j >> 1) & 1;
-                ok = ok && wait_all(smem_u32(&ctl.s[buf]), phase, abort_flag, watchdog, kWdSoftmax) &&
-                     wait_all(smem_u32(&ctl.meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdSoftmax);
+                ok = ok && wait_all(smem_u32(&ctl.meta[j % kMetas]), (j / kMetas) & 1, smem_u32(&ctl.s[buf]), phase, abort_flag, watchdog, kWdSoftmax);
                 if (!ok) {
                     meet();
                     meet();
@@ -716,19 +720,21 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     if (!ok) break;
                     release(kuse);
                 }
+                // What the products need beside the probabilities is waited for ahead of them.
+                if (all_there(vuse) && !CACHED) {
+                    ok = wait_all(smem_u32(&ctl.meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdMma);
+                    const bool clean = all_valid(ctl.metas[j % kMetas]);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&ctl.used[j % kMetas]));
+                    if (!clean && ok) {
+                        if (lane == 0) mbar_arrive(smem_u32(&ctl.landed));
+                        ok = wait_all(smem_u32(&ctl.fixed), mends & 1, abort_flag, watchdog, kWdMma);
+                        ++mends;
+                    }
+                }
+                if (ok && !S::kAhead && j + 1 < n) all_there(kuse);
                 for (int i = lo; i < hi && ok; ++i) {
                     ok = wait_all(smem_u32(&ctl.p[NT == 2 ? i : j & 1]), NT == 2 ? j & 1 : (j >> 1) & 1, abort_flag, watchdog, kWdMma);
-                    if (i == lo && all_there(vuse) && !CACHED) {
-                        ok = wait_all(smem_u32(&ctl.meta[j % kMetas]), (j / kMetas) & 1, abort_flag, watchdog, kWdMma);
-                        const bool clean = all_valid(ctl.metas[j % kMetas]);
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(smem_u32(&ctl.used[j % kMetas]));
-                        if (!clean && ok) {
-                            if (lane == 0) mbar_arrive(smem_u32(&ctl.landed));
-                            ok = wait_all(smem_u32(&ctl.fixed), mends & 1, abort_flag, watchdog, kWdMma);
-                            ++mends;
-                        }
-                    }
                     if (!ok) break;
                     tc_fence_after();
                     products(j, i);
@@ -736,11 +742,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                         if (elect_one()) mma_commit(smem_u32(&ctl.o[i]));
                         __syncwarp();
                     }
-                    if (!S::kAhead && j + 1 < n) {
-                        if (i == 0 && !all_there(kuse)) break;
-                        tc_fence_after();
-                        scores(j + 1, i);
-                    }
+                    if (!S::kAhead && j + 1 < n) scores(j + 1, i);
                 }
                 if (!ok) break;
                 release(vuse);
