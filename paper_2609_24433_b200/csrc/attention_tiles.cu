@@ -403,11 +403,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&ctl.free[mine]));
-                    if (j > 0) {                                 // the last product has read its probabilities
-                        ok = wait_all(smem_u32(&ctl.o[mine]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
-                        if (!ok) continue;
-                        tc_fence_after();
-                    }
                 }
                 // ---- a new base
                 const int now_e = CACHED ? meta.e : e;
@@ -418,8 +413,8 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     base = now;
                     l *= keep;
                     if (j > 0) {
-                        if (NT == 1) {
-                            ok = wait_all(smem_u32(&ctl.o[0]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
+                        if (S::kAhead) {
+                            ok = wait_all(smem_u32(&ctl.o[mine]), (j - 1) & 1, abort_flag, watchdog, kWdSoftmax);
                             if (!ok) continue;
                             tc_fence_after();
                         }
@@ -437,9 +432,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     e = now_e;
                 }
                 const float minus = base == -INFINITY ? 0.0f : -base;
-                if (S::kEarly && j + mine > 0) {                 // its turn at the exponentials
-                    ok = wait_all(smem_u32(&ctl.turn[warp]), (j - 1 + mine) & 1, abort_flag, watchdog, kWdSoftmax);
+                if (S::kEarly && j + mine > 0) {                 // its turn at the exponentials; the last product has read its probabilities
+                    const uint32_t turn = smem_u32(&ctl.turn[warp]), turn_phase = (j - 1 + mine) & 1;
+                    ok = wait_all(j > 0 ? smem_u32(&ctl.o[mine]) : turn, j > 0 ? (j - 1) & 1 : turn_phase, turn, turn_phase, abort_flag, watchdog, kWdSoftmax);
                     if (!ok) continue;
+                    tc_fence_after();
                 }
                 // ---- probabilities, over the scores or beside them
                 float2 sum0 = make_float2(0.0f, 0.0f), sum1 = sum0;
