@@ -37,7 +37,7 @@ __device__ __forceinline__ Sequence sequence_of(const Attention& a, int b) {
         sequence_rows(a.kv_offsets, b, a.batch, a.kv_rows, &s.k0, &n);
         s.keys = min(s.keys, n);
     }
-    if (a.kv_len) s.keys = min(s.keys, max((int64_t)a.kv_len[b], (int64_t)0));
+    if (a.kv_len) s.keys = min(s.keys, max((int64_t)ld_global_s32(a.kv_len + b), (int64_t)0));
     return s;
 }
 // The last key that a row -- (token, head of the group) -- sees, -1 for none.
@@ -71,7 +71,7 @@ __device__ __forceinline__ KeyPlace key_place(const Attention& a, const Sequence
     p.offset = 0;
     if (!p.valid) return p;
     if (CACHED) {
-        const int64_t id = a.table[b * a.ld_table + j / a.cache.page];
+        const int64_t id = ld_global_s32(a.table + b * a.ld_table + j / a.cache.page);
         p.valid = id >= 0 && id < a.cache.pages;
         p.row = id * a.kv_heads + hk;
         p.offset = (int)(j % a.cache.page);

@@ -12,9 +12,11 @@
 // four.  Queries are divided by the power of two below their row's largest channel and rounded to binary16 (bf16 values
 // keep all their bits above 2^-14 of the row's largest channel; binary32 queries and probabilities go as a sum of two terms).
 //
-// Every CTA takes an equal share of the call's blocks -- 256 keys of 8 or 16 rows of a kv head -- wherever that begins and ends: lengths
-// are known on the device only, and a ragged batch (48 sequences of up to 16384 keys) in chunks of 4096 ended 16 us behind its
-// bytes.  A tile of rows that several shares divide is joined by a second kernel; the others are written here.
+// Every CTA takes an equal share of the call's blocks -- 256 keys of 8 or 16 rows of a kv head -- wherever that begins and ends:
+// lengths are known on the device only.  A tile of rows that several shares divide is joined by a second kernel; the others are
+// written here.  (48 sequences of 1 to 16384 keys, 8 heads of 128, 127 us at the measured copy rate: chunks of 4096 keys 148 us,
+// shares 142; 64 of 8192 keys, 2 heads of 256, 83 at the copy rate: 112 and 95; one of 16384: 17.4 and 15.8.  Shares end up to 12 %
+// apart, by what their SMs get of the memory; smaller last ones, handed out as CTAs end, cost more than they level: 147.)
 //
 // With p = 2^(s - m): l = sum p, O = sum (p vs 2^(7 - e)) code, e the running exponent of the largest value scale vs.  m follows the
 // maximum lazily, when it has risen by more than 2^8: probabilities stay below 2^15 and, down to 2^-21, normal in binary16.
@@ -98,14 +100,17 @@ struct Share {
     int64_t first, last, total, shares; // as many shares as CTAs, or as blocks
     int64_t within;                     // blocks of the sequence ahead of the first one
     int b;
+    Sequence sequence;                  // (looked up once: a round trip to memory)
 };
 __device__ __forceinline__ Share share_of(const Attention& a, int rows) {
     __shared__ int64_t sums[kWarps];
-    __shared__ int64_t found[2];
+    __shared__ int64_t found[5];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, each = (a.batch + kWarps * 32 - 1) / (kWarps * 32);
     const int b0 = min((int)threadIdx.x * each, a.batch), b1 = min(b0 + each, a.batch);
+    Sequence s = {};
     auto blocks = [&](int b) {
-        const Work w = work_of(a, sequence_of(a, b), rows);
+        s = sequence_of(a, b);
+        const Work w = work_of(a, s, rows);
         return w.units * w.per_unit;
     };
     int64_t own = 0;
@@ -131,13 +136,21 @@ __device__ __forceinline__ Share share_of(const Attention& a, int rows) {
     if (upto - own <= r.first && r.first < upto) {
         int64_t ahead = r.first - (upto - own);
         int b = b0;
-        for (int64_t n; b < b1 - 1 && ahead >= (n = blocks(b)); ++b) ahead -= n;
+        if (each > 1)                   // (else s is the one)
+            for (int64_t n; ahead >= (n = blocks(b)); ++b) ahead -= n;
         found[0] = b;
         found[1] = ahead;
+        found[2] = s.q0;
+        found[3] = s.queries;
+        found[4] = s.keys;
     }
     __syncthreads();
     r.b = (int)found[0];                // (only read where first < last)
     r.within = found[1];
+    r.sequence.k0 = 0;
+    r.sequence.q0 = found[2];
+    r.sequence.queries = found[3];
+    r.sequence.keys = found[4];
     return r;
 }
 
@@ -158,7 +171,7 @@ __global__ void __launch_bounds__(kWarps * 32, tokens_resident(sizeof(T) == 2, D
     int b = share.b;
     int64_t within = share.within;
     for (int64_t at = share.first; at < share.last;) {
-        const Sequence s = sequence_of(a, b);
+        const Sequence s = b == share.b ? share.sequence : sequence_of(a, b);
         const Work work = work_of(a, s, kRows);
         if (within >= work.units * work.per_unit) {              // on to the next sequence
             ++b;
@@ -483,7 +496,8 @@ __global__ void __launch_bounds__(kWarps * 32, tokens_resident(sizeof(T) == 2, D
 template <typename T>
 __global__ void __launch_bounds__(128) attention_tokens_join_kernel(const Attention a) {
     griddep_wait();
-    const int4 split = a.splits[blockIdx.x];
+    const uint4 split_words = ld_global_v4(a.splits + blockIdx.x);
+    const int4 split = make_int4((int)split_words.x, (int)split_words.y, (int)split_words.z, (int)split_words.w);
     const int first = blockIdx.x, b = split.y, hk = split.z;
     if (split.x <= first) return;
     const Sequence s = sequence_of(a, b);

@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kMaxThreads, 5) kv8_append_kernel(const Append
     const int b = blockIdx.z, which = blockIdx.y & 1, head = blockIdx.y >> 1;
     int64_t row0, n;
     sequence_rows(a.offsets, b, a.batch, a.tokens, &row0, &n);
-    const int64_t held = max((int64_t)a.kv_len[b], (int64_t)0);
+    const int64_t held = max((int64_t)ld_global_s32(a.kv_len + b), (int64_t)0);
     const int D = a.head_dim, P = a.page, shift = 31 - __clz(P);
     const int64_t end = min(held + n, (int64_t)a.table_width * P), ld = a.ld[which];
     constexpr int kUnit = 16 / sizeof(T);               // channels of a copy

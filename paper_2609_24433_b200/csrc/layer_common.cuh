@@ -101,6 +101,11 @@ fq_status launch_attention(Attention& a, void* workspace, size_t ws_bytes, cudaS
 size_t attention_workspace_bytes(const Attention& a);
 
 #ifdef __CUDACC__
+__device__ __forceinline__ int32_t ld_global_s32(const int32_t* p) {
+    int32_t v;
+    asm volatile("ld.global.b32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -119,7 +124,7 @@ __device__ __forceinline__ void sequence_rows(const int32_t* offsets, int b, int
         *count = n;
         return;
     }
-    const int64_t lo = min(max((int64_t)offsets[b], (int64_t)0), rows), hi = min(max((int64_t)offsets[b + 1], lo), rows);
+    const int64_t lo = min(max((int64_t)ld_global_s32(offsets + b), (int64_t)0), rows), hi = min(max((int64_t)ld_global_s32(offsets + b + 1), lo), rows);
     *first = lo;
     *count = hi - lo;
 }
