@@ -60,7 +60,6 @@ __device__ __forceinline__ TileKeys tile_keys(const Attention& a, const Sequence
 struct KeyPlace {
     bool valid;
     int64_t row;                        // of the keys, or page * kv_heads + head
-    int offset;                         // in the page
 };
 // Key j of sequence b (j < end where it may be read at all).
 template <bool CACHED>
@@ -68,13 +67,11 @@ __device__ __forceinline__ KeyPlace key_place(const Attention& a, const Sequence
     KeyPlace p;
     p.valid = j < end;
     p.row = 0;
-    p.offset = 0;
     if (!p.valid) return p;
     if (CACHED) {
         const int64_t id = ld_global_s32(a.table + b * a.ld_table + j / a.cache.page);
         p.valid = id >= 0 && id < a.cache.pages;
         p.row = id * a.kv_heads + hk;
-        p.offset = (int)(j % a.cache.page);
     } else {
         p.row = s.k0 + j;
         p.valid = !a.key_mask || a.key_mask[p.row] != 0;
@@ -88,26 +85,9 @@ __device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
     asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "l"(p));
     return make_float4(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u), __uint_as_float(y << 16), __uint_as_float(y & 0xffff0000u));
 }
-__device__ __forceinline__ float load1(const float* p) { return ld_global_f32(p); }
-__device__ __forceinline__ float load1(const __nv_bfloat16* p) { return __uint_as_float(ld_global_u16(p) << 16); }
-__device__ __forceinline__ void store1(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store1(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
 
 __device__ __forceinline__ void store4(float* p, float x, float y, float z, float w) { *reinterpret_cast<float4*>(p) = make_float4(x, y, z, w); }
 __device__ __forceinline__ void store4(__nv_bfloat16* p, float x, float y, float z, float w) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x, y), pack_bf16(z, w)); }
-
-template <typename T, bool CACHED>
-__device__ __forceinline__ float4 load_key4(const Attention& a, const KeyPlace& p, int hk, int d) {
-    if (!CACHED) return load4(static_cast<const T*>(a.k) + p.row * a.ldk + (int64_t)hk * a.head_dim + d);
-    const uint32_t w = ld_global_u32(a.cache.k + (p.row * a.cache.page + p.offset) * a.head_dim + d);
-    const float f = ld_global_f32(a.cache.k_scale + p.row);
-    return make_float4((float)(int8_t)w * f, (float)(int8_t)(w >> 8) * f, (float)(int8_t)(w >> 16) * f, (float)(int8_t)(w >> 24) * f);
-}
-template <typename T, bool CACHED>
-__device__ __forceinline__ float load_value(const Attention& a, const KeyPlace& p, int hk, int d) {
-    if (!CACHED) return load1(static_cast<const T*>(a.v) + p.row * a.ldv + (int64_t)hk * a.head_dim + d);
-    return (float)a.cache.v[(p.row * a.head_dim + d) * a.cache.page + p.offset] * ld_global_f32(a.cache.v_scale + p.row);
-}
 
 // Joins n partial results of a row, at(c) their places: o = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c.  WARPS warps (1, or
 // all 4 of the CTA) take them in turn, four at a time under way each: a lone sequence has few rows and many chunks (16384 keys,

@@ -2,7 +2,8 @@
 // [unit][channel][key], unit a (sequence, kv head).  Keys without a page become zeros.  Bound by memory: one byte in, two out.
 //
 // A CTA takes 128 keys of a unit: 16 codes a thread and turn, of keys along the channels, of values along the keys, as their
-// pages keep them, so that no transposition is needed anywhere.
+// pages keep them, so that no transposition is needed anywhere.  (32 sequences of 866 keys, one head of 256: 14 us under a profiler,
+// of which 7 are the 43 MB; 15.5 with one load at a time.)
 #include "attention_common.cuh"
 
 #include <cuda_fp16.h>
