@@ -493,6 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 ok = wait_all(smem_u32(&ctl.o[mine]), S::kAhead ? (n - 1) & 1 : 0, abort_flag, watchdog, kWdSoftmax);
                 tc_fence_after();
             }
+            if (base == -INFINITY) l = 0.0f;                     // (2^-126 for each masked key that ex2_polynomial had: their 1 / l is infinite)
             if (kSplit > 1) {
                 seat[split * NT * 128] = l;
                 meet();

@@ -432,6 +432,18 @@ def test_attention_kv8_many_queries_of_every_width(Hq, Hk, D, P, queries):
 
 
 @gpu
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("scale", [0.999, 0.51, 1.0, 3e-30])
+def test_attention_kv8_rows_that_see_nothing_whatever_the_scales(D, scale):
+    """Causal, more queries than keys, of few and of many tiles: the first rows are zeros."""
+    cache = filled_cache(64, 2, D, 16, 76)
+    cache.v_scale.fill_(scale)
+    table = table_of(64, 3, 20, 77)
+    check_cache_attention(cache, table, [119, 300, 1], [123, 700, 40], 4, "bf16", True, seed=78)
+    check_cache_attention(cache, table, [1, 2, 0], [2, 3, 2], 4, "bf16", True, seed=79, max_q=3)
+
+
+@gpu
 def test_attention_kv8_widens_in_several_passes():
     """More (sequence, head) pairs than the widened codes of one pass hold."""
     cache = filled_cache(60, 4, 256, 128, 73)
