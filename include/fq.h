@@ -390,7 +390,9 @@ fq_status fq_kv8_append(const void* k, const void* v, fq_dtype xt, int64_t token
  * causal: query i of n sees keys j <= kv_len - n + i, else all.  A query without a key gives zeros.
  * o = sum_j p_j v_j / sum_j p_j, p_j = exp(scale (q . k_j) - max).  bf16 queries are multiplied as binary16 after
  * a power of two per row has been taken out (exact but for channels 2^-14 below the row's largest), probabilities as binary16
- * (11 bits), their exponentials to 2^-18, sums in binary32.  max_q: no sequence has more queries (0: unknown); a hint.
+ * (11 bits), their exponentials to 2^-18, sums in binary32.  binary32 queries of at most 16 rows a kv head: queries and
+ * probabilities as sums of two binary16 terms (22 bits).  Either way what lies below 2^-31 of the sequence's and head's largest
+ * value, seen or not, may be lost: scales of pages that are further apart than that.  max_q: no sequence has more queries (0: unknown); a hint.
  * workspace device, fq_attention_kv8_workspace_bytes(..) bytes (ragged: q_offsets is given), 256-byte aligned, scratch (many
  * queries: up to 256 MiB of it hold codes as binary16, more only where one sequence's head does not fit); NULL where that is 0. */
 fq_status fq_attention_kv8(const void* q, fq_dtype dt, int64_t q_rows, int64_t ldq, int q_heads, const fq_kv8_cache* cache,

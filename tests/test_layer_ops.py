@@ -6,8 +6,10 @@ Bounds (u = 2^-24, the half step of binary32; h = half a step of the output's ty
   append     codes equal (each is the rounding of an exact quotient), scales within u
   attention  a score is off by at most (D + 8) u A, A = scale max_j sum_d |q_d k_jd|, which scales a probability by e^(that);
              numerator and denominator each: 2 ((D + 8) u A) + (L + 16) u; bf16 calls may take the exponential to 2^-18,
-             and their rounded probabilities add 2^-8 (bf16) or 2^-11 (binary16) of W = sum_j p_j |v_j|; then h |y|.  A probability beside the largest, 1, may underflow: each of L
-             terms loses at most 2^-25 (binary16, whose numbers below 2^-14 are multiples of 2^-24) or 2^-126 of V = max_j |v_j|
+             and their rounded probabilities add 2^-8 (bf16) or 2^-11 (binary16) of W = sum_j p_j |v_j|; then h |y|.  A probability beside the largest, 1, may underflow: each
+             of L terms loses at most 2^-126 of V = max_j |v_j| -- or, over the cache, where p vs 2^(7-e) goes as one binary16 term
+             (binary32 rows, 16 at most: two), a multiple of 2^-24: 2^-25, times a code of at most 127 and 2^(e-7), with the largest value
+             127 vs >= 127 2^(e-1): 2^-31 of the largest value of any channel of the head, seen or not.  Two terms keep 2^-22 of p
 """
 import math
 import os
@@ -302,10 +304,12 @@ def attention_reference(q, k, v, scale, seen):
             v.abs().amax(0)[None])
 
 
-def assert_attention(got, want, A, W, V, L, rounded):
+def assert_attention(got, want, A, W, V, L, rounded, two_terms=False):
     D = want.shape[-1]
     bound = (2 * (2 * (D + 8) * U * A + (L + 16) * U + (2.0 ** -18 if rounded else 0.0)) + rounded) * W + HALF[got.dtype] * want.abs()
-    bound = bound + L * (2.0 ** -25 if rounded == 2.0 ** -11 else 2.0 ** -126) * V
+    bound = bound + L * 2.0 ** -126 * V + (2.0 ** -22 * W if two_terms else 0.0)
+    if rounded == 2.0 ** -11 or two_terms:
+        bound = bound + L * 2.0 ** -31 * V.amax(-1, keepdim=True)
     off = (got.double().view_as(want) - want).abs()
     assert torch.isfinite(got).all()
     assert (off <= bound).all(), f"{(off / bound.clamp_min(1e-300)).max().item():.3g} of the bound"
@@ -323,7 +327,7 @@ def dense(cache, table, b, n):
     return k, v, ok
 
 
-def check_cache_attention(cache, table, lens, queries, Hq, dtype, causal, scale=None, seed=0, max_kv=0, **kw):
+def check_cache_attention(cache, table, lens, queries, Hq, dtype, causal, scale=None, seed=0, max_kv=0, two_terms=False, **kw):
     D, rows = cache.head_dim, sum(queries)
     q = rand((rows + 3, Hq * D), seed, TYPES[dtype], gain=1.5)
     y = torch.full((rows + 3, Hq * D), 7.0, dtype=TYPES[dtype], device="cuda")
@@ -337,7 +341,7 @@ def check_cache_attention(cache, table, lens, queries, Hq, dtype, causal, scale=
         last = torch.arange(T, device="cuda")[:, None] + (n - T if causal else n)
         seen = ok[None] & (torch.arange(n, device="cuda")[None] <= last)
         want, A, W, V = attention_reference(q[at:at + T].double().view(T, Hq, D), k, v, scale, seen)
-        assert_attention(y[at:at + T], want, A, W, V, n, 2.0 ** -11 if dtype == "bf16" else 0.0)
+        assert_attention(y[at:at + T], want, A, W, V, n, 2.0 ** -11 if dtype == "bf16" else 0.0, two_terms)
         empty = ~seen.any(1)
         assert (y[at:at + T][empty] == 0).all()
         at += T
@@ -463,6 +467,15 @@ def test_attention_kv8_peaked_scores_and_repeated_pages():
     cache.k_scale[table[0, 30].item()] *= 30
     check_cache_attention(cache, table, [2100, 700], [1, 1], 8, "bf16", True, scale=1.0, seed=33)
     check_cache_attention(cache, table, [2100, 700], [20, 30], 8, "bf16", True, scale=1.0, seed=34)
+
+
+@gpu
+def test_attention_kv8_peaked_scores_of_binary32_rows():
+    """Channels where the value beside the largest probability is next to nothing, so that only small terms are left."""
+    for D, Hq, Hk, T in ((64, 3, 1, 2), (128, 12, 3, 1), (192, 8, 1, 2)):
+        cache = filled_cache(41, Hk, D, 16, 44)
+        table = table_of(41, 2, 20, 45)
+        check_cache_attention(cache, table, [27, 300], [T, T], Hq, "f32", True, scale=1.0, seed=46, two_terms=True)
 
 
 @gpu
