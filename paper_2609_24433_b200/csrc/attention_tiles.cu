@@ -45,6 +45,7 @@ static_assert(256 * kRegsSoftmax + 256 * kRegsOther <= kThreads * kRegsLaunch, "
 constexpr int kKeys = 128;
 constexpr int kMetas = 4;
 constexpr float kSlack = 8.0f;          // log2 of how far a row's maximum may rise over its base
+constexpr float kHuge = 4096.0f;        // bases from here on are subtracted from rounded scores
 
 constexpr uint32_t kWdProducer = 0x800u, kWdMma = 0x1000u, kWdSoftmax = 0x2000u;
 
@@ -435,7 +436,18 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     }
                     e = now_e;
                 }
-                const float minus = base == -INFINITY ? 0.0f : -base;
+                // score - base is one FMA, exact up to the base's own rounding: of a base of 2^27 that is up to 2^3, by which the largest
+                // probability would miss 1 (and its 16 bits).  Huge scores are rounded as their base was and subtracted here.
+                float minus = base == -INFINITY ? 0.0f : -base;
+                const bool huge = fabsf(minus) >= kHuge;
+                if (__any_sync(0xffffffffu, huge)) {
+#pragma unroll
+                    for (int i = 0; i < kCols; ++i) {
+                        const float x = __uint_as_float(v[i]);
+                        v[i] = huge ? __float_as_uint(__fadd_rn(__fmul_rn(x, fmaxf(CACHED ? factor * ks[i / 16] : factor, FLT_MIN)), minus)) : v[i];
+                    }
+                    minus = huge ? 0.0f : minus;
+                }
                 if (S::kEarly && j + mine > 0) {                 // its turn at the exponentials; the last product has read its probabilities
                     const uint32_t turn = smem_u32(&ctl.turn[warp]), turn_phase = (j - 1 + mine) & 1;
                     ok = wait_all(j > 0 ? smem_u32(&ctl.o[mine]) : turn, j > 0 ? (j - 1) & 1 : turn_phase, turn, turn_phase, abort_flag, watchdog, kWdSoftmax);
@@ -450,7 +462,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     uint32_t p[16];
 #pragma unroll
                     for (int g = 2 * c; g < 2 * c + 2; ++g) {
-                        const float f = fmaxf(CACHED ? factor * ks[g] : factor, FLT_MIN);
+                        const float f = huge ? 1.0f : fmaxf(CACHED ? factor * ks[g] : factor, FLT_MIN);
                         const float z = CACHED ? minus + meta.lvf[split * (kCols / 16) + g] : minus;
 #pragma unroll
                         for (int i = 0; i < 16; i += 2) {

@@ -746,3 +746,29 @@ print("fine")
 """
     got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=ROOT)
     assert got.returncode == 0 and "fine" in got.stdout, got.stderr[-2000:]
+
+
+@gpu
+@pytest.mark.parametrize("size", [1e5, 1e8, 1e12, 1e25])
+@pytest.mark.parametrize("D,T,dtype", [(64, 40, "bf16"), (64, 300, "bf16"), (128, 300, "bf16"), (256, 40, "bf16"), (64, 1, "bf16"), (64, 1, "f32"), (64, 40, "f32")])
+def test_attention_of_huge_scores_takes_the_largest(D, T, dtype, size):
+    """Scores whose binary32 steps are large, and further apart than their error, which is (D + 8) u A: the key with the largest one has
+    probability 1.  It takes one rounding of at most 2^-8 (rows; over the cache 2^-11), the store half a step; exponentials are good to 2^-18."""
+    L = 700
+    q = rand((T, 2 * D), 151, TYPES[dtype], gain=size)
+    cache = filled_cache(30, 2, D, 32, 152)
+    table = table_of(30, 1, 22, 153)
+    k, v, _ = dense(cache, table, 0, L)
+    ks, vs = (rand((L, 2 * D), 154 + i, TYPES[dtype]) for i in range(2))
+    calls = [(fq.attention_kv8(q, 2, cache, table, ints([L]), causal=False), k, v, 2.0 ** -11 if dtype == "bf16" else 2.0 ** -22),
+             (fq.cross_attention(q, ks, vs, 2, 2, 1), ks.double().view(L, 2, D), vs.double().view(L, 2, D), 2.0 ** -8 if dtype == "bf16" else 0.0)]
+    for got, k, v, rounded in calls:
+        x = q.double().view(T, 2, D)
+        s = torch.einsum("thd,lhd->thl", x, k) * D ** -0.5
+        A = (torch.einsum("thd,lhd->thl", x.abs(), k.abs()) * D ** -0.5).amax(-1)
+        two = s.topk(2, -1)
+        clear = two.values[..., 0] - two.values[..., 1] > 4 * (D + 8) * U * A + 64
+        assert clear.sum() > 0.5 * clear.numel()
+        want = torch.stack([v[two.indices[:, h, 0], h] for h in range(2)], 1)
+        off = (got.double().view(T, 2, D) - want).abs()
+        assert (off <= (rounded + 2.0 ** -16 + HALF[got.dtype]) * want.abs())[clear].all()
