@@ -89,7 +89,12 @@ __device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
 __device__ __forceinline__ void store4(float* p, float x, float y, float z, float w) { *reinterpret_cast<float4*>(p) = make_float4(x, y, z, w); }
 __device__ __forceinline__ void store4(__nv_bfloat16* p, float x, float y, float z, float w) { *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16(x, y), pack_bf16(z, w)); }
 
-// Joins n partial results of a row, at(c) their places: o = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c.  WARPS warps (1, or
+// 1 / l of a row with the maximum m and the sum l: 0 for a row that sees no key (m = -inf, which no seen score leaves: a maximum is
+// -FLT_MAX at least).  NaN where the scores that it sees are all -inf or there is a +inf, so that no term is left, as in the formula.
+__device__ __forceinline__ float reciprocal_sum(float m, float l) { return l == 0.0f ? (m == -INFINITY ? 0.0f : __int_as_float(0x7fffffff)) : 1.0f / l; }
+
+// Joins n partial results of a row, at(c) their places: o = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c.  (The maximum passes over
+// a NaN among the m_c, whose weight carries it on.)  WARPS warps (1, or
 // all 4 of the CTA) take them in turn, four at a time under way each: a lone sequence has few rows and many chunks (16384 keys,
 // 32 heads of 128 in 64 chunks: the whole call 51 us with one warp a row and one chunk at a time, 17 so).  Fixed order of sums.
 template <typename T, int WARPS, typename At>
@@ -145,7 +150,7 @@ __device__ __forceinline__ void join_row(const Attention& a, int n, At at, T* y)
         }
         if (part == 1) p = o;
     }
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const float inv = reciprocal_sum(m, l);
     if (low && part == 0) store4(y + 4 * lane, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
     if (high && part == (WARPS > 1 ? 1 : 0)) store4(y + 128 + 4 * lane, p.x * inv, p.y * inv, p.z * inv, p.w * inv);
 }

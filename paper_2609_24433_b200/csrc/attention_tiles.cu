@@ -109,9 +109,15 @@ __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
 }
 __device__ __forceinline__ int exponent_of(float x) { return (int)((__float_as_uint(x) >> 23) & 255) - 127; }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+// Maxima that a NaN among the operands reaches.
 __device__ __forceinline__ float max3(float x, uint32_t y, uint32_t z) {
     float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(__uint_as_float(y)), "f"(__uint_as_float(z)));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(__uint_as_float(y)), "f"(__uint_as_float(z)));
+    return r;
+}
+__device__ __forceinline__ float max2(float x, float y) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
     return r;
 }
 __device__ __forceinline__ float ex2(float x) {
@@ -366,12 +372,13 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 const uint32_t p_addr = (S::kEarly ? lanes + 384 + 64 * mine : lanes + 128 * buf) + split * (kCols / 2);
                 const int lim = (int)min(max(limit64 - (k0 + (int64_t)j * kKeys), (int64_t)-1), (int64_t)kKeys) - split * kCols;
                 uint32_t seen[kCols / 32];
-                bool partly = false;
+                bool partly = false, sees = false;
 #pragma unroll
                 for (int c = 0; c < kCols / 32; ++c) {
                     const int x = lim - 32 * c;
                     seen[c] = meta.valid[split * (kCols / 32) + c] & (x < 0 ? 0u : x >= 31 ? ~0u : (2u << x) - 1u);
                     partly = partly || seen[c] != ~0u;
+                    sees = sees || seen[c] != 0u;
                 }
                 const bool masked = __any_sync(0xffffffffu, partly);
                 const float* const ks = meta.ks + split * (kCols / 16);
@@ -394,14 +401,15 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                         x = max3(x, v[16 * g + i], v[16 * g + i + 1]);
                         y = max3(y, v[16 * g + i + 2], v[16 * g + i + 3]);
                     }
-                    top = fmaxf(top, CACHED ? fmaxf(x, y) * fmaxf(factor * ks[g], FLT_MIN) : fmaxf(x, y));
+                    top = max2(top, CACHED ? max2(x, y) * fmaxf(factor * ks[g], FLT_MIN) : max2(x, y));
                 }
                 if (!CACHED) top *= fmaxf(factor, FLT_MIN);
+                if (sees) top = max2(top, -FLT_MAX);             // (-inf stays to rows that see nothing)
                 if (kSplit > 1) {
                     seat[split * NT * 128] = top;
                     meet();                                      // (and all of them have read their scores)
 #pragma unroll
-                    for (int i = 0; i < kSplit; ++i) top = fmaxf(top, seat[i * NT * 128]);
+                    for (int i = 0; i < kSplit; ++i) top = max2(top, seat[i * NT * 128]);
                     meet();                                      // (the next maxima may come)
                 }
                 if (S::kEarly) {
@@ -411,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 }
                 // ---- a new base
                 const int now_e = CACHED ? meta.e : e;
-                const bool rise = top > base + kSlack || (base == -INFINITY && top > base);
+                const bool rise = !(top <= base + kSlack);       // (a NaN, too: it becomes the base, so that all of the row is NaN)
                 if (__any_sync(0xffffffffu, rise || now_e != e)) {
                     const float now = rise ? top : base;
                     const float keep = rise ? exp2f(base - now) : 1.0f;                // (from nothing: 0)
@@ -505,7 +513,6 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 ok = wait_all(smem_u32(&ctl.o[mine]), S::kAhead ? (n - 1) & 1 : 0, abort_flag, watchdog, kWdSoftmax);
                 tc_fence_after();
             }
-            if (base == -INFINITY) l = 0.0f;                     // (2^-126 for each masked key that ex2_polynomial had: their 1 / l is infinite)
             if (kSplit > 1) {
                 seat[split * NT * 128] = l;
                 meet();
@@ -513,10 +520,14 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
 #pragma unroll
                 for (int i = 0; i < kSplit; ++i) l += seat[i * NT * 128];
             }
+            // The key with the base has 2^0, give or take the roundings.  What is far below is no sum but the 2^-126, by `inv` up to 2^-66,
+            // that ex2_polynomial gives each key at -inf, masked or not.
+            if (l < 0x1p-20f) l = 0.0f;
+            const bool any = base != -INFINITY;                  // the row sees a key
             if (ok) {
                 const int64_t at = (token * a.q_heads + head) * a.chunks + chunk;
                 const float whole = CACHED ? power_of_two(e / 2) : 1.0f, rest = CACHED ? power_of_two(e - e / 2 - 7) : 1.0f;
-                const float inv = direct ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f;
+                const float inv = direct ? reciprocal_sum(base, l) : 1.0f;
                 __nv_bfloat16* y = static_cast<__nv_bfloat16*>(a.y) + token * a.ldy + head * D + split * kOCols;
                 float* part = direct ? nullptr : a.part + at * D + split * kOCols;
 #pragma unroll 1
@@ -528,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                     }
                     float f[16];
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) f[i] = n > 0 && l > 0.0f ? __uint_as_float(o[i]) * whole * rest * inv : 0.0f;
+                    for (int i = 0; i < 16; ++i) f[i] = any ? __uint_as_float(o[i]) * whole * rest * inv : 0.0f;
                     if (!there || split * kOCols + c >= D) continue;           // (D is a multiple of 16)
 #pragma unroll
                     for (int x = 0; x < 16; x += 8) {

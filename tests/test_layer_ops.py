@@ -748,6 +748,127 @@ print("fine")
     assert got.returncode == 0 and "fine" in got.stdout, got.stderr[-2000:]
 
 
+# ------------------------------------------------------------------------------------------- numbers that are not finite
+def plain_attention(q, k, v, scale, seen):
+    """The formula in 64 bits, whatever the numbers: q [T, Hq, D], k, v [L, Hk, D], seen [T, L] -> [T, Hq, D].  A query without a key
+    gives zeros; values of keys that no query sees do not enter."""
+    Hq, Hk = q.shape[1], k.shape[1]
+    k, v = (t.masked_fill(~seen.any(0)[:, None, None], 0.0).repeat_interleave(Hq // Hk, 1) for t in (k, v))
+    s = torch.where(seen[None], (q.transpose(0, 1)[:, :, None] * k.transpose(0, 1)[:, None]).sum(-1) * scale, -math.inf)
+    p = torch.exp(s - s.amax(-1, keepdim=True))
+    p = torch.where(seen[None], p, 0.0)
+    o = (p[..., None] * v.transpose(0, 1)[:, None]).sum(2) / p.sum(-1)[..., None]
+    return torch.where(seen.any(1)[None, :, None], o, 0.0).transpose(0, 1)
+
+
+def assert_same_kind(got, want):
+    """NaN where the formula has it, and infinities with its signs."""
+    got = got.double().view_as(want)
+    assert torch.equal(got.isnan(), want.isnan()), f"{(got.isnan() != want.isnan()).sum().item()} of {got.numel()} numbers are NaN on one side only"
+    assert torch.equal(got.isposinf(), want.isposinf()) and torch.equal(got.isneginf(), want.isneginf())
+
+
+NOT_FINITE = [math.nan, math.inf, -math.inf]
+
+
+@gpu
+@pytest.mark.parametrize("bad", NOT_FINITE)
+@pytest.mark.parametrize("Hq,Hk,D,T,dtype", [
+    (4, 2, 64, 40, "bf16"), (2, 1, 64, 300, "bf16"), (2, 1, 128, 300, "bf16"), (8, 1, 256, 40, "bf16")])
+@pytest.mark.parametrize("n", [1, 200, 2100])
+def test_attention_kv8_of_queries_that_are_not_finite(bad, Hq, Hk, D, T, dtype, n):
+    """A row with a channel that is not finite is NaN where it sees a key (every score is NaN or infinite, and the largest less itself
+    is NaN), zeros where it sees none; all other rows are what they were."""
+    cache = filled_cache(70, Hk, D, 32, 121)
+    table = table_of(70, 1, 70, 122)
+    q = rand((T, Hq * D), 123, TYPES[dtype])
+    kv = ints([n])
+    for causal in (True, False):
+        want = fq.attention_kv8(q, Hq, cache, table, kv, causal=causal)
+        x = q.clone()
+        rows = sorted({0, T // 3, T - 1})
+        for i, r in enumerate(rows):
+            x[r, (Hq - 1) * D + (5 + 17 * i) % D] = bad
+        got = fq.attention_kv8(x, Hq, cache, table, kv, causal=causal)
+        for r in rows:
+            sees = n > 0 and (not causal or n - T + r >= 0)
+            tail = got[r, (Hq - 1) * D:]
+            assert tail.isnan().all() if sees else (tail == 0).all(), (r, tail[:4])
+            want[r, (Hq - 1) * D:] = got[r, (Hq - 1) * D:] = 0
+        assert torch.equal(got, want)
+
+
+@gpu
+@pytest.mark.parametrize("Hq,Hk,D,T,L,B,dtype", [
+    (4, 2, 64, 40, 200, 2, "bf16"), (2, 2, 64, 300, 250, 1, "bf16"), (2, 1, 128, 300, 200, 1, "bf16"), (4, 1, 256, 40, 200, 2, "bf16"),
+    (4, 2, 64, 40, 2100, 2, "bf16"), (2, 1, 64, 300, 2100, 1, "bf16"), (2, 1, 128, 300, 2100, 1, "bf16"), (4, 1, 256, 40, 2100, 1, "bf16"),   # chunks
+    (4, 4, 64, 9, 700, 40, "bf16"),                                                                                                         # long, one chunk
+    (4, 2, 64, 3, 200, 2, "f32"), (4, 2, 64, 40, 200, 2, "f32"), (4, 2, 128, 40, 2100, 2, "f32")])
+def test_cross_attention_of_numbers_that_are_not_finite(Hq, Hk, D, T, L, B, dtype):
+    q, k, v = (rand((B * n, h * D), 131 + i, TYPES[dtype]) for i, (n, h) in enumerate(((T, Hq), (L, Hk), (L, Hk))))
+    mask = torch.rand(B * L, device="cuda", generator=torch.Generator(device="cuda").manual_seed(134)) > 0.1
+    clean = fq.cross_attention(q, k, v, Hq, Hk, B, key_mask=mask)
+
+    def check(q, k, v, mask, touched):
+        got = fq.cross_attention(q, k, v, Hq, Hk, B, key_mask=mask)
+        want = torch.cat([plain_attention(q[b * T:(b + 1) * T].double().view(T, Hq, D), k[b * L:(b + 1) * L].double().view(L, Hk, D),
+                                          v[b * L:(b + 1) * L].double().view(L, Hk, D), D ** -0.5, mask[b * L:(b + 1) * L][None].expand(T, -1))
+                          for b in touched])
+        rows = torch.cat([torch.arange(b * T, (b + 1) * T, device="cuda") for b in touched])
+        assert_same_kind(got[rows], want)
+        rest = torch.ones(B * T, dtype=torch.bool, device="cuda")
+        rest[rows] = False
+        assert torch.equal(got[rest], clean[rest])
+        # what is finite is near: a score loses (D + 8) u A, a probability 2^-8 at most, the store half a step (see the top of this file)
+        fine = want.isfinite()
+        size = v.double().masked_fill(~v.isfinite(), 0.0).abs().max()
+        assert ((got[rows].double().view_as(want) - want)[fine].abs() <= 2.0 ** -6 * size).all()
+        return got
+
+    for bad in NOT_FINITE:
+        x = q.clone()
+        x[0, 3] = x[T - 1, Hq * D - 1] = x[T // 2, D] = bad
+        check(x, k, v, mask, [0])
+        for j in (0, 1, 2, 15, 16 * (L // 32) + 1, L - 1):
+            seen = mask.clone()
+            seen[j] = True
+            clean = fq.cross_attention(q, k, v, Hq, Hk, B, key_mask=seen)
+            x = k.clone()
+            x[j, D - 2] = bad
+            check(q, x, v, seen, [0])
+            x = v.clone()
+            x[j, Hk * D - 3] = bad
+            check(q, k, x, seen, [0])
+            seen[j] = False                             # behind the mask it does not matter
+            x, z = k.clone(), v.clone()
+            x[j], z[j] = bad, bad
+            assert torch.equal(fq.cross_attention(q, x, z, Hq, Hk, B, key_mask=seen), fq.cross_attention(q, k, v, Hq, Hk, B, key_mask=seen))
+        clean = fq.cross_attention(q, k, v, Hq, Hk, B, key_mask=mask)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("Hq,D,T,L", [(2, 64, 40, 200), (2, 64, 300, 2100), (2, 128, 300, 2100), (1, 256, 40, 2100), (2, 64, 3, 1)])
+def test_cross_attention_of_scores_that_are_all_minus_infinity(Hq, D, T, L, dtype):
+    """exp(-inf - (-inf)): NaN, as the formula has it, and not the zeros of a query without a key; keys at minus infinity beside others
+    count for nothing, a whole chunk of them too."""
+    q, k, v = (rand((n, Hq * D), 141 + i, TYPES[dtype]) for i, n in enumerate((T, L, L)))
+    q[:, 0] = 1.0
+    low = k.clone()
+    low[:, 0] = -math.inf
+    got = fq.cross_attention(q, low, v, Hq, Hq, 1)
+    assert got[:, :D].isnan().all()
+    assert torch.equal(got[:, D:], fq.cross_attention(q, k, v, Hq, Hq, 1)[:, D:])
+    if L > 1:
+        keep = torch.zeros(L, dtype=torch.bool, device="cuda")
+        keep[[L - 1, L // 3]] = True
+        low = k.clone()
+        low[~keep, 0] = -math.inf
+        got = fq.cross_attention(q, low, v, Hq, Hq, 1)[:, :D]
+        want = plain_attention(q.double().view(T, Hq, D), k.double().view(L, Hq, D), v.double().view(L, Hq, D), D ** -0.5, keep[None].expand(T, -1))[:, 0]
+        assert ((got.double() - want).abs() <= 2.0 ** -6 * v.double().abs().max()).all()
+
+
 @gpu
 @pytest.mark.parametrize("size", [1e5, 1e8, 1e12, 1e25])
 @pytest.mark.parametrize("D,T,dtype", [(64, 40, "bf16"), (64, 300, "bf16"), (128, 300, "bf16"), (256, 40, "bf16"), (64, 1, "bf16"), (64, 1, "f32"), (64, 40, "f32")])
