@@ -388,6 +388,8 @@ fq_status fq_kv8_append(const void* k, const void* v, fq_dtype xt, int64_t token
  * Query head h reads kv head h / (q_heads / heads).  kv_len device int32[batch]: keys of each sequence, those of this
  * step's tokens included; cut to table_width pages and, where max_kv > 0, to max_kv (which sizes the launch and the workspace).
  * causal: query i of n sees keys j <= kv_len - n + i, else all.  A query without a key gives zeros.
+ * A query with a channel that is NaN or infinite gives NaN in all channels of that head where it sees a key; codes are finite, and the
+ * scales of pages have to be.  No other row is touched by it.
  * o = sum_j p_j v_j / sum_j p_j, p_j = exp(scale (q . k_j) - max).  bf16 queries are multiplied as binary16 after
  * a power of two per row has been taken out (exact but for channels 2^-14 below the row's largest), probabilities as binary16
  * (11 bits), their exponentials to 2^-18, sums in binary32.  binary32 queries of at most 16 rows a kv head: queries and
@@ -407,6 +409,8 @@ size_t fq_attention_kv8_workspace_bytes(fq_dtype dt, int64_t q_rows, int q_heads
  * will do).  Rows kv_offsets[b] .. kv_offsets[b+1] belong to sequence b (NULL: kv_rows / batch each: a padded batch); of them
  * the first kv_len[b] are keys (NULL: all), and of those the ones whose key_mask byte is not 0 (device uint8[kv_rows], NULL:
  * all).  What masked rows hold does not matter, infinities and NaN included.  A query without a key gives zeros.
+ * Rows that are seen may hold anything, and count by the formula: a score that is NaN or +infinity makes its query's head NaN, as scores
+ * that are all -infinity do; one at -infinity beside others has probability 0; what is not finite in v reaches its channel.
  * No causal order.  D a multiple of 16, at most 256.  max_q, max_kv: as above (0: unknown; sequences are cut to max_kv keys).
  * bf16: the probabilities, exponentials to 2^-18, are rounded to bf16 ahead of the product with v; sums in binary32. */
 fq_status fq_cross_attention(const void* q, fq_dtype dt, int64_t q_rows, int64_t ldq, int q_heads, const void* k, const void* v,

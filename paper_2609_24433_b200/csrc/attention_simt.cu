@@ -9,6 +9,8 @@
 // (with values read one by one, and a key's place looked up for each of them, 1055 and 1032).
 #include "attention_common.cuh"
 
+#include <float.h>
+
 namespace fq {
 namespace {
 
@@ -123,13 +125,13 @@ __global__ void __launch_bounds__(kThreads) attention_simt_kernel(const Attentio
             }
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                float top = -INFINITY;
+                float top = -INFINITY;                  // (stays so to a row that sees nothing, and to no other)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int t = tx + 16 * j;
                     const bool seen = places[t] >= 0 && j0 + t <= limit[i];
                     acc[i][j] = seen ? acc[i][j] * a.scale_log2 : -INFINITY;
-                    top = fmaxf(top, acc[i][j]);
+                    if (seen) top = fmaxf(fmaxf(top, -FLT_MAX), acc[i][j]);
                 }
 #pragma unroll
                 for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
@@ -178,7 +180,7 @@ __global__ void __launch_bounds__(kThreads) attention_simt_kernel(const Attentio
             if (row >= s.queries * G) continue;
             const int64_t token = s.q0 + row / G, head = hk * G + row % G;
             if (tk.chunks <= 1) {
-                const float inv = l[i] > 0.0f ? 1.0f / l[i] : 0.0f;
+                const float inv = reciprocal_sum(m[i], l[i]);
                 float* y = static_cast<float*>(a.y) + token * a.ldy + head * D;
 #pragma unroll
                 for (int j = 0; j < DT; j += 4)

@@ -23,6 +23,7 @@
 #include "attention_common.cuh"
 
 #include <cuda_fp16.h>
+#include <float.h>
 
 namespace fq {
 namespace {
@@ -355,8 +356,8 @@ __global__ void __launch_bounds__(kWarps * 32, tokens_resident(sizeof(T) == 2, D
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int x = 0; x < 4; ++x) sc[nq][i][x] *= f[x & 1];
+                const int from = j0 + 16 * (g >> 1) + (g & 1);   // this lane's first token
                 if (!clean) {
-                    const int from = j0 + 16 * (g >> 1) + (g & 1);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -371,6 +372,7 @@ __global__ void __launch_bounds__(kWarps * 32, tokens_resident(sizeof(T) == 2, D
                 bool rise = grown;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
+                    if (there && from <= limit[nq][c]) top[c] = fmaxf(top[c], -FLT_MAX);        // (-inf stays to a row that sees nothing)
 #pragma unroll
                     for (int x = 4; x < 32; x <<= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(0xffffffffu, top[c], x));
                     const bool up = top[c] > m[nq][c] + kSlack || (m[nq][c] == -INFINITY && top[c] > m[nq][c]);
@@ -480,7 +482,7 @@ __global__ void __launch_bounds__(kWarps * 32, tokens_resident(sizeof(T) == 2, D
             }
             if (whole) {
                 const int64_t token = s.q0 + row / a.group, head = hk * a.group + row % a.group;
-                const float inv = sum > 0.0f ? 1.0f / sum : 0.0f;
+                const float inv = reciprocal_sum(top, sum);
                 store4(static_cast<T*>(a.y) + token * a.ldy + head * D + d, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
             } else {
                 const int64_t seat = tokens_seat(blockIdx.x, block == 0) * kRows + r;

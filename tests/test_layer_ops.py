@@ -774,7 +774,9 @@ NOT_FINITE = [math.nan, math.inf, -math.inf]
 @gpu
 @pytest.mark.parametrize("bad", NOT_FINITE)
 @pytest.mark.parametrize("Hq,Hk,D,T,dtype", [
-    (4, 2, 64, 40, "bf16"), (2, 1, 64, 300, "bf16"), (2, 1, 128, 300, "bf16"), (8, 1, 256, 40, "bf16")])
+    (8, 1, 64, 1, "bf16"), (8, 1, 256, 2, "bf16"), (3, 1, 128, 1, "f32"),                   # few queries: one and two tiles of columns, two terms
+    (4, 2, 64, 40, "bf16"), (2, 1, 64, 300, "bf16"), (2, 1, 128, 300, "bf16"), (8, 1, 256, 40, "bf16"),
+    (4, 2, 64, 40, "f32")])
 @pytest.mark.parametrize("n", [1, 200, 2100])
 def test_attention_kv8_of_queries_that_are_not_finite(bad, Hq, Hk, D, T, dtype, n):
     """A row with a channel that is not finite is NaN where it sees a key (every score is NaN or infinite, and the largest less itself
@@ -847,7 +849,7 @@ def test_cross_attention_of_numbers_that_are_not_finite(Hq, Hk, D, T, L, B, dtyp
 
 
 @gpu
-@pytest.mark.parametrize("dtype", ["bf16"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("Hq,D,T,L", [(2, 64, 40, 200), (2, 64, 300, 2100), (2, 128, 300, 2100), (1, 256, 40, 2100), (2, 64, 3, 1)])
 def test_cross_attention_of_scores_that_are_all_minus_infinity(Hq, D, T, L, dtype):
     """exp(-inf - (-inf)): NaN, as the formula has it, and not the zeros of a query without a key; keys at minus infinity beside others
