@@ -321,6 +321,12 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.q) + token * a.ldq + head * D;
                 const uint32_t dst = q_smem + mine * S::kQTile + (r % 128) * 128;
                 float down = 1.0f;
+                // (Factors are held at FLT_MIN or more below, where a masked -inf needs one; products of rows reach 2^128 and would show it.)
+                const bool tiny = !CACHED && a.scale_log2 < FLT_MIN;
+                if (tiny) {
+                    down = 0x1p-64f;
+                    factor = a.scale_log2 * 0x1p64f;
+                }
                 if (CACHED) {
                     float top = 0.0f;
 #pragma unroll 8
@@ -342,6 +348,11 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                         uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                         for (int i = 0; i < 4; ++i) w[i] = pack_half(__uint_as_float(w[i] << 16) * down, __uint_as_float(w[i] & 0xffff0000u) * down);
+                        v = make_uint4(w[0], w[1], w[2], w[3]);
+                    } else if (tiny) {
+                        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = pack_bf16(__uint_as_float(w[i] << 16) * down, __uint_as_float(w[i] & 0xffff0000u) * down);
                         v = make_uint4(w[0], w[1], w[2], w[3]);
                     }
                     sts128(dst + (d / 64) * 16384 + ((((d % 64) / 8) ^ (r & 7)) * 16), v.x, v.y, v.z, v.w);

@@ -895,3 +895,19 @@ def test_attention_of_huge_scores_takes_the_largest(D, T, dtype, size):
         want = torch.stack([v[two.indices[:, h, 0], h] for h in range(2)], 1)
         off = (got.double().view(T, 2, D) - want).abs()
         assert (off <= (rounded + 2.0 ** -16 + HALF[got.dtype]) * want.abs())[clear].all()
+
+
+@gpu
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -140, 2.0 ** -127])
+@pytest.mark.parametrize("D,T,dtype", [(64, 40, "bf16"), (64, 300, "bf16"), (128, 300, "bf16"), (256, 40, "bf16"), (64, 40, "f32")])
+def test_attention_of_scales_below_the_smallest_normal_number(D, T, dtype, scale):
+    """Products up to the largest binary32 numbers: no scale is raised to what would tell them apart."""
+    L, g = 300, 2.2e18 * (64 / D) ** 0.25
+    q, k = (rand((n, 2 * D), 161 + i, TYPES[dtype], gain=g) for i, n in enumerate((T, L)))
+    v = rand((L, 2 * D), 163, TYPES[dtype])
+    got = fq.cross_attention(q, k, v, 2, 2, 1, scale=scale)
+    want, A, W, V = attention_reference(q.double().view(T, 2, D), k.double().view(L, 2, D), v.double().view(L, 2, D), scale,
+                                     torch.ones(T, L, dtype=torch.bool, device="cuda"))
+    assert_attention(got, want, A, W, V, L, 2.0 ** -8 if dtype == "bf16" else 0.0)
+    cache = filled_cache(12, 2, D, 32, 164)
+    check_cache_attention(cache, table_of(12, 1, 10, 165), [L], [T], 2, dtype, False, scale=scale, seed=166)
