@@ -104,7 +104,8 @@ fq_status launch_attention(Attention& a, void* workspace, size_t ws_bytes, cudaS
 
 namespace {
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool aligned(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+bool aligned16(const void* p) { return aligned(p, 16); }
 
 fq_status check_arch() {
     const int major = device_cc_major();
@@ -121,7 +122,7 @@ fq_status check_cache(const fq_kv8_cache* c) {
     if (c->head_dim % 16 != 0 || c->head_dim > 256) return FQ_ERR_UNSUPPORTED;
     if (c->page != 16 && c->page != 32 && c->page != 64 && c->page != 128) return FQ_ERR_UNSUPPORTED;
     if (c->pages > 0 && (!c->k || !c->v || !c->k_scale || !c->v_scale)) return FQ_ERR_INVALID_ARG;
-    if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->k_scale) || !aligned16(c->v_scale)) return FQ_ERR_ALIGNMENT;
+    if (!aligned16(c->k) || !aligned16(c->v) || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return FQ_ERR_ALIGNMENT;
     return FQ_OK;
 }
 fq_status check_table(const int32_t* table, int64_t ld, int64_t width, int batch) {
@@ -210,7 +211,7 @@ fq_status fq_qk_norm_rope(const void* qkv, fq_dtype xt, int64_t M, int64_t ldx, 
     if (!qkv || ldx < width || (rotary_dim > 0 && (!positions || !frequencies))) return FQ_ERR_INVALID_ARG;
     if ((q_heads > 0 && (!q || ldq < (int64_t)q_heads * head_dim)) || (k_heads > 0 && (!k || ldk < (int64_t)k_heads * head_dim))) return FQ_ERR_INVALID_ARG;
     if (!aligned16(qkv) || ldx % 8 != 0 || (q_heads > 0 && (!aligned16(q) || ldq % 8 != 0)) || (k_heads > 0 && (!aligned16(k) || ldk % 8 != 0)) ||
-        (q_gain && !aligned16(q_gain)) || (k_gain && !aligned16(k_gain)) || (rotary_dim > 0 && (!aligned16(positions) || !aligned16(frequencies))))
+        (q_gain && !aligned16(q_gain)) || (k_gain && !aligned16(k_gain)) || (rotary_dim > 0 && (!aligned(positions, 4) || !aligned(frequencies, 8))))
         return FQ_ERR_ALIGNMENT;
     const fq_status st = check_arch();
     if (st != FQ_OK) return st;

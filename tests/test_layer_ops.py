@@ -911,3 +911,27 @@ def test_attention_of_scales_below_the_smallest_normal_number(D, T, dtype, scale
     assert_attention(got, want, A, W, V, L, 2.0 ** -8 if dtype == "bf16" else 0.0)
     cache = filled_cache(12, 2, D, 32, 164)
     check_cache_attention(cache, table_of(12, 1, 10, 165), [L], [T], 2, dtype, False, scale=scale, seed=166)
+
+
+@gpu
+def test_positions_frequencies_and_page_scales_begin_anywhere():
+    """Views that start inside an allocation: these arrays are read one element at a time."""
+    M, D = 40, 64
+    x = rand((M, 4 * D), 171, torch.bfloat16)
+    positions, freq = ints(range(M + 1)), torch.cat([torch.zeros(1, dtype=torch.float64, device="cuda"), fq.rope_frequencies(D)])
+    want = fq.qk_norm_rope(x, 2, 1, D, positions[1:].clone(), freq[1:].clone())
+    got = fq.qk_norm_rope(x, 2, 1, D, positions[1:], freq[1:])
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    aligned = filled_cache(6, 1, D, 16, 172)
+    scales = torch.empty(2, 7, device="cuda")
+    other = fq.KV8Cache(aligned.k.clone(), aligned.v.clone(), scales[0, 1:].view(6, 1), scales[1, :6].view(6, 1))
+    other.k_scale.copy_(aligned.k_scale)
+    other.v_scale.copy_(aligned.v_scale)
+    table, new = ints([[2, 0, 1, 5]]), rand((M, D), 173, torch.bfloat16)
+    for c in (aligned, other):
+        fq.kv8_append(new, new, c, table, ints([3]))
+    for a, b in zip(aligned.tensors, other.tensors):
+        assert torch.equal(a, b)
+    for T, t in ((1, torch.bfloat16), (M, torch.bfloat16), (M, torch.float32)):
+        q = rand((T, 2 * D), 174, t)
+        assert torch.equal(*(fq.attention_kv8(q, 2, c, table, ints([M + 3])) for c in (aligned, other)))

@@ -135,3 +135,13 @@ def test_a_cache_of_other_shapes_or_types_is_refused():
     for bad in ((k[0], v, s, s), (k, k, s, s), (k, v.float(), s, s), (k, v, s.double(), s), (k, v, s, s[:, :2]), (k, v.transpose(2, 3).contiguous().transpose(2, 3), s, s.t().contiguous().t())):
         with pytest.raises(ValueError):
             fq.KV8Cache(*bad)
+
+
+def test_arrays_that_do_not_begin_on_an_element_are_refused(lib):
+    for at in (4097, 4098, 4099):
+        assert rope(lib, positions=ctypes.c_void_p(at)) == fq.ERR_ALIGNMENT
+        assert append(lib, Cache(4096, 4096, at, 4096, 4, 2, 64, 16)) == append(lib, Cache(4096, 4096, 4096, at, 4, 2, 64, 16)) == fq.ERR_ALIGNMENT
+        assert attend(lib, Cache(4096, 4096, 4096, at, 4, 2, 64, 16)) == fq.ERR_ALIGNMENT
+    for at in (4098, 4100):
+        assert lib.fq_qk_norm_rope(ONE, 1, L(4), L(512), 4, 2, 64, NULL, NULL, F(1e-6), ONE, ctypes.c_void_p(at), 64, 0, F(1.0), ONE, L(256), ONE, L(128),
+                                   1, NULL) == fq.ERR_ALIGNMENT
