@@ -323,8 +323,8 @@ fq_status fq_device_status(uint32_t* detail);
  * positions on what the fused qkv projection wrote, a cache of 8-bit keys and values, attention over it, and attention
  * to an encoder's states.  Forward only, like the rest of this library.  Head h of a row is its channels [h D, (h+1) D).
  * Statistics, sums and softmax are binary32; one rounding at the store (except where stated).
- * Rows, gains and the codes of a cache begin on 16 bytes, leading dimensions are multiples of 8; positions, frequencies, lengths, offsets,
- * tables and the scales of pages begin on an element.
+ * Rows, gains and the codes of a cache begin on 16 bytes, leading dimensions are multiples of 8 (of 4 in binary32); positions,
+ * frequencies, lengths, offsets, tables and the scales of pages begin on an element.
  *
  * ---- rotary frequencies (host) ----------------------------------------------------------------
  * frequencies host double[rotary_dim / 2], radians per position: f_i = base^(-2i/rotary_dim), then by `scaling`

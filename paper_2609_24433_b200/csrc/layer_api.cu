@@ -106,6 +106,7 @@ namespace {
 
 bool aligned(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 bool aligned16(const void* p) { return aligned(p, 16); }
+bool aligned_ld(int64_t ld, fq_dtype t) { return ld % (t == FQ_F32 ? 4 : 8) == 0; }          // rows begin on 16 bytes
 
 fq_status check_arch() {
     const int major = device_cc_major();
@@ -143,9 +144,9 @@ fq_status check_heads(Attention& a) {
     else if (a.max_q == 0 || a.max_q > a.q_rows) a.max_q = a.q_rows;
     return FQ_OK;
 }
-fq_status check_rows(const void* q, int64_t ldq, const void* y, int64_t ldy, int64_t width) {
+fq_status check_rows(const void* q, int64_t ldq, const void* y, int64_t ldy, int64_t width, fq_dtype t) {
     if (!q || !y || ldq < width || ldy < width) return FQ_ERR_INVALID_ARG;
-    if (!aligned16(q) || !aligned16(y) || ldq % 8 != 0 || ldy % 8 != 0) return FQ_ERR_ALIGNMENT;
+    if (!aligned16(q) || !aligned16(y) || !aligned_ld(ldq, t) || !aligned_ld(ldy, t)) return FQ_ERR_ALIGNMENT;
     return FQ_OK;
 }
 
@@ -210,7 +211,8 @@ fq_status fq_qk_norm_rope(const void* qkv, fq_dtype xt, int64_t M, int64_t ldx, 
     const int64_t width = (int64_t)(q_heads + k_heads) * head_dim;
     if (!qkv || ldx < width || (rotary_dim > 0 && (!positions || !frequencies))) return FQ_ERR_INVALID_ARG;
     if ((q_heads > 0 && (!q || ldq < (int64_t)q_heads * head_dim)) || (k_heads > 0 && (!k || ldk < (int64_t)k_heads * head_dim))) return FQ_ERR_INVALID_ARG;
-    if (!aligned16(qkv) || ldx % 8 != 0 || (q_heads > 0 && (!aligned16(q) || ldq % 8 != 0)) || (k_heads > 0 && (!aligned16(k) || ldk % 8 != 0)) ||
+    if (!aligned16(qkv) || !aligned_ld(ldx, xt) || (q_heads > 0 && (!aligned16(q) || !aligned_ld(ldq, yt))) ||
+        (k_heads > 0 && (!aligned16(k) || !aligned_ld(ldk, yt))) ||
         (q_gain && !aligned16(q_gain)) || (k_gain && !aligned16(k_gain)) || (rotary_dim > 0 && (!aligned(positions, 4) || !aligned(frequencies, 8))))
         return FQ_ERR_ALIGNMENT;
     const fq_status st = check_arch();
@@ -235,7 +237,7 @@ fq_status fq_kv8_append(const void* k, const void* v, fq_dtype xt, int64_t token
     if (tokens == 0 || batch == 0 || table_width == 0 || cache->pages == 0) return FQ_OK;
     const int64_t width = (int64_t)cache->heads * cache->head_dim;
     if (!k || !v || !kv_len || ldk < width || ldv < width) return FQ_ERR_INVALID_ARG;
-    if (!aligned16(k) || !aligned16(v) || ldk % 8 != 0 || ldv % 8 != 0) return FQ_ERR_ALIGNMENT;
+    if (!aligned16(k) || !aligned16(v) || !aligned_ld(ldk, xt) || !aligned_ld(ldv, xt)) return FQ_ERR_ALIGNMENT;
     st = check_arch();
     if (st != FQ_OK) return st;
     Kv8Append a = {};
@@ -265,7 +267,7 @@ fq_status fq_attention_kv8(const void* q, fq_dtype dt, int64_t q_rows, int64_t l
     if (!(scale >= 0.0f) || isinf(scale * 1.44269504088896341f)) return FQ_ERR_INVALID_ARG;
     if (q_rows == 0 || batch == 0) return FQ_OK;
     if (!kv_len) return FQ_ERR_INVALID_ARG;
-    st = check_rows(q, ldq, y, ldy, (int64_t)q_heads * a.head_dim);
+    st = check_rows(q, ldq, y, ldy, (int64_t)q_heads * a.head_dim, dt);
     if (st != FQ_OK) return st;
     st = check_arch();
     if (st != FQ_OK) return st;
@@ -291,10 +293,10 @@ fq_status fq_cross_attention(const void* q, fq_dtype dt, int64_t q_rows, int64_t
     if (st != FQ_OK) return st;
     if (!(scale >= 0.0f) || isinf(scale * 1.44269504088896341f)) return FQ_ERR_INVALID_ARG;
     if (q_rows == 0 || batch == 0) return FQ_OK;
-    st = check_rows(q, ldq, y, ldy, (int64_t)q_heads * head_dim);
+    st = check_rows(q, ldq, y, ldy, (int64_t)q_heads * head_dim, dt);
     if (st != FQ_OK) return st;
     if (kv_rows > 0) {
-        st = check_rows(k, ldk, v, ldv, (int64_t)kv_heads * head_dim);
+        st = check_rows(k, ldk, v, ldv, (int64_t)kv_heads * head_dim, dt);
         if (st != FQ_OK) return st;
     }
     st = check_arch();

@@ -935,3 +935,32 @@ def test_positions_frequencies_and_page_scales_begin_anywhere():
     for T, t in ((1, torch.bfloat16), (M, torch.bfloat16), (M, torch.float32)):
         q = rand((T, 2 * D), 174, t)
         assert torch.equal(*(fq.attention_kv8(q, 2, c, table, ints([M + 3])) for c in (aligned, other)))
+
+
+@gpu
+def test_binary32_rows_with_leading_dimensions_of_four():
+    """16 bytes are four binary32 channels."""
+    D, T, L = 48, 40, 300
+
+    def rows(n, width, seed):
+        t = torch.full((n, width + 4), 7.0, device="cuda")
+        t[:, :width] = rand((n, width), seed)
+        return t[:, :width]
+
+    qkv, positions, freq = rows(T, 4 * D, 181), ints(range(T)), fq.rope_frequencies(D)
+    q, k = rows(T, 2 * D, 182), rows(T, D, 183)
+    fq.qk_norm_rope(qkv, 2, 1, D, positions, freq, q=q, k=k)
+    for got, want in zip((q, k), fq.qk_norm_rope(qkv.contiguous(), 2, 1, D, positions, freq)):
+        assert torch.equal(got, want)
+    new, caches, table = rows(L, D, 184), [filled_cache(20, 1, D, 16, 185) for _ in range(2)], table_of(20, 1, 20, 186)
+    for x, c in zip((new, new.contiguous()), caches):
+        fq.kv8_append(x, x, c, table, ints([5]))
+    for a, b in zip(caches[0].tensors, caches[1].tensors):
+        assert torch.equal(a, b)
+    for n in (1, T):
+        y = rows(n, 2 * D, 187)
+        fq.attention_kv8(q[:n], 2, caches[0], table, ints([L]), y=y)
+        assert torch.equal(y, fq.attention_kv8(q[:n].contiguous(), 2, caches[0], table, ints([L])))
+        fq.cross_attention(q[:n], new, new, 2, 1, 1, y=y)
+        assert torch.equal(y, fq.cross_attention(q[:n].contiguous(), new.contiguous(), new.contiguous(), 2, 1, 1))
+        assert (y._base[:, 2 * D:] == 7).all()

@@ -145,3 +145,10 @@ def test_arrays_that_do_not_begin_on_an_element_are_refused(lib):
     for at in (4098, 4100):
         assert lib.fq_qk_norm_rope(ONE, 1, L(4), L(512), 4, 2, 64, NULL, NULL, F(1e-6), ONE, ctypes.c_void_p(at), 64, 0, F(1.0), ONE, L(256), ONE, L(128),
                                    1, NULL) == fq.ERR_ALIGNMENT
+
+
+def test_leading_dimensions_by_type(lib):
+    for bad in (dict(ldx=518, xt=0), dict(ldq=258, yt=0), dict(ldk=130, yt=0), dict(ldq=260, xt=0), dict(ldk=132, xt=0)):
+        assert rope(lib, **bad) == fq.ERR_ALIGNMENT, bad
+    assert append(lib, cache(), ldk=130, xt=0) == append(lib, cache(), ldk=132) == fq.ERR_ALIGNMENT
+    assert attend(lib, cache(), ldq=258, dt=0) == cross(lib, ldq=258, dt=0) == cross(lib, ldk=130, dt=0) == fq.ERR_ALIGNMENT
