@@ -397,6 +397,7 @@ fq_status fq_kv8_append(const void* k, const void* v, fq_dtype xt, int64_t token
  * (11 bits), their exponentials to 2^-18, sums in binary32.  binary32 queries of at most 16 rows a kv head: queries and
  * probabilities as sums of two binary16 terms (22 bits).  Either way what lies below 2^-31 of the sequence's and head's largest
  * value, seen or not, may be lost: scales of pages that are further apart than that.  max_q: no sequence has more queries (0: unknown); a hint.
+ * batch * heads may pass 65535 where a kv head has at most 16 query rows, max_q * q_heads / heads.
  * workspace device, fq_attention_kv8_workspace_bytes(..) bytes (ragged: q_offsets is given), 256-byte aligned, scratch (many
  * queries: up to 256 MiB of it hold codes as binary16, more only where one sequence's head does not fit); NULL where that is 0. */
 fq_status fq_attention_kv8(const void* q, fq_dtype dt, int64_t q_rows, int64_t ldq, int q_heads, const fq_kv8_cache* cache,
@@ -413,7 +414,7 @@ size_t fq_attention_kv8_workspace_bytes(fq_dtype dt, int64_t q_rows, int q_heads
  * all).  What masked rows hold does not matter, infinities and NaN included.  A query without a key gives zeros.
  * Rows that are seen may hold anything, and count by the formula: a score that is NaN or +infinity makes its query's head NaN, as scores
  * that are all -infinity do; one at -infinity beside others has probability 0; what is not finite in v reaches its channel.
- * No causal order.  D a multiple of 16, at most 256.  max_q, max_kv: as above (0: unknown; sequences are cut to max_kv keys).
+ * No causal order.  D a multiple of 16, at most 256; batch * kv_heads at most 65535.  max_q, max_kv: as above (0: unknown; sequences are cut to max_kv keys).
  * bf16: the probabilities, exponentials to 2^-18, are rounded to bf16 ahead of the product with v; sums in binary32. */
 fq_status fq_cross_attention(const void* q, fq_dtype dt, int64_t q_rows, int64_t ldq, int q_heads, const void* k, const void* v,
                              int64_t kv_rows, int64_t ldk, int64_t ldv, int kv_heads, int head_dim, int batch, const int32_t* q_offsets,

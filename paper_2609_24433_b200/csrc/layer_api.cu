@@ -14,8 +14,9 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Tile and chunk of a call.  Chunks are what fills the SMs where rows, heads and sequences are few.
 enum class Route { Simt, Tokens, Tiles };
+Route route_of(const Attention& a) { return a.cached && a.max_q * a.group <= 16 ? Route::Tokens : a.dt == FQ_BF16 ? Route::Tiles : Route::Simt; }
 Route plan(Attention& a) {
-    const Route route = a.cached && a.max_q * a.group <= 16 ? Route::Tokens : a.dt == FQ_BF16 ? Route::Tiles : Route::Simt;
+    const Route route = route_of(a);
     int64_t wave = 2 * 148;
     if (route == Route::Tokens) {
         a.tile_rows = a.dt == FQ_F32 || a.max_q * a.group <= 8 ? 8 : 16;     // (two terms of sixteen rows pass the registers)
@@ -55,8 +56,9 @@ size_t ml_bytes(const Attention& a, Route route) {
 constexpr size_t kWideBytes = 256ull << 20;
 size_t wide_bytes(Attention& a, Route route) {
     a.first_unit = 0;
-    a.units = a.batch * a.kv_heads;
     a.wide_keys = 0;
+    if (route == Route::Tokens) return 0;                        // (equal shares, whatever the pairs: there may be more than an int holds)
+    a.units = a.batch * a.kv_heads;
     if (route != Route::Tiles || !a.cached) return 0;
     a.wide_keys = ceil_div(a.max_kv, 128) * 128;
     const size_t unit = (size_t)a.wide_keys * a.head_dim * 4;
@@ -137,11 +139,12 @@ fq_status check_heads(Attention& a) {
     if (!valid_dtype(a.dt)) return FQ_ERR_INVALID_ARG;
     if (a.q_heads % a.kv_heads != 0) return FQ_ERR_INVALID_ARG;
     if (a.head_dim % 16 != 0 || a.head_dim > 256) return FQ_ERR_UNSUPPORTED;
-    if (a.q_rows >= kMaxRows || (int64_t)a.batch * a.kv_heads > kMaxGridYZ) return FQ_ERR_UNSUPPORTED;
+    if (a.q_rows >= kMaxRows) return FQ_ERR_UNSUPPORTED;
     if (!a.q_offsets && a.batch > 0 && a.q_rows % a.batch != 0) return FQ_ERR_INVALID_ARG;
     a.group = a.q_heads / a.kv_heads;
     if (!a.q_offsets) a.max_q = a.batch > 0 ? a.q_rows / a.batch : 0;
     else if (a.max_q == 0 || a.max_q > a.q_rows) a.max_q = a.q_rows;
+    if (route_of(a) != Route::Tokens && (int64_t)a.batch * a.kv_heads > kMaxGridYZ) return FQ_ERR_UNSUPPORTED;
     return FQ_OK;
 }
 fq_status check_rows(const void* q, int64_t ldq, const void* y, int64_t ldy, int64_t width, fq_dtype t) {

@@ -964,3 +964,19 @@ def test_binary32_rows_with_leading_dimensions_of_four():
         fq.cross_attention(q[:n], new, new, 2, 1, 1, y=y)
         assert torch.equal(y, fq.cross_attention(q[:n].contiguous(), new.contiguous(), new.contiguous(), 2, 1, 1))
         assert (y._base[:, 2 * D:] == 7).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_kv8_single_tokens_of_more_sequences_than_a_grid_has_rows(dtype):
+    B, H, D = 8200, 8, 16                               # 65600 (sequence, head) pairs
+    cache = filled_cache(300, H, D, 16, 191)
+    table = torch.randint(0, 300, (B, 2), generator=torch.Generator().manual_seed(192)).int().cuda()
+    lens = torch.randint(0, 33, (B,), generator=torch.Generator().manual_seed(193)).int().cuda()
+    q = rand((B, H * D), 194, TYPES[dtype])
+    got = fq.attention_kv8(q, H, cache, table, lens)
+    for rows in (slice(0, B // 2), slice(B // 2, B)):
+        assert torch.equal(got[rows], fq.attention_kv8(q[rows], H, cache, table[rows], lens[rows]))
+    with pytest.raises(fq.FqError) as e:                # (other kernels have a grid of them)
+        fq.attention_kv8(rand((3 * B, 8 * H * D), 195, TYPES[dtype]), 8 * H, cache, table, lens)
+    assert e.value.status == fq.ERR_UNSUPPORTED

@@ -152,3 +152,11 @@ def test_leading_dimensions_by_type(lib):
         assert rope(lib, **bad) == fq.ERR_ALIGNMENT, bad
     assert append(lib, cache(), ldk=130, xt=0) == append(lib, cache(), ldk=132) == fq.ERR_ALIGNMENT
     assert attend(lib, cache(), ldq=258, dt=0) == cross(lib, ldq=258, dt=0) == cross(lib, ldk=130, dt=0) == fq.ERR_ALIGNMENT
+
+
+def test_pairs_of_sequence_and_head_by_route(lib):
+    """Single tokens take as many as there are; the other kernels have a grid of them."""
+    c = cache(heads=8, head_dim=16)
+    assert lib.fq_attention_kv8_workspace_bytes(1, 70000, 8, ctypes.byref(c), 1000, 70000, 0, 0, 0) > 0
+    assert attend(lib, c, rows=3 * 8200, batch=8200, hq=64, ldq=1024) == fq.ERR_UNSUPPORTED
+    assert cross(lib, rows=8200, batch=8200, kv_rows=8200, hq=8, hk=8, D=16) == fq.ERR_UNSUPPORTED
