@@ -241,6 +241,7 @@ fq_status fq_kv8_append(const void* k, const void* v, fq_dtype xt, int64_t token
     const int64_t width = (int64_t)cache->heads * cache->head_dim;
     if (!k || !v || !kv_len || ldk < width || ldv < width) return FQ_ERR_INVALID_ARG;
     if (!aligned16(k) || !aligned16(v) || !aligned_ld(ldk, xt) || !aligned_ld(ldv, xt)) return FQ_ERR_ALIGNMENT;
+    if (!aligned(table, 4) || !aligned(kv_len, 4) || !aligned(offsets, 4)) return FQ_ERR_ALIGNMENT;
     st = check_arch();
     if (st != FQ_OK) return st;
     Kv8Append a = {};
@@ -272,6 +273,7 @@ fq_status fq_attention_kv8(const void* q, fq_dtype dt, int64_t q_rows, int64_t l
     if (!kv_len) return FQ_ERR_INVALID_ARG;
     st = check_rows(q, ldq, y, ldy, (int64_t)q_heads * a.head_dim, dt);
     if (st != FQ_OK) return st;
+    if (!aligned(table, 4) || !aligned(kv_len, 4) || !aligned(q_offsets, 4)) return FQ_ERR_ALIGNMENT;
     st = check_arch();
     if (st != FQ_OK) return st;
     a.q = q; a.y = y; a.ldq = ldq; a.ldy = ldy; a.kv_len = kv_len; a.scale_log2 = scale * 1.44269504088896341f; a.causal = causal != 0;
@@ -302,6 +304,7 @@ fq_status fq_cross_attention(const void* q, fq_dtype dt, int64_t q_rows, int64_t
         st = check_rows(k, ldk, v, ldv, (int64_t)kv_heads * head_dim, dt);
         if (st != FQ_OK) return st;
     }
+    if (!aligned(q_offsets, 4) || !aligned(kv_offsets, 4) || !aligned(kv_len, 4)) return FQ_ERR_ALIGNMENT;
     st = check_arch();
     if (st != FQ_OK) return st;
     a.q = q; a.y = y; a.ldq = ldq; a.ldy = ldy; a.k = k; a.v = v; a.ldk = ldk; a.ldv = ldv; a.kv_len = kv_len; a.key_mask = key_mask;

@@ -160,3 +160,13 @@ def test_pairs_of_sequence_and_head_by_route(lib):
     assert lib.fq_attention_kv8_workspace_bytes(1, 70000, 8, ctypes.byref(c), 1000, 70000, 0, 0, 0) > 0
     assert attend(lib, c, rows=3 * 8200, batch=8200, hq=64, ldq=1024) == fq.ERR_UNSUPPORTED
     assert cross(lib, rows=8200, batch=8200, kv_rows=8200, hq=8, hk=8, D=16) == fq.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("at", [4097, 4098, 4099])
+def test_lengths_offsets_and_tables_that_do_not_begin_on_an_element_are_refused(lib, at):
+    odd = ctypes.c_void_p(at)
+    for which in ("table", "lens", "offsets"):
+        assert append(lib, cache(), **{which: odd}) == attend(lib, cache(), **{which: odd}) == fq.ERR_ALIGNMENT, which
+    for arrays in ((odd, NULL, NULL), (NULL, odd, NULL), (NULL, NULL, odd)):
+        assert lib.fq_cross_attention(ONE, 1, L(4), L(256), 4, ONE, ONE, L(8), L(128), L(128), 2, 64, 2, *arrays, NULL, L(0), L(0), F(1.0), ONE, L(256),
+                                      NULL, Z(0), NULL) == fq.ERR_ALIGNMENT
