@@ -980,3 +980,64 @@ def test_attention_kv8_single_tokens_of_more_sequences_than_a_grid_has_rows(dtyp
     with pytest.raises(fq.FqError) as e:                # (other kernels have a grid of them)
         fq.attention_kv8(rand((3 * B, 8 * H * D), 195, TYPES[dtype]), 8 * H, cache, table, lens)
     assert e.value.status == fq.ERR_UNSUPPORTED
+
+
+# ------------------------------------------------------------------------------------------- offsets that nobody has checked
+def inside(t, edge):
+    """t as an inner slice of a larger tensor, with `edge` in 40 rows on either side of it: (slice, whole)."""
+    whole = torch.full((len(t) + 80, *t.shape[1:]), edge, dtype=t.dtype, device="cuda")
+    whole[40:-40] = t
+    return whole[40:-40], whole
+
+
+def edges_are(whole, edge):
+    return bool((whole[:40] == edge).all() and (whole[-40:] == edge).all())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_by_offsets_that_leave_the_rows_or_fall(dtype):
+    """They are cut to the rows that there are: what is around the rows, the pages and the scales is neither read nor written."""
+    H, D, P = 2, 32, 16
+    start = filled_cache(8, H, D, P, 201)
+    table = ints([[5, 1, 3], [0, 4, 6]])
+    x = rand((90, 2 * H * D), 202, TYPES[dtype])
+    for bad, cut in (([80, 500, 10], [80, 90, 90]), ([-30, 20, 2 ** 31 - 1], [0, 20, 90]), ([50, 40, 45], [50, 50, 50]), ([-9, -5, 3], [0, 0, 3])):
+        kv, _ = inside(x, math.nan)
+        parts = [inside(t, e) for t, e in zip(start.tensors, (77, 77, 9.0, 9.0))]
+        cache = fq.KV8Cache(*(p[0] for p in parts))
+        fq.kv8_append(kv[:, :H * D], kv[:, H * D:], cache, table, ints([3, 7]), ints(bad))
+        want = fq.KV8Cache(*(t.clone() for t in start.tensors))
+        # ([50, 40, 45]: the second sequence begins at row 40)
+        if bad == [50, 40, 45]:
+            fq.kv8_append(x[40:45, :H * D], x[40:45, H * D:], want, table[1:], ints([7]))
+        else:
+            fq.kv8_append(x[:, :H * D], x[:, H * D:], want, table, ints([3, 7]), ints(cut))
+        for (got, whole), t, e in zip(parts, want.tensors, (77, 77, 9.0, 9.0)):
+            assert torch.equal(got, t) and edges_are(whole, e)
+        if bad[0] == 80:                                # ten rows behind three that were held: the first page of sequence 0
+            changed = [p for p in range(8) if not torch.equal(cache.k[p], start.k[p]) or not torch.equal(cache.v[p], start.v[p])]
+            assert changed == [5]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hk,D,max_q", [(2, 2, 64, 1), (4, 1, 64, 3), (2, 1, 128, 0), (4, 2, 256, 0), (2, 2, 64, 0)])
+def test_attention_by_offsets_that_leave_the_rows_or_fall(Hq, Hk, D, max_q, dtype):
+    t = TYPES[dtype]
+    rows, keys = 300, 400
+    xq, xk, xv = (rand((n, h * D), 211 + i, t) for i, (n, h) in enumerate(((rows, Hq), (keys, Hk), (keys, Hk))))
+    start = filled_cache(40, Hk, D, 16, 214)
+    table = table_of(40, 2, 20, 215)
+    for bad, cut in (([-5, 130, 9000], [0, 130, 300]), ([250, 2 ** 31 - 1, 10], [250, 300, 300]), ([-8, -3, 70], [0, 0, 70])):
+        for k_bad, k_cut in (([30, 700, 10], [30, 400, 400]), ([-40, 200, 401], [0, 200, 400])):
+            (q, _), (k, _), (v, _), (y, around) = (inside(x, e) for x, e in ((xq, math.nan), (xk, math.nan), (xv, math.nan), (torch.full_like(xq, 7.0), 7.0)))
+            fq.cross_attention(q, k, v, Hq, Hk, 2, ints(bad), ints(k_bad), max_q=max_q, y=y)
+            want = fq.cross_attention(xq, xk, xv, Hq, Hk, 2, ints(cut), ints(k_cut), max_q=max_q, y=torch.full_like(xq, 7.0))
+            assert torch.equal(y, want) and edges_are(around, 7.0)
+        parts = [inside(x, e) for x, e in zip(start.tensors, (77, 77, math.nan, math.nan))]
+        y, around = inside(torch.full_like(xq, 7.0), 7.0)
+        fq.attention_kv8(q, Hq, fq.KV8Cache(*(p[0] for p in parts)), table, ints([290, 2 ** 31 - 1]), ints(bad), max_q=max_q, y=y)
+        want = fq.attention_kv8(xq, Hq, start, table, ints([290, 320]), ints(cut), max_q=max_q, y=torch.full_like(xq, 7.0))
+        assert torch.equal(y, want) and edges_are(around, 7.0)
+        assert torch.isfinite(y).all() and (y[:max(0, cut[0])] == 7).all() and (y[cut[2]:] == 7).all()
