@@ -388,7 +388,8 @@ fq_status fq_kv8_append(const void* k, const void* v, fq_dtype xt, int64_t token
  * q device [q_rows, q_heads D] of dtype dt; y likewise, same dtype.  Rows q_offsets[b] .. q_offsets[b+1] are the queries of
  * sequence b (device int32[batch + 1]; NULL: q_rows / batch each); rows that belong to none are left as they were.
  * Query head h reads kv head h / (q_heads / heads).  kv_len device int32[batch]: keys of each sequence, those of this
- * step's tokens included; cut to table_width pages and, where max_kv > 0, to max_kv (which sizes the launch and the workspace).
+ * step's tokens included; cut to table_width pages and, where max_kv > 0, to max_kv (which sizes the launch and the workspace: worth
+ * giving where tables are wider than the sequences are long, most of all with many queries, whose launches and scratch go by it).
  * causal: query i of n sees keys j <= kv_len - n + i, else all.  A query without a key gives zeros.
  * A query with a channel that is NaN or infinite gives NaN in all channels of that head where it sees a key; codes are finite, and the
  * scales of pages have to be.  No other row is touched by it.

@@ -13,18 +13,20 @@
 // or few rows) S is double-buffered instead.
 //
 // The maximum is followed lazily: O and l are rescaled only where a row's maximum has risen by more than 2^8 over the base they
-// were built with, so almost never behind the first tiles; probabilities then reach 256, which changes no relative rounding.
+// were built with, so almost never behind the first tiles; probabilities then reach 256, which changes no relative rounding.  Maxima
+// carry NaN, and a row's maximum is -inf where it sees no key and nowhere else.
 //
 // Cache: the codes come widened to binary16, exactly, by a kernel ahead (attention_widen.cu): as many row tiles read a key as there
 // are, and widening it for each of them on its way into the stages bounded the kernel (4 warps at it: 32 x 50 queries x 8 heads of
 // 256 over 866 keys 49 us, 3 x 4096 tokens x 16 heads of 128 over 6656 keys 660).  The scale of a page's keys multiplies S per 16
 // columns; that of its values multiplies the probabilities, over 2^e with e the running exponent of the largest one:
 // P = p vs 2^(7 - e) <= 2^15.  Queries: binary16 behind a power of two per row.
-// Measured: 16 x 1023 queries x 4100 states, 16 heads of 64: 470 us = 580 TFLOP/s (the exponential unit alone: 245 us); 3 x 4096 queries
-// over 6656 cached keys, 16/4 heads of 128, causal, with the widening: 487 us; 8 x 1024 queries x 4096 states, 16 heads of 128: 291 us
-// = 940 TFLOP/s over the 3.5 waves of its CTAs.  Bound by what each row tile does in turn -- scores, maximum, exponentials, hand-over --
+// Measured: 16 x 1023 queries x 4100 states, 16 heads of 64: 458 to 479 us = 575 to 600 TFLOP/s (the exponential unit alone: 245 us); 3 x 4096
+// queries over 6656 cached keys, 16/4 heads of 128, causal, with the widening: 490 to 500 us; 8 x 1024 queries x 4096 states, 16 heads of
+// 128: 298 us = 920 TFLOP/s over the 3.5 waves of its CTAs.  Bound by what each row tile does in turn -- scores, maximum, exponentials, hand-over --
 // of which a scheduler has two to overlap.
-// Rows: bf16 operands.  The scores of masked keys are replaced; their values are zeroed in shared memory, in the tiles that have
+// Rows: bf16 operands, the probabilities too, as an MMA takes one type and values of any size are no binary16: at most 2^-8 each, which puts
+// results 2.1e-3 to 2.3e-3 from those of 64 bits where bf16 outputs alone are 1.7e-3 away.  The scores of masked keys are replaced; their values are zeroed in shared memory, in the tiles that have
 // any, ahead of the product: 0 times a masked NaN would reach the sums.
 #include "act_common.cuh"
 #include "attention_common.cuh"

@@ -2,7 +2,8 @@
 //
 // Bound by the cache's bytes, so everything serves the loads: no thread waits for another on the way from memory to the
 // matrix instructions.  Each lane copies (cp.async, 16 bytes) exactly the bytes that it will multiply into slots of its own, in
-// pieces of 64 tokens x 64 channels four ahead, and waits for nothing but its own copies: no barrier until the end of a chunk.
+// pieces of 64 tokens x 64 channels four ahead, and waits for nothing but its own copies: no barrier until the end of
+// a share's part of a tile.
 //
 // The products run transposed, S^T = K Q^T and O^T = V^T P^T: the cache's operand then fills the 16 rows of a warp-level MMA
 // (m16n8k16, binary16 in, binary32 out) and the few queries its 8 columns, with no row idle at one query of a group of eight.

@@ -12,8 +12,12 @@ namespace fq {
 namespace {
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Tile and chunk of a call.  Chunks are what fills the SMs where rows, heads and sequences are few.
+// Tile and chunk of a call.  Chunks are what fills the SMs where rows, heads and sequences are few; they are planned for the row tiles of
+// the whole call, also where its widened codes take several passes (wide_bytes), each of which then has a part of them.
 enum class Route { Simt, Tokens, Tiles };
+// 16 rows are what the few-queries kernel takes in one pass over the cache.  That is not where the two are level: with as many passes as
+// it takes, at 18 / 32 / 64 / 128 rows, 16 sequences of 8192 keys, 8 heads of 128: 115 / 119 / 208 / 390 us, on tcgen05 behind the
+// widening 351 / 352 / 353 / 360; 32 of 866 keys, one head of 256: 23 / 23 / 33 / 61 and 31 / 32 / 34 / 43.
 Route route_of(const Attention& a) { return a.cached && a.max_q * a.group <= 16 ? Route::Tokens : a.dt == FQ_BF16 ? Route::Tiles : Route::Simt; }
 Route plan(Attention& a) {
     const Route route = route_of(a);
