@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) attention_tiles_kernel(const Atte
                 }
                 // ---- a new base
                 const int now_e = CACHED ? meta.e : e;
-                const bool rise = !(top <= base + kSlack);       // (a NaN, too: it becomes the base, so that all of the row is NaN)
+                const bool rise = !(top <= base + kSlack) && base == base;      // (a NaN becomes the base and stays it: all of the row is NaN)
                 if (__any_sync(0xffffffffu, rise || now_e != e)) {
                     const float now = rise ? top : base;
                     const float keep = rise ? exp2f(base - now) : 1.0f;                // (from nothing: 0)

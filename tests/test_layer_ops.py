@@ -849,6 +849,32 @@ def test_cross_attention_of_numbers_that_are_not_finite(Hq, Hk, D, T, L, B, dtyp
 
 
 @gpu
+@pytest.mark.parametrize("bad", NOT_FINITE)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,D,T,L", [(2, 64, 40, 200), (2, 64, 300, 200), (2, 128, 300, 250), (1, 256, 40, 200), (2, 64, 40, 1500), (2, 128, 300, 1500)])
+def test_attention_of_numbers_that_are_not_finite_ahead_of_keys_that_are_masked(Hq, D, T, L, dtype, bad):
+    """The last tiles of keys, and the last chunks, hold nothing that a row sees, whatever it saw ahead of them."""
+    q, k, v = (rand((n, Hq * D), 221 + i, TYPES[dtype]) for i, n in enumerate((T, L, L)))
+    mask = torch.ones(L, dtype=torch.bool, device="cuda")
+    mask[100:] = False
+    x = k.clone()
+    x[50, 7] = bad
+    want = plain_attention(q.double().view(T, Hq, D), x.double().view(L, Hq, D), v.double().view(L, Hq, D), D ** -0.5, mask[None].expand(T, -1))
+    assert_same_kind(fq.cross_attention(q, x, v, Hq, Hq, 1, key_mask=mask), want)
+    x = q.clone()
+    x[T // 2, 7] = bad
+    want = plain_attention(x.double().view(T, Hq, D), k.double().view(L, Hq, D), v.double().view(L, Hq, D), D ** -0.5, mask[None].expand(T, -1))
+    assert_same_kind(fq.cross_attention(x, k, v, Hq, Hq, 1, key_mask=mask), want)
+    cache = filled_cache(100, Hq, D, 16, 224)
+    table = table_of(100, 1, 100, 225)
+    table[0, 6:] = -1                                   # no pages behind 96 keys
+    got = fq.attention_kv8(x, Hq, cache, table, ints([L]), causal=False)
+    assert got[T // 2, :D].isnan().all() and torch.isfinite(got[T // 2, D:]).all()
+    rest = torch.arange(T, device="cuda") != T // 2
+    assert torch.equal(got[rest], fq.attention_kv8(q, Hq, cache, table, ints([L]), causal=False)[rest])
+
+
+@gpu
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("Hq,D,T,L", [(2, 64, 40, 200), (2, 64, 300, 2100), (2, 128, 300, 2100), (1, 256, 40, 2100), (2, 64, 3, 1)])
 def test_cross_attention_of_scores_that_are_all_minus_infinity(Hq, D, T, L, dtype):
