@@ -424,6 +424,77 @@ fq_status fq_cross_attention(const void* q, fq_dtype dt, int64_t q_rows, int64_t
 size_t fq_cross_attention_workspace_bytes(fq_dtype dt, int64_t q_rows, int q_heads, int64_t kv_rows, int kv_heads, int head_dim,
                                           int batch, int ragged_q, int ragged_kv, int64_t max_q, int64_t max_kv);
 
+/* ==== projections in microscaled 4-bit floating point ================================================
+ * The tensor cores of sm_100 have no 4-bit integers; the 4-bit type that they multiply is e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives) with one scale for each block of channels.  These calls are the runtime path of a projection site in that
+ * type: the transform of fq_quantize_act, codes with block scales, a product whose block scales the tensor cores apply, and the
+ * rescale + bias epilogue of Eq. 8 with binary32 accumulators.  Forward only.
+ *   FQ_MXFP4  blocks of 32 channels, scales e8m0 (2^(E-127));
+ *   FQ_NVFP4  blocks of 16 channels, scales e4m3, and a binary32 step for each row.
+ * Layout: codes [rows, K/2] bytes, row pitch K/2, the even channel in the low nibble.  Block scales in tiles of 128 rows x 4 blocks,
+ * 512 bytes each, fq_fp4_scale_bytes() in all: the byte of (row, block) is byte (row % 32) * 16 + (row % 128) / 32 * 4 + block % 4 of
+ * tile (row / 128) * ceil(blocks / 4) + block / 4, blocks = K / 32 or K / 16; places past the last row or block hold 0.  Steps float[rows].
+ * A row's value is code * scale * step.
+ * Quantiser, for a transformed row z (z = R S^-1 x in binary32 as for fq_quantize_act), each line binary32 operations rounded to nearest:
+ *   FQ_MXFP4  m = max |z| of the block, E = max(0, exponent of m - 2) with the exponent field of binary32, code = e2m1(z 2^(127-E)), step 1;
+ *   FQ_NVFP4  step d = max |z| of the row * fl(1/2688) (6 * 448; a row with d < 2^-100 is the zero token: step, scales and codes 0), i = 1/d,
+ *             S = e4m3((m i) * fl(1/6)), q = i/S (0 where S = 0), code = e2m1(z q);
+ * e2m1 and e4m3 round to nearest, ties to even, and saturate; a zero keeps its sign.
+ * K a multiple of 32, at most 32768; hadamard_block a power of two in [1, 256] dividing K; N a multiple of 8.
+ * Codes, scales, x, y and multipliers begin on 16 bytes, steps on an element; leading dimensions are multiples of 8. */
+typedef enum { FQ_MXFP4 = 0, FQ_NVFP4 = 1 } fq_fp4_format;
+typedef struct fq_fp4_weights fq_fp4_weights;
+
+/* Bytes of the block scales of `rows` rows of K channels (host; 0 for arguments that no call takes). */
+size_t fq_fp4_scale_bytes(int64_t rows, int64_t K, fq_fp4_format format);
+
+/* ---- offline ----------------------------------------------------------------------------------
+ * fq_fold_weights_fp4: as fq_fold_weights (W~ = W S R^T), rows rounded by the quantiser above.  fq_fp4_weights_import: codes, scales,
+ * steps s^W[N] (NULL: 1), multiplier g[K] (NULL: the constant block^-1/2) and bias (NULL: 0) as fq_fp4_weights_export writes them, for
+ * instance of a checkpoint that is in one of the formats already; the scales' unused places need not be 0 here.
+ * Both allocate and synchronise the stream.  A handle is read-only at run time: calls on several streams may share it. */
+fq_status fq_fold_weights_fp4(const void* W, fq_dtype wt, int64_t N, int64_t K, int64_t ldw, const float* smooth, const float* bias,
+                              int hadamard_block, fq_fp4_format format, void* stream, fq_fp4_weights** out);
+fq_status fq_fp4_weights_import(const void* codes, const void* scales, const float* w_scale, const float* mult_g, const float* bias,
+                                int64_t N, int64_t K, int hadamard_block, fq_fp4_format format, void* stream, fq_fp4_weights** out);
+/* Any destination may be NULL to skip it. */
+fq_status fq_fp4_weights_export(const fq_fp4_weights* w, void* codes, void* scales, float* w_scale, float* mult_g, float* bias, void* stream);
+fq_status fq_fp4_weights_info(const fq_fp4_weights* w, int64_t* N, int64_t* K, int* hadamard_block, fq_fp4_format* format);
+const float* fq_fp4_weights_multiplier(const fq_fp4_weights* w);     /* device, valid until destroy */
+fq_status fq_fp4_weights_destroy(fq_fp4_weights* w);                 /* NULL is accepted */
+
+/* ---- run time ---------------------------------------------------------------------------------
+ * fq_quantize_act_fp4: x device [M, K] of dtype xt; mult_g device float[K] or NULL (the constant block^-1/2).
+ * fq_gemm_fp4: y[t][j] = (sum of code products with their block scales) * (a_delta[t] s^W_j) + b_j; codes, scales and steps as
+ *   fq_quantize_act_fp4 writes them for the handle's K and format.  Scales past the last row are not read into any output; those past
+ *   the last block have to be 0.  No workspace.  One set of codes serves several handles of a site.
+ * fq_linear_fp4: both; codes, scales and steps live in the workspace, 256-byte aligned, fq_linear_fp4_workspace_bytes() bytes, scratch. */
+fq_status fq_quantize_act_fp4(const void* x, fq_dtype xt, int64_t M, int64_t K, int64_t ldx, const float* mult_g, int hadamard_block,
+                              fq_fp4_format format, void* codes_out, void* scales_out, float* delta_out, void* stream);
+fq_status fq_gemm_fp4(const void* a_codes, const void* a_scales, const float* a_delta, int64_t M, const fq_fp4_weights* W, void* y,
+                      fq_dtype yt, int64_t ldy, void* stream);
+fq_status fq_linear_fp4(const void* x, fq_dtype xt, int64_t M, int64_t ldx, const fq_fp4_weights* W, void* y, fq_dtype yt, int64_t ldy,
+                        void* workspace, size_t ws_bytes, void* stream);
+size_t fq_linear_fp4_workspace_bytes(int64_t M, int64_t K, fq_fp4_format format);
+
+/* ==== RMS norm with the residual's addition, ending in codes =============================================
+ * What stands ahead of a layer's qkv and gate/up sites, in one pass: the residual stream h = x + residual (rounded to xt, written),
+ * its RMS norm, the site's transform and its quantiser.  With rms = sqrt(mean(h^2) + eps) the site's input is h / rms; the quantiser is
+ * positively homogeneous (Prop. 2), so the codes (and block scales) are those of h, and the division goes into the step:
+ *   bits 8 or 4: as fq_quantize_act of h, but for its step d, which is (clip_ratio * max |z|) * fl(1/q) here (a product in place of the
+ *     quotient: one unit in the last place at most); codes round(z * (1/d)), delta = d / rms, both 0 where d < 2^-126;
+ *   fp4: codes and scales of fq_quantize_act_fp4 of h, delta = its step / rms  (FQ_MXFP4: 1 / rms).
+ * A learned gain belongs into mult_g (gain_c * (1/s_c) * block^-1/2, see fq_weights_set_multiplier); NULL: the constant block^-1/2.
+ * residual device [M, K] of dtype xt, leading dimension ldr, or NULL: the stream is x as it is, and h has to be NULL.  Otherwise h
+ * device [M, K] of dtype xt; it may be the very memory of x or of residual (same address and leading dimension), else nothing may
+ * overlap.  eps >= 0.  The sum of squares is binary32 (binary64 where that overflows or vanishes). */
+fq_status fq_rmsnorm_quantize_act(const void* x, const void* residual, fq_dtype xt, int64_t M, int64_t K, int64_t ldx, int64_t ldr,
+                                  float eps, void* h, int64_t ldh, const float* mult_g, int hadamard_block, int bits, float clip_ratio,
+                                  void* codes_out, float* delta_out, void* stream);
+fq_status fq_rmsnorm_quantize_act_fp4(const void* x, const void* residual, fq_dtype xt, int64_t M, int64_t K, int64_t ldx, int64_t ldr,
+                                      float eps, void* h, int64_t ldh, const float* mult_g, int hadamard_block, fq_fp4_format format,
+                                      void* codes_out, void* scales_out, float* delta_out, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

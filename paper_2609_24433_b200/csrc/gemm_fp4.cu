@@ -1,0 +1,456 @@
+// Product of e2m1 codes with block scales on the 5th-generation tensor cores (sm_100a):
+//   acc[j][t] = sum_b Sw[j][b] Sa[t][b] sum_{c in b} qW[j][c] qA[t][c]   tcgen05.mma with block scales, binary32 in TMEM
+//   y[t][j]   = (delta_t s^W_j) acc + b_j
+//
+// Orientation as in the integer product: the MMA's 128 rows are output channels, its columns (16..256) tokens, so one kernel
+// takes a single token as well as a long batch, and at few tokens the weights go from HBM straight into the tensor cores, with
+// nothing to unpack.
+//
+// Operands: 256 channels a stage.  Codes arrive by TMA, two to a byte, K-major rows of 128 bytes with the 128-byte swizzle; an MMA
+// takes 64 channels (32 bytes).  Block scales arrive as whole tiles of 512 bytes (128 rows x 4 blocks: the order in which
+// tcgen05.cp spreads them over TMEM, one lane a row of 32, four columns a tile) and are copied to TMEM by the issuing thread
+// ahead of the stage's MMAs.  Their TMEM columns go by the stage, so that whoever refills a stage knows that the MMAs that
+// read them have ended.
+//
+// Roles: warp 0 TMA producer, warp 1 MMA issuer and TMEM allocator, warps 2-9 epilogue.
+// CTAS = 2: a pair works on 256 channels, each CTA loading its 128 weight rows and half of the tokens' codes, but the scales of
+// all tokens.  SPLIT: the CTAs (or pairs) of a cluster share one tile along K and exchange binary32 sums through the cluster's
+// shared memory, added in the order of the slices: the result does not depend on timing.
+// Every wait on a barrier is bounded (see ptx_sm100.cuh).
+#include <cuda_bf16.h>
+
+#include "act_common.cuh"
+#include "fp4_common.cuh"
+#include "ptx_sm100.cuh"
+#include "tc_sm100.cuh"
+
+namespace fq {
+namespace {
+
+constexpr int kThreads = 320;
+constexpr int kEpi = 8;                  // epilogue warps
+constexpr int kRows = 128;               // channels of a CTA's tile
+constexpr int kStageK = 256;             // channels of K a stage
+constexpr int kMostStages = 8;
+constexpr int kScaleCols = 256;          // TMEM columns from here on hold scales, those before accumulators
+constexpr size_t kSmemMost = 226 * 1024;
+
+struct GemmParams {
+    int64_t M, N, ldy;
+    int K, bt, stages, m_tiles, n_tiles, band;
+    int split;                           // slices of K, each CTA (pair) of a cluster one
+    int kb;                              // stages of all of K
+    int xa;                              // scale tiles across a tile's tokens
+    int units, unit_step;
+    const float* delta;
+    const float* w_scale;
+    const float* bias;
+    void* y;
+    int bf16;
+    uint32_t* watchdog;
+};
+
+enum : uint32_t { kWdProducer = 1u, kWdMmaFull = 2u, kWdMmaAcc = 4u, kWdEpilogue = 8u };
+
+template <int CTAS>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
+    if (CTAS == 1) {
+        tma_load_2d(dst, map, c0, c1, bar);
+    } else {                             // counted on the barrier of the pair's even CTA
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar & 0xFEFFFFFFu)
+            : "memory");
+    }
+}
+template <int CTAS>
+__device__ __forceinline__ void tma_load_tiles(uint32_t dst, const CUtensorMap* map, int tile, int rows, uint32_t bar) {
+    if (CTAS == 1)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(tile), "r"(rows), "r"(bar)
+            : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+            ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(tile), "r"(rows), "r"(bar & 0xFEFFFFFFu)
+            : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cta(uint32_t bar, uint32_t rank) {
+    asm volatile(
+        "{\n\t.reg .b32 ra;\n\t"
+        "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
+        "mbarrier.arrive.shared::cluster.b64 _, [ra];\n\t}"
+        ::"r"(bar), "r"(rank)
+        : "memory");
+}
+// 512 bytes of scales (32 rows of 16 bytes, 8-row groups 128 bytes apart) to four TMEM columns of all four lane quadrants.
+template <int CTAS>
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t smem) {
+    const uint64_t desc = (uint64_t)((smem & 0x3FFFFu) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+    if (CTAS == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+template <int CTAS, bool NV>
+__device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+#define FQ_MMA_FP4(CG, KIND)                                                                             \
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                        \
+                 "tcgen05.mma.cta_group::" CG "." KIND " [%0], %1, %2, %3, [%4], [%5], p;\n\t}"           \
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory")
+    if (CTAS == 1 && NV) FQ_MMA_FP4("1", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+    else if (CTAS == 1) FQ_MMA_FP4("1", "kind::mxf4.block_scale.scale_vec::2X");
+    else if (NV) FQ_MMA_FP4("2", "kind::mxf4nvf4.block_scale.scale_vec::4X");
+    else FQ_MMA_FP4("2", "kind::mxf4.block_scale.scale_vec::2X");
+#undef FQ_MMA_FP4
+}
+template <int CTAS>
+__device__ __forceinline__ void commit(uint32_t bar, uint16_t mask) {
+    if (CTAS == 1) mma_commit(bar);
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(mask)
+                     : "memory");
+}
+// Instruction descriptor: e2m1 x e2m1, both K-major, scales e4m3 or e8m0, M = m, N = n.
+__device__ __forceinline__ uint32_t instr_desc_fp4(int m, int n, bool nv) {
+    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((nv ? 0u : 1u) << 23) | ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(taddr)
+                 : "memory");
+}
+__device__ __forceinline__ void st_cluster_v4(uint32_t addr, const uint32_t* r) {
+    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+
+template <int CTAS, bool NV, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 1)
+gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_x,
+                const __grid_constant__ CUtensorMap map_xs, const GemmParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t s_full[kMostStages], s_empty[kMostStages], s_acc_full[2], s_acc_empty[2];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort;
+    constexpr int kTiles = NV ? 4 : 2;                       // scale tiles of a stage's 256 channels
+    constexpr uint32_t kWBytes = kRows * 128, kWScale = kTiles * 512;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int* abort_flag = &s_abort;
+    const uint32_t rank = CTAS == 2 || SPLIT ? cluster_ctarank() : 0u;
+    const uint32_t half = CTAS == 2 ? rank & 1u : 0u, pair_base = rank & ~1u;
+    const bool leader = half == 0;
+    const int slice = SPLIT ? (int)(rank / CTAS) : 0;
+    const int bt_cta = p.bt / CTAS;
+    const uint32_t x_bytes = (uint32_t)bt_cta * 128u, x_scale = (uint32_t)p.xa * kWScale;
+    const uint32_t stage_bytes = kWBytes + x_bytes + kWScale + x_scale;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    // [weight codes][token codes] of all stages (1024-byte aligned), then their scales
+    const uint32_t s_w = base, s_x = s_w + (uint32_t)p.stages * kWBytes, s_ws = s_x + (uint32_t)p.stages * x_bytes, s_xs = s_ws + (uint32_t)p.stages * kWScale;
+
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        for (int s = 0; s < p.stages; ++s) {
+            mbar_init(smem_u32(&s_full[s]), 1);
+            mbar_init(smem_u32(&s_empty[s]), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(smem_u32(&s_acc_full[a]), 1);
+            mbar_init(smem_u32(&s_acc_empty[a]), kEpi * CTAS);
+        }
+        fence_mbarrier_init();
+        fence_proxy_async_smem();
+    }
+    if (warp == 1) tmem_alloc<CTAS>(smem_u32(&s_tmem), 512u);
+    tc_fence_before();
+    __syncthreads();
+    if (CTAS == 2 || SPLIT) cluster_sync_all();              // the other CTAs' barriers exist
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    if (warp >= 2) griddep_wait();                           // (the producer waits ahead of the tokens' first copy)
+    griddep_launch_dependents();
+
+    const int accs = p.bt <= 128 ? 2 : 1, acc_cols = kScaleCols / accs;
+    const int slot_cols = kTiles * 4 * (1 + p.xa);           // TMEM columns of a stage's scales
+    const int cluster = SPLIT ? p.split * CTAS : CTAS;
+    const int unit0 = (int)blockIdx.x / cluster;
+    const int kb0 = SPLIT ? p.kb * slice / p.split : 0, kb1 = SPLIT ? p.kb * (slice + 1) / p.split : p.kb;
+    // token tiles in bands, within a band channel tile by channel tile: what runs at a time covers a block of the output
+    auto tile_of = [&](int unit, int* m, int* n) {
+        const int b = unit / (p.band * p.n_tiles), r = unit - b * (p.band * p.n_tiles), rows = min(p.band, p.m_tiles - b * p.band);
+        *m = b * p.band + r % rows;
+        *n = r / rows;
+    };
+    auto columns = [&](int m) {                              // tokens of a tile, rounded up to what an MMA takes
+        const int64_t left = p.M - (int64_t)m * p.bt;
+        return left >= p.bt ? p.bt : ((int)left + 16 * CTAS - 1) / (16 * CTAS) * (16 * CTAS);
+    };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ producer
+        bool ok = true;
+        int stage = 0;
+        uint32_t phase = 0;
+        // a weight handle is complete before the call: its first stages come while the kernel ahead still runs
+        int ahead = 0;
+        auto weights = [&](int n, int kb, int s) {
+            const uint32_t bar = smem_u32(&s_full[s]);
+            if (leader) mbar_arrive_expect_tx(bar, stage_bytes * CTAS);
+            tma_load<CTAS>(s_w + s * kWBytes, &map_w, kb * 128, (n * CTAS + (int)half) * kRows, bar);
+            tma_load_tiles<CTAS>(s_ws + s * kWScale, &map_ws, kb * kTiles, n * CTAS + (int)half, bar);
+        };
+        if (unit0 < p.units) {
+            int m, n;
+            tile_of(unit0, &m, &n);
+            ahead = min(p.stages, kb1 - kb0);
+            if (elect_one())
+                for (int i = 0; i < ahead; ++i) weights(n, kb0 + i, i);
+            __syncwarp();
+        }
+        griddep_wait();
+        for (int unit = unit0; unit < p.units && ok; unit += p.unit_step) {
+            int m, n;
+            tile_of(unit, &m, &n);
+            const int t0 = m * p.bt + (int)half * (columns(m) / CTAS);
+            for (int kb = kb0; kb < kb1; ++kb) {
+                ok = mbar_wait_all_lazy(smem_u32(&s_empty[stage]), phase ^ 1u, abort_flag, p.watchdog, kWdProducer);
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t bar = smem_u32(&s_full[stage]);
+                    if (ahead == 0) weights(n, kb, stage);
+                    tma_load<CTAS>(s_x + stage * x_bytes, &map_x, kb * 128, t0, bar);
+                    tma_load_tiles<CTAS>(s_xs + stage * x_scale, &map_xs, kb * kTiles, m * (p.bt / 128), bar);
+                }
+                __syncwarp();
+                if (ahead > 0) --ahead;
+                if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+            }
+        }
+        if (!ok && lane == 0) drain_after_abort();
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ MMA issuer
+        if (leader) {
+            bool ok = true;
+            int stage = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            const uint16_t mask = (uint16_t)(3u << pair_base);
+            for (int unit = unit0; unit < p.units && ok; unit += p.unit_step) {
+                int m, n;
+                tile_of(unit, &m, &n);
+                const uint32_t idesc0 = instr_desc_fp4(kRows * CTAS, columns(m), NV);
+                ok = mbar_wait_all(smem_u32(&s_acc_empty[acc]), acc_phase ^ 1u, abort_flag, p.watchdog, kWdMmaAcc);
+                if (!ok) break;
+                const uint32_t d = tmem + (uint32_t)(acc * acc_cols);
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    ok = mbar_wait_all(smem_u32(&s_full[stage]), phase, abort_flag, p.watchdog, kWdMmaFull);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t wcol = tmem + kScaleCols + (uint32_t)(stage * slot_cols), xcol = wcol + kTiles * 4;
+                        // (what lies past K's last scale tile is never multiplied: zeros times whatever a scale holds)
+                        const int steps = min(4, (p.K - kb * kStageK + 63) / 64);
+#pragma unroll
+                        for (int a = 0; a < kTiles; ++a) {
+                            copy_scales<CTAS>(wcol + a * 4, s_ws + stage * kWScale + a * 512);
+                            for (int x = 0; x < p.xa; ++x)
+                                copy_scales<CTAS>(xcol + (a * p.xa + x) * 4, s_xs + stage * x_scale + (x * kTiles + a) * 512);
+                        }
+                        const uint64_t wd = smem_desc_sw128(s_w + stage * kWBytes), xd = smem_desc_sw128(s_x + stage * x_bytes);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (j < steps) {
+                                const int a = NV ? j : j / 2;
+                                const uint32_t id = NV ? 0u : (uint32_t)(j & 1) * 2u;         // which two of a tile's four blocks
+                                mma_fp4<CTAS, NV>(d, wd + 2 * j, xd + 2 * j, idesc0 | id << 29 | id << 4, wcol + a * 4, xcol + a * p.xa * 4, kb != kb0 || j != 0);
+                            }
+                        }
+                        commit<CTAS>(smem_u32(&s_empty[stage]), mask);
+                        if (kb == kb1 - 1) commit<CTAS>(smem_u32(&s_acc_full[acc]), mask);
+                    }
+                    __syncwarp();
+                    if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+                }
+                if (++acc == accs) { acc = 0; acc_phase ^= 1u; }
+            }
+        }
+    }
+    // ------------------------------------------------------------ epilogue
+    const int quad = warp & 3, set = (warp - 2) >> 2;
+    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+    auto store = [&](int64_t t, int64_t j, float v) {
+        if (p.bf16) static_cast<__nv_bfloat16*>(p.y)[t * p.ldy + j] = __float2bfloat16_rn(v);
+        else static_cast<float*>(p.y)[t * p.ldy + j] = v;
+    };
+    bool ok = true;
+    if (warp >= 2) {
+        int acc = 0;
+        uint32_t phase = 0;
+        for (int unit = unit0; unit < p.units; unit += p.unit_step) {
+            int m, n;
+            tile_of(unit, &m, &n);
+            const int64_t j = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32 + lane, t0 = (int64_t)m * p.bt;
+            const bool j_ok = j < p.N;
+            const float sw = j_ok ? __ldg(p.w_scale + j) : 0.0f, bj = j_ok ? __ldg(p.bias + j) : 0.0f;
+            ok = mbar_wait_warp_relaxed(smem_u32(&s_acc_full[acc]), phase, abort_flag, p.watchdog, kWdEpilogue);
+            if (!ok) break;
+            tc_fence_after();
+            // (SPLIT: one tile a cluster, finished below)
+            for (int c = SPLIT ? p.bt : set * 16; c < p.bt && t0 + c < p.M; c += 32) {
+                uint32_t r[16];
+                tmem_ld16(tmem + lanes + (uint32_t)(acc * acc_cols + c), r);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (t0 + c + i < p.M && j_ok) store(t0 + c + i, j, fmaf(__uint_as_float(r[i]), ld_global_f32(p.delta + t0 + c + i) * sw, bj));
+            }
+            if (SPLIT) break;
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (CTAS == 1) mbar_arrive(smem_u32(&s_acc_empty[acc]));
+                else mbar_arrive_cta(smem_u32(&s_acc_empty[acc]), pair_base);
+            }
+            if (++acc == accs) { acc = 0; phase ^= 1u; }
+        }
+    }
+    if (SPLIT) {
+        // Four tokens at a time are finished by slice (chunk % split): the others store their sums into its shared memory,
+        // [sender][chunk / split][channel][4 tokens], where the stages were -- behind a barrier, all MMAs of the cluster have ended.
+        int m, n;
+        tile_of(unit0, &m, &n);
+        const int64_t j = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32 + lane, t0 = (int64_t)m * p.bt;
+        const int chunks = columns(m) / 4, per = (chunks + p.split - 1) / p.split, channel = quad * 32 + lane;
+        __syncwarp();
+        cluster_sync_all();
+        if (warp >= 2 && ok) {
+            for (int c = set; c < chunks; c += 2) {
+                const int owner = c % p.split;
+                if (owner == slice) continue;
+                uint32_t r[4];
+                tmem_ld4(tmem + lanes + (uint32_t)(c * 4), r);
+                tmem_ld_wait();
+                st_cluster_v4(cluster_address(base + (uint32_t)(((slice * per + c / p.split) * kRows + channel) * 16), (uint32_t)(owner * CTAS) + half), r);
+            }
+        }
+        __syncwarp();
+        cluster_sync_all();
+        if (warp >= 2 && ok) {
+            const bool j_ok = j < p.N;
+            const float sw = j_ok ? __ldg(p.w_scale + j) : 0.0f, bj = j_ok ? __ldg(p.bias + j) : 0.0f;
+            for (int c = set; c < chunks; c += 2) {
+                if (c % p.split != slice || t0 + c * 4 >= p.M) continue;
+                uint32_t r[4];
+                tmem_ld4(tmem + lanes + (uint32_t)(c * 4), r);
+                tmem_ld_wait();
+                float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                for (int q = 0; q < p.split; ++q) {
+                    uint4 o = make_uint4(r[0], r[1], r[2], r[3]);
+                    if (q != slice) o = lds128(base + (uint32_t)(((q * per + c / p.split) * kRows + channel) * 16));
+                    s[0] += __uint_as_float(o.x); s[1] += __uint_as_float(o.y); s[2] += __uint_as_float(o.z); s[3] += __uint_as_float(o.w);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (t0 + c * 4 + i < p.M && j_ok) store(t0 + c * 4 + i, j, fmaf(s[i], ld_global_f32(p.delta + t0 + c * 4 + i) * sw, bj));
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (CTAS == 2) cluster_sync_all();                       // neither leaves while the other may still signal it
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc<CTAS>(tmem, 512u);
+    }
+}
+
+// ---- host ----------------------------------------------------------------------------------------
+bool code_map(CUtensorMap* map, const uint8_t* codes, int64_t rows, int64_t K, int box_rows) {
+    const uint64_t dims[2] = {(uint64_t)K / 2, (uint64_t)rows}, strides[1] = {(uint64_t)K / 2};
+    const uint32_t box[2] = {128, (uint32_t)box_rows};
+    return encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, codes, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+bool scale_map(CUtensorMap* map, const uint8_t* scales, int64_t rows, int64_t K, fq_fp4_format f, int box_rows) {
+    const int64_t tiles = fp4_scale_tiles(K, f);
+    const uint64_t dims[3] = {128, (uint64_t)tiles, (uint64_t)((rows + 127) / 128)}, strides[2] = {512, (uint64_t)tiles * 512};
+    const uint32_t box[3] = {128, f == FQ_NVFP4 ? 4u : 2u, (uint32_t)box_rows};
+    return encode_tiled(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, scales, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
+struct Plan {
+    int ctas, bt, split;
+};
+Plan plan(int64_t M, int64_t N, int64_t K) {
+    Plan r = {1, 0, 1};
+    const int sms = device_sm_count();
+    r.bt = M <= 256 ? (int)((M + 15) / 16 * 16) : 256;
+    const int64_t pairs = (N + 255) / 256 * ((M + 255) / 256);
+    if (M > 128 && pairs * 2 >= sms / 2) {
+        r.ctas = 2;
+        r.bt = M <= 256 ? (int)((M + 31) / 32 * 32) : 256;
+    }
+    const int64_t tiles = (N + 128 * r.ctas - 1) / (128 * r.ctas) * ((M + r.bt - 1) / r.bt);
+    const int64_t kb = (K + kStageK - 1) / kStageK;
+    while (r.split * r.ctas < 8 && tiles * r.ctas * r.split * 2 <= sms && kb >= r.split * 4) r.split *= 2;
+    return r;
+}
+
+template <int CTAS, bool NV, bool SPLIT>
+cudaError_t launch(const CUtensorMap& w, const CUtensorMap& ws, const CUtensorMap& x, const CUtensorMap& xs, const GemmParams& p, int grid, size_t smem,
+                   cudaStream_t stream) {
+    auto kern = gemm_fp4_kernel<CTAS, NV, SPLIT>;
+    const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, (unsigned)(CTAS * p.split), w, ws, x, xs, p);
+}
+template <int CTAS>
+cudaError_t launch(bool nv, bool split, const CUtensorMap& w, const CUtensorMap& ws, const CUtensorMap& x, const CUtensorMap& xs, const GemmParams& p, int grid,
+                   size_t smem, cudaStream_t stream) {
+    if (nv) return split ? launch<CTAS, true, true>(w, ws, x, xs, p, grid, smem, stream) : launch<CTAS, true, false>(w, ws, x, xs, p, grid, smem, stream);
+    return split ? launch<CTAS, false, true>(w, ws, x, xs, p, grid, smem, stream) : launch<CTAS, false, false>(w, ws, x, xs, p, grid, smem, stream);
+}
+
+}  // namespace
+
+bool fp4_weight_maps(Fp4Weights& W) {
+    return W.N == 0 || (code_map(&W.map_codes, W.codes, W.N, W.K, kRows) && scale_map(&W.map_scales, W.scales, W.N, W.K, W.format, 1));
+}
+
+fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const float* delta, int64_t M, const Fp4Weights& W, void* y,
+                          fq_dtype yt, int64_t ldy, cudaStream_t stream) {
+    if (M == 0 || W.N == 0) return FQ_OK;
+    const int sms = device_sm_count();
+    const Plan r = plan(M, W.N, W.K);
+    const bool nv = W.format == FQ_NVFP4;
+    GemmParams p = {};
+    p.M = M; p.N = W.N; p.K = (int)W.K; p.ldy = ldy;
+    p.bt = r.bt;
+    p.split = r.split;
+    p.kb = (int)((W.K + kStageK - 1) / kStageK);
+    p.xa = (r.bt + 127) / 128;
+    p.m_tiles = (int)((M + r.bt - 1) / r.bt);
+    p.n_tiles = (int)((W.N + kRows * r.ctas - 1) / (kRows * r.ctas));
+    p.band = p.m_tiles >= 16 ? 8 : p.m_tiles;
+    p.units = p.m_tiles * p.n_tiles;
+    p.delta = delta; p.w_scale = W.w_scale; p.bias = W.bias;
+    p.y = y; p.bf16 = yt == FQ_BF16;
+    p.watchdog = watchdog_device_ptr();
+    if (!p.watchdog) return FQ_ERR_CUDA;
+    const int tiles = nv ? 4 : 2;
+    const size_t stage = (size_t)kRows * 128 + (size_t)(r.bt / r.ctas) * 128 + (size_t)tiles * 512 * (1 + p.xa);
+    const int slots = 256 / (tiles * 4 * (1 + p.xa));        // TMEM columns for scales
+    p.stages = (int)((kSmemMost - 1024) / stage);
+    if (p.stages > kMostStages) p.stages = kMostStages;
+    if (p.stages > slots) p.stages = slots;
+    size_t smem = 1024 + stage * (size_t)p.stages;
+    CUtensorMap x, xs;
+    if (!code_map(&x, codes, M, W.K, r.bt / r.ctas) || !scale_map(&xs, scales, M, W.K, W.format, p.xa)) return FQ_ERR_CUDA;
+    const int units = r.split > 1 ? p.units : (p.units < sms / r.ctas ? p.units : sms / r.ctas);
+    p.unit_step = units;
+    const int grid = units * r.ctas * r.split;
+    const cudaError_t e = r.ctas == 2 ? launch<2>(nv, r.split > 1, W.map_codes, W.map_scales, x, xs, p, grid, smem, stream)
+                                      : launch<1>(nv, r.split > 1, W.map_codes, W.map_scales, x, xs, p, grid, smem, stream);
+    return e == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
+}
+
+}  // namespace fq

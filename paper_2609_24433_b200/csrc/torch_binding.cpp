@@ -529,10 +529,200 @@ PyObject* cross_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- projections in microscaled 4-bit floating point, norms that end in codes ----
+// A contiguous tensor of `bytes` bytes or float elements: the caller's, or a new one of `size`.
+struct FlatOut {
+    at::Tensor t;
+    FlatOut(PyObject* given, at::ScalarType type, int64_t count, const char* what) {
+        if (none(given)) return;
+        t = on_device(tensor(given), what);
+        if (t.scalar_type() != type || !t.is_contiguous() || t.numel() != count) {
+            PyErr_Format(PyExc_ValueError, "%s has to be a contiguous %s tensor of %lld elements", what, at::toString(type), (long long)count);
+            throw Refused();
+        }
+    }
+    void make(at::IntArrayRef size, at::ScalarType type, const at::Tensor& like) {
+        if (!t.defined()) t = fresh(size, type, like);
+    }
+    template <typename T = void>
+    T* data() { return static_cast<T*>(t.data_ptr()); }
+};
+PyObject* tuple_of(std::initializer_list<at::Tensor> list) {
+    PyObject* r = PyTuple_New((Py_ssize_t)list.size());
+    if (!r) return nullptr;
+    Py_ssize_t i = 0;
+    for (const at::Tensor& t : list) PyTuple_SET_ITEM(r, i++, THPVariable_Wrap(t));
+    return r;
+}
+fq_fp4_format format_of(long long f) { return f == FQ_MXFP4 || f == FQ_NVFP4 ? static_cast<fq_fp4_format>(f) : static_cast<fq_fp4_format>(7); }
+bool known(fq_fp4_format f) { return f == FQ_MXFP4 || f == FQ_NVFP4; }
+
+// quantize_act_fp4(x, multiplier address, block, format, codes, scales, delta) -> (codes, scales, delta)
+PyObject* quantize_act_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 7);
+        const at::Tensor& x = on_device(rowmajor(a[0]), "x");
+        const float* g = static_cast<const float*>(address(a[1]));
+        const int64_t M = x.size(0), K = x.size(1);
+        const long long block = integer(a[2]);
+        const fq_fp4_format f = format_of(integer(a[3]));
+        const fq_dtype xt = dtype_of(x.scalar_type());
+        if (!known(f)) return status(FQ_ERR_INVALID_ARG);
+        const int64_t sb = (int64_t)fq_fp4_scale_bytes(M, K, f);
+        FlatOut codes(a[4], at::kByte, M * (K / 2), "codes"), scales(a[5], at::kByte, sb, "scales"), delta(a[6], at::kFloat, M, "delta");
+        fq_status s;
+        {
+            const Unlocked nogil;
+            codes.make({M, K / 2}, at::kByte, x);
+            scales.make({sb}, at::kByte, x);
+            delta.make({M}, at::kFloat, x);
+            s = fq_quantize_act_fp4(x.data_ptr(), xt, M, K, pitch(x), g, block == (int)block ? (int)block : 0, f, codes.data(), scales.data(),
+                                    delta.data<float>(), stream());
+        }
+        return s == FQ_OK ? tuple_of({codes.t, scales.t, delta.t}) : status(s);
+    });
+}
+
+// gemm_fp4(codes, scales, delta, handle, K, N, format, out_dtype, y)
+PyObject* gemm_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 9);
+        const fq_fp4_weights* W = static_cast<const fq_fp4_weights*>(address(a[3]));
+        const int64_t K = integer(a[4]), N = integer(a[5]);
+        const fq_fp4_format f = format_of(integer(a[6]));
+        const at::Tensor& codes = rows_of(a[0], K / 2, "codes");
+        const int64_t M = codes.size(0);
+        if (codes.scalar_type() != at::kByte || !codes.is_contiguous()) {
+            PyErr_SetString(PyExc_ValueError, "codes have to be contiguous uint8");
+            throw Refused();
+        }
+        const at::Tensor& scales = vector_of(a[1], at::kByte, (int64_t)fq_fp4_scale_bytes(M, K, f), "scales");
+        const at::Tensor& delta = vector_of(a[2], at::kFloat, M, "delta");
+        Output type(a[8], a[7]);
+        RowsOut y(a[8], M, N, type.type, "y");
+        fq_status s;
+        {
+            const Unlocked nogil;
+            y.make(M, N, type.type, codes);
+            s = fq_gemm_fp4(codes.data_ptr(), scales.data_ptr(), static_cast<const float*>(delta.data_ptr()), M, W, y.t.data_ptr(), type.dt, pitch(y.t),
+                            stream());
+        }
+        return s == FQ_OK ? THPVariable_Wrap(std::move(y.t)) : status(s);
+    });
+}
+
+// linear_fp4(x, handle, K, N, format, out_dtype, y, workspace)
+PyObject* linear_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 8);
+        const fq_fp4_weights* W = static_cast<const fq_fp4_weights*>(address(a[1]));
+        const int64_t K = integer(a[2]), N = integer(a[3]);
+        const fq_fp4_format f = format_of(integer(a[4]));
+        const at::Tensor& x = rows_of(a[0], K, "x");
+        const int64_t M = x.size(0);
+        const fq_dtype xt = dtype_of(x.scalar_type());
+        Output type(a[6], a[5]);
+        RowsOut y(a[6], M, N, type.type, "y");
+        if (!none(a[7])) {
+            const at::Tensor& t = on_device(tensor(a[7]), "workspace");
+            if (t.scalar_type() != at::kByte || !t.is_contiguous()) {
+                PyErr_SetString(PyExc_ValueError, "workspace has to be contiguous uint8");
+                throw Refused();
+            }
+        }
+        Workspace ws(a[7]);
+        fq_status s;
+        {
+            const Unlocked nogil;
+            y.make(M, N, type.type, x);
+            ws.make([&] { return fq_linear_fp4_workspace_bytes(M, K, f); }, x);
+            s = fq_linear_fp4(x.data_ptr(), xt, M, pitch(x), W, y.t.data_ptr(), type.dt, pitch(y.t), ws.p, ws.bytes, stream());
+        }
+        return s == FQ_OK ? THPVariable_Wrap(std::move(y.t)) : status(s);
+    });
+}
+
+// What the two norms share: x, residual and the stream that they add up to.
+struct NormRows {
+    const at::Tensor& x;
+    const at::Tensor* residual;
+    int64_t M, K;
+    fq_dtype xt;
+    RowsOut h;
+    NormRows(PyObject* xo, PyObject* ro, PyObject* ho)
+        : x(on_device(rowmajor(xo), "x")), residual(none(ro) ? nullptr : &rows_of(ro, x.size(1), "residual")), M(x.size(0)), K(x.size(1)),
+          xt(dtype_of(x.scalar_type())), h(ho, x.size(0), x.size(1), x.scalar_type(), "h") {
+        if (residual && (residual->size(0) != M || residual->scalar_type() != x.scalar_type())) {
+            PyErr_SetString(PyExc_ValueError, "x and residual have to have the same rows and dtype");
+            throw Refused();
+        }
+        if (!residual && h.t.defined()) {
+            PyErr_SetString(PyExc_ValueError, "h is written where there is a residual");
+            throw Refused();
+        }
+    }
+    void make() { if (residual) h.make(M, K, x.scalar_type(), x); }
+    const void* rp() const { return residual ? residual->data_ptr() : nullptr; }
+    int64_t ldr() const { return residual ? pitch(*residual) : 0; }
+    void* hp() { return residual ? h.t.data_ptr() : nullptr; }
+    int64_t ldh() { return residual ? pitch(h.t) : 0; }
+    const at::Tensor& stream_rows() { return residual ? h.t : x; }
+};
+
+// rmsnorm_quantize_act(x, residual, multiplier address, block, bits, eps, clip_ratio, h, codes, delta) -> (h, codes, delta)
+PyObject* rmsnorm_quantize_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 10);
+        NormRows r(a[0], a[1], a[7]);
+        const float* g = static_cast<const float*>(address(a[2]));
+        const long long block = integer(a[3]), bits = integer(a[4]);
+        const float eps = real(a[5]), clip = real(a[6]);
+        if (bits != 4 && bits != 8) return status(FQ_ERR_INVALID_ARG);
+        FlatOut codes(a[8], at::kByte, r.M * (r.K * bits / 8), "codes"), delta(a[9], at::kFloat, r.M, "delta");
+        fq_status s;
+        {
+            const Unlocked nogil;
+            r.make();
+            codes.make({r.M, r.K * bits / 8}, at::kByte, r.x);
+            delta.make({r.M}, at::kFloat, r.x);
+            s = fq_rmsnorm_quantize_act(r.x.data_ptr(), r.rp(), r.xt, r.M, r.K, pitch(r.x), r.ldr(), eps, r.hp(), r.ldh(), g,
+                                        block == (int)block ? (int)block : 0, (int)bits, clip, codes.data(), delta.data<float>(), stream());
+        }
+        return s == FQ_OK ? tuple_of({r.stream_rows(), codes.t, delta.t}) : status(s);
+    });
+}
+
+// rmsnorm_quantize_act_fp4(x, residual, multiplier address, block, format, eps, h, codes, scales, delta) -> (h, codes, scales, delta)
+PyObject* rmsnorm_quantize_act_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        arguments(n, 10);
+        NormRows r(a[0], a[1], a[6]);
+        const float* g = static_cast<const float*>(address(a[2]));
+        const long long block = integer(a[3]);
+        const fq_fp4_format f = format_of(integer(a[4]));
+        const float eps = real(a[5]);
+        if (!known(f)) return status(FQ_ERR_INVALID_ARG);
+        const int64_t sb = (int64_t)fq_fp4_scale_bytes(r.M, r.K, f);
+        FlatOut codes(a[7], at::kByte, r.M * (r.K / 2), "codes"), scales(a[8], at::kByte, sb, "scales"), delta(a[9], at::kFloat, r.M, "delta");
+        fq_status s;
+        {
+            const Unlocked nogil;
+            r.make();
+            codes.make({r.M, r.K / 2}, at::kByte, r.x);
+            scales.make({sb}, at::kByte, r.x);
+            delta.make({r.M}, at::kFloat, r.x);
+            s = fq_rmsnorm_quantize_act_fp4(r.x.data_ptr(), r.rp(), r.xt, r.M, r.K, pitch(r.x), r.ldr(), eps, r.hp(), r.ldh(), g,
+                                            block == (int)block ? (int)block : 0, f, codes.data(), scales.data(), delta.data<float>(), stream());
+        }
+        return s == FQ_OK ? tuple_of({r.stream_rows(), codes.t, scales.t, delta.t}) : status(s);
+    });
+}
+
 #define FQ_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FQ_METHOD(linear), FQ_METHOD(linear_gated), FQ_METHOD(gemm), FQ_METHOD(quantize_act), FQ_METHOD(quantize_act_composite),
                          FQ_METHOD(linear_w4a16), FQ_METHOD(qk_norm_rope), FQ_METHOD(kv8_append),
-                         FQ_METHOD(attention_kv8), FQ_METHOD(cross_attention), {nullptr, nullptr, 0, nullptr}};
+                         FQ_METHOD(attention_kv8), FQ_METHOD(cross_attention), FQ_METHOD(quantize_act_fp4), FQ_METHOD(gemm_fp4),
+                         FQ_METHOD(linear_fp4), FQ_METHOD(rmsnorm_quantize_act), FQ_METHOD(rmsnorm_quantize_act_fp4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

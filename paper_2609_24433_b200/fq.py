@@ -33,6 +33,9 @@ EXPORTS = [
     "fq_quantize_act_gated", "fq_linear_gated", "fq_watchdog_selftest",
     "fq_rope_frequencies", "fq_qk_norm_rope", "fq_kv8_append", "fq_attention_kv8", "fq_attention_kv8_workspace_bytes",
     "fq_cross_attention", "fq_cross_attention_workspace_bytes",
+    "fq_fp4_scale_bytes", "fq_fold_weights_fp4", "fq_fp4_weights_import", "fq_fp4_weights_export", "fq_fp4_weights_info",
+    "fq_fp4_weights_multiplier", "fq_fp4_weights_destroy", "fq_quantize_act_fp4", "fq_gemm_fp4", "fq_linear_fp4",
+    "fq_linear_fp4_workspace_bytes", "fq_rmsnorm_quantize_act", "fq_rmsnorm_quantize_act_fp4",
 ]
 
 _lib = None
@@ -70,6 +73,11 @@ def lib() -> ctypes.CDLL:
         L.fq_cross_attention_workspace_bytes.argtypes = [ctypes.c_int, ctypes.c_int64, ctypes.c_int, ctypes.c_int64, ctypes.c_int,
                                                          ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int64,
                                                          ctypes.c_int64]
+        L.fq_fp4_weights_multiplier.restype = ctypes.c_void_p
+        L.fq_fp4_weights_multiplier.argtypes = [ctypes.c_void_p]
+        for f in (L.fq_fp4_scale_bytes, L.fq_linear_fp4_workspace_bytes):
+            f.restype = ctypes.c_size_t
+            f.argtypes = [ctypes.c_int64, ctypes.c_int64, ctypes.c_int]
         _lib = L
     return _lib
 
@@ -455,6 +463,133 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_heads: 
         scale = _scale(scale, q.shape[1] // q_heads)
     return _result(_native().cross_attention(q, k, v, q_heads, kv_heads, batch, q_offsets, kv_offsets, kv_len, key_mask, max_q, max_kv,
                                              1.0 if scale is None else scale, y, workspace), "fq_cross_attention")
+
+
+# ---- projections in microscaled 4-bit floating point ----------------------------------------------------
+MXFP4, NVFP4 = 0, 1
+
+
+def fp4_scale_bytes(rows: int, K: int, format: int) -> int:
+    return int(lib().fq_fp4_scale_bytes(rows, K, format))
+
+
+class Fp4Weights:
+    """Owner of an ``fq_fp4_weights`` handle."""
+
+    def __init__(self, handle: int):
+        self._h = ctypes.c_void_p(handle)
+        n, k = ctypes.c_int64(), ctypes.c_int64()
+        blk, fmt = ctypes.c_int(), ctypes.c_int()
+        _check(lib().fq_fp4_weights_info(self._h, ctypes.byref(n), ctypes.byref(k), ctypes.byref(blk), ctypes.byref(fmt)), "fq_fp4_weights_info")
+        self.N, self.K, self.block, self.format = n.value, k.value, blk.value, fmt.value
+
+    @property
+    def address(self) -> int:
+        if self._h is None:
+            raise RuntimeError("weights handle already destroyed")
+        return self._h.value
+
+    def multiplier_ptr(self) -> int:
+        return int(lib().fq_fp4_weights_multiplier(self.address) or 0)
+
+    def export(self) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+        """(codes u8 [N, K/2], scales u8 (tiles), w_scale [N], mult_g [K], bias [N]) as new device tensors."""
+        dev = torch.device("cuda", torch.cuda.current_device())
+        codes = torch.empty((self.N, self.K // 2), dtype=torch.uint8, device=dev)
+        scales = torch.empty(fp4_scale_bytes(self.N, self.K, self.format), dtype=torch.uint8, device=dev)
+        ws, g, b = (torch.empty(n, dtype=torch.float32, device=dev) for n in (self.N, self.K, self.N))
+        _check(lib().fq_fp4_weights_export(ctypes.c_void_p(self.address), _ptr(codes), _ptr(scales), _ptr(ws), _ptr(g), _ptr(b), _stream()),
+               "fq_fp4_weights_export")
+        return codes, scales, ws, g, b
+
+    def destroy(self):
+        if self._h is not None:
+            lib().fq_fp4_weights_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def _floats(t: Optional[torch.Tensor], size: int, what: str) -> ctypes.c_void_p:
+    if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or t.numel() != size or not t.is_contiguous() or not t.is_cuda
+                          or t.device.index != torch.cuda.current_device()):
+        raise ValueError(f"{what} has to be a contiguous float32 tensor of {size} elements on the current CUDA device")
+    return _ptr(t)
+
+
+def fold_weights_fp4(W: torch.Tensor, smooth: Optional[torch.Tensor], bias: Optional[torch.Tensor], hadamard_block: int,
+                     format: int = NVFP4) -> Fp4Weights:
+    """Fold smoothing and rotation into W and round its rows to e2m1 with block scales."""
+    W = _rowmajor(W)
+    if not W.is_cuda or W.device.index != torch.cuda.current_device():
+        raise ValueError("W has to be on the current CUDA device")
+    N, K = W.shape
+    out = ctypes.c_void_p()
+    _check(lib().fq_fold_weights_fp4(_ptr(W), _dt(W), ctypes.c_int64(N), ctypes.c_int64(K), ctypes.c_int64(W.stride(0) if N > 1 else (K + 7) // 8 * 8),
+                                     _floats(smooth, K, "smooth"), _floats(bias, N, "bias"), ctypes.c_int(hadamard_block), ctypes.c_int(format),
+                                     _stream(), ctypes.byref(out)), "fq_fold_weights_fp4")
+    return Fp4Weights(out.value)
+
+
+def weights_import_fp4(codes: torch.Tensor, scales: torch.Tensor, w_scale: Optional[torch.Tensor], mult_g: Optional[torch.Tensor],
+                       bias: Optional[torch.Tensor], K: int, hadamard_block: int, format: int = NVFP4) -> Fp4Weights:
+    """A handle of codes u8 [N, K/2] and block scales in tiles (see ``fp4_scale_bytes``), as a checkpoint or ``export`` has them."""
+    N = codes.shape[0]
+    for name, t, n in (("codes", codes, N * (K // 2)), ("scales", scales, fp4_scale_bytes(N, K, format))):
+        if t.dtype != torch.uint8 or t.numel() != n or not t.is_contiguous() or not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{name} has to be a contiguous uint8 tensor of {n} bytes on the current CUDA device")
+    out = ctypes.c_void_p()
+    _check(lib().fq_fp4_weights_import(_ptr(codes), _ptr(scales), _floats(w_scale, N, "w_scale"), _floats(mult_g, K, "mult_g"),
+                                       _floats(bias, N, "bias"), ctypes.c_int64(N), ctypes.c_int64(K), ctypes.c_int(hadamard_block),
+                                       ctypes.c_int(format), _stream(), ctypes.byref(out)), "fq_fp4_weights_import")
+    return Fp4Weights(out.value)
+
+
+def _multiplier(mult_g, K: int) -> int:
+    """Address of a site's multiplier: a float32 tensor, a handle's own, or None (the constant block^-1/2)."""
+    if isinstance(mult_g, (Weights, Fp4Weights)):
+        if mult_g.K != K:
+            raise ValueError(f"the handle has {mult_g.K} channels, the rows {K}")
+        if isinstance(mult_g, Weights) and (mult_g.fold_after or lib().fq_weights_composite(mult_g.handle)):
+            raise ValueError("the multiplier of a fold-after or composite site does not stand ahead of the butterflies")
+        return mult_g.multiplier_ptr()
+    return _floats(mult_g, K, "mult_g").value or 0
+
+
+def quantize_act_fp4(x: torch.Tensor, mult_g, hadamard_block: int, format: int = NVFP4, codes=None, scales=None, delta=None):
+    """(codes u8 [M, K/2], block scales u8 in tiles, steps [M]).  ``mult_g``: device float tensor, a handle (its multiplier) or None."""
+    return _result(_native().quantize_act_fp4(x, _multiplier(mult_g, x.shape[-1]), hadamard_block, format, codes, scales, delta),
+                   "fq_quantize_act_fp4")
+
+
+def gemm_fp4(a_codes: torch.Tensor, a_scales: torch.Tensor, a_delta: torch.Tensor, W: Fp4Weights, out_dtype=torch.float32, y=None):
+    """y = product of codes and block scales, times steps and s^W, plus bias."""
+    return _result(_native().gemm_fp4(a_codes, a_scales, a_delta, W.address, W.K, W.N, W.format, out_dtype, y), "fq_gemm_fp4")
+
+
+def linear_fp4(x: torch.Tensor, W: Fp4Weights, out_dtype=torch.float32, y=None, workspace=None):
+    """The whole projection: transform, quantiser and product."""
+    return _result(_native().linear_fp4(x, W.address, W.K, W.N, W.format, out_dtype, y, workspace), "fq_linear_fp4")
+
+
+# ---- RMS norm with the residual's addition, ending in codes ------------------------------------------------
+def rmsnorm_quantize_act(x: torch.Tensor, residual: Optional[torch.Tensor], mult_g, hadamard_block: int, bits: int, eps: float = 1e-6,
+                         clip_ratio: float = 1.0, h=None, codes=None, delta=None):
+    """(h, codes u8 [M, K*bits/8], steps [M]): h = x + residual (x itself without one) and the codes of h / rms(h) for a site whose
+    multiplier is ``mult_g`` (device float tensor, a Weights or None)."""
+    return _result(_native().rmsnorm_quantize_act(x, residual, _multiplier(mult_g, x.shape[-1]), hadamard_block, bits, eps, clip_ratio, h, codes, delta),
+                   "fq_rmsnorm_quantize_act")
+
+
+def rmsnorm_quantize_act_fp4(x: torch.Tensor, residual: Optional[torch.Tensor], mult_g, hadamard_block: int, format: int = NVFP4,
+                             eps: float = 1e-6, h=None, codes=None, scales=None, delta=None):
+    """(h, codes u8 [M, K/2], block scales, steps [M]) of the same in e2m1."""
+    return _result(_native().rmsnorm_quantize_act_fp4(x, residual, _multiplier(mult_g, x.shape[-1]), hadamard_block, format, eps, h, codes, scales, delta),
+                   "fq_rmsnorm_quantize_act_fp4")
 
 
 def gemm_acc_i32(a_codes, W: Weights, workspace=None) -> torch.Tensor:
