@@ -34,6 +34,7 @@ constexpr int kStageK = 256;             // channels of K a stage
 constexpr int kMostStages = 8;
 constexpr int kScaleCols = 256;          // TMEM columns from here on hold scales, those before accumulators
 constexpr size_t kSmemMost = 226 * 1024;
+constexpr size_t kOutBytes = kEpi * 2048;    // two output buffers for each epilogue warp
 
 struct GemmParams {
     int64_t M, N, ldy;
@@ -114,11 +115,31 @@ __device__ __forceinline__ void commit(uint32_t bar, uint16_t mask) {
 __device__ __forceinline__ uint32_t instr_desc_fp4(int m, int n, bool nv) {
     return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((nv ? 0u : 1u) << 23) | ((uint32_t)(m >> 4) << 24);
 }
-__device__ __forceinline__ void tmem_ld4(uint32_t taddr, uint32_t* r) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+// 16 TMEM lanes x 16 columns as a warp-level MMA accumulator has them: thread T holds, for column groups n = 0, 1,
+//   r[4n + 0], r[4n + 1] = lane T/4, columns 8n + 2(T%4) and the next;  r[4n + 2], r[4n + 3] = lane T/4 + 8, the same columns.
+// With channels on the lanes and tokens on the columns such a pair, rounded to 16 bits, is what stmatrix stores transposed.
+__device__ __forceinline__ void tmem_ld_16x256b_x2(uint32_t taddr, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                  : "r"(taddr)
                  : "memory");
+}
+__device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
+                 ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int c0, int c1, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(src)
+                 : "memory");
+}
+// One channel at two adjacent tokens, rounded to bf16, the earlier token in the low half.
+__device__ __forceinline__ uint32_t scale_pair(uint32_t a0, uint32_t a1, float2 d, float sw, float bj) {
+    const float2 v = f2_fma(make_float2(__uint_as_float(a0), __uint_as_float(a1)), f2_mul(d, make_float2(sw, sw)), make_float2(bj, bj));
+    uint32_t w;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(v.y), "f"(v.x));
+    return w;
 }
 __device__ __forceinline__ void st_cluster_v4(uint32_t addr, const uint32_t* r) {
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
@@ -127,7 +148,7 @@ __device__ __forceinline__ void st_cluster_v4(uint32_t addr, const uint32_t* r) 
 template <int CTAS, bool NV, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_x,
-                const __grid_constant__ CUtensorMap map_xs, const GemmParams p) {
+                const __grid_constant__ CUtensorMap map_xs, const __grid_constant__ CUtensorMap map_y, const GemmParams p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t s_full[kMostStages], s_empty[kMostStages], s_acc_full[2], s_acc_empty[2];
     __shared__ uint32_t s_tmem;
@@ -146,7 +167,8 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     const uint32_t stage_bytes = kWBytes + x_bytes + kWScale + x_scale;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     // [weight codes][token codes] of all stages (1024-byte aligned), then their scales
-    const uint32_t s_w = base, s_x = s_w + (uint32_t)p.stages * kWBytes, s_ws = s_x + (uint32_t)p.stages * x_bytes, s_xs = s_ws + (uint32_t)p.stages * kWScale;
+    const uint32_t s_w = base, s_x = s_w + (uint32_t)p.stages * kWBytes, s_ws = s_x + (uint32_t)p.stages * x_bytes, s_xs = s_ws + (uint32_t)p.stages * kWScale,
+                   s_out = s_xs + (uint32_t)p.stages * x_scale;
 
     if (threadIdx.x == 0) {
         s_abort = 0;
@@ -275,85 +297,149 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         }
     }
     // ------------------------------------------------------------ epilogue
+    // Two warps to a quadrant of lanes, alternating chunks of 16 tokens: chunk n of a warp begins at token (set + 2n) * 16.
     const int quad = warp & 3, set = (warp - 2) >> 2;
     const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    auto store = [&](int64_t t, int64_t j, float v) {
-        if (p.bf16) static_cast<__nv_bfloat16*>(p.y)[t * p.ldy + j] = __float2bfloat16_rn(v);
-        else static_cast<float*>(p.y)[t * p.ldy + j] = v;
-    };
     bool ok = true;
+    float steps[4], sw4[4], bj4[4];          // steps of the warp's tokens: lanes 16 (n & 1) .. of steps[n / 2]
+    int stores = 0;
+    auto constants = [&](int m, int n) {
+        const int64_t jq = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32, t0 = (int64_t)m * p.bt;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = (set + 2 * (2 * i + (lane >> 4))) * 16 + (lane & 15);
+            steps[i] = t < p.bt && t0 + t < p.M ? ld_global_f32(p.delta + t0 + t) : 0.0f;
+            const int64_t j = jq + (p.bf16 ? (lane >> 2) + 8 * i : lane);       // bf16: the channels of this thread's fragments
+            sw4[i] = j < p.N ? __ldg(p.w_scale + j) : 0.0f;
+            bj4[i] = j < p.N ? __ldg(p.bias + j) : 0.0f;
+        }
+    };
+    // Sums of one chunk, as fragments for bf16 outputs (channels 0..15, 16..31 of the quadrant), else a thread one channel.
+    auto fetch = [&](uint32_t column, uint32_t* r) {
+        if (p.bf16) {
+            tmem_ld_16x256b_x2(tmem + lanes + column, r);
+            tmem_ld_16x256b_x2(tmem + lanes + (16u << 16) + column, r + 8);
+        } else {
+            tmem_ld16(tmem + lanes + column, r);
+        }
+    };
+    auto emit = [&](const uint32_t* r, int i, int64_t tc, int64_t jq) {
+        const float step = i < 2 ? steps[0] : i < 4 ? steps[1] : i < 6 ? steps[2] : steps[3];
+        const int from = 16 * (i & 1);
+        if (p.bf16) {
+            // scaled in pairs, stored token-major into 1 KB of [16 tokens][32 channels] (64-byte swizzle) by transposing matrix
+            // stores, and sent off as one bulk store, which clips what lies past M or N; two buffers alternate
+            const int a = from + 2 * (lane & 3);
+            const float2 d0 = make_float2(__shfl_sync(0xffffffffu, step, a), __shfl_sync(0xffffffffu, step, a + 1));
+            const float2 d1 = make_float2(__shfl_sync(0xffffffffu, step, a + 8), __shfl_sync(0xffffffffu, step, a + 9));
+            const uint32_t tok = (uint32_t)((lane >> 4) * 8 + (lane & 7)), ch = (uint32_t)((lane >> 3) & 1), mix = (tok >> 1) & 3u;
+            const uint32_t buf = s_out + (uint32_t)((warp - 2) * 2 + (stores & 1)) * 1024u;
+            if (stores >= 2) {
+                if (lane == 0) bulk_wait_read<1>();
+                __syncwarp();
+            }
+            stmatrix_x4_trans(buf + tok * 64u + ((ch ^ mix) << 4), scale_pair(r[0], r[1], d0, sw4[0], bj4[0]), scale_pair(r[2], r[3], d0, sw4[1], bj4[1]),
+                              scale_pair(r[4], r[5], d1, sw4[0], bj4[0]), scale_pair(r[6], r[7], d1, sw4[1], bj4[1]));
+            stmatrix_x4_trans(buf + tok * 64u + (((ch + 2u) ^ mix) << 4), scale_pair(r[8], r[9], d0, sw4[2], bj4[2]),
+                              scale_pair(r[10], r[11], d0, sw4[3], bj4[3]), scale_pair(r[12], r[13], d1, sw4[2], bj4[2]),
+                              scale_pair(r[14], r[15], d1, sw4[3], bj4[3]));
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0 && jq < p.N) {
+                tma_store_2d(&map_y, (int)(jq * 2), (int)tc, buf);
+                bulk_commit();
+            }
+            ++stores;
+        } else {
+            float* y = static_cast<float*>(p.y) + tc * p.ldy + jq + lane;
+            const bool j_ok = jq + lane < p.N;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+                const float d = __shfl_sync(0xffffffffu, step, from + k);
+                if (tc + k < p.M && j_ok) y[k * p.ldy] = __fmaf_rn(__uint_as_float(r[k]), d * sw4[0], bj4[0]);
+            }
+        }
+    };
     if (warp >= 2) {
         int acc = 0;
         uint32_t phase = 0;
         for (int unit = unit0; unit < p.units; unit += p.unit_step) {
             int m, n;
             tile_of(unit, &m, &n);
-            const int64_t j = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32 + lane, t0 = (int64_t)m * p.bt;
-            const bool j_ok = j < p.N;
-            const float sw = j_ok ? __ldg(p.w_scale + j) : 0.0f, bj = j_ok ? __ldg(p.bias + j) : 0.0f;
+            const int64_t jq = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32, t0 = (int64_t)m * p.bt;
+            constants(m, n);
             ok = mbar_wait_warp_relaxed(smem_u32(&s_acc_full[acc]), phase, abort_flag, p.watchdog, kWdEpilogue);
             if (!ok) break;
             tc_fence_after();
-            // (SPLIT: one tile a cluster, finished below)
-            for (int c = SPLIT ? p.bt : set * 16; c < p.bt && t0 + c < p.M; c += 32) {
-                uint32_t r[16];
-                tmem_ld16(tmem + lanes + (uint32_t)(acc * acc_cols + c), r);
-                tmem_ld_wait();
+            if (SPLIT) break;                                // one tile a cluster: below
+            // all of the warp's sums into registers, so that the next tile's MMAs may have the columns
+            const int cols = columns(m);
+            uint32_t r[8][16];
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (t0 + c + i < p.M && j_ok) store(t0 + c + i, j, fmaf(__uint_as_float(r[i]), ld_global_f32(p.delta + t0 + c + i) * sw, bj));
-            }
-            if (SPLIT) break;
+            for (int i = 0; i < 8; ++i)
+                if ((set + 2 * i) * 16 < cols) fetch((uint32_t)(acc * acc_cols + (set + 2 * i) * 16), r[i]);
+            tmem_ld_wait();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) {
                 if (CTAS == 1) mbar_arrive(smem_u32(&s_acc_empty[acc]));
                 else mbar_arrive_cta(smem_u32(&s_acc_empty[acc]), pair_base);
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if ((set + 2 * i) * 16 < cols && t0 + (set + 2 * i) * 16 < p.M) emit(r[i], i, t0 + (set + 2 * i) * 16, jq);
             if (++acc == accs) { acc = 0; phase ^= 1u; }
         }
     }
     if (SPLIT) {
-        // Four tokens at a time are finished by slice (chunk % split): the others store their sums into its shared memory,
-        // [sender][chunk / split][channel][4 tokens], where the stages were -- behind a barrier, all MMAs of the cluster have ended.
+        // Chunk c of 16 tokens is finished by slice c % split: the others store their sums into its shared memory, as the threads hold
+        // them, where the stages were -- behind a barrier, all MMAs of the cluster have ended.  Added in the order of the slices.
         int m, n;
         tile_of(unit0, &m, &n);
-        const int64_t j = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32 + lane, t0 = (int64_t)m * p.bt;
-        const int chunks = columns(m) / 4, per = (chunks + p.split - 1) / p.split, channel = quad * 32 + lane;
+        const int64_t jq = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32, t0 = (int64_t)m * p.bt;
+        const int chunks = columns(m) / 16, per = (chunks + p.split - 1) / p.split;
+        // [sender][chunk / split][quarter][thread of four warps] 16 bytes
+        auto place = [&](int sender, int c, int q) { return base + (uint32_t)((((sender * per + c / p.split) * 4 + q) * 128 + quad * 32 + lane) * 16); };
         __syncwarp();
         cluster_sync_all();
         if (warp >= 2 && ok) {
             for (int c = set; c < chunks; c += 2) {
                 const int owner = c % p.split;
                 if (owner == slice) continue;
-                uint32_t r[4];
-                tmem_ld4(tmem + lanes + (uint32_t)(c * 4), r);
+                uint32_t r[16];
+                fetch((uint32_t)(c * 16), r);
                 tmem_ld_wait();
-                st_cluster_v4(cluster_address(base + (uint32_t)(((slice * per + c / p.split) * kRows + channel) * 16), (uint32_t)(owner * CTAS) + half), r);
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    st_cluster_v4(cluster_address(place(slice - (slice > owner ? 1 : 0), c, q), (uint32_t)(owner * CTAS) + half), r + 4 * q);
             }
         }
         __syncwarp();
         cluster_sync_all();
         if (warp >= 2 && ok) {
-            const bool j_ok = j < p.N;
-            const float sw = j_ok ? __ldg(p.w_scale + j) : 0.0f, bj = j_ok ? __ldg(p.bias + j) : 0.0f;
-            for (int c = set; c < chunks; c += 2) {
-                if (c % p.split != slice || t0 + c * 4 >= p.M) continue;
-                uint32_t r[4];
-                tmem_ld4(tmem + lanes + (uint32_t)(c * 4), r);
+            for (int c = set, i = 0; c < chunks; c += 2, ++i) {
+                if (c % p.split != slice || t0 + c * 16 >= p.M) continue;
+                uint32_t r[16], sum[16];
+                fetch((uint32_t)(c * 16), r);
                 tmem_ld_wait();
-                float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                for (int q = 0; q < p.split; ++q) {
-                    uint4 o = make_uint4(r[0], r[1], r[2], r[3]);
-                    if (q != slice) o = lds128(base + (uint32_t)(((q * per + c / p.split) * kRows + channel) * 16));
-                    s[0] += __uint_as_float(o.x); s[1] += __uint_as_float(o.y); s[2] += __uint_as_float(o.z); s[3] += __uint_as_float(o.w);
-                }
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (t0 + c * 4 + i < p.M && j_ok) store(t0 + c * 4 + i, j, fmaf(s[i], ld_global_f32(p.delta + t0 + c * 4 + i) * sw, bj));
+                for (int k = 0; k < 16; ++k) sum[k] = 0u;
+                for (int s = 0; s < p.split; ++s) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint4 o = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
+                        if (s != slice) o = lds128(place(s - (s > slice ? 1 : 0), c, q));
+                        const uint32_t w[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) sum[4 * q + k] = __float_as_uint(__fadd_rn(__uint_as_float(sum[4 * q + k]), __uint_as_float(w[k])));
+                    }
+                }
+                emit(sum, i, t0 + c * 16, jq);
             }
         }
     }
+    // the stores have read their buffers before the CTA gives up its shared memory
+    if (warp >= 2 && p.bf16 && lane == 0) bulk_wait_read<0>();
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -396,18 +482,18 @@ Plan plan(int64_t M, int64_t N, int64_t K) {
 }
 
 template <int CTAS, bool NV, bool SPLIT>
-cudaError_t launch(const CUtensorMap& w, const CUtensorMap& ws, const CUtensorMap& x, const CUtensorMap& xs, const GemmParams& p, int grid, size_t smem,
-                   cudaStream_t stream) {
+cudaError_t launch(const CUtensorMap& w, const CUtensorMap& ws, const CUtensorMap& x, const CUtensorMap& xs, const CUtensorMap& y,
+                   const GemmParams& p, int grid, size_t smem, cudaStream_t stream) {
     auto kern = gemm_fp4_kernel<CTAS, NV, SPLIT>;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, (unsigned)(CTAS * p.split), w, ws, x, xs, p);
+    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, (unsigned)(CTAS * p.split), w, ws, x, xs, y, p);
 }
 template <int CTAS>
-cudaError_t launch(bool nv, bool split, const CUtensorMap& w, const CUtensorMap& ws, const CUtensorMap& x, const CUtensorMap& xs, const GemmParams& p, int grid,
-                   size_t smem, cudaStream_t stream) {
-    if (nv) return split ? launch<CTAS, true, true>(w, ws, x, xs, p, grid, smem, stream) : launch<CTAS, true, false>(w, ws, x, xs, p, grid, smem, stream);
-    return split ? launch<CTAS, false, true>(w, ws, x, xs, p, grid, smem, stream) : launch<CTAS, false, false>(w, ws, x, xs, p, grid, smem, stream);
+cudaError_t launch(bool nv, bool split, const CUtensorMap& w, const CUtensorMap& ws, const CUtensorMap& x, const CUtensorMap& xs, const CUtensorMap& y,
+                   const GemmParams& p, int grid, size_t smem, cudaStream_t stream) {
+    if (nv) return split ? launch<CTAS, true, true>(w, ws, x, xs, y, p, grid, smem, stream) : launch<CTAS, true, false>(w, ws, x, xs, y, p, grid, smem, stream);
+    return split ? launch<CTAS, false, true>(w, ws, x, xs, y, p, grid, smem, stream) : launch<CTAS, false, false>(w, ws, x, xs, y, p, grid, smem, stream);
 }
 
 }  // namespace
@@ -439,17 +525,24 @@ fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const flo
     const int tiles = nv ? 4 : 2;
     const size_t stage = (size_t)kRows * 128 + (size_t)(r.bt / r.ctas) * 128 + (size_t)tiles * 512 * (1 + p.xa);
     const int slots = 256 / (tiles * 4 * (1 + p.xa));        // TMEM columns for scales
-    p.stages = (int)((kSmemMost - 1024) / stage);
+    p.stages = (int)((kSmemMost - 1024 - kOutBytes) / stage);
     if (p.stages > kMostStages) p.stages = kMostStages;
     if (p.stages > slots) p.stages = slots;
-    size_t smem = 1024 + stage * (size_t)p.stages;
+    const size_t smem = 1024 + stage * (size_t)p.stages + kOutBytes;
     CUtensorMap x, xs;
     if (!code_map(&x, codes, M, W.K, r.bt / r.ctas) || !scale_map(&xs, scales, M, W.K, W.format, p.xa)) return FQ_ERR_CUDA;
+    // outputs in bf16 leave in boxes of [16 tokens][32 channels]
+    CUtensorMap map_y = x;
+    if (p.bf16) {
+        const uint64_t dims[2] = {(uint64_t)W.N * 2, (uint64_t)M}, strides[1] = {(uint64_t)ldy * 2};
+        const uint32_t box[2] = {64, 16};
+        if (!encode_tiled(&map_y, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, y, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_64B)) return FQ_ERR_CUDA;
+    }
     const int units = r.split > 1 ? p.units : (p.units < sms / r.ctas ? p.units : sms / r.ctas);
     p.unit_step = units;
     const int grid = units * r.ctas * r.split;
-    const cudaError_t e = r.ctas == 2 ? launch<2>(nv, r.split > 1, W.map_codes, W.map_scales, x, xs, p, grid, smem, stream)
-                                      : launch<1>(nv, r.split > 1, W.map_codes, W.map_scales, x, xs, p, grid, smem, stream);
+    const cudaError_t e = r.ctas == 2 ? launch<2>(nv, r.split > 1, W.map_codes, W.map_scales, x, xs, map_y, p, grid, smem, stream)
+                                      : launch<1>(nv, r.split > 1, W.map_codes, W.map_scales, x, xs, map_y, p, grid, smem, stream);
     return e == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
