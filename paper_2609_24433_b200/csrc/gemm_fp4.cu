@@ -41,7 +41,6 @@ struct GemmParams {
     int K, bt, stages, m_tiles, n_tiles, band;
     int split;                           // slices of K, each CTA (pair) of a cluster one
     int kb;                              // stages of all of K
-    int xa;                              // scale tiles across a tile's tokens
     int units, unit_step;
     const float* delta;
     const float* w_scale;
@@ -85,31 +84,71 @@ __device__ __forceinline__ void mbar_arrive_cta(uint32_t bar, uint32_t rank) {
         ::"r"(bar), "r"(rank)
         : "memory");
 }
-// 512 bytes of scales (32 rows of 16 bytes, 8-row groups 128 bytes apart) to four TMEM columns of all four lane quadrants.
-template <int CTAS>
-__device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t smem) {
-    const uint64_t desc = (uint64_t)((smem & 0x3FFFFu) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
-    if (CTAS == 1) asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-    else asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+// The work of one stage as ONE block of PTX: scale tiles to TMEM (512 bytes each, 32 rows of 16 bytes, to four columns of all four
+// lane quadrants), four MMAs of 64 channels, the commits.  The whole warp runs it and the lane that elect.sync picks issues: the
+// operands are then computed by the warp as a whole, which is much cheaper than by one lane of a divergent warp.
+//   %0 accumulator column  %1, %2 matrix descriptors (weights, tokens)  %3, %4 descriptors of their scales  %5 TMEM column of the scales
+//   %6 instruction descriptor  %7 add to what the accumulator holds  %8 MMAs of the stage  %9 the stage's barrier
+//   %10 the accumulator's barrier, 0: not its last stage  %11 (pairs) cluster ranks whose barriers the commits arrive at
+#define FQ_CP(CG, SRC, OFF, COL)                                                     \
+    "add.u64 t, " SRC ", " OFF ";\n\tadd.u32 c, %5, " COL ";\n\t"                     \
+    "@pl tcgen05.cp.cta_group::" CG ".32x128b.warpx4 [c], t;\n\t"
+#define FQ_MMA(CG, KIND, STEP, SA, SB, ID, PRED, ACC)                                                        \
+    "add.u64 t, %1, " STEP ";\n\tadd.u64 u, %2, " STEP ";\n\tadd.u32 c, %5, " SA ";\n\tadd.u32 e, %5, " SB ";\n\t" \
+    "or.b32 f, %6, " ID ";\n\t"                                                                               \
+    "@" PRED " tcgen05.mma.cta_group::" CG "." KIND " [%0], t, u, f, [c], [e], " ACC ";\n\t"
+#define FQ_HEAD                                                                                  \
+    "{\n\t.reg .pred pl, p1, p2, p3, pa, pt, pc;\n\t.reg .b64 t, u;\n\t.reg .b32 c, e, f;\n\t"     \
+    "elect.sync _|pl, 0xffffffff;\n\t"                                                           \
+    "setp.ne.b32 pa, %7, 0;\n\tsetp.eq.b32 pt, %0, %0;\n\t"                                      \
+    "setp.gt.and.s32 p1, %8, 1, pl;\n\tsetp.gt.and.s32 p2, %8, 2, pl;\n\tsetp.gt.and.s32 p3, %8, 3, pl;\n\t" \
+    "setp.ne.and.b32 pc, %10, 0, pl;\n\t"
+#define FQ_COMMIT_1                                                                                \
+    "@pl tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%9];\n\t"          \
+    "@pc tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%10];\n\t}"
+#define FQ_COMMIT_2                                                                                                \
+    "@pl tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%9], %11;\n\t"  \
+    "@pc tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%10], %11;\n\t}"
+#define FQ_KIND_NV "kind::mxf4nvf4.block_scale.scale_vec::4X"
+#define FQ_KIND_MX "kind::mxf4.block_scale.scale_vec::2X"
+#define FQ_ID_ODD "1073741856"           /* blocks 2 and 3 of a scale tile, both operands: 2 << 29 | 2 << 4 */
+#define FQ_STAGE_NV1(CG)                                                                                                          \
+    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "16") FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "20")                     \
+    FQ_CP(CG, "%3", "64", "8") FQ_CP(CG, "%4", "64", "24") FQ_CP(CG, "%3", "96", "12") FQ_CP(CG, "%4", "96", "28")                  \
+    FQ_MMA(CG, FQ_KIND_NV, "0", "0", "16", "0", "pl", "pa") FQ_MMA(CG, FQ_KIND_NV, "2", "4", "20", "0", "p1", "pt")                 \
+    FQ_MMA(CG, FQ_KIND_NV, "4", "8", "24", "0", "p2", "pt") FQ_MMA(CG, FQ_KIND_NV, "6", "12", "28", "0", "p3", "pt")
+#define FQ_STAGE_NV2(CG)                                                                                                          \
+    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "16") FQ_CP(CG, "%4", "128", "20") FQ_CP(CG, "%3", "32", "4")                    \
+    FQ_CP(CG, "%4", "32", "24") FQ_CP(CG, "%4", "160", "28") FQ_CP(CG, "%3", "64", "8") FQ_CP(CG, "%4", "64", "32")                 \
+    FQ_CP(CG, "%4", "192", "36") FQ_CP(CG, "%3", "96", "12") FQ_CP(CG, "%4", "96", "40") FQ_CP(CG, "%4", "224", "44")               \
+    FQ_MMA(CG, FQ_KIND_NV, "0", "0", "16", "0", "pl", "pa") FQ_MMA(CG, FQ_KIND_NV, "2", "4", "24", "0", "p1", "pt")                 \
+    FQ_MMA(CG, FQ_KIND_NV, "4", "8", "32", "0", "p2", "pt") FQ_MMA(CG, FQ_KIND_NV, "6", "12", "40", "0", "p3", "pt")
+#define FQ_STAGE_MX1(CG)                                                                                                          \
+    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "8") FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "12")                      \
+    FQ_MMA(CG, FQ_KIND_MX, "0", "0", "8", "0", "pl", "pa") FQ_MMA(CG, FQ_KIND_MX, "2", "0", "8", FQ_ID_ODD, "p1", "pt")             \
+    FQ_MMA(CG, FQ_KIND_MX, "4", "4", "12", "0", "p2", "pt") FQ_MMA(CG, FQ_KIND_MX, "6", "4", "12", FQ_ID_ODD, "p3", "pt")
+#define FQ_STAGE_MX2(CG)                                                                                                          \
+    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "8") FQ_CP(CG, "%4", "64", "12")                                                 \
+    FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "16") FQ_CP(CG, "%4", "96", "20")                                              \
+    FQ_MMA(CG, FQ_KIND_MX, "0", "0", "8", "0", "pl", "pa") FQ_MMA(CG, FQ_KIND_MX, "2", "0", "8", FQ_ID_ODD, "p1", "pt")             \
+    FQ_MMA(CG, FQ_KIND_MX, "4", "4", "16", "0", "p2", "pt") FQ_MMA(CG, FQ_KIND_MX, "6", "4", "16", FQ_ID_ODD, "p3", "pt")
+template <int CTAS, bool NV, int XA>
+__device__ __forceinline__ void issue_stage(uint32_t d, uint64_t wd, uint64_t xd, uint64_t ws, uint64_t xs, uint32_t cols, uint32_t idesc, uint32_t accumulate,
+                                            int steps, uint32_t bar_stage, uint32_t bar_acc, uint16_t mask) {
+#define FQ_STAGE(BODY, COMMIT)                                                                                               \
+    asm volatile(FQ_HEAD BODY COMMIT ::"r"(d), "l"(wd), "l"(xd), "l"(ws), "l"(xs), "r"(cols), "r"(idesc), "r"(accumulate),   \
+                 "r"(steps), "r"(bar_stage), "r"(bar_acc), "h"(mask) : "memory")
+    if constexpr (CTAS == 1 && NV && XA == 1) FQ_STAGE(FQ_STAGE_NV1("1"), FQ_COMMIT_1);
+    else if constexpr (CTAS == 1 && NV) FQ_STAGE(FQ_STAGE_NV2("1"), FQ_COMMIT_1);
+    else if constexpr (CTAS == 1 && XA == 1) FQ_STAGE(FQ_STAGE_MX1("1"), FQ_COMMIT_1);
+    else if constexpr (CTAS == 1) FQ_STAGE(FQ_STAGE_MX2("1"), FQ_COMMIT_1);
+    else if constexpr (NV) FQ_STAGE(FQ_STAGE_NV2("2"), FQ_COMMIT_2);
+    else FQ_STAGE(FQ_STAGE_MX2("2"), FQ_COMMIT_2);
+#undef FQ_STAGE
 }
-template <int CTAS, bool NV>
-__device__ __forceinline__ void mma_fp4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
-#define FQ_MMA_FP4(CG, KIND)                                                                             \
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                        \
-                 "tcgen05.mma.cta_group::" CG "." KIND " [%0], %1, %2, %3, [%4], [%5], p;\n\t}"           \
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory")
-    if (CTAS == 1 && NV) FQ_MMA_FP4("1", "kind::mxf4nvf4.block_scale.scale_vec::4X");
-    else if (CTAS == 1) FQ_MMA_FP4("1", "kind::mxf4.block_scale.scale_vec::2X");
-    else if (NV) FQ_MMA_FP4("2", "kind::mxf4nvf4.block_scale.scale_vec::4X");
-    else FQ_MMA_FP4("2", "kind::mxf4.block_scale.scale_vec::2X");
-#undef FQ_MMA_FP4
-}
-template <int CTAS>
-__device__ __forceinline__ void commit(uint32_t bar, uint16_t mask) {
-    if (CTAS == 1) mma_commit(bar);
-    else
-        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(mask)
-                     : "memory");
+// Shared-memory descriptor of a run of scale tiles (no swizzle, 8-row groups 128 bytes apart).
+__device__ __forceinline__ uint64_t scale_desc(uint32_t smem) {
+    return (uint64_t)((smem & 0x3FFFFu) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 // Instruction descriptor: e2m1 x e2m1, both K-major, scales e4m3 or e8m0, M = m, N = n.
 __device__ __forceinline__ uint32_t instr_desc_fp4(int m, int n, bool nv) {
@@ -145,7 +184,8 @@ __device__ __forceinline__ void st_cluster_v4(uint32_t addr, const uint32_t* r) 
     asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
 
-template <int CTAS, bool NV, bool SPLIT>
+// XA: scale tiles across a tile's tokens (two for more than 128, and for pairs).
+template <int CTAS, bool NV, bool SPLIT, int XA>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_x,
                 const __grid_constant__ CUtensorMap map_xs, const __grid_constant__ CUtensorMap map_y, const GemmParams p) {
@@ -163,7 +203,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     const bool leader = half == 0;
     const int slice = SPLIT ? (int)(rank / CTAS) : 0;
     const int bt_cta = p.bt / CTAS;
-    const uint32_t x_bytes = (uint32_t)bt_cta * 128u, x_scale = (uint32_t)p.xa * kWScale;
+    const uint32_t x_bytes = (uint32_t)bt_cta * 128u, x_scale = (uint32_t)XA * kWScale;
     const uint32_t stage_bytes = kWBytes + x_bytes + kWScale + x_scale;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     // [weight codes][token codes] of all stages (1024-byte aligned), then their scales
@@ -193,7 +233,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     griddep_launch_dependents();
 
     const int accs = p.bt <= 128 ? 2 : 1, acc_cols = kScaleCols / accs;
-    const int slot_cols = kTiles * 4 * (1 + p.xa);           // TMEM columns of a stage's scales
+    const int slot_cols = kTiles * 4 * (1 + XA);             // TMEM columns of a stage's scales
     const int cluster = SPLIT ? p.split * CTAS : CTAS;
     const int unit0 = (int)blockIdx.x / cluster;
     const int kb0 = SPLIT ? p.kb * slice / p.split : 0, kb1 = SPLIT ? p.kb * (slice + 1) / p.split : p.kb;
@@ -259,7 +299,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             for (int unit = unit0; unit < p.units && ok; unit += p.unit_step) {
                 int m, n;
                 tile_of(unit, &m, &n);
-                const uint32_t idesc0 = instr_desc_fp4(kRows * CTAS, columns(m), NV);
+                const uint32_t idesc = instr_desc_fp4(kRows * CTAS, columns(m), NV);
                 ok = mbar_wait_all(smem_u32(&s_acc_empty[acc]), acc_phase ^ 1u, abort_flag, p.watchdog, kWdMmaAcc);
                 if (!ok) break;
                 const uint32_t d = tmem + (uint32_t)(acc * acc_cols);
@@ -267,29 +307,11 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                     ok = mbar_wait_all(smem_u32(&s_full[stage]), phase, abort_flag, p.watchdog, kWdMmaFull);
                     if (!ok) break;
                     tc_fence_after();
-                    if (elect_one()) {
-                        const uint32_t wcol = tmem + kScaleCols + (uint32_t)(stage * slot_cols), xcol = wcol + kTiles * 4;
-                        // (what lies past K's last scale tile is never multiplied: zeros times whatever a scale holds)
-                        const int steps = min(4, (p.K - kb * kStageK + 63) / 64);
-#pragma unroll
-                        for (int a = 0; a < kTiles; ++a) {
-                            copy_scales<CTAS>(wcol + a * 4, s_ws + stage * kWScale + a * 512);
-                            for (int x = 0; x < p.xa; ++x)
-                                copy_scales<CTAS>(xcol + (a * p.xa + x) * 4, s_xs + stage * x_scale + (x * kTiles + a) * 512);
-                        }
-                        const uint64_t wd = smem_desc_sw128(s_w + stage * kWBytes), xd = smem_desc_sw128(s_x + stage * x_bytes);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (j < steps) {
-                                const int a = NV ? j : j / 2;
-                                const uint32_t id = NV ? 0u : (uint32_t)(j & 1) * 2u;         // which two of a tile's four blocks
-                                mma_fp4<CTAS, NV>(d, wd + 2 * j, xd + 2 * j, idesc0 | id << 29 | id << 4, wcol + a * 4, xcol + a * p.xa * 4, kb != kb0 || j != 0);
-                            }
-                        }
-                        commit<CTAS>(smem_u32(&s_empty[stage]), mask);
-                        if (kb == kb1 - 1) commit<CTAS>(smem_u32(&s_acc_full[acc]), mask);
-                    }
-                    __syncwarp();
+                    // (what lies past K's last scale tile is never multiplied: zeros times whatever a scale holds)
+                    issue_stage<CTAS, NV, XA>(d, smem_desc_sw128(s_w + stage * kWBytes), smem_desc_sw128(s_x + stage * x_bytes), scale_desc(s_ws + stage * kWScale),
+                                              scale_desc(s_xs + stage * x_scale), tmem + kScaleCols + (uint32_t)(stage * slot_cols), idesc,
+                                              kb != kb0 ? 1u : 0u, (p.K - kb * kStageK + 63) / 64, smem_u32(&s_empty[stage]),
+                                              kb == kb1 - 1 ? smem_u32(&s_acc_full[acc]) : 0u, mask);
                     if (++stage == p.stages) { stage = 0; phase ^= 1u; }
                 }
                 if (++acc == accs) { acc = 0; acc_phase ^= 1u; }
@@ -481,19 +503,20 @@ Plan plan(int64_t M, int64_t N, int64_t K) {
     return r;
 }
 
-template <int CTAS, bool NV, bool SPLIT>
-cudaError_t launch(const CUtensorMap& w, const CUtensorMap& ws, const CUtensorMap& x, const CUtensorMap& xs, const CUtensorMap& y,
-                   const GemmParams& p, int grid, size_t smem, cudaStream_t stream) {
-    auto kern = gemm_fp4_kernel<CTAS, NV, SPLIT>;
+struct Maps {
+    CUtensorMap x, xs, y;
+};
+template <int CTAS, bool NV, bool SPLIT, int XA>
+cudaError_t launch(const Fp4Weights& W, const Maps& maps, const GemmParams& p, int grid, size_t smem, cudaStream_t stream) {
+    auto kern = gemm_fp4_kernel<CTAS, NV, SPLIT, XA>;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, (unsigned)(CTAS * p.split), w, ws, x, xs, y, p);
+    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, (unsigned)(CTAS * p.split), W.map_codes, W.map_scales, maps.x, maps.xs, maps.y, p);
 }
-template <int CTAS>
-cudaError_t launch(bool nv, bool split, const CUtensorMap& w, const CUtensorMap& ws, const CUtensorMap& x, const CUtensorMap& xs, const CUtensorMap& y,
-                   const GemmParams& p, int grid, size_t smem, cudaStream_t stream) {
-    if (nv) return split ? launch<CTAS, true, true>(w, ws, x, xs, y, p, grid, smem, stream) : launch<CTAS, true, false>(w, ws, x, xs, y, p, grid, smem, stream);
-    return split ? launch<CTAS, false, true>(w, ws, x, xs, y, p, grid, smem, stream) : launch<CTAS, false, false>(w, ws, x, xs, y, p, grid, smem, stream);
+template <int CTAS, int XA>
+cudaError_t launch(const Fp4Weights& W, const Maps& maps, const GemmParams& p, int grid, size_t smem, cudaStream_t stream) {
+    if (W.format == FQ_NVFP4) return p.split > 1 ? launch<CTAS, true, true, XA>(W, maps, p, grid, smem, stream) : launch<CTAS, true, false, XA>(W, maps, p, grid, smem, stream);
+    return p.split > 1 ? launch<CTAS, false, true, XA>(W, maps, p, grid, smem, stream) : launch<CTAS, false, false, XA>(W, maps, p, grid, smem, stream);
 }
 
 }  // namespace
@@ -513,7 +536,7 @@ fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const flo
     p.bt = r.bt;
     p.split = r.split;
     p.kb = (int)((W.K + kStageK - 1) / kStageK);
-    p.xa = (r.bt + 127) / 128;
+    const int xa = r.ctas == 2 || r.bt > 128 ? 2 : 1;
     p.m_tiles = (int)((M + r.bt - 1) / r.bt);
     p.n_tiles = (int)((W.N + kRows * r.ctas - 1) / (kRows * r.ctas));
     p.band = p.m_tiles >= 16 ? 8 : p.m_tiles;
@@ -523,26 +546,27 @@ fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const flo
     p.watchdog = watchdog_device_ptr();
     if (!p.watchdog) return FQ_ERR_CUDA;
     const int tiles = nv ? 4 : 2;
-    const size_t stage = (size_t)kRows * 128 + (size_t)(r.bt / r.ctas) * 128 + (size_t)tiles * 512 * (1 + p.xa);
-    const int slots = 256 / (tiles * 4 * (1 + p.xa));        // TMEM columns for scales
+    const size_t stage = (size_t)kRows * 128 + (size_t)(r.bt / r.ctas) * 128 + (size_t)tiles * 512 * (1 + xa);
+    const int slots = 256 / (tiles * 4 * (1 + xa));        // TMEM columns for scales
     p.stages = (int)((kSmemMost - 1024 - kOutBytes) / stage);
     if (p.stages > kMostStages) p.stages = kMostStages;
     if (p.stages > slots) p.stages = slots;
     const size_t smem = 1024 + stage * (size_t)p.stages + kOutBytes;
-    CUtensorMap x, xs;
-    if (!code_map(&x, codes, M, W.K, r.bt / r.ctas) || !scale_map(&xs, scales, M, W.K, W.format, p.xa)) return FQ_ERR_CUDA;
+    Maps maps;
+    if (!code_map(&maps.x, codes, M, W.K, r.bt / r.ctas) || !scale_map(&maps.xs, scales, M, W.K, W.format, xa)) return FQ_ERR_CUDA;
     // outputs in bf16 leave in boxes of [16 tokens][32 channels]
-    CUtensorMap map_y = x;
+    maps.y = maps.x;
     if (p.bf16) {
         const uint64_t dims[2] = {(uint64_t)W.N * 2, (uint64_t)M}, strides[1] = {(uint64_t)ldy * 2};
         const uint32_t box[2] = {64, 16};
-        if (!encode_tiled(&map_y, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, y, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_64B)) return FQ_ERR_CUDA;
+        if (!encode_tiled(&maps.y, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, y, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_64B)) return FQ_ERR_CUDA;
     }
     const int units = r.split > 1 ? p.units : (p.units < sms / r.ctas ? p.units : sms / r.ctas);
     p.unit_step = units;
     const int grid = units * r.ctas * r.split;
-    const cudaError_t e = r.ctas == 2 ? launch<2>(nv, r.split > 1, W.map_codes, W.map_scales, x, xs, map_y, p, grid, smem, stream)
-                                      : launch<1>(nv, r.split > 1, W.map_codes, W.map_scales, x, xs, map_y, p, grid, smem, stream);
+    const cudaError_t e = r.ctas == 2 ? launch<2, 2>(W, maps, p, grid, smem, stream)
+                          : xa == 2  ? launch<1, 2>(W, maps, p, grid, smem, stream)
+                                     : launch<1, 1>(W, maps, p, grid, smem, stream);
     return e == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
 }
 
