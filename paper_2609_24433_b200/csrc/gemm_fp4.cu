@@ -34,11 +34,12 @@ constexpr int kStageK = 256;             // channels of K a stage
 constexpr int kMostStages = 8;
 constexpr int kScaleCols = 256;          // TMEM columns from here on hold scales, those before accumulators
 constexpr size_t kSmemMost = 226 * 1024;
-constexpr size_t kOutBytes = kEpi * 2048;    // two output buffers for each epilogue warp
+constexpr int kOutBuffers = 4;           // of an epilogue warp, 1 KB each
+constexpr size_t kOutBytes = (size_t)kEpi * kOutBuffers * 1024;
 
 struct GemmParams {
     int64_t M, N, ldy;
-    int K, bt, stages, m_tiles, n_tiles, band;
+    int K, bt, stages, m_full, n_tiles, band;   // (m_full: token tiles of bt tokens)
     int split;                           // slices of K, each CTA (pair) of a cluster one
     int kb;                              // stages of all of K
     int units, unit_step;
@@ -237,9 +238,16 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     const int cluster = SPLIT ? p.split * CTAS : CTAS;
     const int unit0 = (int)blockIdx.x / cluster;
     const int kb0 = SPLIT ? p.kb * slice / p.split : 0, kb1 = SPLIT ? p.kb * (slice + 1) / p.split : p.kb;
-    // token tiles in bands, within a band channel tile by channel tile: what runs at a time covers a block of the output
+    // Token tiles in bands, within a band channel tile by channel tile: what runs at a time covers a block of the output.  A last
+    // token tile that is not full comes behind all others, where its shorter units even out what the CTAs have left.
     auto tile_of = [&](int unit, int* m, int* n) {
-        const int b = unit / (p.band * p.n_tiles), r = unit - b * (p.band * p.n_tiles), rows = min(p.band, p.m_tiles - b * p.band);
+        const int full = p.m_full * p.n_tiles;
+        if (unit >= full) {
+            *m = p.m_full;
+            *n = unit - full;
+            return;
+        }
+        const int b = unit / (p.band * p.n_tiles), r = unit - b * (p.band * p.n_tiles), rows = min(p.band, p.m_full - b * p.band);
         *m = b * p.band + r % rows;
         *n = r / rows;
     };
@@ -350,14 +358,14 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         const int from = 16 * (i & 1);
         if (p.bf16) {
             // scaled in pairs, stored token-major into 1 KB of [16 tokens][32 channels] (64-byte swizzle) by transposing matrix
-            // stores, and sent off as one bulk store, which clips what lies past M or N; two buffers alternate
+            // stores, and sent off as one bulk store, which clips what lies past M or N
             const int a = from + 2 * (lane & 3);
             const float2 d0 = make_float2(__shfl_sync(0xffffffffu, step, a), __shfl_sync(0xffffffffu, step, a + 1));
             const float2 d1 = make_float2(__shfl_sync(0xffffffffu, step, a + 8), __shfl_sync(0xffffffffu, step, a + 9));
             const uint32_t tok = (uint32_t)((lane >> 4) * 8 + (lane & 7)), ch = (uint32_t)((lane >> 3) & 1), mix = (tok >> 1) & 3u;
-            const uint32_t buf = s_out + (uint32_t)((warp - 2) * 2 + (stores & 1)) * 1024u;
-            if (stores >= 2) {
-                if (lane == 0) bulk_wait_read<1>();
+            const uint32_t buf = s_out + (uint32_t)((warp - 2) * kOutBuffers + stores % kOutBuffers) * 1024u;
+            if (stores >= kOutBuffers) {
+                if (lane == 0) bulk_wait_read<kOutBuffers - 1>();
                 __syncwarp();
             }
             stmatrix_x4_trans(buf + tok * 64u + ((ch ^ mix) << 4), scale_pair(r[0], r[1], d0, sw4[0], bj4[0]), scale_pair(r[2], r[3], d0, sw4[1], bj4[1]),
@@ -390,7 +398,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             tile_of(unit, &m, &n);
             const int64_t jq = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32, t0 = (int64_t)m * p.bt;
             constants(m, n);
-            ok = mbar_wait_warp_relaxed(smem_u32(&s_acc_full[acc]), phase, abort_flag, p.watchdog, kWdEpilogue);
+            ok = mbar_wait_all(smem_u32(&s_acc_full[acc]), phase, abort_flag, p.watchdog, kWdEpilogue);
             if (!ok) break;
             tc_fence_after();
             if (SPLIT) break;                                // one tile a cluster: below
@@ -537,10 +545,10 @@ fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const flo
     p.split = r.split;
     p.kb = (int)((W.K + kStageK - 1) / kStageK);
     const int xa = r.ctas == 2 || r.bt > 128 ? 2 : 1;
-    p.m_tiles = (int)((M + r.bt - 1) / r.bt);
+    p.m_full = (int)(M / r.bt);
     p.n_tiles = (int)((W.N + kRows * r.ctas - 1) / (kRows * r.ctas));
-    p.band = p.m_tiles >= 16 ? 8 : p.m_tiles;
-    p.units = p.m_tiles * p.n_tiles;
+    p.band = p.m_full >= 16 ? 8 : p.m_full > 0 ? p.m_full : 1;
+    p.units = (p.m_full + (M % r.bt ? 1 : 0)) * p.n_tiles;
     p.delta = delta; p.w_scale = W.w_scale; p.bias = W.bias;
     p.y = y; p.bf16 = yt == FQ_BF16;
     p.watchdog = watchdog_device_ptr();
