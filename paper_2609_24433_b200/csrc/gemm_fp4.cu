@@ -38,7 +38,7 @@ constexpr int kOutBuffers = 4;           // of an epilogue warp, 1 KB each
 constexpr size_t kOutBytes = (size_t)kEpi * kOutBuffers * 1024;
 
 struct GemmParams {
-    int64_t M, N, ldy;
+    int64_t M, N;
     int K, bt, stages, m_full, n_tiles, band;   // (m_full: token tiles of bt tokens)
     int split;                           // slices of K, each CTA (pair) of a cluster one
     int kb;                              // stages of all of K
@@ -46,7 +46,6 @@ struct GemmParams {
     const float* delta;
     const float* w_scale;
     const float* bias;
-    void* y;
     int bf16;
     uint32_t* watchdog;
 };
@@ -381,13 +380,24 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             }
             ++stores;
         } else {
-            float* y = static_cast<float*>(p.y) + tc * p.ldy + jq + lane;
-            const bool j_ok = jq + lane < p.N;
+            // [16 tokens][32 channels] of 2 KB
+            const uint32_t buf = s_out + (uint32_t)((warp - 2) * kOutBuffers + stores % (kOutBuffers / 2) * 2) * 1024u;
+            if (stores >= kOutBuffers / 2) {
+                if (lane == 0) bulk_wait_read<kOutBuffers / 2 - 1>();
+                __syncwarp();
+            }
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
                 const float d = __shfl_sync(0xffffffffu, step, from + k);
-                if (tc + k < p.M && j_ok) y[k * p.ldy] = __fmaf_rn(__uint_as_float(r[k]), d * sw4[0], bj4[0]);
+                sts32(buf + (uint32_t)(k * 128 + lane * 4), __float_as_uint(__fmaf_rn(__uint_as_float(r[k]), d * sw4[0], bj4[0])));
             }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0 && jq < p.N) {
+                tma_store_2d(&map_y, (int)(jq * 4), (int)tc, buf);
+                bulk_commit();
+            }
+            ++stores;
         }
     };
     if (warp >= 2) {
@@ -469,7 +479,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         }
     }
     // the stores have read their buffers before the CTA gives up its shared memory
-    if (warp >= 2 && p.bf16 && lane == 0) bulk_wait_read<0>();
+    if (warp >= 2 && lane == 0) bulk_wait_read<0>();
     __syncwarp();
     tc_fence_before();
     __syncthreads();
@@ -540,7 +550,7 @@ fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const flo
     const Plan r = plan(M, W.N, W.K);
     const bool nv = W.format == FQ_NVFP4;
     GemmParams p = {};
-    p.M = M; p.N = W.N; p.K = (int)W.K; p.ldy = ldy;
+    p.M = M; p.N = W.N; p.K = (int)W.K;
     p.bt = r.bt;
     p.split = r.split;
     p.kb = (int)((W.K + kStageK - 1) / kStageK);
@@ -550,7 +560,7 @@ fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const flo
     p.band = p.m_full >= 16 ? 8 : p.m_full > 0 ? p.m_full : 1;
     p.units = (p.m_full + (M % r.bt ? 1 : 0)) * p.n_tiles;
     p.delta = delta; p.w_scale = W.w_scale; p.bias = W.bias;
-    p.y = y; p.bf16 = yt == FQ_BF16;
+    p.bf16 = yt == FQ_BF16;
     p.watchdog = watchdog_device_ptr();
     if (!p.watchdog) return FQ_ERR_CUDA;
     const int tiles = nv ? 4 : 2;
@@ -562,12 +572,12 @@ fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const flo
     const size_t smem = 1024 + stage * (size_t)p.stages + kOutBytes;
     Maps maps;
     if (!code_map(&maps.x, codes, M, W.K, r.bt / r.ctas) || !scale_map(&maps.xs, scales, M, W.K, W.format, xa)) return FQ_ERR_CUDA;
-    // outputs in bf16 leave in boxes of [16 tokens][32 channels]
-    maps.y = maps.x;
-    if (p.bf16) {
-        const uint64_t dims[2] = {(uint64_t)W.N * 2, (uint64_t)M}, strides[1] = {(uint64_t)ldy * 2};
-        const uint32_t box[2] = {64, 16};
-        if (!encode_tiled(&maps.y, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, y, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_64B)) return FQ_ERR_CUDA;
+    {   // outputs leave in boxes of [16 tokens][32 channels]
+        const int e = p.bf16 ? 2 : 4;
+        const uint64_t dims[2] = {(uint64_t)W.N * e, (uint64_t)M}, strides[1] = {(uint64_t)ldy * e};
+        const uint32_t box[2] = {32u * e, 16};
+        if (!encode_tiled(&maps.y, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, y, dims, strides, box, p.bf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE))
+            return FQ_ERR_CUDA;
     }
     const int units = r.split > 1 ? p.units : (p.units < sms / r.ctas ? p.units : sms / r.ctas);
     p.unit_step = units;
