@@ -12,7 +12,7 @@
 // ahead of the stage's MMAs.  Their TMEM columns go by the stage, so that whoever refills a stage knows that the MMAs that
 // read them have ended.
 //
-// Roles: warp 0 TMA producer, warp 1 MMA issuer and TMEM allocator, warps 2-9 epilogue.
+// Roles: warp 0 producer of weights, warp 1 MMA issuer and TMEM allocator, warps 2-9 epilogue, warp 10 producer of tokens.
 // CTAS = 2: a pair works on 256 channels, each CTA loading its 128 weight rows and half of the tokens' codes, but the scales of
 // all tokens.  SPLIT: the CTAs (or pairs) of a cluster share one tile along K and exchange binary32 sums through the cluster's
 // shared memory, added in the order of the slices: the result does not depend on timing.
@@ -27,30 +27,38 @@
 namespace fq {
 namespace {
 
-constexpr int kThreads = 320;
-constexpr int kEpi = 8;                  // epilogue warps
+constexpr int kEpi = 16;                 // epilogue warps, from warp 2 on
+constexpr int kSets = kEpi / 4;          // of them to a quadrant of lanes
+constexpr int kChunks = 16 / kSets;      // chunks of 16 tokens of a warp at most
+constexpr int kTokenWarp = 2 + kEpi;
+constexpr int kThreads = 32 * (kTokenWarp + 1);
 constexpr int kRows = 128;               // channels of a CTA's tile
 constexpr int kStageK = 256;             // channels of K a stage
 constexpr int kMostStages = 8;
 constexpr int kScaleCols = 256;          // TMEM columns from here on hold scales, those before accumulators
-constexpr size_t kSmemMost = 226 * 1024;
-constexpr int kOutBuffers = 4;           // of an epilogue warp, 1 KB each
-constexpr size_t kOutBytes = (size_t)kEpi * kOutBuffers * 1024;
+constexpr size_t kSmemMost = 224 * 1024; // (and 2.3 KB of static shared memory)
+constexpr uint32_t kOutBytesWarp = 2048; // outputs of an epilogue warp on their way out: 16 tokens x 32 channels
+constexpr uint32_t kOutBytes = kEpi * kOutBytesWarp;
+constexpr size_t kRingMost = kSmemMost - 1024 - kOutBytes;       // stages, and what slices of K receive
 
 struct GemmParams {
-    int64_t M, N;
+    int64_t M, N, ldy;
     int K, bt, stages, m_full, n_tiles, band;   // (m_full: token tiles of bt tokens)
     int split;                           // slices of K, each CTA (pair) of a cluster one
     int kb;                              // stages of all of K
     int units, unit_step;
+    uint32_t ring;                       // bytes of the stages, a multiple of 1024
+    int per;                             // SPLIT: chunks that a slice finishes
+    int shared_ring;                     // SPLIT: sums are received where the stages were
     const float* delta;
     const float* w_scale;
     const float* bias;
+    void* y;
     int bf16;
     uint32_t* watchdog;
 };
 
-enum : uint32_t { kWdProducer = 1u, kWdMmaFull = 2u, kWdMmaAcc = 4u, kWdEpilogue = 8u };
+enum : uint32_t { kWdProducer = 1u, kWdMmaFull = 2u, kWdMmaAcc = 4u, kWdEpilogue = 8u, kWdSums = 128u };
 
 template <int CTAS>
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
@@ -76,11 +84,14 @@ __device__ __forceinline__ void tma_load_tiles(uint32_t dst, const CUtensorMap* 
             ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(tile), "r"(rows), "r"(bar & 0xFEFFFFFFu)
             : "memory");
 }
+// Arrival at the barrier of another CTA of the cluster, which orders no memory: what it announces are loads that have returned and
+// MMAs that have ended.  (With a release ahead of it, which waits for the warp's stores, the tensor cores stood still 1200 cycles longer
+// between two tiles.)
 __device__ __forceinline__ void mbar_arrive_cta(uint32_t bar, uint32_t rank) {
     asm volatile(
         "{\n\t.reg .b32 ra;\n\t"
         "mapa.shared::cluster.u32 ra, %0, %1;\n\t"
-        "mbarrier.arrive.shared::cluster.b64 _, [ra];\n\t}"
+        "mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [ra];\n\t}"
         ::"r"(bar), "r"(rank)
         : "memory");
 }
@@ -112,26 +123,38 @@ __device__ __forceinline__ void mbar_arrive_cta(uint32_t bar, uint32_t rank) {
 #define FQ_KIND_NV "kind::mxf4nvf4.block_scale.scale_vec::4X"
 #define FQ_KIND_MX "kind::mxf4.block_scale.scale_vec::2X"
 #define FQ_ID_ODD "1073741856"           /* blocks 2 and 3 of a scale tile, both operands: 2 << 29 | 2 << 4 */
-#define FQ_STAGE_NV1(CG)                                                                                                          \
-    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "16") FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "20")                     \
-    FQ_CP(CG, "%3", "64", "8") FQ_CP(CG, "%4", "64", "24") FQ_CP(CG, "%3", "96", "12") FQ_CP(CG, "%4", "96", "28")                  \
-    FQ_MMA(CG, FQ_KIND_NV, "0", "0", "16", "0", "pl", "pa") FQ_MMA(CG, FQ_KIND_NV, "2", "4", "20", "0", "p1", "pt")                 \
-    FQ_MMA(CG, FQ_KIND_NV, "4", "8", "24", "0", "p2", "pt") FQ_MMA(CG, FQ_KIND_NV, "6", "12", "28", "0", "p3", "pt")
-#define FQ_STAGE_NV2(CG)                                                                                                          \
-    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "16") FQ_CP(CG, "%4", "128", "20") FQ_CP(CG, "%3", "32", "4")                    \
-    FQ_CP(CG, "%4", "32", "24") FQ_CP(CG, "%4", "160", "28") FQ_CP(CG, "%3", "64", "8") FQ_CP(CG, "%4", "64", "32")                 \
-    FQ_CP(CG, "%4", "192", "36") FQ_CP(CG, "%3", "96", "12") FQ_CP(CG, "%4", "96", "40") FQ_CP(CG, "%4", "224", "44")               \
-    FQ_MMA(CG, FQ_KIND_NV, "0", "0", "16", "0", "pl", "pa") FQ_MMA(CG, FQ_KIND_NV, "2", "4", "24", "0", "p1", "pt")                 \
-    FQ_MMA(CG, FQ_KIND_NV, "4", "8", "32", "0", "p2", "pt") FQ_MMA(CG, FQ_KIND_NV, "6", "12", "40", "0", "p3", "pt")
-#define FQ_STAGE_MX1(CG)                                                                                                          \
-    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "8") FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "12")                      \
-    FQ_MMA(CG, FQ_KIND_MX, "0", "0", "8", "0", "pl", "pa") FQ_MMA(CG, FQ_KIND_MX, "2", "0", "8", FQ_ID_ODD, "p1", "pt")             \
-    FQ_MMA(CG, FQ_KIND_MX, "4", "4", "12", "0", "p2", "pt") FQ_MMA(CG, FQ_KIND_MX, "6", "4", "12", FQ_ID_ODD, "p3", "pt")
-#define FQ_STAGE_MX2(CG)                                                                                                          \
-    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "8") FQ_CP(CG, "%4", "64", "12")                                                 \
-    FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "16") FQ_CP(CG, "%4", "96", "20")                                              \
-    FQ_MMA(CG, FQ_KIND_MX, "0", "0", "8", "0", "pl", "pa") FQ_MMA(CG, FQ_KIND_MX, "2", "0", "8", FQ_ID_ODD, "p1", "pt")             \
-    FQ_MMA(CG, FQ_KIND_MX, "4", "4", "16", "0", "p2", "pt") FQ_MMA(CG, FQ_KIND_MX, "6", "4", "16", FQ_ID_ODD, "p3", "pt")
+#define FQ_STAGE_NV1(CG) \
+    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "16") \
+    FQ_MMA(CG, FQ_KIND_NV, "0", "0", "16", "0", "pl", "pa") \
+    FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "20") \
+    FQ_MMA(CG, FQ_KIND_NV, "2", "4", "20", "0", "p1", "pt") \
+    FQ_CP(CG, "%3", "64", "8") FQ_CP(CG, "%4", "64", "24") \
+    FQ_MMA(CG, FQ_KIND_NV, "4", "8", "24", "0", "p2", "pt") \
+    FQ_CP(CG, "%3", "96", "12") FQ_CP(CG, "%4", "96", "28") \
+    FQ_MMA(CG, FQ_KIND_NV, "6", "12", "28", "0", "p3", "pt")
+#define FQ_STAGE_NV2(CG) \
+    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "16") FQ_CP(CG, "%4", "128", "20") \
+    FQ_MMA(CG, FQ_KIND_NV, "0", "0", "16", "0", "pl", "pa") \
+    FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "24") FQ_CP(CG, "%4", "160", "28") \
+    FQ_MMA(CG, FQ_KIND_NV, "2", "4", "24", "0", "p1", "pt") \
+    FQ_CP(CG, "%3", "64", "8") FQ_CP(CG, "%4", "64", "32") FQ_CP(CG, "%4", "192", "36") \
+    FQ_MMA(CG, FQ_KIND_NV, "4", "8", "32", "0", "p2", "pt") \
+    FQ_CP(CG, "%3", "96", "12") FQ_CP(CG, "%4", "96", "40") FQ_CP(CG, "%4", "224", "44") \
+    FQ_MMA(CG, FQ_KIND_NV, "6", "12", "40", "0", "p3", "pt")
+#define FQ_STAGE_MX1(CG) \
+    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "8") \
+    FQ_MMA(CG, FQ_KIND_MX, "0", "0", "8", "0", "pl", "pa") \
+    FQ_MMA(CG, FQ_KIND_MX, "2", "0", "8", FQ_ID_ODD, "p1", "pt") \
+    FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "12") \
+    FQ_MMA(CG, FQ_KIND_MX, "4", "4", "12", "0", "p2", "pt") \
+    FQ_MMA(CG, FQ_KIND_MX, "6", "4", "12", FQ_ID_ODD, "p3", "pt")
+#define FQ_STAGE_MX2(CG) \
+    FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "8") FQ_CP(CG, "%4", "64", "12") \
+    FQ_MMA(CG, FQ_KIND_MX, "0", "0", "8", "0", "pl", "pa") \
+    FQ_MMA(CG, FQ_KIND_MX, "2", "0", "8", FQ_ID_ODD, "p1", "pt") \
+    FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "16") FQ_CP(CG, "%4", "96", "20") \
+    FQ_MMA(CG, FQ_KIND_MX, "4", "4", "16", "0", "p2", "pt") \
+    FQ_MMA(CG, FQ_KIND_MX, "6", "4", "16", FQ_ID_ODD, "p3", "pt")
 template <int CTAS, bool NV, int XA>
 __device__ __forceinline__ void issue_stage(uint32_t d, uint64_t wd, uint64_t xd, uint64_t ws, uint64_t xs, uint32_t cols, uint32_t idesc, uint32_t accumulate,
                                             int steps, uint32_t bar_stage, uint32_t bar_acc, uint16_t mask) {
@@ -165,13 +188,7 @@ __device__ __forceinline__ void tmem_ld_16x256b_x2(uint32_t taddr, uint32_t* r) 
 }
 __device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3) {
     asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
-                 ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3)
-                 : "memory");
-}
-__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int c0, int c1, uint32_t src) {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
-                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(src)
-                 : "memory");
+                 ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3));
 }
 // One channel at two adjacent tokens, rounded to bf16, the earlier token in the low half.
 __device__ __forceinline__ uint32_t scale_pair(uint32_t a0, uint32_t a1, float2 d, float sw, float bj) {
@@ -180,17 +197,26 @@ __device__ __forceinline__ uint32_t scale_pair(uint32_t a0, uint32_t a1, float2 
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w) : "f"(v.y), "f"(v.x));
     return w;
 }
-__device__ __forceinline__ void st_cluster_v4(uint32_t addr, const uint32_t* r) {
-    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+// 16 bytes into another CTA's shared memory, counted on a barrier there.
+__device__ __forceinline__ void st_async_v4(uint32_t addr, const uint32_t* r, uint32_t bar) {
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v4.b32 [%0], {%1, %2, %3, %4}, [%5];"
+                 ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(bar)
+                 : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
+// (no memory clobber, as the matrix stores: the fence behind them orders them)
+__device__ __forceinline__ void sts32_loose(uint32_t addr, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;" ::"r"(addr), "r"(v)); }
 
 // XA: scale tiles across a tile's tokens (two for more than 128, and for pairs).
 template <int CTAS, bool NV, bool SPLIT, int XA>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_x,
-                const __grid_constant__ CUtensorMap map_xs, const __grid_constant__ CUtensorMap map_y, const GemmParams p) {
+                const __grid_constant__ CUtensorMap map_xs, const GemmParams p) {
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t s_full[kMostStages], s_empty[kMostStages], s_acc_full[2], s_acc_empty[2];
+    __shared__ uint64_t s_full[kMostStages], s_empty[kMostStages], s_acc_full[2], s_acc_empty[2], s_ended, s_sums;
+    __shared__ __align__(16) float s_steps[kEpi][32];        // of the tokens that each epilogue warp is at
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
     constexpr int kTiles = NV ? 4 : 2;                       // scale tiles of a stage's 256 channels
@@ -202,35 +228,11 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     const uint32_t half = CTAS == 2 ? rank & 1u : 0u, pair_base = rank & ~1u;
     const bool leader = half == 0;
     const int slice = SPLIT ? (int)(rank / CTAS) : 0;
-    const int bt_cta = p.bt / CTAS;
-    const uint32_t x_bytes = (uint32_t)bt_cta * 128u, x_scale = (uint32_t)XA * kWScale;
-    const uint32_t stage_bytes = kWBytes + x_bytes + kWScale + x_scale;
+    const uint32_t x_bytes = (uint32_t)(p.bt / CTAS) * 128u, x_scale = (uint32_t)XA * kWScale;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     // [weight codes][token codes] of all stages (1024-byte aligned), then their scales
     const uint32_t s_w = base, s_x = s_w + (uint32_t)p.stages * kWBytes, s_ws = s_x + (uint32_t)p.stages * x_bytes, s_xs = s_ws + (uint32_t)p.stages * kWScale,
-                   s_out = s_xs + (uint32_t)p.stages * x_scale;
-
-    if (threadIdx.x == 0) {
-        s_abort = 0;
-        for (int s = 0; s < p.stages; ++s) {
-            mbar_init(smem_u32(&s_full[s]), 1);
-            mbar_init(smem_u32(&s_empty[s]), 1);
-        }
-        for (int a = 0; a < 2; ++a) {
-            mbar_init(smem_u32(&s_acc_full[a]), 1);
-            mbar_init(smem_u32(&s_acc_empty[a]), kEpi * CTAS);
-        }
-        fence_mbarrier_init();
-        fence_proxy_async_smem();
-    }
-    if (warp == 1) tmem_alloc<CTAS>(smem_u32(&s_tmem), 512u);
-    tc_fence_before();
-    __syncthreads();
-    if (CTAS == 2 || SPLIT) cluster_sync_all();              // the other CTAs' barriers exist
-    tc_fence_after();
-    const uint32_t tmem = s_tmem;
-    if (warp >= 2) griddep_wait();                           // (the producer waits ahead of the tokens' first copy)
-    griddep_launch_dependents();
+                   s_out = base + p.ring;
 
     const int accs = p.bt <= 128 ? 2 : 1, acc_cols = kScaleCols / accs;
     const int slot_cols = kTiles * 4 * (1 + XA);             // TMEM columns of a stage's scales
@@ -254,44 +256,85 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         const int64_t left = p.M - (int64_t)m * p.bt;
         return left >= p.bt ? p.bt : ((int)left + 16 * CTAS - 1) / (16 * CTAS) * (16 * CTAS);
     };
-
-    if (warp == 0) {
-        // ------------------------------------------------------------ producer
-        bool ok = true;
-        int stage = 0;
-        uint32_t phase = 0;
-        // a weight handle is complete before the call: its first stages come while the kernel ahead still runs
-        int ahead = 0;
-        auto weights = [&](int n, int kb, int s) {
-            const uint32_t bar = smem_u32(&s_full[s]);
-            if (leader) mbar_arrive_expect_tx(bar, stage_bytes * CTAS);
-            tma_load<CTAS>(s_w + s * kWBytes, &map_w, kb * 128, (n * CTAS + (int)half) * kRows, bar);
-            tma_load_tiles<CTAS>(s_ws + s * kWScale, &map_ws, kb * kTiles, n * CTAS + (int)half, bar);
-        };
-        if (unit0 < p.units) {
+    auto load_weights = [&](int n, int kb, int s) {
+        const uint32_t bar = smem_u32(&s_full[s]);
+        if (leader) mbar_arrive_expect_tx(bar, (kWBytes + kWScale) * CTAS);
+        tma_load<CTAS>(s_w + s * kWBytes, &map_w, kb * 128, (n * CTAS + (int)half) * kRows, bar);
+        tma_load_tiles<CTAS>(s_ws + s * kWScale, &map_ws, kb * kTiles, n * CTAS + (int)half, bar);
+    };
+    // A weight handle is complete before the call: its first stages come while the kernel ahead still runs, and (single CTAs, whose
+    // loads concern nobody else) while this one is being set up.
+    const int ahead = unit0 < p.units ? min(p.stages, kb1 - kb0) : 0;
+    auto first_weights = [&]() {
+        if (ahead > 0 && elect_one()) {
             int m, n;
             tile_of(unit0, &m, &n);
-            ahead = min(p.stages, kb1 - kb0);
-            if (elect_one())
-                for (int i = 0; i < ahead; ++i) weights(n, kb0 + i, i);
-            __syncwarp();
+            for (int i = 0; i < ahead; ++i) load_weights(n, kb0 + i, i);
         }
-        griddep_wait();
+        __syncwarp();
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            s_abort = 0;
+            for (int s = 0; s < p.stages; ++s) {
+                mbar_init(smem_u32(&s_full[s]), 2);          // both producers
+                mbar_init(smem_u32(&s_empty[s]), 1);
+            }
+            for (int a = 0; a < 2; ++a) {
+                mbar_init(smem_u32(&s_acc_full[a]), 1);
+                mbar_init(smem_u32(&s_acc_empty[a]), kEpi * CTAS);
+            }
+            mbar_init(smem_u32(&s_ended), (uint32_t)p.split);
+            mbar_init(smem_u32(&s_sums), 1);
+            fence_mbarrier_init();
+            fence_proxy_async_smem();
+        }
+        __syncwarp();
+        if (CTAS == 1) first_weights();
+    } else if (warp == 1) {
+        tmem_alloc<CTAS>(smem_u32(&s_tmem), 512u);
+    } else if (warp == kTokenWarp && lane == 0) {
+        prefetch_map(&map_x);
+        prefetch_map(&map_xs);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (CTAS == 2) cluster_sync_all();                       // the other CTAs' barriers exist
+    else if (SPLIT) cluster_arrive();                        // (awaited ahead of the first word to another CTA)
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    if (warp >= 2) griddep_wait();
+    griddep_launch_dependents();
+
+    if (warp == 0 || warp == kTokenWarp) {
+        // ------------------------------------------------------------ producers: of weights, of tokens
+        if (CTAS == 2 && warp == 0) first_weights();
+        bool ok = true;
+        int stage = 0, there = warp == 0 ? ahead : 0;
+        uint32_t phase = 0;
         for (int unit = unit0; unit < p.units && ok; unit += p.unit_step) {
             int m, n;
             tile_of(unit, &m, &n);
             const int t0 = m * p.bt + (int)half * (columns(m) / CTAS);
             for (int kb = kb0; kb < kb1; ++kb) {
-                ok = mbar_wait_all_lazy(smem_u32(&s_empty[stage]), phase ^ 1u, abort_flag, p.watchdog, kWdProducer);
-                if (!ok) break;
-                if (elect_one()) {
-                    const uint32_t bar = smem_u32(&s_full[stage]);
-                    if (ahead == 0) weights(n, kb, stage);
-                    tma_load<CTAS>(s_x + stage * x_bytes, &map_x, kb * 128, t0, bar);
-                    tma_load_tiles<CTAS>(s_xs + stage * x_scale, &map_xs, kb * kTiles, m * (p.bt / 128), bar);
+                if (there > 0) {
+                    --there;
+                } else {
+                    ok = mbar_wait_all_lazy(smem_u32(&s_empty[stage]), phase ^ 1u, abort_flag, p.watchdog, kWdProducer);
+                    if (!ok) break;
+                    if (elect_one()) {
+                        if (warp == 0) {
+                            load_weights(n, kb, stage);
+                        } else {
+                            const uint32_t bar = smem_u32(&s_full[stage]);
+                            if (leader) mbar_arrive_expect_tx(bar, (x_bytes + x_scale) * CTAS);
+                            tma_load<CTAS>(s_x + stage * x_bytes, &map_x, kb * 128, t0, bar);
+                            tma_load_tiles<CTAS>(s_xs + stage * x_scale, &map_xs, kb * kTiles, m * (p.bt / 128), bar);
+                        }
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
-                if (ahead > 0) --ahead;
                 if (++stage == p.stages) { stage = 0; phase ^= 1u; }
             }
         }
@@ -324,166 +367,187 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 if (++acc == accs) { acc = 0; acc_phase ^= 1u; }
             }
         }
-    }
-    // ------------------------------------------------------------ epilogue
-    // Two warps to a quadrant of lanes, alternating chunks of 16 tokens: chunk n of a warp begins at token (set + 2n) * 16.
-    const int quad = warp & 3, set = (warp - 2) >> 2;
-    const uint32_t lanes = (uint32_t)(quad * 32) << 16;
-    bool ok = true;
-    float steps[4], sw4[4], bj4[4];          // steps of the warp's tokens: lanes 16 (n & 1) .. of steps[n / 2]
-    int stores = 0;
-    auto constants = [&](int m, int n) {
-        const int64_t jq = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32, t0 = (int64_t)m * p.bt;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int t = (set + 2 * (2 * i + (lane >> 4))) * 16 + (lane & 15);
-            steps[i] = t < p.bt && t0 + t < p.M ? ld_global_f32(p.delta + t0 + t) : 0.0f;
-            const int64_t j = jq + (p.bf16 ? (lane >> 2) + 8 * i : lane);       // bf16: the channels of this thread's fragments
-            sw4[i] = j < p.N ? __ldg(p.w_scale + j) : 0.0f;
-            bj4[i] = j < p.N ? __ldg(p.bias + j) : 0.0f;
-        }
-    };
-    // Sums of one chunk, as fragments for bf16 outputs (channels 0..15, 16..31 of the quadrant), else a thread one channel.
-    auto fetch = [&](uint32_t column, uint32_t* r) {
-        if (p.bf16) {
-            tmem_ld_16x256b_x2(tmem + lanes + column, r);
-            tmem_ld_16x256b_x2(tmem + lanes + (16u << 16) + column, r + 8);
-        } else {
-            tmem_ld16(tmem + lanes + column, r);
-        }
-    };
-    auto emit = [&](const uint32_t* r, int i, int64_t tc, int64_t jq) {
-        const float step = i < 2 ? steps[0] : i < 4 ? steps[1] : i < 6 ? steps[2] : steps[3];
-        const int from = 16 * (i & 1);
-        if (p.bf16) {
-            // scaled in pairs, stored token-major into 1 KB of [16 tokens][32 channels] (64-byte swizzle) by transposing matrix
-            // stores, and sent off as one bulk store, which clips what lies past M or N
-            const int a = from + 2 * (lane & 3);
-            const float2 d0 = make_float2(__shfl_sync(0xffffffffu, step, a), __shfl_sync(0xffffffffu, step, a + 1));
-            const float2 d1 = make_float2(__shfl_sync(0xffffffffu, step, a + 8), __shfl_sync(0xffffffffu, step, a + 9));
-            const uint32_t tok = (uint32_t)((lane >> 4) * 8 + (lane & 7)), ch = (uint32_t)((lane >> 3) & 1), mix = (tok >> 1) & 3u;
-            const uint32_t buf = s_out + (uint32_t)((warp - 2) * kOutBuffers + stores % kOutBuffers) * 1024u;
-            if (stores >= kOutBuffers) {
-                if (lane == 0) bulk_wait_read<kOutBuffers - 1>();
-                __syncwarp();
-            }
-            stmatrix_x4_trans(buf + tok * 64u + ((ch ^ mix) << 4), scale_pair(r[0], r[1], d0, sw4[0], bj4[0]), scale_pair(r[2], r[3], d0, sw4[1], bj4[1]),
-                              scale_pair(r[4], r[5], d1, sw4[0], bj4[0]), scale_pair(r[6], r[7], d1, sw4[1], bj4[1]));
-            stmatrix_x4_trans(buf + tok * 64u + (((ch + 2u) ^ mix) << 4), scale_pair(r[8], r[9], d0, sw4[2], bj4[2]),
-                              scale_pair(r[10], r[11], d0, sw4[3], bj4[3]), scale_pair(r[12], r[13], d1, sw4[2], bj4[2]),
-                              scale_pair(r[14], r[15], d1, sw4[3], bj4[3]));
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0 && jq < p.N) {
-                tma_store_2d(&map_y, (int)(jq * 2), (int)tc, buf);
-                bulk_commit();
-            }
-            ++stores;
-        } else {
-            // [16 tokens][32 channels] of 2 KB
-            const uint32_t buf = s_out + (uint32_t)((warp - 2) * kOutBuffers + stores % (kOutBuffers / 2) * 2) * 1024u;
-            if (stores >= kOutBuffers / 2) {
-                if (lane == 0) bulk_wait_read<kOutBuffers / 2 - 1>();
-                __syncwarp();
-            }
-#pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                const float d = __shfl_sync(0xffffffffu, step, from + k);
-                sts32(buf + (uint32_t)(k * 128 + lane * 4), __float_as_uint(__fmaf_rn(__uint_as_float(r[k]), d * sw4[0], bj4[0])));
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0 && jq < p.N) {
-                tma_store_2d(&map_y, (int)(jq * 4), (int)tc, buf);
-                bulk_commit();
-            }
-            ++stores;
-        }
-    };
-    if (warp >= 2) {
-        int acc = 0;
-        uint32_t phase = 0;
-        for (int unit = unit0; unit < p.units; unit += p.unit_step) {
-            int m, n;
-            tile_of(unit, &m, &n);
+    } else {
+        // ------------------------------------------------------------ epilogue
+        // kSets warps to a quadrant of lanes, alternating chunks of 16 tokens: chunk i of set s begins at token (s + kSets i) * 16.
+        const int quad = warp & 3, set = (warp - 2) >> 2;
+        const uint32_t lanes = (uint32_t)(quad * 32) << 16;
+        float* const steps = s_steps[warp - 2];
+        auto token = [&](int i) { return (set + kSets * i) * 16; };
+        bool ok = true;
+        float sw4[4], bj4[4], step2[kChunks / 2];        // step2[k]: steps of chunks 2k and 2k + 1, a lane each
+        auto constants = [&](int m, int n) {
             const int64_t jq = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32, t0 = (int64_t)m * p.bt;
-            constants(m, n);
-            ok = mbar_wait_all(smem_u32(&s_acc_full[acc]), phase, abort_flag, p.watchdog, kWdEpilogue);
-            if (!ok) break;
-            tc_fence_after();
-            if (SPLIT) break;                                // one tile a cluster: below
-            // all of the warp's sums into registers, so that the next tile's MMAs may have the columns
-            const int cols = columns(m);
-            uint32_t r[8][16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if ((set + 2 * i) * 16 < cols) fetch((uint32_t)(acc * acc_cols + (set + 2 * i) * 16), r[i]);
-            tmem_ld_wait();
-            tc_fence_before();
+            for (int i = 0; i < kChunks / 2; ++i) {
+                const int t = token(2 * i + (lane >> 4)) + (lane & 15);
+                step2[i] = t < p.bt && t0 + t < p.M ? ld_global_f32(p.delta + t0 + t) : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t j = jq + (p.bf16 ? (lane >> 2) + 8 * i : lane);       // bf16: the channels of this thread's fragments
+                sw4[i] = j < p.N ? __ldg(p.w_scale + j) : 0.0f;
+                bj4[i] = j < p.N ? __ldg(p.bias + j) : 0.0f;
+            }
+        };
+        // Sums of one chunk, as fragments for bf16 outputs (channels 0..15, 16..31 of the quadrant), else a thread one channel.
+        auto fetch = [&](uint32_t column, uint32_t* r) {
+            if (p.bf16) {
+                tmem_ld_16x256b_x2(tmem + lanes + column, r);
+                tmem_ld_16x256b_x2(tmem + lanes + (16u << 16) + column, r + 8);
+            } else {
+                tmem_ld16(tmem + lanes + column, r);
+            }
+        };
+        // Outputs of chunk i, token-major through the warp's own shared memory, then 16 bytes a lane.  (Bulk stores queue behind the
+        // loads of the stages: waiting for one to have read its buffer took 1000 cycles a chunk.)
+        auto emit = [&](const uint32_t* r, int i, int64_t t0, int64_t jq) {
+            const uint32_t buf = s_out + (uint32_t)(warp - 2) * kOutBytesWarp;
             __syncwarp();
-            if (lane == 0) {
-                if (CTAS == 1) mbar_arrive(smem_u32(&s_acc_empty[acc]));
-                else mbar_arrive_cta(smem_u32(&s_acc_empty[acc]), pair_base);
+            if ((i & 1) == 0 || SPLIT) {
+                float st = step2[0];
+#pragma unroll
+                for (int k = 1; k < kChunks / 2; ++k) st = i / 2 == k ? step2[k] : st;
+                steps[lane] = st;
+                __syncwarp();
             }
+            const float* const st = steps + (i & 1) * 16;
+            const int64_t tc = t0 + token(i);
+            if (p.bf16) {
+                // scaled in pairs, [16 tokens][32 channels] by transposing matrix stores (16-byte pieces of a row mixed by token / 2)
+                const float2 d0 = *reinterpret_cast<const float2*>(st + 2 * (lane & 3)), d1 = *reinterpret_cast<const float2*>(st + 8 + 2 * (lane & 3));
+                const uint32_t tok = (uint32_t)((lane >> 4) * 8 + (lane & 7)), ch = (uint32_t)((lane >> 3) & 1), mix = (tok >> 1) & 3u;
+                const uint32_t to = buf + tok * 64u;
+                stmatrix_x4_trans(to + ((ch ^ mix) << 4), scale_pair(r[0], r[1], d0, sw4[0], bj4[0]), scale_pair(r[2], r[3], d0, sw4[1], bj4[1]),
+                                  scale_pair(r[4], r[5], d1, sw4[0], bj4[0]), scale_pair(r[6], r[7], d1, sw4[1], bj4[1]));
+                stmatrix_x4_trans(to + (((ch + 2u) ^ mix) << 4), scale_pair(r[8], r[9], d0, sw4[2], bj4[2]), scale_pair(r[10], r[11], d0, sw4[3], bj4[3]),
+                                  scale_pair(r[12], r[13], d1, sw4[2], bj4[2]), scale_pair(r[14], r[15], d1, sw4[3], bj4[3]));
+                __syncwarp();
+                const int row = lane >> 2, piece = lane & 3;
+                __nv_bfloat16* y = static_cast<__nv_bfloat16*>(p.y) + (tc + row) * p.ldy + jq + piece * 8;
+                const bool j_ok = jq + piece * 8 < p.N;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if ((set + 2 * i) * 16 < cols && t0 + (set + 2 * i) * 16 < p.M) emit(r[i], i, t0 + (set + 2 * i) * 16, jq);
-            if (++acc == accs) { acc = 0; phase ^= 1u; }
-        }
-    }
-    if (SPLIT) {
-        // Chunk c of 16 tokens is finished by slice c % split: the others store their sums into its shared memory, as the threads hold
-        // them, where the stages were -- behind a barrier, all MMAs of the cluster have ended.  Added in the order of the slices.
-        int m, n;
-        tile_of(unit0, &m, &n);
-        const int64_t jq = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32, t0 = (int64_t)m * p.bt;
-        const int chunks = columns(m) / 16, per = (chunks + p.split - 1) / p.split;
-        // [sender][chunk / split][quarter][thread of four warps] 16 bytes
-        auto place = [&](int sender, int c, int q) { return base + (uint32_t)((((sender * per + c / p.split) * 4 + q) * 128 + quad * 32 + lane) * 16); };
-        __syncwarp();
-        cluster_sync_all();
-        if (warp >= 2 && ok) {
-            for (int c = set; c < chunks; c += 2) {
-                const int owner = c % p.split;
-                if (owner == slice) continue;
-                uint32_t r[16];
-                fetch((uint32_t)(c * 16), r);
-                tmem_ld_wait();
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    st_cluster_v4(cluster_address(place(slice - (slice > owner ? 1 : 0), c, q), (uint32_t)(owner * CTAS) + half), r + 4 * q);
-            }
-        }
-        __syncwarp();
-        cluster_sync_all();
-        if (warp >= 2 && ok) {
-            for (int c = set, i = 0; c < chunks; c += 2, ++i) {
-                if (c % p.split != slice || t0 + c * 16 >= p.M) continue;
-                uint32_t r[16], sum[16];
-                fetch((uint32_t)(c * 16), r);
-                tmem_ld_wait();
-#pragma unroll
-                for (int k = 0; k < 16; ++k) sum[k] = 0u;
-                for (int s = 0; s < p.split; ++s) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint4 o = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
-                        if (s != slice) o = lds128(place(s - (s > slice ? 1 : 0), c, q));
-                        const uint32_t w[4] = {o.x, o.y, o.z, o.w};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) sum[4 * q + k] = __float_as_uint(__fadd_rn(__uint_as_float(sum[4 * q + k]), __uint_as_float(w[k])));
-                    }
+                for (int k = 0; k < 2; ++k) {
+                    const uint4 v = lds128(buf + (uint32_t)((k * 8 + row) * 64 + ((piece ^ ((row >> 1) & 3)) << 4)));
+                    if (j_ok && tc + k * 8 + row < p.M) *reinterpret_cast<uint4*>(y + k * 8 * p.ldy) = v;
                 }
-                emit(sum, i, t0 + c * 16, jq);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 16; ++k) {
+                    const float4 q = reinterpret_cast<const float4*>(st)[k / 4];
+                    const float d = k % 4 == 0 ? q.x : k % 4 == 1 ? q.y : k % 4 == 2 ? q.z : q.w;
+                    sts32_loose(buf + (uint32_t)(k * 128 + lane * 4), __float_as_uint(__fmaf_rn(__uint_as_float(r[k]), d * sw4[0], bj4[0])));
+                }
+                __syncwarp();
+                const int row = lane >> 3, piece = lane & 7;
+                float* y = static_cast<float*>(p.y) + (tc + row) * p.ldy + jq + piece * 4;
+                const bool j_ok = jq + piece * 4 < p.N;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint4 v = lds128(buf + (uint32_t)((k * 4 + row) * 128 + piece * 16));
+                    if (j_ok && tc + k * 4 + row < p.M) *reinterpret_cast<uint4*>(y + k * 4 * p.ldy) = v;
+                }
+            }
+        };
+        if constexpr (!SPLIT) {
+            int acc = 0;
+            uint32_t phase = 0;
+            for (int unit = unit0; unit < p.units; unit += p.unit_step) {
+                int m, n;
+                tile_of(unit, &m, &n);
+                const int64_t jq = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32, t0 = (int64_t)m * p.bt;
+                const int cols = (int)min((int64_t)p.bt, p.M - t0);                 // tokens of the tile
+                constants(m, n);
+                ok = mbar_wait_all(smem_u32(&s_acc_full[acc]), phase, abort_flag, p.watchdog, kWdEpilogue);
+                if (!ok) break;
+                tc_fence_after();
+                // all of the warp's sums into registers, so that the next tile's MMAs may have the columns
+                uint32_t r[kChunks][16];
+#pragma unroll
+                for (int i = 0; i < kChunks; ++i)
+                    if (token(i) < cols) fetch((uint32_t)(acc * acc_cols + token(i)), r[i]);
+                tmem_ld_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (leader) mbar_arrive(smem_u32(&s_acc_empty[acc]));
+                    else mbar_arrive_cta(smem_u32(&s_acc_empty[acc]), pair_base);
+                }
+#pragma unroll
+                for (int i = 0; i < kChunks; ++i)
+                    if (token(i) < cols) emit(r[i], i, t0, jq);
+                if (++acc == accs) { acc = 0; phase ^= 1u; }
+            }
+        }
+        if constexpr (SPLIT) {
+            // Slice s finishes the tile's chunks s * per .. (s + 1) * per: the others store their sums into its shared memory, as the
+            // threads hold them, counted in bytes on its barrier.  They have a place of their own there, or (p.shared_ring) the one of
+            // the stages, once the MMAs of all slices have ended, which each tells the others.  Each slice adds to its own sums the
+            // others' in their order.
+            int m, n;
+            tile_of(unit0, &m, &n);
+            const int64_t jq = (int64_t)(n * CTAS + (int)half) * kRows + quad * 32, t0 = (int64_t)m * p.bt;
+            const int cols = (int)min((int64_t)p.bt, p.M - t0), chunks = (cols + 15) / 16, per = p.per;
+            const uint32_t received = p.shared_ring ? base : s_out + kOutBytes;
+            auto place = [&](int sender, int c) { return received + (uint32_t)((sender * per + c) * 4 + quad) * 2048u + (uint32_t)lane * 16u; };
+            constants(m, n);
+            ok = mbar_wait_all(smem_u32(&s_acc_full[0]), 0u, abort_flag, p.watchdog, kWdEpilogue);
+            tc_fence_after();
+            if (CTAS == 1) cluster_wait();                   // the others are there
+            if (ok) {
+                const int mine = max(0, min(per, chunks - slice * per));
+                if (warp == 2 && lane == 0) mbar_arrive_expect_tx(smem_u32(&s_sums), (uint32_t)((p.split - 1) * mine) * 8192u);
+                if (p.shared_ring) {
+                    if (warp == 2 && lane < p.split) mbar_arrive_cta(smem_u32(&s_ended), (uint32_t)(lane * CTAS) + half);
+                    __syncwarp();
+                    ok = mbar_wait_all(smem_u32(&s_ended), 0u, abort_flag, p.watchdog, kWdSums);
+                }
+                if (ok) {
+                    for (int i = 0; i < kChunks; ++i) {
+                        const int c = token(i) / 16, owner = c / per;
+                        if (c >= chunks) break;
+                        if (owner == slice) continue;
+                        uint32_t r[16];
+                        fetch((uint32_t)(c * 16), r);
+                        tmem_ld_wait();
+                        const uint32_t to = (uint32_t)(owner * CTAS) + half, bar = cluster_address(smem_u32(&s_sums), to);
+                        const uint32_t at = cluster_address(place(slice - (slice > owner ? 1 : 0), c - owner * per), to);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) st_async_v4(at + (uint32_t)(q * 512), r + 4 * q, bar);
+                    }
+                    if (mine > 0) ok = mbar_wait_all(smem_u32(&s_sums), 0u, abort_flag, p.watchdog, kWdSums);
+                }
+            }
+            if (ok) {
+                for (int i = 0; i < kChunks; ++i) {
+                    const int c = token(i) / 16;
+                    if (c >= chunks) break;
+                    if (c / per != slice) continue;
+                    uint32_t r[16];
+                    fetch((uint32_t)(c * 16), r);
+                    tmem_ld_wait();
+                    for (int s = 0; s < p.split - 1; ++s) {
+                        const uint32_t from = place(s, c - slice * per);
+                        uint4 o[4];
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) o[q] = lds128(from + (uint32_t)(q * 512));
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const uint32_t w[4] = {o[q].x, o[q].y, o[q].z, o[q].w};
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) r[4 * q + k] = __float_as_uint(__fadd_rn(__uint_as_float(r[4 * q + k]), __uint_as_float(w[k])));
+                        }
+                    }
+                    emit(r, i, t0, jq);
+                }
             }
         }
     }
-    // the stores have read their buffers before the CTA gives up its shared memory
-    if (warp >= 2 && lane == 0) bulk_wait_read<0>();
     __syncwarp();
+    if (SPLIT && CTAS == 1 && (warp < 2 || warp == kTokenWarp)) cluster_wait();
     tc_fence_before();
     __syncthreads();
-    if (CTAS == 2) cluster_sync_all();                       // neither leaves while the other may still signal it
+    if (CTAS == 2 || SPLIT) cluster_sync_all();              // nobody leaves while another may still signal it
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc<CTAS>(tmem, 512u);
@@ -506,6 +570,8 @@ bool scale_map(CUtensorMap* map, const uint8_t* scales, int64_t rows, int64_t K,
 struct Plan {
     int ctas, bt, split;
 };
+// What a slice of K receives from the others.
+size_t split_bytes(int bt, int split) { return (size_t)(split - 1) * ((bt / 16 + split - 1) / split) * 8192; }
 Plan plan(int64_t M, int64_t N, int64_t K) {
     Plan r = {1, 0, 1};
     const int sms = device_sm_count();
@@ -522,14 +588,14 @@ Plan plan(int64_t M, int64_t N, int64_t K) {
 }
 
 struct Maps {
-    CUtensorMap x, xs, y;
+    CUtensorMap x, xs;
 };
 template <int CTAS, bool NV, bool SPLIT, int XA>
 cudaError_t launch(const Fp4Weights& W, const Maps& maps, const GemmParams& p, int grid, size_t smem, cudaStream_t stream) {
     auto kern = gemm_fp4_kernel<CTAS, NV, SPLIT, XA>;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, (unsigned)(CTAS * p.split), W.map_codes, W.map_scales, maps.x, maps.xs, maps.y, p);
+    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, (unsigned)(CTAS * p.split), W.map_codes, W.map_scales, maps.x, maps.xs, p);
 }
 template <int CTAS, int XA>
 cudaError_t launch(const Fp4Weights& W, const Maps& maps, const GemmParams& p, int grid, size_t smem, cudaStream_t stream) {
@@ -550,7 +616,7 @@ fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const flo
     const Plan r = plan(M, W.N, W.K);
     const bool nv = W.format == FQ_NVFP4;
     GemmParams p = {};
-    p.M = M; p.N = W.N; p.K = (int)W.K;
+    p.M = M; p.N = W.N; p.K = (int)W.K; p.ldy = ldy;
     p.bt = r.bt;
     p.split = r.split;
     p.kb = (int)((W.K + kStageK - 1) / kStageK);
@@ -560,25 +626,31 @@ fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const flo
     p.band = p.m_full >= 16 ? 8 : p.m_full > 0 ? p.m_full : 1;
     p.units = (p.m_full + (M % r.bt ? 1 : 0)) * p.n_tiles;
     p.delta = delta; p.w_scale = W.w_scale; p.bias = W.bias;
+    p.y = y;
     p.bf16 = yt == FQ_BF16;
     p.watchdog = watchdog_device_ptr();
     if (!p.watchdog) return FQ_ERR_CUDA;
     const int tiles = nv ? 4 : 2;
     const size_t stage = (size_t)kRows * 128 + (size_t)(r.bt / r.ctas) * 128 + (size_t)tiles * 512 * (1 + xa);
     const int slots = 256 / (tiles * 4 * (1 + xa));        // TMEM columns for scales
-    p.stages = (int)((kSmemMost - 1024 - kOutBytes) / stage);
-    if (p.stages > kMostStages) p.stages = kMostStages;
-    if (p.stages > slots) p.stages = slots;
-    const size_t smem = 1024 + stage * (size_t)p.stages + kOutBytes;
+    auto fit = [&](size_t bytes) {
+        const int most = slots < kMostStages ? slots : kMostStages;
+        return (int)(bytes / stage) < most ? (int)(bytes / stage) : most;
+    };
+    // received sums beside the stages where at least five are left, else in their place (96 KB of them at most: two stages hold more)
+    const size_t sums = split_bytes(r.bt, r.split);
+    p.stages = fit(kRingMost);
+    p.per = (r.bt / 16 + r.split - 1) / r.split;
+    if (r.split > 1) {
+        const int beside = fit(kRingMost - sums);
+        p.shared_ring = beside < 5 && beside < p.stages;
+        if (!p.shared_ring) p.stages = beside;
+    }
+    p.ring = (uint32_t)(stage * (size_t)p.stages);
+    if (p.shared_ring && p.ring < sums) p.ring = (uint32_t)sums;
+    const size_t smem = 1024 + p.ring + kOutBytes + (p.shared_ring ? 0 : sums);
     Maps maps;
     if (!code_map(&maps.x, codes, M, W.K, r.bt / r.ctas) || !scale_map(&maps.xs, scales, M, W.K, W.format, xa)) return FQ_ERR_CUDA;
-    {   // outputs leave in boxes of [16 tokens][32 channels]
-        const int e = p.bf16 ? 2 : 4;
-        const uint64_t dims[2] = {(uint64_t)W.N * e, (uint64_t)M}, strides[1] = {(uint64_t)ldy * e};
-        const uint32_t box[2] = {32u * e, 16};
-        if (!encode_tiled(&maps.y, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, y, dims, strides, box, p.bf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE))
-            return FQ_ERR_CUDA;
-    }
     const int units = r.split > 1 ? p.units : (p.units < sms / r.ctas ? p.units : sms / r.ctas);
     p.unit_step = units;
     const int grid = units * r.ctas * r.split;
