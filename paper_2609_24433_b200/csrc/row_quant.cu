@@ -13,6 +13,7 @@
 #include "act_common.cuh"
 #include "fp4_common.cuh"
 #include "ptx_sm100.cuh"
+#include "row_quant.cuh"
 
 namespace fq {
 namespace {
@@ -71,29 +72,6 @@ struct Raw {
         }
     }
 };
-
-// Eight e2m1 codes, element 0 in the lowest nibble.
-__device__ __forceinline__ uint32_t pack_e2m1(const float* v) {
-    uint32_t r;
-    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
-        "mov.b32 %0, {a, b, c, d};\n\t}"
-        : "=r"(r)
-        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
-    return r;
-}
-// e4m3 of a non-negative number, and what it stands for.
-__device__ __forceinline__ uint32_t to_e4m3(float v, float* back) {
-    uint16_t b;
-    uint32_t h2;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(0.0f), "f"(v));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h2) : "h"(b));
-    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.f32.f16 %0, l;\n\t}" : "=f"(*back) : "r"(h2));
-    return b & 0xffu;
-}
 
 // CACHE: the multiplier's slice stays in registers and the next row is requested while this one is worked on (at most 512
 // threads); otherwise both are read where they are needed.
@@ -239,26 +217,19 @@ __global__ void __launch_bounds__(CACHE ? 512 : 1024) row_quantize_kernel(const 
         float total = ss;
         if (kReduce) {
             m = warp_max_nonneg(m);
-            if (NORM) {
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-            }
+            if (NORM) total = warp_sum(total);
             if (wpr > 1) {
                 if (lane == 0) s_part[buf][warp] = make_float2(m, total);
                 __syncthreads();
                 const float2 t = lane < wpr ? s_part[buf][r_in_cta * wpr + lane] : make_float2(0.0f, 0.0f);
                 m = warp_max_nonneg(t.x);
-                if (NORM && t_in_row < 32) {
-                    total = t.y;
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-                }
+                if (NORM && t_in_row < 32) total = warp_sum(t.y);
             }
         }
         // 1 / rms of the row, for its first warp
         float rinv = 1.0f;
         if (NORM && t_in_row < 32) {
-            if (row < p.rows && m > 0.0f && (total > 1e37f || (total < 1e-30f && p.eps < 1e-20f))) {
+            if (row < p.rows && m > 0.0f && !sum_in_range(total, p.eps)) {
                 // squares out of binary32's range: the row once more, in binary64 (the stream was written ahead of the barrier;
                 // rows of a single warp have it ordered by the warp's own)
                 __syncwarp();
@@ -271,8 +242,7 @@ __global__ void __launch_bounds__(CACHE ? 512 : 1024) row_quantize_kernel(const 
                 for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
                 rinv = (float)(1.0 / sqrt(s / p.K + (double)p.eps));
             } else {
-                const float ms = __fadd_rn(__fdiv_rn(total, (float)p.K), p.eps);
-                rinv = ms > 0.0f ? __fdiv_rn(1.0f, __fsqrt_rn(ms)) : 0.0f;
+                rinv = inverse_rms(total, p.K, p.eps);
             }
         }
 
@@ -284,25 +254,20 @@ __global__ void __launch_bounds__(CACHE ? 512 : 1024) row_quantize_kernel(const 
                 // a block of 32 channels: E = 32 a thread's own, E = 16 two lanes'
                 float mb = mine;
                 if (E == 16) mb = fmaxf(mb, __shfl_xor_sync(0xffffffffu, mb, 1));
-                const int e = max((int)(__float_as_uint(mb) >> 23) - 2, 0);
-                qlo = qhi = __uint_as_float((uint32_t)(254 - e) << 23);
+                const uint32_t byte = mx_scale(mb, &qlo);
+                qhi = qlo;
                 constexpr int kThreads = E == 16 ? 2 : 1;      // threads of a block
-                if (col_ok && lane % kThreads == 0) word = (uint32_t)e << (8 * ((lane / kThreads) & 3));
+                if (col_ok && lane % kThreads == 0) word = byte << (8 * ((lane / kThreads) & 3));
             } else {
-                d = __fmul_rn(m, 1.0f / 2688.0f);
-                float inv = 0.0f;
-                if (d >= 7.888609052e-31f) inv = __fdiv_rn(1.0f, d);          // 2^-100
-                else d = 0.0f;
-                float s0, s1;
+                float inv;
+                d = nv_step(m, &inv);
                 if (E == 16) {
-                    word = to_e4m3(__fmul_rn(__fmul_rn(mine, inv), 0.166666672f), &s0) << (8 * (lane & 3));
-                    qlo = qhi = s0 > 0.0f ? __fdiv_rn(inv, s0) : 0.0f;
+                    word = nv_scale(mine, inv, &qlo) << (8 * (lane & 3));
+                    qhi = qlo;
                 } else {
-                    word = to_e4m3(__fmul_rn(__fmul_rn(mlo, inv), 0.166666672f), &s0);
-                    word |= to_e4m3(__fmul_rn(__fmul_rn(mhi, inv), 0.166666672f), &s1) << 8;
+                    word = nv_scale(mlo, inv, &qlo);
+                    word |= nv_scale(mhi, inv, &qhi) << 8;
                     word <<= 16 * (lane & 1);
-                    qlo = s0 > 0.0f ? __fdiv_rn(inv, s0) : 0.0f;
-                    qhi = s1 > 0.0f ? __fdiv_rn(inv, s1) : 0.0f;
                 }
                 if (!col_ok) word = 0u;
             }
@@ -329,9 +294,8 @@ __global__ void __launch_bounds__(CACHE ? 512 : 1024) row_quantize_kernel(const 
                 if (t_in_row == 0) p.delta[row] = NORM ? __fmul_rn(d, rinv) : d;
             }
         } else {
-            float d = __fmul_rn(__fmul_rn(p.clip_ratio, m), 1.0f / (FMT == 0 ? 7.0f : 127.0f)), inv = 0.0f;
-            if (d >= FLT_MIN) inv = __fdiv_rn(1.0f, d);
-            else d = 0.0f;
+            float inv;
+            const float d = int_step(m, p.clip_ratio, 1.0f / (FMT == 0 ? 7.0f : 127.0f), &inv);
             // round to nearest even: the low bits of t + 1.5 * 2^23 hold the two's-complement integer
             uint32_t b[E];
 #pragma unroll
@@ -408,6 +372,10 @@ __global__ void fill_kernel(float* p, float v, int64_t n) {
 
 cudaError_t launch_row_quantize(const RowQuant& q, cudaStream_t stream) {
     if (q.rows == 0) return cudaSuccess;
+    {   // batches of some length stream through a ring of rows in shared memory
+        const cudaError_t e = launch_row_quantize_ring(q, stream);
+        if (e != cudaErrorNotSupported) return e;
+    }
     const bool fp4 = q.fmt == RowFmt::Mx || q.fmt == RowFmt::Nv;
     RowParams p = {};
     p.x = q.x; p.residual = q.residual; p.h = q.h;

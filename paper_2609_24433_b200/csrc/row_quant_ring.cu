@@ -1,0 +1,524 @@
+// Rows to codes, for batches of some length: the arithmetic of row_quantize_kernel, bit for bit, with the rows (and those of the
+// residual) fetched by TMA into a ring in shared memory.
+//
+// What the kernel that keeps rows in registers spends its time on are shuffles (16 channels a thread: four butterfly stages of
+// 256 channels go across lanes, one shuffle a value each, and an SM has one warp's shuffle a cycle) and rows that wait for
+// registers.  Here a thread has E = 64 (or 32) consecutive channels, which only a copy through shared memory gives without reading
+// memory in strides: strides 1 .. 32 run in registers, two values an instruction, and at most two stages across lanes; and the rows
+// under way take no registers.
+//   - One CTA of 16 warps an SM, in row groups of gw warps; a group works on one row at a time and has `depth` slots.
+//   - A row is a box of 128-byte lines with the 128-byte swizzle, so that reading 64..256 bytes a thread has no bank conflicts; the
+//     multiplier lies beside it in the order that the packed multiply takes.
+//   - The stream h = x + residual is written over x in its slot and leaves as a bulk store of the whole row.
+//   - E = 64: a thread holds the four block scales of 64 channels of e2m1 with e4m3 scales: one word of its scale tile.
+#include <cuda_bf16.h>
+#include <string.h>
+
+#include "act_common.cuh"
+#include "fp4_common.cuh"
+#include "ptx_sm100.cuh"
+#include "row_quant.cuh"
+
+namespace fq {
+namespace {
+
+constexpr int kThreads = 512, kWarps = kThreads / 32, kMostSlots = 64;
+
+struct RingArgs {
+    int64_t rows, rows_pad;
+    int K, block, gw, ngroups, depth;
+    float eps, cnorm, clip_ratio;
+    const float* mult;
+    int mult_ready, residual;
+    uint8_t* codes;
+    uint8_t* scales;
+    int scale_tiles;
+    float* delta;
+    uint32_t row_bytes;      // of one row in a slot, rounded up to 1024
+    uint32_t slot_bytes;
+    uint32_t mult_bytes;     // rounded up to 1024
+    uint32_t stage_off;      // codes of a warp on their way out (8-bit codes)
+    uint32_t* watchdog;
+};
+
+__device__ __forceinline__ uint32_t swz128(uint32_t off) { return off ^ (((off >> 7) & 7u) << 4); }
+__device__ __forceinline__ void tma_load_row(uint32_t dst, const CUtensorMap* map, int row, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %3}], [%4];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void tma_store_row(const CUtensorMap* map, int row, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %1, %2}], [%3];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(src)
+                 : "memory");
+}
+// Barrier of a row group that also ANDs a predicate.
+__device__ __forceinline__ bool group_and(int id, int threads, bool pred) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 q, %3, 0;\n\t"
+        "bar.red.and.pred p, %1, %2, q;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(r)
+        : "r"(id), "r"(threads), "r"((uint32_t)pred)
+        : "memory");
+    return r != 0;
+}
+__device__ __forceinline__ float max3_abs(float m, float x, float y) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(m), "f"(fabsf(x)), "f"(fabsf(y)));
+    return r;
+}
+// (not volatile: may be batched and hoisted; their addresses are pinned behind the wait that makes the data valid)
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 v;
+    asm("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ float4 lds128f_ordered(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ uint4 lds128_ordered(uint32_t addr) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ void pin(uint32_t& addr) { asm volatile("" : "+r"(addr) : : "memory"); }
+// 16-byte piece i of a thread's slice of a swizzled row, whose (at most two) 128-byte lines begin at line0, line1.
+__device__ __forceinline__ uint32_t piece(uint32_t line0, uint32_t line1, int i) { return (i < 8 ? line0 : line1) ^ (uint32_t)((i & 7) << 4); }
+__device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {          // in binary32, rounded once
+    const float2 s = f2_add(make_float2(__uint_as_float(a << 16), __uint_as_float(a & 0xffff0000u)),
+                            make_float2(__uint_as_float(b << 16), __uint_as_float(b & 0xffff0000u)));
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(s.y), "f"(s.x));
+    return r;
+}
+__device__ __forceinline__ uint32_t add_f32(uint32_t a, uint32_t b) { return __float_as_uint(__fadd_rn(__uint_as_float(a), __uint_as_float(b))); }
+
+template <typename XT, int E, int FMT, bool NORM>
+__global__ void __launch_bounds__(kThreads, 1)
+row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_h,
+                         const RingArgs p) {
+    constexpr bool kFp4 = FMT >= 3, kMx = FMT == 3;
+    constexpr int H = E / 2;                               // v[i] = (channel i, channel i + H)
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t s_full[kMostSlots];
+    __shared__ float2 s_part[2][kWarps];
+    __shared__ int s_abort;
+
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int ngroups = p.ngroups, group = warp / p.gw, wg = warp - group * p.gw;
+    const bool idle = group >= ngroups;                    // warps left over
+    const int col0 = (wg * 32 + lane) * E;
+    const bool col_ok = col0 < p.K && !idle;
+    const bool leader = wg == 0 && lane == 0 && !idle;
+    volatile int* abort_flag = &s_abort;
+    const bool residual = NORM && p.residual != 0;
+
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+
+    if (threadIdx.x == 0) {
+        s_abort = 0;
+        for (int s = 0; s < ngroups * p.depth; ++s) mbar_init(smem_u32(&s_full[s]), 1);
+        fence_mbarrier_init();
+        fence_proxy_async_smem();
+    }
+    auto stage_multiplier = [&]() {
+        if (!p.mult) return;
+        // a thread's slice as pairs (g[q], g[q + H]), its 16-byte pieces mixed by the slice's number
+        for (int i = threadIdx.x * 4; i < p.K; i += kThreads * 4) {
+            const float4 g4 = ld_global_f4(p.mult + i);
+            const float gv[4] = {g4.x, g4.y, g4.z, g4.w};
+            const uint32_t slice = (uint32_t)i / E, key = (slice & 7u) << 4;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t q = ((uint32_t)i % E) + k, off = q < H ? q * 8u : (q - H) * 8u + 4u;
+                *reinterpret_cast<float*>(gen + ((slice * (E * 4u) + off) ^ key)) = gv[k];
+            }
+        }
+    };
+    if (p.mult_ready) stage_multiplier();
+    __syncthreads();                                       // barriers before any copy
+    griddep_wait();
+    griddep_launch_dependents();
+
+    const int rows = (int)p.rows, first = group * (int)gridDim.x + (int)blockIdx.x, step = (int)gridDim.x * ngroups;
+    const uint32_t tx = (uint32_t)p.K * (uint32_t)sizeof(XT) * (residual ? 2u : 1u);
+    const uint32_t slot0 = base + p.mult_bytes + (uint32_t)(group * p.depth) * p.slot_bytes;
+    uint64_t* const full0 = &s_full[group * p.depth];
+    auto request = [&](int d, int row) {
+        const uint32_t bar = smem_u32(&full0[d]), slot = slot0 + (uint32_t)d * p.slot_bytes;
+        mbar_arrive_expect_tx(bar, tx);
+        tma_load_row(slot, &map_x, row, bar);
+        if (residual) tma_load_row(slot + p.row_bytes, &map_r, row, bar);
+    };
+    int issued = 0;
+    if (leader) {
+        for (int d = 0; d < p.depth; ++d) {
+            const int r = first + d * step;
+            if (r < rows) { request(d, r); ++issued; }
+        }
+    }
+    if (!p.mult_ready) stage_multiplier();
+    __syncthreads();
+
+    // scale tiles of the rows that only pad the last one
+    if (kFp4)
+        for (int64_t row = p.rows + blockIdx.x; row < p.rows_pad; row += gridDim.x)
+            for (int t = threadIdx.x; t < p.scale_tiles; t += kThreads)
+                *reinterpret_cast<uint32_t*>(p.scales + ((row >> 7) * p.scale_tiles + t) * 512 + (row & 31) * 16 + ((row & 127) >> 5) * 4) = 0u;
+    if (idle) return;
+
+    const uint32_t xs0 = swz128((uint32_t)col0 * (uint32_t)sizeof(XT)), xs1 = swz128((uint32_t)col0 * (uint32_t)sizeof(XT) + 128u);
+    const uint32_t gkey = (uint32_t)((col0 / E) & 7) << 4;
+    const uint32_t g0 = base + (((uint32_t)col0 * 4u) ^ gkey), g1 = base + (((uint32_t)col0 * 4u + 128u) ^ gkey);
+    const float2 neg1 = make_float2(-1.0f, -1.0f);
+    const uint32_t stage = base + p.stage_off + (uint32_t)(warp * 32 * E);
+
+    int n = 0, d = 0;
+    uint32_t ph = 0;
+    for (int row = first; row < rows; row += step, ++n) {
+        bool ok = mbar_wait_all(smem_u32(&full0[d]), ph, abort_flag, p.watchdog, 0x100u);
+        const uint32_t slot = slot0 + (uint32_t)d * p.slot_bytes;
+        float2 v[H];
+        float ss = 0.0f;
+        if (col_ok) {
+            uint32_t x0 = slot + xs0, x1 = slot + xs1;
+            pin(x0);
+            pin(x1);
+            constexpr int kPieces = H * (int)sizeof(XT) / 16;      // of half a slice
+            constexpr int kPer = 16 / (int)sizeof(XT);             // channels of a piece
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const uint32_t alo = piece(x0, x1, i), ahi = piece(x0, x1, i + kPieces);
+                uint4 lo = lds128(alo), hi = lds128(ahi);
+                if (residual) {
+                    const uint4 rl = lds128(alo + p.row_bytes), rh = lds128(ahi + p.row_bytes);
+                    if (sizeof(XT) == 2) {
+                        lo = make_uint4(add_bf16x2(lo.x, rl.x), add_bf16x2(lo.y, rl.y), add_bf16x2(lo.z, rl.z), add_bf16x2(lo.w, rl.w));
+                        hi = make_uint4(add_bf16x2(hi.x, rh.x), add_bf16x2(hi.y, rh.y), add_bf16x2(hi.z, rh.z), add_bf16x2(hi.w, rh.w));
+                    } else {
+                        lo = make_uint4(add_f32(lo.x, rl.x), add_f32(lo.y, rl.y), add_f32(lo.z, rl.z), add_f32(lo.w, rl.w));
+                        hi = make_uint4(add_f32(hi.x, rh.x), add_f32(hi.y, rh.y), add_f32(hi.z, rh.z), add_f32(hi.w, rh.w));
+                    }
+                    sts128(alo, lo);
+                    sts128(ahi, hi);
+                }
+                const uint32_t wl[4] = {lo.x, lo.y, lo.z, lo.w}, wh[4] = {hi.x, hi.y, hi.z, hi.w};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (sizeof(XT) == 2) {
+                        v[kPer * i + 2 * j + 0] = make_float2(__uint_as_float(wl[j] << 16), __uint_as_float(wh[j] << 16));
+                        v[kPer * i + (2 * j + 1) % kPer] = make_float2(__uint_as_float(wl[j] & 0xffff0000u), __uint_as_float(wh[j] & 0xffff0000u));
+                    } else {
+                        v[kPer * i + j % kPer] = make_float2(__uint_as_float(wl[j]), __uint_as_float(wh[j]));
+                    }
+                }
+            }
+            if (NORM) {
+                float2 s2 = make_float2(0.0f, 0.0f), t2 = s2;
+#pragma unroll
+                for (int i = 0; i < H; i += 2) {
+                    s2 = f2_fma(v[i], v[i], s2);
+                    t2 = f2_fma(v[i + 1], v[i + 1], t2);
+                }
+                ss = (s2.x + s2.y) + (t2.x + t2.y);
+            }
+            if (p.mult) {
+#pragma unroll
+                for (int i = 0; i < H / 2; ++i) {
+                    const float4 q = lds128f_ordered(piece(g0, g1, i));
+                    v[2 * i + 0] = f2_mul(v[2 * i + 0], make_float2(q.x, q.y));
+                    v[2 * i + 1] = f2_mul(v[2 * i + 1], make_float2(q.z, q.w));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < H; ++i) v[i] = f2_mul(v[i], make_float2(p.cnorm, p.cnorm));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < H; ++i) v[i] = make_float2(0.0f, 0.0f);
+        }
+#pragma unroll
+        for (int s = 1; s < H; s <<= 1) {
+            if (s < p.block) {
+#pragma unroll
+                for (int i = 0; i < H; ++i) {
+                    if ((i & s) == 0) {
+                        const float2 a = v[i], b = v[i + s];
+                        v[i] = f2_add(a, b);
+                        v[i + s] = f2_fma(b, neg1, a);         // a - b, exact product
+                    }
+                }
+            }
+        }
+        if (H < p.block) {
+#pragma unroll
+            for (int i = 0; i < H; ++i) v[i] = make_float2(__fadd_rn(v[i].x, v[i].y), __fsub_rn(v[i].x, v[i].y));
+        }
+        for (int s = E; s < p.block; s <<= 1) {
+            const int lm = s / E;
+            const float sgn = (lane & lm) ? -1.0f : 1.0f;
+#pragma unroll
+            for (int i = 0; i < H; ++i) {
+                const float2 o = make_float2(__shfl_xor_sync(0xffffffffu, v[i].x, lm), __shfl_xor_sync(0xffffffffu, v[i].y, lm));
+                v[i] = f2_fma(v[i], make_float2(sgn, sgn), o);
+            }
+        }
+        // largest magnitudes of the thread's blocks of 16 channels (32: E = 32 has two of 16, one of 32)
+        float mb[E / 16];
+#pragma unroll
+        for (int b = 0; b < E / 32; ++b) {
+            float lo = 0.0f, hi = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                lo = max3_abs(lo, v[16 * b + i].x, v[16 * b + i + 1].x);
+                hi = max3_abs(hi, v[16 * b + i].y, v[16 * b + i + 1].y);
+            }
+            mb[b] = lo;
+            mb[b + E / 32] = hi;
+        }
+        float m = mb[0];
+#pragma unroll
+        for (int b = 1; b < E / 16; ++b) m = fmaxf(m, mb[b]);
+        m = warp_max_nonneg(m);
+        float total = NORM ? warp_sum(ss) : 0.0f;
+        if (residual) fence_proxy_async_smem();               // the stream's row, written here, is read by the copy engine
+        if (p.gw > 1) {
+            if (lane == 0) s_part[n & 1][warp] = make_float2(m, total);
+            ok = group_and(1 + group, p.gw * 32, ok);
+            const float2 t = lane < p.gw ? s_part[n & 1][group * p.gw + lane] : make_float2(0.0f, 0.0f);
+            m = warp_max_nonneg(t.x);
+            if (NORM && wg == 0) total = warp_sum(t.y);
+        } else {
+            __syncwarp();
+        }
+        if (!ok) break;
+        float rinv = 1.0f;
+        if (NORM && wg == 0) {
+            if (m > 0.0f && !sum_in_range(total, p.eps)) {
+                double s = 0.0;                                // the row as it lies in its slot, in binary64
+                for (uint32_t at = (uint32_t)lane * 4u; at < (uint32_t)p.K * (uint32_t)sizeof(XT); at += 128u) {
+                    const uint32_t w = *reinterpret_cast<const volatile uint32_t*>(gen + (slot - base) + at);
+                    if (sizeof(XT) == 2) {
+                        const double a = (double)__uint_as_float(w << 16), b = (double)__uint_as_float(w & 0xffff0000u);
+                        s += a * a + b * b;
+                    } else {
+                        s += (double)__uint_as_float(w) * (double)__uint_as_float(w);
+                    }
+                }
+                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                rinv = (float)(1.0 / sqrt(s / p.K + (double)p.eps));
+            } else {
+                rinv = inverse_rms(total, p.K, p.eps);
+            }
+            __syncwarp();
+        }
+        // Every warp of the group has read the slot.  Without a residual it is refilled here; with one its row goes out first, and the
+        // slot of the row before, whose store has had time to read it, is refilled (of a single slot: its own).
+        if (leader) {
+            if (residual) {
+                tma_store_row(&map_h, row, slot);
+                bulk_commit();
+                if (p.depth == 1) {
+                    bulk_wait_read<0>();
+                    if (row + step < rows) { request(0, row + step); ++issued; }
+                } else if (n > 0) {
+                    const int nr = row + (p.depth - 1) * step;
+                    bulk_wait_read<1>();
+                    if (nr < rows) { request(d == 0 ? p.depth - 1 : d - 1, nr); ++issued; }
+                }
+            } else if (row + p.depth * step < rows) {
+                fence_proxy_async_smem();
+                request(d, row + p.depth * step);
+                ++issued;
+            }
+        }
+        float dl = 1.0f;
+        if (kFp4) {
+            float q[E / 16];
+            uint32_t word = 0u;
+            if (kMx) {
+#pragma unroll
+                for (int b = 0; b < E / 32; ++b) {
+                    // (E = 64: halves of 32 channels; E = 32: one block across both halves)
+                    const float mm = E == 64 ? fmaxf(mb[(2 * b) % (E / 16)], mb[(2 * b + 1) % (E / 16)]) : fmaxf(mb[0], mb[1]);
+                    float qq;
+                    word |= mx_scale(mm, &qq) << (8 * b);
+                    q[(2 * b) % (E / 16)] = q[(2 * b + 1) % (E / 16)] = qq;
+                }
+                if (!col_ok) word = 0u;
+                constexpr int kShare = 128 / E;                // threads of a word
+                word <<= 8 * (E / 32) * (lane % kShare);
+#pragma unroll
+                for (int o = 1; o < kShare; o <<= 1) word |= __shfl_xor_sync(0xffffffffu, word, o);
+            } else {
+                float inv;
+                dl = nv_step(m, &inv);
+#pragma unroll
+                for (int b = 0; b < E / 16; ++b) word |= nv_scale(mb[b], inv, &q[b]) << (8 * b);
+                if (!col_ok) word = 0u;
+                if (E == 32) {
+                    word <<= 16 * (lane & 1);
+                    word |= __shfl_xor_sync(0xffffffffu, word, 1);
+                }
+            }
+            const int tile = col0 / (kMx ? 128 : 64);
+            if (tile < p.scale_tiles && lane % ((kMx ? 128 : 64) / E) == 0)
+                *reinterpret_cast<uint32_t*>(p.scales + ((int64_t)(row >> 7) * p.scale_tiles + tile) * 512 + (row & 31) * 16 + ((row & 127) >> 5) * 4) = word;
+            uint32_t w[E / 8];
+#pragma unroll
+            for (int b = 0; b < E / 32; ++b) {
+                const float2 q2 = make_float2(q[b], q[b + E / 32]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float lo[8], hi[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float2 t = f2_mul(v[16 * b + 8 * j + i], q2);
+                        lo[i] = t.x;
+                        hi[i] = t.y;
+                    }
+                    w[2 * b + j] = pack_e2m1(lo);
+                    w[2 * b + j + E / 16] = pack_e2m1(hi);
+                }
+            }
+            if (col_ok) {
+                uint4* dst = reinterpret_cast<uint4*>(p.codes + (int64_t)row * (p.K / 2) + col0 / 2);
+#pragma unroll
+                for (int j = 0; j < E / 32; ++j) dst[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+            }
+        } else {
+            constexpr int kPer = FMT == 0 ? 8 : 4, kWords = H / kPer;      // codes of a word, words of a half
+            constexpr float kMost = FMT == 0 ? 7.0f : 127.0f;
+            float inv;
+            dl = int_step(m, p.clip_ratio, 1.0f / kMost, &inv);
+            uint32_t w[2 * kWords];
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) {
+                uint32_t bl[kPer], bh[kPer];
+#pragma unroll
+                for (int i = 0; i < kPer; ++i) {
+                    float2 t = f2_mul(v[kPer * j + i], make_float2(inv, inv));
+                    if (p.clip_ratio < 1.0f) {
+                        t.x = fminf(fmaxf(t.x, -kMost), kMost);
+                        t.y = fminf(fmaxf(t.y, -kMost), kMost);
+                    }
+                    // (as a packed FMA by 1: a packed multiply ahead of a packed add may be fused, which rounds ties differently)
+                    t = f2_fma(t, make_float2(1.0f, 1.0f), make_float2(12582912.0f, 12582912.0f));
+                    bl[i] = __float_as_uint(t.x);
+                    bh[i] = __float_as_uint(t.y);
+                }
+                w[j] = pack_word<FMT>(bl);
+                w[kWords + j] = pack_word<FMT>(bh);
+            }
+            if (FMT == 1) {
+                // E bytes a thread: through shared memory (pieces mixed by the lane), so that a warp's store is one run
+                constexpr int kP = E / 16;
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < kP; ++j)
+                    sts128(stage + (uint32_t)(lane * E) + (uint32_t)((j ^ ((lane * E >> 7) & (kP - 1))) << 4),
+                           make_uint4(w[(4 * j) % (2 * kWords)], w[(4 * j + 1) % (2 * kWords)], w[(4 * j + 2) % (2 * kWords)], w[(4 * j + 3) % (2 * kWords)]));
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < kP; ++j) {
+                    const int at = j * 32 + lane, owner = at / kP, pc = at % kP;           // 16-byte piece `at` of the warp's run
+                    const uint4 o = lds128_ordered(stage + (uint32_t)(owner * E) + (uint32_t)((pc ^ ((owner * E >> 7) & (kP - 1))) << 4));
+                    if (wg * 32 * E + at * 16 < p.K) *reinterpret_cast<uint4*>(p.codes + (int64_t)row * p.K + wg * 32 * E + at * 16) = o;
+                }
+            } else if (col_ok) {
+                uint4* dst = reinterpret_cast<uint4*>(p.codes + (int64_t)row * (p.K / 2) + col0 / 2);
+#pragma unroll
+                for (int j = 0; j < E / 32; ++j) dst[j] = make_uint4(w[(4 * j) % (2 * kWords)], w[(4 * j + 1) % (2 * kWords)], w[(4 * j + 2) % (2 * kWords)], w[(4 * j + 3) % (2 * kWords)]);
+            }
+        }
+        if (leader) p.delta[row] = NORM ? __fmul_rn(dl, rinv) : dl;
+        if (++d == p.depth) { d = 0; ph ^= 1u; }
+    }
+    if (leader && residual) bulk_wait_read<0>();             // the last rows have left shared memory
+    // winding down after an expired wait: copies under way land first
+    if (leader && *abort_flag) {
+        for (int k = n; k < issued; ++k) {
+            const uint64_t t0 = global_timer_ns();
+            while (!mbar_try_wait(smem_u32(&full0[k % p.depth]), (uint32_t)((k / p.depth) & 1)))
+                if (global_timer_ns() - t0 > kWaitLimitNs) { atomicOr(p.watchdog, 0x200u); break; }
+        }
+    }
+}
+
+struct RowMaps {
+    CUtensorMap x, r, h;
+};
+template <typename XT, int E, int FMT, bool NORM>
+cudaError_t go(const RowMaps& maps, const RingArgs& p, int grid, size_t smem, cudaStream_t stream) {
+    auto kern = row_quantize_ring_kernel<XT, E, FMT, NORM>;
+    const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, 1u, maps.x, maps.r, maps.h, p);
+}
+template <typename XT, int E>
+cudaError_t by_format(const RowQuant& q, const RowMaps& maps, const RingArgs& p, int grid, size_t smem, cudaStream_t stream) {
+    switch (q.fmt) {
+        case RowFmt::Int4: return go<XT, E, 0, true>(maps, p, grid, smem, stream);
+        case RowFmt::Int8: return go<XT, E, 1, true>(maps, p, grid, smem, stream);
+        case RowFmt::Mx: return q.norm ? go<XT, E, 3, true>(maps, p, grid, smem, stream) : go<XT, E, 3, false>(maps, p, grid, smem, stream);
+        case RowFmt::Nv: return q.norm ? go<XT, E, 4, true>(maps, p, grid, smem, stream) : go<XT, E, 4, false>(maps, p, grid, smem, stream);
+    }
+    return cudaErrorInvalidValue;
+}
+
+}  // namespace
+
+cudaError_t launch_row_quantize_ring(const RowQuant& q, cudaStream_t stream) {
+    const size_t esz = q.xt == FQ_BF16 ? 2 : 4, row = (size_t)q.K * esz;
+    const int sms = device_sm_count();
+    // whole 128-byte lines, at most 256 of them (a box); rows enough for several a group
+    if (row % 128 != 0 || row > 32768 || q.rows < 2 * sms || q.rows * q.K < (int64_t)sms * 8192 || q.rows > 0x7fffffff - 4096 * 16) return cudaErrorNotSupported;
+    const int e = q.K % 64 == 0 && q.K >= 1536 ? 64 : 32;
+    const int gw = (int)((q.K + 32 * e - 1) / (32 * e));
+    if (gw > kWarps) return cudaErrorNotSupported;
+    RingArgs p = {};
+    p.row_bytes = (uint32_t)align_up(row, 1024);
+    p.slot_bytes = p.row_bytes * (q.residual ? 2 : 1);
+    p.mult_bytes = q.mult ? (uint32_t)align_up(sizeof(float) * (size_t)q.K, 1024) : 0;
+    const size_t stage = q.fmt == RowFmt::Int8 ? (size_t)kThreads * e : 0, room = 220 * 1024 - stage - p.mult_bytes;
+    const int slots = (int)(room / p.slot_bytes);
+    p.ngroups = slots < kWarps / gw ? slots : kWarps / gw;    // (rows so long that some warps stay idle)
+    if (p.ngroups < 1) return cudaErrorNotSupported;
+    p.depth = slots / p.ngroups < 4 ? slots / p.ngroups : 4;
+    const bool fp4 = q.fmt == RowFmt::Mx || q.fmt == RowFmt::Nv;
+    p.rows = q.rows;
+    p.rows_pad = fp4 ? (q.rows + 127) / 128 * 128 : q.rows;
+    p.K = (int)q.K; p.block = q.block; p.gw = gw;
+    p.eps = q.eps; p.cnorm = q.cnorm; p.clip_ratio = q.clip_ratio;
+    p.mult = q.mult; p.mult_ready = q.mult_ready ? 1 : 0; p.residual = q.residual ? 1 : 0;
+    p.codes = q.codes; p.scales = q.scales; p.delta = q.delta;
+    p.scale_tiles = fp4 ? (int)fp4_scale_tiles(q.K, q.fmt == RowFmt::Nv ? FQ_NVFP4 : FQ_MXFP4) : 0;
+    p.stage_off = p.mult_bytes + p.slot_bytes * (uint32_t)(p.ngroups * p.depth);
+    p.watchdog = watchdog_device_ptr();
+    if (!p.watchdog) return cudaErrorUnknown;
+    RowMaps maps;
+    auto map = [&](CUtensorMap* m, const void* ptr, int64_t ld) {
+        const uint64_t dims[3] = {128 / esz, row / 128, (uint64_t)q.rows}, strides[2] = {128, (uint64_t)ld * esz};
+        const uint32_t box[3] = {(uint32_t)(128 / esz), (uint32_t)(row / 128), 1};
+        return encode_tiled(m, esz == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+    };
+    if (!map(&maps.x, q.x, q.ldx)) return cudaErrorNotSupported;
+    maps.r = maps.h = maps.x;
+    if (q.residual && (!map(&maps.r, q.residual, q.ldr) || !map(&maps.h, q.h, q.ldh))) return cudaErrorNotSupported;
+    const size_t smem = 1024 + p.stage_off + stage;
+    const int grid = (int)(q.rows < sms ? q.rows : sms);
+    if (q.xt == FQ_F32) return e == 64 ? by_format<float, 64>(q, maps, p, grid, smem, stream) : by_format<float, 32>(q, maps, p, grid, smem, stream);
+    return e == 64 ? by_format<__nv_bfloat16, 64>(q, maps, p, grid, smem, stream) : by_format<__nv_bfloat16, 32>(q, maps, p, grid, smem, stream);
+}
+
+}  // namespace fq

@@ -41,16 +41,9 @@ def rotate(x, g, block):
 def tiles(scales):
     rows, blocks = scales.shape
     t, a = -(-rows // 128), -(-blocks // 4)
-    out = np.zeros((t, a, 32, 4, 4), np.uint8)
-    for r in range(rows):
-        for b in range(blocks):
-            out[r // 128, b // 4, r % 32, r % 128 // 32, b % 4] = scales[r, b]
-    return out.reshape(-1)
-
-
-def untiled(flat, rows, blocks):
-    t, a = -(-rows // 128), -(-blocks // 4)
-    return flat.reshape(t, a, 32, 4, 4).transpose(0, 3, 2, 1, 4).reshape(t * 128, a * 4)[:rows, :blocks]
+    out = np.zeros((t * 128, a * 4), np.uint8)
+    out[:rows, :blocks] = scales
+    return out.reshape(t, 4, 32, a, 4).transpose(0, 3, 2, 1, 4).reshape(-1)
 
 
 def quantize(z, form):
@@ -120,7 +113,10 @@ def check_status():
 @pytest.mark.parametrize("M,K,block,dtype", [
     (1, 32, 1, "f32"), (3, 32, 32, "bf16"), (2, 96, 16, "bf16"), (127, 256, 256, "f32"), (128, 160, 8, "bf16"), (129, 512, 64, "bf16"),
     (300, 1120, 32, "f32"), (50, 1024, 64, "bf16"), (5, 2080, 4, "f32"), (33, 4096, 128, "bf16"), (7, 8192, 256, "f32"),
-    (4, 8224, 32, "bf16"), (3, 16384, 256, "bf16"), (3, 16384, 2, "f32"), (2, 16416, 32, "bf16"), (2, 32768, 256, "f32"), (1000, 64, 64, "bf16")])
+    (4, 8224, 32, "bf16"), (3, 16384, 256, "bf16"), (3, 16384, 2, "f32"), (2, 16416, 32, "bf16"), (2, 32768, 256, "f32"), (1000, 64, 64, "bf16"),
+    # batches that stream through shared memory
+    (700, 2048, 128, "bf16"), (600, 2048, 256, "f32"), (1301, 1024, 64, "bf16"), (1500, 960, 32, "f32"), (1297, 1088, 16, "bf16"), (300, 5120, 1, "bf16"),
+    (301, 5120, 256, "f32"), (297, 8192, 128, "f32"), (296, 16384, 256, "bf16"), (2500, 512, 2, "bf16")])
 def test_quantize_bits(form, M, K, block, dtype):
     rng = np.random.default_rng(M * 7 + K)
     x = dev(tokens(rng, M, K), dtype)
@@ -335,7 +331,10 @@ def norm_reference(x, residual, dtype):
 @pytest.mark.parametrize("M,K,block,dtype,residual", [
     (1, 32, 1, "f32", True), (50, 1024, 64, "bf16", True), (129, 96, 32, "bf16", False), (5, 2048, 1, "bf16", True), (33, 5120, 256, "f32", True),
     (3, 8192, 128, "bf16", True), (4, 8224, 8, "f32", True), (3, 16384, 256, "bf16", False), (2, 16416, 32, "f32", True), (2, 32768, 256, "bf16", True),
-    (700, 64, 16, "f32", False)])
+    (700, 64, 16, "f32", False),
+    # batches that stream through shared memory
+    (700, 2048, 128, "bf16", True), (601, 2048, 256, "f32", True), (1301, 1024, 1, "bf16", True), (1500, 960, 32, "f32", False), (1297, 1088, 16, "bf16", False),
+    (301, 5120, 256, "f32", True), (297, 8192, 64, "f32", True), (300, 16384, 256, "bf16", True), (299, 5120, 1, "bf16", True)])
 def test_norm(form, M, K, block, dtype, residual):
     rng = np.random.default_rng(M + K)
     x = dev(tokens(rng, M, K), dtype)
@@ -358,9 +357,9 @@ def test_norm(form, M, K, block, dtype, residual):
     assert bool(((steps.double() - want).abs() <= 27 * 2.0 ** -24 * want).all())
 
 
+@pytest.mark.parametrize("M,K", [(90, 288), (1400, 1024), (310, 8192)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_norm_in_place_and_strided(dtype):
-    M, K = 90, 288
+def test_norm_in_place_and_strided(dtype, M, K):
     rng = np.random.default_rng(2)
     x, r = dev(tokens(rng, M, K), dtype), dev(tokens(rng, M, K), dtype)
     h, codes, steps = fq.rmsnorm_quantize_act(x, r, None, 32, 8)
@@ -380,26 +379,28 @@ def test_norm_in_place_and_strided(dtype):
     assert bool((wide[2] == 9.0).all())
 
 
-@pytest.mark.parametrize("K", [96, 4096, 16416])
+@pytest.mark.parametrize("K,repeat", [(96, 1), (4096, 1), (16416, 1), (4096, 60), (1024, 250)])
+@pytest.mark.parametrize("residual", [False, True])
 @pytest.mark.parametrize("form", ["int8", "mx", "nv"])
-def test_norm_extremes(form, K):
-    """Rows whose squares leave binary32, zero rows with and without eps, clipping."""
+def test_norm_extremes(form, K, repeat, residual):
+    """Rows whose squares leave binary32, zero rows with and without eps, in short batches and in ones that stream."""
     rng = np.random.default_rng(4)
-    base = rng.standard_normal((6, K)).astype(np.float32)
-    scale = np.array([1e25, 1e-25, 0.0, 1.0, 1e19, 1e-19], np.float32)[:, None]
+    base = np.tile(rng.standard_normal((6, K)).astype(np.float32), (repeat, 1))
+    scale = np.tile(np.array([1e25, 1e-25, 0.0, 1.0, 1e19, 1e-19], np.float32), repeat)[:, None]
     x = dev(base * scale)
+    zero = torch.zeros_like(x) if residual else None
     for eps in (0.0, 1e-6):
-        out = fq.rmsnorm_quantize_act(x, None, None, 1, 8, eps) if form == "int8" else fq.rmsnorm_quantize_act_fp4(x, None, None, 1, FORMATS[form], eps)
+        out = fq.rmsnorm_quantize_act(x, zero, None, 1, 8, eps) if form == "int8" else fq.rmsnorm_quantize_act_fp4(x, zero, None, 1, FORMATS[form], eps)
         d = (fq.quantize_act(x, None, 1, 8) if form == "int8" else fq.quantize_act_fp4(x, None, 1, FORMATS[form]))[-1]
         rms = (x.double().square().mean(1) + eps).sqrt()
         want = torch.where(d > 0, d.double() / rms, 0.0)
         got = out[-1].double()
         assert bool(torch.isfinite(got).all())
-        live = torch.tensor([0, 1, 3, 4, 5], device="cuda")
+        live = torch.tensor([i for i in range(6 * repeat) if i % 6 != 2], device="cuda")
         # (a result below binary32's normal numbers keeps a half of 2^-149)
         assert bool(((got - want)[live].abs() <= 27 * 2.0 ** -24 * want[live] + 2.0 ** -149).all())
         if form != "mx":
-            assert float(got[2]) == 0.0
+            assert bool((got[2::6] == 0.0).all())
 
 
 def test_norm_clip():
