@@ -101,11 +101,12 @@ __device__ __forceinline__ void mbar_arrive_cta(uint32_t bar, uint32_t rank) {
 //   %0 accumulator column  %1, %2 matrix descriptors (weights, tokens)  %3, %4 descriptors of their scales  %5 TMEM column of the scales
 //   %6 instruction descriptor  %7 add to what the accumulator holds  %8 MMAs of the stage  %9 the stage's barrier
 //   %10 the accumulator's barrier, 0: not its last stage  %11 (pairs) cluster ranks whose barriers the commits arrive at
+//   %12 TMEM column of the scales of the tile's first token: a tile of 64 tokens may begin in the middle of a scale tile
 #define FQ_CP(CG, SRC, OFF, COL)                                                     \
     "add.u64 t, " SRC ", " OFF ";\n\tadd.u32 c, %5, " COL ";\n\t"                     \
     "@pl tcgen05.cp.cta_group::" CG ".32x128b.warpx4 [c], t;\n\t"
 #define FQ_MMA(CG, KIND, STEP, SA, SB, ID, PRED, ACC)                                                        \
-    "add.u64 t, %1, " STEP ";\n\tadd.u64 u, %2, " STEP ";\n\tadd.u32 c, %5, " SA ";\n\tadd.u32 e, %5, " SB ";\n\t" \
+    "add.u64 t, %1, " STEP ";\n\tadd.u64 u, %2, " STEP ";\n\tadd.u32 c, %5, " SA ";\n\tadd.u32 e, %12, " SB ";\n\t" \
     "or.b32 f, %6, " ID ";\n\t"                                                                               \
     "@" PRED " tcgen05.mma.cta_group::" CG "." KIND " [%0], t, u, f, [c], [e], " ACC ";\n\t"
 #define FQ_HEAD                                                                                  \
@@ -125,42 +126,42 @@ __device__ __forceinline__ void mbar_arrive_cta(uint32_t bar, uint32_t rank) {
 #define FQ_ID_ODD "1073741856"           /* blocks 2 and 3 of a scale tile, both operands: 2 << 29 | 2 << 4 */
 #define FQ_STAGE_NV1(CG) \
     FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "16") \
-    FQ_MMA(CG, FQ_KIND_NV, "0", "0", "16", "0", "pl", "pa") \
+    FQ_MMA(CG, FQ_KIND_NV, "0", "0", "0", "0", "pl", "pa") \
     FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "20") \
-    FQ_MMA(CG, FQ_KIND_NV, "2", "4", "20", "0", "p1", "pt") \
+    FQ_MMA(CG, FQ_KIND_NV, "2", "4", "4", "0", "p1", "pt") \
     FQ_CP(CG, "%3", "64", "8") FQ_CP(CG, "%4", "64", "24") \
-    FQ_MMA(CG, FQ_KIND_NV, "4", "8", "24", "0", "p2", "pt") \
+    FQ_MMA(CG, FQ_KIND_NV, "4", "8", "8", "0", "p2", "pt") \
     FQ_CP(CG, "%3", "96", "12") FQ_CP(CG, "%4", "96", "28") \
-    FQ_MMA(CG, FQ_KIND_NV, "6", "12", "28", "0", "p3", "pt")
+    FQ_MMA(CG, FQ_KIND_NV, "6", "12", "12", "0", "p3", "pt")
 #define FQ_STAGE_NV2(CG) \
     FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "16") FQ_CP(CG, "%4", "128", "20") \
-    FQ_MMA(CG, FQ_KIND_NV, "0", "0", "16", "0", "pl", "pa") \
+    FQ_MMA(CG, FQ_KIND_NV, "0", "0", "0", "0", "pl", "pa") \
     FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "24") FQ_CP(CG, "%4", "160", "28") \
-    FQ_MMA(CG, FQ_KIND_NV, "2", "4", "24", "0", "p1", "pt") \
+    FQ_MMA(CG, FQ_KIND_NV, "2", "4", "8", "0", "p1", "pt") \
     FQ_CP(CG, "%3", "64", "8") FQ_CP(CG, "%4", "64", "32") FQ_CP(CG, "%4", "192", "36") \
-    FQ_MMA(CG, FQ_KIND_NV, "4", "8", "32", "0", "p2", "pt") \
+    FQ_MMA(CG, FQ_KIND_NV, "4", "8", "16", "0", "p2", "pt") \
     FQ_CP(CG, "%3", "96", "12") FQ_CP(CG, "%4", "96", "40") FQ_CP(CG, "%4", "224", "44") \
-    FQ_MMA(CG, FQ_KIND_NV, "6", "12", "40", "0", "p3", "pt")
+    FQ_MMA(CG, FQ_KIND_NV, "6", "12", "24", "0", "p3", "pt")
 #define FQ_STAGE_MX1(CG) \
     FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "8") \
-    FQ_MMA(CG, FQ_KIND_MX, "0", "0", "8", "0", "pl", "pa") \
-    FQ_MMA(CG, FQ_KIND_MX, "2", "0", "8", FQ_ID_ODD, "p1", "pt") \
+    FQ_MMA(CG, FQ_KIND_MX, "0", "0", "0", "0", "pl", "pa") \
+    FQ_MMA(CG, FQ_KIND_MX, "2", "0", "0", FQ_ID_ODD, "p1", "pt") \
     FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "12") \
-    FQ_MMA(CG, FQ_KIND_MX, "4", "4", "12", "0", "p2", "pt") \
-    FQ_MMA(CG, FQ_KIND_MX, "6", "4", "12", FQ_ID_ODD, "p3", "pt")
+    FQ_MMA(CG, FQ_KIND_MX, "4", "4", "4", "0", "p2", "pt") \
+    FQ_MMA(CG, FQ_KIND_MX, "6", "4", "4", FQ_ID_ODD, "p3", "pt")
 #define FQ_STAGE_MX2(CG) \
     FQ_CP(CG, "%3", "0", "0") FQ_CP(CG, "%4", "0", "8") FQ_CP(CG, "%4", "64", "12") \
-    FQ_MMA(CG, FQ_KIND_MX, "0", "0", "8", "0", "pl", "pa") \
-    FQ_MMA(CG, FQ_KIND_MX, "2", "0", "8", FQ_ID_ODD, "p1", "pt") \
+    FQ_MMA(CG, FQ_KIND_MX, "0", "0", "0", "0", "pl", "pa") \
+    FQ_MMA(CG, FQ_KIND_MX, "2", "0", "0", FQ_ID_ODD, "p1", "pt") \
     FQ_CP(CG, "%3", "32", "4") FQ_CP(CG, "%4", "32", "16") FQ_CP(CG, "%4", "96", "20") \
-    FQ_MMA(CG, FQ_KIND_MX, "4", "4", "16", "0", "p2", "pt") \
-    FQ_MMA(CG, FQ_KIND_MX, "6", "4", "16", FQ_ID_ODD, "p3", "pt")
+    FQ_MMA(CG, FQ_KIND_MX, "4", "4", "8", "0", "p2", "pt") \
+    FQ_MMA(CG, FQ_KIND_MX, "6", "4", "8", FQ_ID_ODD, "p3", "pt")
 template <int CTAS, bool NV, int XA>
-__device__ __forceinline__ void issue_stage(uint32_t d, uint64_t wd, uint64_t xd, uint64_t ws, uint64_t xs, uint32_t cols, uint32_t idesc, uint32_t accumulate,
-                                            int steps, uint32_t bar_stage, uint32_t bar_acc, uint16_t mask) {
+__device__ __forceinline__ void issue_stage(uint32_t d, uint64_t wd, uint64_t xd, uint64_t ws, uint64_t xs, uint32_t cols, uint32_t xcols, uint32_t idesc,
+                                            uint32_t accumulate, int steps, uint32_t bar_stage, uint32_t bar_acc, uint16_t mask) {
 #define FQ_STAGE(BODY, COMMIT)                                                                                               \
     asm volatile(FQ_HEAD BODY COMMIT ::"r"(d), "l"(wd), "l"(xd), "l"(ws), "l"(xs), "r"(cols), "r"(idesc), "r"(accumulate),   \
-                 "r"(steps), "r"(bar_stage), "r"(bar_acc), "h"(mask) : "memory")
+                 "r"(steps), "r"(bar_stage), "r"(bar_acc), "h"(mask), "r"(xcols) : "memory")
     if constexpr (CTAS == 1 && NV && XA == 1) FQ_STAGE(FQ_STAGE_NV1("1"), FQ_COMMIT_1);
     else if constexpr (CTAS == 1 && NV) FQ_STAGE(FQ_STAGE_NV2("1"), FQ_COMMIT_1);
     else if constexpr (CTAS == 1 && XA == 1) FQ_STAGE(FQ_STAGE_MX1("1"), FQ_COMMIT_1);
@@ -264,12 +265,13 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     };
     // A weight handle is complete before the call: its first stages come while the kernel ahead still runs, and (single CTAs, whose
     // loads concern nobody else) while this one is being set up.
-    const int ahead = unit0 < p.units ? min(p.stages, kb1 - kb0) : 0;
-    auto first_weights = [&]() {
-        if (ahead > 0 && elect_one()) {
+    // (Two of them: a copy takes its issuer 50 cycles, and everybody waits for the set-up.)
+    const int ahead = unit0 < p.units ? min(p.stages, kb1 - kb0) : 0, early = CTAS == 1 ? min(ahead, 2) : 0;
+    auto first_weights = [&](int from, int to) {
+        if (from < to && elect_one()) {
             int m, n;
             tile_of(unit0, &m, &n);
-            for (int i = 0; i < ahead; ++i) load_weights(n, kb0 + i, i);
+            for (int i = from; i < to; ++i) load_weights(n, kb0 + i, i);
         }
         __syncwarp();
     };
@@ -291,7 +293,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             fence_proxy_async_smem();
         }
         __syncwarp();
-        if (CTAS == 1) first_weights();
+        first_weights(0, early);
     } else if (warp == 1) {
         tmem_alloc<CTAS>(smem_u32(&s_tmem), 512u);
     } else if (warp == kTokenWarp && lane == 0) {
@@ -309,7 +311,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
 
     if (warp == 0 || warp == kTokenWarp) {
         // ------------------------------------------------------------ producers: of weights, of tokens
-        if (CTAS == 2 && warp == 0) first_weights();
+        if (warp == 0) first_weights(early, ahead);
         bool ok = true;
         int stage = 0, there = warp == 0 ? ahead : 0;
         uint32_t phase = 0;
@@ -330,7 +332,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                             const uint32_t bar = smem_u32(&s_full[stage]);
                             if (leader) mbar_arrive_expect_tx(bar, (x_bytes + x_scale) * CTAS);
                             tma_load<CTAS>(s_x + stage * x_bytes, &map_x, kb * 128, t0, bar);
-                            tma_load_tiles<CTAS>(s_xs + stage * x_scale, &map_xs, kb * kTiles, m * (p.bt / 128), bar);
+                            tma_load_tiles<CTAS>(s_xs + stage * x_scale, &map_xs, kb * kTiles, (int)((int64_t)m * p.bt >> 7), bar);
                         }
                     }
                     __syncwarp();
@@ -353,13 +355,15 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 ok = mbar_wait_all(smem_u32(&s_acc_empty[acc]), acc_phase ^ 1u, abort_flag, p.watchdog, kWdMmaAcc);
                 if (!ok) break;
                 const uint32_t d = tmem + (uint32_t)(acc * acc_cols);
+                const uint32_t first = kTiles * 4 + (uint32_t)(((int64_t)m * p.bt & 127) >> 5);       // columns ahead of the tokens' scales
                 for (int kb = kb0; kb < kb1; ++kb) {
                     ok = mbar_wait_all(smem_u32(&s_full[stage]), phase, abort_flag, p.watchdog, kWdMmaFull);
                     if (!ok) break;
                     tc_fence_after();
                     // (what lies past K's last scale tile is never multiplied: zeros times whatever a scale holds)
                     issue_stage<CTAS, NV, XA>(d, smem_desc_sw128(s_w + stage * kWBytes), smem_desc_sw128(s_x + stage * x_bytes), scale_desc(s_ws + stage * kWScale),
-                                              scale_desc(s_xs + stage * x_scale), tmem + kScaleCols + (uint32_t)(stage * slot_cols), idesc,
+                                              scale_desc(s_xs + stage * x_scale), tmem + kScaleCols + (uint32_t)(stage * slot_cols),
+                                              tmem + kScaleCols + (uint32_t)(stage * slot_cols) + first, idesc,
                                               kb != kb0 ? 1u : 0u, (p.K - kb * kStageK + 63) / 64, smem_u32(&s_empty[stage]),
                                               kb == kb1 - 1 ? smem_u32(&s_acc_full[acc]) : 0u, mask);
                     if (++stage == p.stages) { stage = 0; phase ^= 1u; }
@@ -572,20 +576,46 @@ struct Plan {
 };
 // What a slice of K receives from the others.
 size_t split_bytes(int bt, int split) { return (size_t)(split - 1) * ((bt / 16 + split - 1) / split) * 8192; }
-Plan plan(int64_t M, int64_t N, int64_t K) {
-    Plan r = {1, 0, 1};
+// Tiles (single CTAs of 128 channels x 64, 128 or 256 tokens, or all of them where there are few; pairs of 256 x 256) and slices of K
+// by the time that they are expected to take, in us: so many waves of (stages of a slice, epilogue), and what the slices' exchange
+// adds.  The constants are those of the launches below; measured, the choice against the next best:
+//   1 x 2048 x 2560 two slices 4.8 (one 5.0, four 5.1), 1 x 16384 x 2048 four 8.7 (two 13.2), 1 x 1024 x 4096 one 3.8 (two 4.1),
+//   333 x 1120 x 1000 tiles of 64 tokens 5.0 (128: 6.0), 816 x 2048 x 2560 128 tokens 7.4 (pairs 9.1), 816 x 16384 x 2048 pairs in two
+//   slices 19.7 (one 28.6), 816 x 2048 x 32768 pairs 37.0 (single CTAs 39.8).
+Plan plan(int64_t M, int64_t N, int64_t K, int (*held)(int)) {
     const int sms = device_sm_count();
-    r.bt = M <= 256 ? (int)((M + 15) / 16 * 16) : 256;
-    const int64_t pairs = (N + 255) / 256 * ((M + 255) / 256);
-    if (M > 128 && pairs * 2 >= sms / 2) {
-        r.ctas = 2;
-        r.bt = M <= 256 ? (int)((M + 31) / 32 * 32) : 256;
-    }
-    const int64_t tiles = (N + 128 * r.ctas - 1) / (128 * r.ctas) * ((M + r.bt - 1) / r.bt);
     const int64_t kb = (K + kStageK - 1) / kStageK;
-    while (r.split * r.ctas < 8 && tiles * r.ctas * r.split * 2 <= sms && kb >= r.split * 4) r.split *= 2;
-    return r;
+    Plan best = {1, 256, 1};
+    float least = 0.0f;
+    auto offer = [&](int ctas, int bt, float stage, float epilogue) {
+        const int64_t tiles = (N + 128 * ctas - 1) / (128 * ctas) * ((M + bt - 1) / bt);
+        for (int split = 1; split * ctas <= 8 && split <= kb; split *= 2) {
+            const int cluster = split * ctas;
+            if (split > 1 && tiles * cluster > sms) break;
+            if (cluster > 1 && (held(cluster) == 0 || (split > 1 && tiles > held(cluster)))) continue;
+            const float waves = (float)((tiles * cluster + sms - 1) / sms);
+            float t = waves * ((float)((kb + split - 1) / split) * stage + epilogue);
+            // (clusters of four on most of the device wait for one another's places)
+            if (split > 1) t += (split == 2 ? 0.75f : split == 4 ? 1.5f : 2.6f) + 0.006f * (float)bt + (ctas == 1 && split == 4 && tiles * 4 > 96 ? 1.2f : 0.0f);
+            if (least == 0.0f || t < least) {
+                least = t;
+                best = {ctas, bt, split};
+            }
+        }
+    };
+    if (M <= 128) {
+        const int bt = (int)((M + 15) / 16 * 16);
+        offer(1, bt, 0.29f + 0.0005f * (float)bt, 0.4f + 0.004f * (float)bt);
+    }
+    if (M > 64) offer(1, 64, 0.30f, 0.6f);
+    if (M > 128) {
+        offer(1, 128, 0.36f, 0.9f);
+        offer(1, 256, 0.50f, 1.8f);
+        offer(2, 256, 0.38f, 1.8f);
+    }
+    return best;
 }
+int no_clusters(int) { return 0; }
 
 struct Maps {
     CUtensorMap x, xs;
@@ -609,11 +639,12 @@ bool fp4_weight_maps(Fp4Weights& W) {
     return W.N == 0 || (code_map(&W.map_codes, W.codes, W.N, W.K, kRows) && scale_map(&W.map_scales, W.scales, W.N, W.K, W.format, 1));
 }
 
-fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const float* delta, int64_t M, const Fp4Weights& W, void* y,
-                          fq_dtype yt, int64_t ldy, cudaStream_t stream) {
-    if (M == 0 || W.N == 0) return FQ_OK;
+namespace {
+// *refused: the device did not take the launch's clusters, nothing was enqueued.
+fq_status launch_planned(const uint8_t* codes, const uint8_t* scales, const float* delta, int64_t M, const Fp4Weights& W, void* y, fq_dtype yt,
+                         int64_t ldy, int (*held)(int), cudaStream_t stream, bool* refused) {
     const int sms = device_sm_count();
-    const Plan r = plan(M, W.N, W.K);
+    const Plan r = plan(M, W.N, W.K, held);
     const bool nv = W.format == FQ_NVFP4;
     GemmParams p = {};
     p.M = M; p.N = W.N; p.K = (int)W.K; p.ldy = ldy;
@@ -657,7 +688,17 @@ fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const flo
     const cudaError_t e = r.ctas == 2 ? launch<2, 2>(W, maps, p, grid, smem, stream)
                           : xa == 2  ? launch<1, 2>(W, maps, p, grid, smem, stream)
                                      : launch<1, 1>(W, maps, p, grid, smem, stream);
+    *refused = r.ctas * r.split > 1 && cluster_refused(e);
     return e == cudaSuccess ? FQ_OK : FQ_ERR_CUDA;
+}
+}  // namespace
+
+fq_status launch_gemm_fp4(const uint8_t* codes, const uint8_t* scales, const float* delta, int64_t M, const Fp4Weights& W, void* y, fq_dtype yt,
+                          int64_t ldy, cudaStream_t stream) {
+    if (M == 0 || W.N == 0) return FQ_OK;
+    bool refused = false;
+    const fq_status st = launch_planned(codes, scales, delta, M, W, y, yt, ldy, cluster_capacity, stream, &refused);
+    return refused ? launch_planned(codes, scales, delta, M, W, y, yt, ldy, no_clusters, stream, &refused) : st;
 }
 
 }  // namespace fq

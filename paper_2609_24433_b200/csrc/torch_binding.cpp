@@ -554,16 +554,22 @@ PyObject* tuple_of(std::initializer_list<at::Tensor> list) {
     for (const at::Tensor& t : list) PyTuple_SET_ITEM(r, i++, THPVariable_Wrap(t));
     return r;
 }
+// A site's multiplier: None (the constant block^-1/2), a float tensor of K elements, or the address of a handle's own.
+const float* multiplier_of(PyObject* o, int64_t K) {
+    if (none(o)) return nullptr;
+    if (PyLong_Check(o)) return static_cast<const float*>(address(o));
+    return static_cast<const float*>(vector_of(o, at::kFloat, K, "mult_g").data_ptr());
+}
 fq_fp4_format format_of(long long f) { return f == FQ_MXFP4 || f == FQ_NVFP4 ? static_cast<fq_fp4_format>(f) : static_cast<fq_fp4_format>(7); }
 bool known(fq_fp4_format f) { return f == FQ_MXFP4 || f == FQ_NVFP4; }
 
-// quantize_act_fp4(x, multiplier address, block, format, codes, scales, delta) -> (codes, scales, delta)
+// quantize_act_fp4(x, multiplier, block, format, codes, scales, delta) -> (codes, scales, delta)
 PyObject* quantize_act_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         arguments(n, 7);
         const at::Tensor& x = on_device(rowmajor(a[0]), "x");
-        const float* g = static_cast<const float*>(address(a[1]));
         const int64_t M = x.size(0), K = x.size(1);
+        const float* g = multiplier_of(a[1], K);
         const long long block = integer(a[2]);
         const fq_fp4_format f = format_of(integer(a[3]));
         const fq_dtype xt = dtype_of(x.scalar_type());
@@ -669,12 +675,12 @@ struct NormRows {
     const at::Tensor& stream_rows() { return residual ? h.t : x; }
 };
 
-// rmsnorm_quantize_act(x, residual, multiplier address, block, bits, eps, clip_ratio, h, codes, delta) -> (h, codes, delta)
+// rmsnorm_quantize_act(x, residual, multiplier, block, bits, eps, clip_ratio, h, codes, delta) -> (h, codes, delta)
 PyObject* rmsnorm_quantize_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         arguments(n, 10);
         NormRows r(a[0], a[1], a[7]);
-        const float* g = static_cast<const float*>(address(a[2]));
+        const float* g = multiplier_of(a[2], r.K);
         const long long block = integer(a[3]), bits = integer(a[4]);
         const float eps = real(a[5]), clip = real(a[6]);
         if (bits != 4 && bits != 8) return status(FQ_ERR_INVALID_ARG);
@@ -692,12 +698,12 @@ PyObject* rmsnorm_quantize_act(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// rmsnorm_quantize_act_fp4(x, residual, multiplier address, block, format, eps, h, codes, scales, delta) -> (h, codes, scales, delta)
+// rmsnorm_quantize_act_fp4(x, residual, multiplier, block, format, eps, h, codes, scales, delta) -> (h, codes, scales, delta)
 PyObject* rmsnorm_quantize_act_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         arguments(n, 10);
         NormRows r(a[0], a[1], a[6]);
-        const float* g = static_cast<const float*>(address(a[2]));
+        const float* g = multiplier_of(a[2], r.K);
         const long long block = integer(a[3]);
         const fq_fp4_format f = format_of(integer(a[4]));
         const float eps = real(a[5]);

@@ -482,15 +482,16 @@ class Fp4Weights:
         blk, fmt = ctypes.c_int(), ctypes.c_int()
         _check(lib().fq_fp4_weights_info(self._h, ctypes.byref(n), ctypes.byref(k), ctypes.byref(blk), ctypes.byref(fmt)), "fq_fp4_weights_info")
         self.N, self.K, self.block, self.format = n.value, k.value, blk.value, fmt.value
+        self._addr = self._h.value
 
     @property
     def address(self) -> int:
-        if self._h is None:
+        if self._addr is None:
             raise RuntimeError("weights handle already destroyed")
-        return self._h.value
+        return self._addr
 
     def multiplier_ptr(self) -> int:
-        return int(lib().fq_fp4_weights_multiplier(self.address) or 0)
+        return int(lib().fq_fp4_weights_multiplier(ctypes.c_void_p(self.address)) or 0)
 
     def export(self) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
         """(codes u8 [N, K/2], scales u8 (tiles), w_scale [N], mult_g [K], bias [N]) as new device tensors."""
@@ -505,7 +506,7 @@ class Fp4Weights:
     def destroy(self):
         if self._h is not None:
             lib().fq_fp4_weights_destroy(self._h)
-            self._h = None
+            self._h = self._addr = None
 
     def __del__(self):
         try:
@@ -549,20 +550,22 @@ def weights_import_fp4(codes: torch.Tensor, scales: torch.Tensor, w_scale: Optio
     return Fp4Weights(out.value)
 
 
-def _multiplier(mult_g, K: int) -> int:
-    """Address of a site's multiplier: a float32 tensor, a handle's own, or None (the constant block^-1/2)."""
-    if isinstance(mult_g, (Weights, Fp4Weights)):
-        if mult_g.K != K:
-            raise ValueError(f"the handle has {mult_g.K} channels, the rows {K}")
-        if isinstance(mult_g, Weights) and (mult_g.fold_after or lib().fq_weights_composite(mult_g.handle)):
-            raise ValueError("the multiplier of a fold-after or composite site does not stand ahead of the butterflies")
-        return mult_g.multiplier_ptr()
-    return _floats(mult_g, K, "mult_g").value or 0
+def _multiplier(mult_g, x: torch.Tensor):
+    """What the native call takes for a site's multiplier: a float32 tensor or None as they are, a handle's own by its address."""
+    if mult_g is None or mult_g.__class__ is torch.Tensor:
+        return mult_g
+    if not isinstance(mult_g, (Weights, Fp4Weights)):
+        raise TypeError(f"mult_g has to be a tensor, a handle or None, got {type(mult_g).__name__}")
+    if mult_g.K != x.shape[-1]:
+        raise ValueError(f"the handle has {mult_g.K} channels, the rows {x.shape[-1]}")
+    if isinstance(mult_g, Weights) and (mult_g.fold_after or lib().fq_weights_composite(mult_g.handle)):
+        raise ValueError("the multiplier of a fold-after or composite site does not stand ahead of the butterflies")
+    return mult_g.multiplier_ptr()
 
 
 def quantize_act_fp4(x: torch.Tensor, mult_g, hadamard_block: int, format: int = NVFP4, codes=None, scales=None, delta=None):
     """(codes u8 [M, K/2], block scales u8 in tiles, steps [M]).  ``mult_g``: device float tensor, a handle (its multiplier) or None."""
-    return _result(_native().quantize_act_fp4(x, _multiplier(mult_g, x.shape[-1]), hadamard_block, format, codes, scales, delta),
+    return _result(_native().quantize_act_fp4(x, _multiplier(mult_g, x), hadamard_block, format, codes, scales, delta),
                    "fq_quantize_act_fp4")
 
 
@@ -581,14 +584,14 @@ def rmsnorm_quantize_act(x: torch.Tensor, residual: Optional[torch.Tensor], mult
                          clip_ratio: float = 1.0, h=None, codes=None, delta=None):
     """(h, codes u8 [M, K*bits/8], steps [M]): h = x + residual (x itself without one) and the codes of h / rms(h) for a site whose
     multiplier is ``mult_g`` (device float tensor, a Weights or None)."""
-    return _result(_native().rmsnorm_quantize_act(x, residual, _multiplier(mult_g, x.shape[-1]), hadamard_block, bits, eps, clip_ratio, h, codes, delta),
+    return _result(_native().rmsnorm_quantize_act(x, residual, _multiplier(mult_g, x), hadamard_block, bits, eps, clip_ratio, h, codes, delta),
                    "fq_rmsnorm_quantize_act")
 
 
 def rmsnorm_quantize_act_fp4(x: torch.Tensor, residual: Optional[torch.Tensor], mult_g, hadamard_block: int, format: int = NVFP4,
                              eps: float = 1e-6, h=None, codes=None, scales=None, delta=None):
     """(h, codes u8 [M, K/2], block scales, steps [M]) of the same in e2m1."""
-    return _result(_native().rmsnorm_quantize_act_fp4(x, residual, _multiplier(mult_g, x.shape[-1]), hadamard_block, format, eps, h, codes, scales, delta),
+    return _result(_native().rmsnorm_quantize_act_fp4(x, residual, _multiplier(mult_g, x), hadamard_block, format, eps, h, codes, scales, delta),
                    "fq_rmsnorm_quantize_act_fp4")
 
 
