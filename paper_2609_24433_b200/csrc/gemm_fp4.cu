@@ -27,7 +27,7 @@
 namespace fq {
 namespace {
 
-constexpr int kEpi = 16;                 // epilogue warps, from warp 2 on
+constexpr int kEpi = 8;                 // epilogue warps, from warp 2 on
 constexpr int kSets = kEpi / 4;          // of them to a quadrant of lanes
 constexpr int kChunks = 16 / kSets;      // chunks of 16 tokens of a warp at most
 constexpr int kTokenWarp = 2 + kEpi;
@@ -37,7 +37,7 @@ constexpr int kStageK = 256;             // channels of K a stage
 constexpr int kMostStages = 8;
 constexpr int kScaleCols = 256;          // TMEM columns from here on hold scales, those before accumulators
 constexpr size_t kSmemMost = 224 * 1024; // (and 2.3 KB of static shared memory)
-constexpr uint32_t kOutBytesWarp = 2048; // outputs of an epilogue warp on their way out: 16 tokens x 32 channels
+constexpr uint32_t kOutBytesWarp = 4096; // outputs of an epilogue warp on their way out
 constexpr uint32_t kOutBytes = kEpi * kOutBytesWarp;
 constexpr size_t kRingMost = kSmemMost - 1024 - kOutBytes;       // stages, and what slices of K receive
 
@@ -191,6 +191,11 @@ __device__ __forceinline__ void stmatrix_x4_trans(uint32_t addr, uint32_t r0, ui
     asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};"
                  ::"r"(addr), "r"(r0), "r"(r1), "r"(r2), "r"(r3));
 }
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int c0, int c1, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(src)
+                 : "memory");
+}
 // One channel at two adjacent tokens, rounded to bf16, the earlier token in the low half.
 __device__ __forceinline__ uint32_t scale_pair(uint32_t a0, uint32_t a1, float2 d, float sw, float bj) {
     const float2 v = f2_fma(make_float2(__uint_as_float(a0), __uint_as_float(a1)), f2_mul(d, make_float2(sw, sw)), make_float2(bj, bj));
@@ -214,7 +219,7 @@ __device__ __forceinline__ void sts32_loose(uint32_t addr, uint32_t v) { asm vol
 template <int CTAS, bool NV, bool SPLIT, int XA>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_x,
-                const __grid_constant__ CUtensorMap map_xs, const GemmParams p) {
+                const __grid_constant__ CUtensorMap map_xs, const __grid_constant__ CUtensorMap map_y, const GemmParams p) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t s_full[kMostStages], s_empty[kMostStages], s_acc_full[2], s_acc_empty[2], s_ended, s_sums;
     __shared__ __align__(16) float s_steps[kEpi][32];        // of the tokens that each epilogue warp is at
@@ -299,6 +304,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
     } else if (warp == kTokenWarp && lane == 0) {
         prefetch_map(&map_x);
         prefetch_map(&map_xs);
+        prefetch_map(&map_y);
     }
     tc_fence_before();
     __syncthreads();
@@ -403,22 +409,27 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                 tmem_ld16(tmem + lanes + column, r);
             }
         };
-        // Outputs of chunk i, token-major through the warp's own shared memory, then 16 bytes a lane.  (Bulk stores queue behind the
-        // loads of the stages: waiting for one to have read its buffer took 1000 cycles a chunk.)
+        // Outputs of chunk i, token-major, through one of the warp's buffers, which a bulk store reads; it clips what lies past M or N.
+        int stores = 0;
         auto emit = [&](const uint32_t* r, int i, int64_t t0, int64_t jq) {
-            const uint32_t buf = s_out + (uint32_t)(warp - 2) * kOutBytesWarp;
-            __syncwarp();
-            if ((i & 1) == 0 || SPLIT) {
+            if (((i & 1) == 0 || SPLIT)) {
                 float st = step2[0];
 #pragma unroll
                 for (int k = 1; k < kChunks / 2; ++k) st = i / 2 == k ? step2[k] : st;
-                steps[lane] = st;
                 __syncwarp();
+                steps[lane] = st;
             }
             const float* const st = steps + (i & 1) * 16;
             const int64_t tc = t0 + token(i);
+            if (stores >= (p.bf16 ? 4 : 2)) {
+                if (p.bf16) bulk_wait_read<3>();
+                else bulk_wait_read<1>();
+            }
+            __syncwarp();
+            const uint32_t buf = s_out + (uint32_t)(warp - 2) * kOutBytesWarp + (uint32_t)(p.bf16 ? (stores & 3) * 1024 : (stores & 1) * 2048);
+            ++stores;
             if (p.bf16) {
-                // scaled in pairs, [16 tokens][32 channels] by transposing matrix stores (16-byte pieces of a row mixed by token / 2)
+                // scaled in pairs, [16 tokens][32 channels] by transposing matrix stores (64-byte swizzle)
                 const float2 d0 = *reinterpret_cast<const float2*>(st + 2 * (lane & 3)), d1 = *reinterpret_cast<const float2*>(st + 8 + 2 * (lane & 3));
                 const uint32_t tok = (uint32_t)((lane >> 4) * 8 + (lane & 7)), ch = (uint32_t)((lane >> 3) & 1), mix = (tok >> 1) & 3u;
                 const uint32_t to = buf + tok * 64u;
@@ -426,15 +437,6 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                                   scale_pair(r[4], r[5], d1, sw4[0], bj4[0]), scale_pair(r[6], r[7], d1, sw4[1], bj4[1]));
                 stmatrix_x4_trans(to + (((ch + 2u) ^ mix) << 4), scale_pair(r[8], r[9], d0, sw4[2], bj4[2]), scale_pair(r[10], r[11], d0, sw4[3], bj4[3]),
                                   scale_pair(r[12], r[13], d1, sw4[2], bj4[2]), scale_pair(r[14], r[15], d1, sw4[3], bj4[3]));
-                __syncwarp();
-                const int row = lane >> 2, piece = lane & 3;
-                __nv_bfloat16* y = static_cast<__nv_bfloat16*>(p.y) + (tc + row) * p.ldy + jq + piece * 8;
-                const bool j_ok = jq + piece * 8 < p.N;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint4 v = lds128(buf + (uint32_t)((k * 8 + row) * 64 + ((piece ^ ((row >> 1) & 3)) << 4)));
-                    if (j_ok && tc + k * 8 + row < p.M) *reinterpret_cast<uint4*>(y + k * 8 * p.ldy) = v;
-                }
             } else {
 #pragma unroll
                 for (int k = 0; k < 16; ++k) {
@@ -442,16 +444,14 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                     const float d = k % 4 == 0 ? q.x : k % 4 == 1 ? q.y : k % 4 == 2 ? q.z : q.w;
                     sts32_loose(buf + (uint32_t)(k * 128 + lane * 4), __float_as_uint(__fmaf_rn(__uint_as_float(r[k]), d * sw4[0], bj4[0])));
                 }
-                __syncwarp();
-                const int row = lane >> 3, piece = lane & 7;
-                float* y = static_cast<float*>(p.y) + (tc + row) * p.ldy + jq + piece * 4;
-                const bool j_ok = jq + piece * 4 < p.N;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint4 v = lds128(buf + (uint32_t)((k * 4 + row) * 128 + piece * 16));
-                    if (j_ok && tc + k * 4 + row < p.M) *reinterpret_cast<uint4*>(y + k * 4 * p.ldy) = v;
-                }
             }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (jq < p.N && elect_one()) {
+                tma_store_2d(&map_y, (int)(jq * (p.bf16 ? 2 : 4)), (int)tc, buf);
+                bulk_commit();
+            }
+            __syncwarp();
         };
         if constexpr (!SPLIT) {
             int acc = 0;
@@ -548,6 +548,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         }
     }
     __syncwarp();
+    if (warp >= 2 && warp < kTokenWarp) bulk_wait_read<0>();     // stores have read their buffers before the CTA gives them up
     if (SPLIT && CTAS == 1 && (warp < 2 || warp == kTokenWarp)) cluster_wait();
     tc_fence_before();
     __syncthreads();
@@ -618,14 +619,14 @@ Plan plan(int64_t M, int64_t N, int64_t K, int (*held)(int)) {
 int no_clusters(int) { return 0; }
 
 struct Maps {
-    CUtensorMap x, xs;
+    CUtensorMap x, xs, y;
 };
 template <int CTAS, bool NV, bool SPLIT, int XA>
 cudaError_t launch(const Fp4Weights& W, const Maps& maps, const GemmParams& p, int grid, size_t smem, cudaStream_t stream) {
     auto kern = gemm_fp4_kernel<CTAS, NV, SPLIT, XA>;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, (unsigned)(CTAS * p.split), W.map_codes, W.map_scales, maps.x, maps.xs, p);
+    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, (unsigned)(CTAS * p.split), W.map_codes, W.map_scales, maps.x, maps.xs, maps.y, p);
 }
 template <int CTAS, int XA>
 cudaError_t launch(const Fp4Weights& W, const Maps& maps, const GemmParams& p, int grid, size_t smem, cudaStream_t stream) {
@@ -682,6 +683,13 @@ fq_status launch_planned(const uint8_t* codes, const uint8_t* scales, const floa
     const size_t smem = 1024 + p.ring + kOutBytes + (p.shared_ring ? 0 : sums);
     Maps maps;
     if (!code_map(&maps.x, codes, M, W.K, r.bt / r.ctas) || !scale_map(&maps.xs, scales, M, W.K, W.format, xa)) return FQ_ERR_CUDA;
+    {   // outputs leave in boxes of [16 tokens][32 channels]
+        const int e = p.bf16 ? 2 : 4;
+        const uint64_t dims[2] = {(uint64_t)W.N * e, (uint64_t)M}, strides[1] = {(uint64_t)ldy * e};
+        const uint32_t box[2] = {32u * e, 16};
+        if (!encode_tiled(&maps.y, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, y, dims, strides, box, p.bf16 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_NONE))
+            return FQ_ERR_CUDA;
+    }
     const int units = r.split > 1 ? p.units : (p.units < sms / r.ctas ? p.units : sms / r.ctas);
     p.unit_step = units;
     const int grid = units * r.ctas * r.split;
