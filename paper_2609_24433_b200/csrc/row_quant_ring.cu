@@ -53,6 +53,12 @@ __device__ __forceinline__ void tma_store_row(const CUtensorMap* map, int row, u
                  ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(src)
                  : "memory");
 }
+// The same box as far as L2 only.
+__device__ __forceinline__ void prefetch_row(const CUtensorMap* map, int row) {
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %1, %2}];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row)
+                 : "memory");
+}
 // Barrier of a row group that also ANDs a predicate.
 __device__ __forceinline__ bool group_and(int id, int threads, bool pred) {
     uint32_t r;
@@ -192,6 +198,10 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
     for (int row = first; row < rows; row += step, ++n) {
         bool ok = mbar_wait_all(smem_u32(&full0[d]), ph, abort_flag, p.watchdog, 0x100u);
         const uint32_t slot = slot0 + (uint32_t)d * p.slot_bytes;
+        if (leader && p.depth == 1 && row + step < rows) {     // the next row has no slot yet: to L2 meanwhile
+            prefetch_row(&map_x, row + step);
+            if (residual) prefetch_row(&map_r, row + step);
+        }
         float2 v[H];
         float ss = 0.0f;
         auto load_row = [&]() {
