@@ -440,7 +440,8 @@ size_t fq_cross_attention_workspace_bytes(fq_dtype dt, int64_t q_rows, int q_hea
  *   FQ_NVFP4  step d = max |z| of the row * fl(1/2688) (6 * 448; a row with d < 2^-100 is the zero token: step, scales and codes 0), i = 1/d,
  *             S = e4m3((m i) * fl(1/6)), q = i/S (0 where S = 0), code = e2m1(z q);
  * e2m1 and e4m3 round to nearest, ties to even, and saturate; a zero keeps its sign.
- * K a multiple of 32, at most 32768; hadamard_block a power of two in [1, 256] dividing K; N a multiple of 8.
+ * K a multiple of 32, at most 32768; hadamard_block a power of two in [1, 256] dividing K; N a multiple of 8, at most 2^28; rows of a
+ * call at most 2^31 - 65536.
  * Codes, scales, x, y and multipliers begin on 16 bytes, steps on an element; leading dimensions are multiples of 8. */
 typedef enum { FQ_MXFP4 = 0, FQ_NVFP4 = 1 } fq_fp4_format;
 typedef struct fq_fp4_weights fq_fp4_weights;

@@ -10,7 +10,8 @@ using namespace fq;
 namespace {
 
 constexpr int64_t kMaxRowK = 32768;              // a row lies in the registers of one thread block
-constexpr int64_t kMaxRows = 1ll << 31;          // rows of one call, channels of one handle
+constexpr int64_t kMaxRows = 0x7fff0000;         // rows of one call (indexes of tiles are 32-bit)
+constexpr int64_t kMaxN = 1ll << 28;             // channels of one handle
 
 bool aligned(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 bool aligned16(const void* p) { return aligned(p, 16); }
@@ -79,7 +80,7 @@ fq_status check_handle(int64_t N, int64_t K, int block, fq_fp4_format f) {
     if (N < 0 || !valid_format(f)) return FQ_ERR_INVALID_ARG;
     const fq_status st = check_width(K, block);
     if (st != FQ_OK) return st;
-    return N % 8 == 0 && N <= kMaxRows ? FQ_OK : FQ_ERR_UNSUPPORTED;
+    return N % 8 == 0 && N <= kMaxN ? FQ_OK : FQ_ERR_UNSUPPORTED;
 }
 // A vector of a handle: the caller's or a constant.
 bool vector(float* dst, const float* src, float otherwise, int64_t n, cudaStream_t s) {

@@ -27,7 +27,7 @@
 namespace fq {
 namespace {
 
-constexpr int kEpi = 8;                 // epilogue warps, from warp 2 on
+constexpr int kEpi = 8;                  // epilogue warps, from warp 2 on
 constexpr int kSets = kEpi / 4;          // of them to a quadrant of lanes
 constexpr int kChunks = 16 / kSets;      // chunks of 16 tokens of a warp at most
 constexpr int kTokenWarp = 2 + kEpi;
@@ -36,13 +36,13 @@ constexpr int kRows = 128;               // channels of a CTA's tile
 constexpr int kStageK = 256;             // channels of K a stage
 constexpr int kMostStages = 8;
 constexpr int kScaleCols = 256;          // TMEM columns from here on hold scales, those before accumulators
-constexpr size_t kSmemMost = 224 * 1024; // (and 2.3 KB of static shared memory)
+constexpr size_t kSmemMost = 224 * 1024; // (and 1.3 KB of static shared memory)
 constexpr uint32_t kOutBytesWarp = 4096; // outputs of an epilogue warp on their way out
 constexpr uint32_t kOutBytes = kEpi * kOutBytesWarp;
 constexpr size_t kRingMost = kSmemMost - 1024 - kOutBytes;       // stages, and what slices of K receive
 
 struct GemmParams {
-    int64_t M, N, ldy;
+    int64_t M, N;
     int K, bt, stages, m_full, n_tiles, band;   // (m_full: token tiles of bt tokens)
     int split;                           // slices of K, each CTA (pair) of a cluster one
     int kb;                              // stages of all of K
@@ -53,7 +53,6 @@ struct GemmParams {
     const float* delta;
     const float* w_scale;
     const float* bias;
-    void* y;
     int bf16;
     uint32_t* watchdog;
 };
@@ -412,7 +411,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         // Outputs of chunk i, token-major, through one of the warp's buffers, which a bulk store reads; it clips what lies past M or N.
         int stores = 0;
         auto emit = [&](const uint32_t* r, int i, int64_t t0, int64_t jq) {
-            if (((i & 1) == 0 || SPLIT)) {
+            if ((i & 1) == 0 || SPLIT) {
                 float st = step2[0];
 #pragma unroll
                 for (int k = 1; k < kChunks / 2; ++k) st = i / 2 == k ? step2[k] : st;
@@ -593,12 +592,15 @@ Plan plan(int64_t M, int64_t N, int64_t K, int (*held)(int)) {
         for (int split = 1; split * ctas <= 8 && split <= kb; split *= 2) {
             const int cluster = split * ctas;
             if (split > 1 && tiles * cluster > sms) break;
-            if (cluster > 1 && (held(cluster) == 0 || (split > 1 && tiles > held(cluster)))) continue;
             const float waves = (float)((tiles * cluster + sms - 1) / sms);
             float t = waves * ((float)((kb + split - 1) / split) * stage + epilogue);
             // (clusters of four on most of the device wait for one another's places)
             if (split > 1) t += (split == 2 ? 0.75f : split == 4 ? 1.5f : 2.6f) + 0.006f * (float)bt + (ctas == 1 && split == 4 && tiles * 4 > 96 ? 1.2f : 0.0f);
             if (least == 0.0f || t < least) {
+                if (cluster > 1) {                            // (asked last: it costs the host more than the rest)
+                    const int most = held(cluster);
+                    if (most == 0 || (split > 1 && tiles > most)) continue;
+                }
                 least = t;
                 best = {ctas, bt, split};
             }
@@ -648,7 +650,7 @@ fq_status launch_planned(const uint8_t* codes, const uint8_t* scales, const floa
     const Plan r = plan(M, W.N, W.K, held);
     const bool nv = W.format == FQ_NVFP4;
     GemmParams p = {};
-    p.M = M; p.N = W.N; p.K = (int)W.K; p.ldy = ldy;
+    p.M = M; p.N = W.N; p.K = (int)W.K;
     p.bt = r.bt;
     p.split = r.split;
     p.kb = (int)((W.K + kStageK - 1) / kStageK);
@@ -658,7 +660,6 @@ fq_status launch_planned(const uint8_t* codes, const uint8_t* scales, const floa
     p.band = p.m_full >= 16 ? 8 : p.m_full > 0 ? p.m_full : 1;
     p.units = (p.m_full + (M % r.bt ? 1 : 0)) * p.n_tiles;
     p.delta = delta; p.w_scale = W.w_scale; p.bias = W.bias;
-    p.y = y;
     p.bf16 = yt == FQ_BF16;
     p.watchdog = watchdog_device_ptr();
     if (!p.watchdog) return FQ_ERR_CUDA;

@@ -517,9 +517,10 @@ cudaError_t by_format(const RowQuant& q, const RowMaps& maps, const RingArgs& p,
 
 cudaError_t launch_row_quantize_ring(const RowQuant& q, cudaStream_t stream) {
     const size_t esz = q.xt == FQ_BF16 ? 2 : 4, row = (size_t)q.K * esz;
+    if (q.rows < 256) return cudaErrorNotSupported;
     const int sms = device_sm_count();
     // whole 128-byte lines, at most 256 of them (a box); rows enough for several a group
-    if (row % 128 != 0 || row > 32768 || q.rows < 2 * sms || q.rows * q.K < (int64_t)sms * 8192 || q.rows > 0x7fffffff - 4096 * 16) return cudaErrorNotSupported;
+    if (row % 128 != 0 || row > 32768 || q.rows < 2 * sms || q.rows * q.K < (int64_t)sms * 8192 || q.rows > 0x7fff0000) return cudaErrorNotSupported;
     const int e = q.K % 64 == 0 && q.K >= 1536 ? 64 : 32;
     const int gw = (int)((q.K + 32 * e - 1) / (32 * e));
     if (gw > kWarps) return cudaErrorNotSupported;
