@@ -157,10 +157,10 @@ def test_quantize_special_rows(form):
         assert np.array_equal(host(codes), c)
 
 
+@pytest.mark.parametrize("M,K", [(70, 224), (1300, 1024), (400, 4160)])
 @pytest.mark.parametrize("form", ["mx", "nv"])
-def test_quantize_strides_and_bounds(form):
+def test_quantize_strides_and_bounds(form, M, K):
     """Rows inside a wider matrix, outputs inside wider memory: nothing else is written, every place of the scales is."""
-    M, K = 70, 224
     wide = dev(tokens(np.random.default_rng(1), M, K + 40))
     x = wide[:, 16:16 + K]
     sb = fq.fp4_scale_bytes(M, K, FORMATS[form])
@@ -239,12 +239,29 @@ def assert_product(y, want, size, K):
 @pytest.mark.parametrize("M,N,K", [
     (1, 8, 32), (1, 128, 64), (1, 2560, 2048), (2, 136, 96), (16, 128, 256), (17, 264, 288), (50, 1024, 1024), (64, 256, 512), (100, 512, 16384),
     (128, 128, 128), (129, 384, 320), (200, 2048, 8192), (255, 1000, 1120), (256, 256, 256), (257, 512, 544), (333, 1000, 1120), (300, 4104, 192),
-    (816, 2048, 2048), (513, 10000, 352), (2100, 2600, 1056)])
+    (816, 2048, 2048), (513, 10000, 352), (2100, 2600, 1056), (816, 1024, 8192), (130, 512, 32768), (3, 264, 32736)])
 def test_product(form, M, N, K, dtype):
     a, handle, want, size = product_case(form, M, N, K)
     y = fq.gemm_fp4(*a, handle, TYPES[dtype])
     check_status()
     assert_product(y, want, size, K)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_product_sizes_at_random(seed):
+    """Whatever tiles, slices of K and pairs the sizes lead to."""
+    import random
+    rng = random.Random(seed)
+    form = rng.choice(["mx", "nv"])
+    K = 32 * max(1, int(2 ** rng.uniform(0, 9)))
+    N = 8 * max(1, int(2 ** rng.uniform(0, min(9, 22 - np.log2(K)))))
+    M = max(1, int(2 ** rng.uniform(0, min(11, 22 - np.log2(K)))))
+    a, handle, want, size = product_case(form, M, N, K, seed)
+    dtype = rng.choice(["f32", "bf16"])
+    y = fq.gemm_fp4(*a, handle, TYPES[dtype])
+    assert_product(y, want, size, K)
+    assert torch.equal(fq.gemm_fp4(*a, handle, TYPES[dtype]), y)
+    check_status()
 
 
 def test_product_is_reproducible_and_each_row_its_own():
@@ -472,6 +489,67 @@ def test_streams_and_graphs():
         torch.cuda.synchronize()
         e = fq.rmsnorm_quantize_act_fp4(a, b, h, block)
         assert torch.equal(hh, e[0]) and torch.equal(y, fq.gemm_fp4(*e[1:], h)) and torch.equal(z, fq.linear_fp4(a, h))
+    check_status()
+
+
+def test_first_call_inside_a_capture():
+    """A process whose first calls are captured: every set-up that a launch needs is allowed there."""
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2609_24433_b200 import fq
+M, K, N = 640, 2048, 2560
+h = fq.fold_weights_fp4(torch.randn(N, K, device="cuda"), None, None, 64)
+x, r = (torch.randn(M, K, device="cuda").bfloat16() for _ in range(2))
+short = x[:3].clone()
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    n = fq.rmsnorm_quantize_act_fp4(x, r, h, 64)
+    y = fq.gemm_fp4(*n[1:], h, torch.bfloat16)
+    z = fq.linear_fp4(short, h)
+    w = fq.linear_fp4(x[:200], h)
+for _ in range(2):
+    g.replay()
+torch.cuda.synchronize()
+n2 = fq.rmsnorm_quantize_act_fp4(x, r, h, 64)
+assert all(torch.equal(a, b) for a, b in zip(n, n2))
+assert torch.equal(y, fq.gemm_fp4(*n2[1:], h, torch.bfloat16)) and torch.equal(z, fq.linear_fp4(short, h)) and torch.equal(w, fq.linear_fp4(x[:200], h))
+assert fq.device_status()[0] == fq.OK
+print("captured")
+"""
+    import os
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and "captured" in done.stdout, done.stderr[-2000:]
+
+
+def test_two_threads():
+    """Calls from two Python threads on streams of their own, one handle."""
+    import threading
+    M, N, K, block = 300, 1024, 2048, 128
+    rng = np.random.default_rng(12)
+    h = fq.fold_weights_fp4(dev(rng.standard_normal((N, K)).astype(np.float32)), None, None, block, fq.MXFP4)
+    xs = [dev(tokens(rng, M, K), "bf16") for _ in range(2)]
+    want = [fq.linear_fp4(x, h) for x in xs]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(30):
+                y = fq.linear_fp4(xs[i], h)
+                torch.cuda.current_stream().synchronize()
+                if not torch.equal(y, want[i]):
+                    bad.append(i)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
     check_status()
 
 
