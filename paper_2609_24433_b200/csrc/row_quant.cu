@@ -333,8 +333,13 @@ cudaError_t go(RowParams& p, cudaStream_t stream) {
     p.tpr = (p.K / E + 31) / 32 * 32;
     p.rpc = p.tpr >= 128 ? 1 : 128 / p.tpr;
     const int threads = p.tpr * p.rpc;
-    const int64_t all = (p.rows_pad + p.rpc - 1) / p.rpc, most = (int64_t)device_sm_count() * max_resident_blocks(reinterpret_cast<const void*>(kern), threads);
-    return launch_pdl(kern, (unsigned)(all < most ? all : most), (unsigned)threads, 0, stream, 1u, p);
+    int64_t blocks = (p.rows_pad + p.rpc - 1) / p.rpc;
+    const int sms = device_sm_count();
+    if (blocks > sms) {
+        const int64_t most = (int64_t)sms * max_resident_blocks(reinterpret_cast<const void*>(kern), threads);
+        if (blocks > most) blocks = most;
+    }
+    return launch_pdl(kern, (unsigned)blocks, (unsigned)threads, 0, stream, 1u, p);
 }
 template <typename XT, int FMT, bool NORM>
 cudaError_t by_width(RowParams& p, cudaStream_t stream) {
