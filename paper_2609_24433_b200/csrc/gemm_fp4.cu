@@ -267,6 +267,13 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         tma_load<CTAS>(s_w + s * kWBytes, &map_w, kb * 128, (n * CTAS + (int)half) * kRows, bar);
         tma_load_tiles<CTAS>(s_ws + s * kWScale, &map_ws, kb * kTiles, n * CTAS + (int)half, bar);
     };
+    auto load_tokens = [&](int m, int t0, int kb, int s) {
+        const uint32_t bar = smem_u32(&s_full[s]);
+        if (leader) mbar_arrive_expect_tx(bar, (x_bytes + x_scale) * CTAS);
+        tma_load<CTAS>(s_x + s * x_bytes, &map_x, kb * 128, t0, bar);
+        tma_load_tiles<CTAS>(s_xs + s * x_scale, &map_xs, kb * kTiles, (int)((int64_t)m * p.bt >> 7), bar);
+    };
+    auto first_token = [&](int m) { return m * p.bt + (int)half * (columns(m) / CTAS); };      // that this CTA loads
     // A weight handle is complete before the call: its first stages come while the kernel ahead still runs, and (single CTAs, whose
     // loads concern nobody else) while this one is being set up.
     // (Two of them: a copy takes its issuer 50 cycles, and everybody waits for the set-up.)
@@ -316,14 +323,23 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
 
     if (warp == 0 || warp == kTokenWarp) {
         // ------------------------------------------------------------ producers: of weights, of tokens
-        if (warp == 0) first_weights(early, ahead);
+        // (what needs no wait in one go: with a wait and an election each, the fourth stage's tokens were asked for 700 cycles after the first's)
+        if (warp == 0) {
+            first_weights(early, ahead);
+        } else if (ahead > 0 && elect_one()) {
+            int m, n;
+            tile_of(unit0, &m, &n);
+            const int t0 = first_token(m);
+            for (int i = 0; i < ahead; ++i) load_tokens(m, t0, kb0 + i, i);
+        }
+        __syncwarp();
         bool ok = true;
-        int stage = 0, there = warp == 0 ? ahead : 0;
+        int stage = 0, there = ahead;
         uint32_t phase = 0;
         for (int unit = unit0; unit < p.units && ok; unit += p.unit_step) {
             int m, n;
             tile_of(unit, &m, &n);
-            const int t0 = m * p.bt + (int)half * (columns(m) / CTAS);
+            const int t0 = first_token(m);
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (there > 0) {
                     --there;
@@ -331,14 +347,8 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
                     ok = mbar_wait_all_lazy(smem_u32(&s_empty[stage]), phase ^ 1u, abort_flag, p.watchdog, kWdProducer);
                     if (!ok) break;
                     if (elect_one()) {
-                        if (warp == 0) {
-                            load_weights(n, kb, stage);
-                        } else {
-                            const uint32_t bar = smem_u32(&s_full[stage]);
-                            if (leader) mbar_arrive_expect_tx(bar, (x_bytes + x_scale) * CTAS);
-                            tma_load<CTAS>(s_x + stage * x_bytes, &map_x, kb * 128, t0, bar);
-                            tma_load_tiles<CTAS>(s_xs + stage * x_scale, &map_xs, kb * kTiles, (int)((int64_t)m * p.bt >> 7), bar);
-                        }
+                        if (warp == 0) load_weights(n, kb, stage);
+                        else load_tokens(m, t0, kb, stage);
                     }
                     __syncwarp();
                 }
