@@ -143,15 +143,13 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
     auto stage_multiplier = [&]() {
         if (!p.mult) return;
         // a thread's slice as pairs (g[q], g[q + H]), its 16-byte pieces mixed by the slice's number
-        for (int i = threadIdx.x * 4; i < p.K; i += kThreads * 4) {
-            const float4 g4 = ld_global_f4(p.mult + i);
-            const float gv[4] = {g4.x, g4.y, g4.z, g4.w};
-            const uint32_t slice = (uint32_t)i / E, key = (slice & 7u) << 4;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t q = ((uint32_t)i % E) + k, off = q < H ? q * 8u : (q - H) * 8u + 4u;
-                *reinterpret_cast<float*>(gen + ((slice * (E * 4u) + off) ^ key)) = gv[k];
-            }
+#pragma unroll 4
+        for (int i = threadIdx.x; i < p.K / 8; i += kThreads) {
+            const uint32_t slice = (uint32_t)i / (H / 4), q = (uint32_t)i % (H / 4) * 4u, key = (slice & 7u) << 4;
+            const float4 lo = ld_global_f4(p.mult + slice * E + q), hi = ld_global_f4(p.mult + slice * E + H + q);
+            const uint32_t to = base + slice * (E * 4u);
+            sts128(to + ((q * 8u) ^ key), make_uint4(__float_as_uint(lo.x), __float_as_uint(hi.x), __float_as_uint(lo.y), __float_as_uint(hi.y)));
+            sts128(to + ((q * 8u + 16u) ^ key), make_uint4(__float_as_uint(lo.z), __float_as_uint(hi.z), __float_as_uint(lo.w), __float_as_uint(hi.w)));
         }
     };
     if (p.mult_ready) stage_multiplier();
