@@ -468,7 +468,8 @@ fq_status fq_fp4_weights_destroy(fq_fp4_weights* w);                 /* NULL is 
  * fq_quantize_act_fp4: x device [M, K] of dtype xt; mult_g device float[K] or NULL (the constant block^-1/2).
  * fq_gemm_fp4: y[t][j] = (sum of code products with their block scales) * (a_delta[t] s^W_j) + b_j; codes, scales and steps as
  *   fq_quantize_act_fp4 writes them for the handle's K and format.  Scales past the last row are not read into any output; those past
- *   the last block have to be 0.  No workspace.  One set of codes serves several handles of a site.
+ *   the last block have to be 0.  No workspace.  One set of codes serves several handles of a site.  Sums are binary32, in an order
+ *   that depends on M, N and K alone: the same call gives the same bits.
  * fq_linear_fp4: both; codes, scales and steps live in the workspace, 256-byte aligned, fq_linear_fp4_workspace_bytes() bytes, scratch. */
 fq_status fq_quantize_act_fp4(const void* x, fq_dtype xt, int64_t M, int64_t K, int64_t ldx, const float* mult_g, int hadamard_block,
                               fq_fp4_format format, void* codes_out, void* scales_out, float* delta_out, void* stream);
@@ -488,7 +489,8 @@ size_t fq_linear_fp4_workspace_bytes(int64_t M, int64_t K, fq_fp4_format format)
  * A learned gain belongs into mult_g (gain_c * (1/s_c) * block^-1/2, see fq_weights_set_multiplier); NULL: the constant block^-1/2.
  * residual device [M, K] of dtype xt, leading dimension ldr, or NULL: the stream is x as it is, and h has to be NULL.  Otherwise h
  * device [M, K] of dtype xt; it may be the very memory of x or of residual (same address and leading dimension), else nothing may
- * overlap.  eps >= 0.  The sum of squares is binary32 (binary64 where that overflows or vanishes). */
+ * overlap.  eps >= 0.  The sum of squares is binary32 (binary64 where that overflows or vanishes), in an order that depends on M and K:
+ * h, codes and scales of a row do not depend on the batch around it, the last bits of its delta may. */
 fq_status fq_rmsnorm_quantize_act(const void* x, const void* residual, fq_dtype xt, int64_t M, int64_t K, int64_t ldx, int64_t ldr,
                                   float eps, void* h, int64_t ldh, const float* mult_g, int hadamard_block, int bits, float clip_ratio,
                                   void* codes_out, float* delta_out, void* stream);

@@ -12,7 +12,7 @@
 // ahead of the stage's MMAs.  Their TMEM columns go by the stage, so that whoever refills a stage knows that the MMAs that
 // read them have ended.
 //
-// Roles: warp 0 producer of weights, warp 1 MMA issuer and TMEM allocator, warps 2-9 epilogue, warp 10 producer of tokens.
+// Roles: warp 0 producer of weights, warp 1 MMA issuer and TMEM allocator, then eight or twelve warps epilogue and one producer of tokens.
 // CTAS = 2: a pair works on 256 channels, each CTA loading its 128 weight rows and half of the tokens' codes, but the scales of
 // all tokens.  SPLIT: the CTAs (or pairs) of a cluster share one tile along K and exchange binary32 sums through the cluster's
 // shared memory, added in the order of the slices: the result does not depend on timing.
@@ -27,18 +27,19 @@
 namespace fq {
 namespace {
 
-constexpr int kEpi = 8;                  // epilogue warps, from warp 2 on
-constexpr int kSets = kEpi / 4;          // of them to a quadrant of lanes
-constexpr int kChunks = 16 / kSets;      // chunks of 16 tokens of a warp at most
-constexpr int kTokenWarp = 2 + kEpi;
-constexpr int kThreads = 32 * (kTokenWarp + 1);
+// Epilogue warps, from warp 2 on: twelve read a tile's sums out of TMEM faster than eight (816 x 2048 x 32768 33.7 us, else 34.5; 816 x
+// 2048 x 2560 6.8, else 7.1; sixteen spill).  Eight for slices of single CTAs, which are there for little work: fewer threads are set up
+// faster (one token x 2048 x 2560 4.4 us, else 4.6).
+template <int CTAS, bool SPLIT>
+constexpr int kEpiWarps = CTAS == 1 && SPLIT ? 8 : 12;
+template <int CTAS, bool SPLIT>
+constexpr int kThreads = 32 * (kEpiWarps<CTAS, SPLIT> + 3);
 constexpr int kRows = 128;               // channels of a CTA's tile
 constexpr int kStageK = 256;             // channels of K a stage
 constexpr int kMostStages = 8;
 constexpr int kScaleCols = 256;          // TMEM columns from here on hold scales, those before accumulators
 constexpr size_t kSmemMost = 224 * 1024; // (and 1.3 KB of static shared memory)
-constexpr uint32_t kOutBytesWarp = 4096; // outputs of an epilogue warp on their way out
-constexpr uint32_t kOutBytes = kEpi * kOutBytesWarp;
+constexpr uint32_t kOutBytes = 32768;    // outputs on their way out
 constexpr size_t kRingMost = kSmemMost - 1024 - kOutBytes;       // stages, and what slices of K receive
 
 struct GemmParams {
@@ -216,9 +217,12 @@ __device__ __forceinline__ void sts32_loose(uint32_t addr, uint32_t v) { asm vol
 
 // XA: scale tiles across a tile's tokens (two for more than 128, and for pairs).
 template <int CTAS, bool NV, bool SPLIT, int XA>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__((kThreads<CTAS, SPLIT>), 1)
 gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_ws, const __grid_constant__ CUtensorMap map_x,
                 const __grid_constant__ CUtensorMap map_xs, const __grid_constant__ CUtensorMap map_y, const GemmParams p) {
+    constexpr int kEpi = kEpiWarps<CTAS, SPLIT>, kTokenWarp = 2 + kEpi;
+    constexpr int kSets = kEpi / 4, kChunks = (16 / kSets + 1) / 2 * 2;       // warps to a quadrant of lanes, chunks of 16 tokens of a warp at most
+    constexpr int kBuffers = kEpi == 8 ? 4 : 2;              // of a warp for 16 bf16 tokens, 1 KB each (binary32: half as many)
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t s_full[kMostStages], s_empty[kMostStages], s_acc_full[2], s_acc_empty[2], s_ended, s_sums;
     __shared__ __align__(16) float s_steps[kEpi][32];        // of the tokens that each epilogue warp is at
@@ -388,7 +392,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         }
     } else {
         // ------------------------------------------------------------ epilogue
-        // kSets warps to a quadrant of lanes, alternating chunks of 16 tokens: chunk i of set s begins at token (s + kSets i) * 16.
+        // The warps of a quadrant alternate: chunks of 16 tokens: chunk i of set s begins at token (s + kSets i) * 16.
         const int quad = warp & 3, set = (warp - 2) >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         float* const steps = s_steps[warp - 2];
@@ -430,12 +434,12 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             }
             const float* const st = steps + (i & 1) * 16;
             const int64_t tc = t0 + token(i);
-            if (stores >= (p.bf16 ? 4 : 2)) {
-                if (p.bf16) bulk_wait_read<3>();
-                else bulk_wait_read<1>();
+            if (stores >= (p.bf16 ? kBuffers : kBuffers / 2)) {
+                if (p.bf16) bulk_wait_read<kBuffers - 1>();
+                else bulk_wait_read<kBuffers / 2 - 1>();
             }
             __syncwarp();
-            const uint32_t buf = s_out + (uint32_t)(warp - 2) * kOutBytesWarp + (uint32_t)(p.bf16 ? (stores & 3) * 1024 : (stores & 1) * 2048);
+            const uint32_t buf = s_out + (uint32_t)((warp - 2) * kBuffers + (p.bf16 ? stores % kBuffers : stores % (kBuffers / 2) * 2)) * 1024u;
             ++stores;
             if (p.bf16) {
                 // scaled in pairs, [16 tokens][32 channels] by transposing matrix stores (64-byte swizzle)
@@ -638,7 +642,7 @@ cudaError_t launch(const Fp4Weights& W, const Maps& maps, const GemmParams& p, i
     auto kern = gemm_fp4_kernel<CTAS, NV, SPLIT, XA>;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, (unsigned)(CTAS * p.split), W.map_codes, W.map_scales, maps.x, maps.xs, maps.y, p);
+    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads<CTAS, SPLIT>, smem, stream, (unsigned)(CTAS * p.split), W.map_codes, W.map_scales, maps.x, maps.xs, maps.y, p);
 }
 template <int CTAS, int XA>
 cudaError_t launch(const Fp4Weights& W, const Maps& maps, const GemmParams& p, int grid, size_t smem, cudaStream_t stream) {
