@@ -7,8 +7,9 @@
 // memory in strides: strides 1 .. 32 run in registers, two values an instruction, and at most two stages across lanes; and the rows
 // under way take no registers.
 //   - One CTA of 16 warps an SM, in row groups of gw warps; a group works on one row at a time and has `depth` slots.
-//   - A row is a box of 128-byte lines with the 128-byte swizzle, so that reading 64..256 bytes a thread has no bank conflicts; the
-//     multiplier lies beside it in the order that the packed multiply takes.
+//   - A row is a box (long ones several) of 128-byte lines with the 128-byte swizzle, so that reading 64..256 bytes a thread has no
+//     bank conflicts; the half line that may end a row of bf16 is a copy of its own.  The multiplier lies beside the slots in the
+//     order that the packed multiply takes.
 //   - The stream h = x + residual is written over x in its slot and leaves as a bulk store of the whole row.
 //   - E = 64: a thread holds the four block scales of 64 channels of e2m1 with e4m3 scales: one word of its scale tile.
 #include <cuda_bf16.h>
@@ -34,29 +35,44 @@ struct RingArgs {
     uint8_t* scales;
     int scale_tiles;
     float* delta;
-    uint32_t row_bytes;      // of one row in a slot, rounded up to 1024
+    uint32_t row_bytes;      // of one row in a slot, a multiple of 1024
     uint32_t slot_bytes;
     uint32_t mult_bytes;     // rounded up to 1024
     uint32_t stage_off;      // codes of a warp on their way out (8-bit codes)
     uint32_t* watchdog;
 };
+// Rows of several boxes, or with a half line behind them.
+struct LongArgs : RingArgs {
+    int boxes, box_lines, lines;             // (whole lines)
+    uint32_t tail_off;       // bf16 rows of an odd number of 64-byte halves: where in a slot the last one lies, 0: none
+    uint32_t tx;             // bytes of a slot's copies
+    const uint8_t* x;        // (for the halves)
+    const uint8_t* r;
+    uint8_t* h;
+    int64_t pitch_x, pitch_r, pitch_h;       // bytes
+};
+template <bool BOXES> struct ArgsOf { using type = RingArgs; };
+template <> struct ArgsOf<true> { using type = LongArgs; };
 
 __device__ __forceinline__ uint32_t swz128(uint32_t off) { return off ^ (((off >> 7) & 7u) << 4); }
-__device__ __forceinline__ void tma_load_row(uint32_t dst, const CUtensorMap* map, int row, uint32_t bar) {
+__device__ __forceinline__ void tma_load_lines(uint32_t dst, const CUtensorMap* map, int line, int row, uint32_t bar) {
     asm volatile(
-        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %3}], [%4];"
-        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(bar)
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(line), "r"(row), "r"(bar)
         : "memory");
 }
-__device__ __forceinline__ void tma_store_row(const CUtensorMap* map, int row, uint32_t src) {
-    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %1, %2}], [%3];"
-                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row), "r"(src)
+__device__ __forceinline__ void tma_store_lines(const CUtensorMap* map, int line, int row, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(line), "r"(row), "r"(src)
                  : "memory");
 }
+__device__ __forceinline__ void bulk_store_1d(void* dst, uint32_t src, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
 // The same box as far as L2 only.
-__device__ __forceinline__ void prefetch_row(const CUtensorMap* map, int row) {
-    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %1, %2}];"
-                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(row)
+__device__ __forceinline__ void prefetch_lines(const CUtensorMap* map, int line, int row) {
+    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];"
+                 ::"l"(reinterpret_cast<uint64_t>(map)), "r"(0), "r"(line), "r"(row)
                  : "memory");
 }
 // Barrier of a row group that also ANDs a predicate.
@@ -109,14 +125,20 @@ __device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b) {        
 __device__ __forceinline__ uint32_t add_f32(uint32_t a, uint32_t b) { return __float_as_uint(__fadd_rn(__uint_as_float(a), __uint_as_float(b))); }
 
 // BLOCK: channels of the rotation, 0: p.block.  (Branches between the stages cost more than the stages: 13056 x 2048 in blocks of 128,
-// MXFP4, 24.9 us with and 21.0 without them.)
-template <typename XT, int E, int FMT, bool NORM, int BLOCK>
+// MXFP4, 24.9 us with and 20.8 without them.)  BOXES: rows of LongArgs; the others keep to arguments of 512 bytes, since with more
+// of them the same code spills (21.7 us).
+template <typename XT, int E, int FMT, bool NORM, int BLOCK, bool BOXES>
 __global__ void __launch_bounds__(kThreads, 1)
 row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_r, const __grid_constant__ CUtensorMap map_h,
-                         const RingArgs p) {
+                         const typename ArgsOf<BOXES>::type p) {
     constexpr bool kFp4 = FMT >= 3, kMx = FMT == 3;
     constexpr int H = E / 2;                               // v[i] = (channel i, channel i + H)
     const int block = BLOCK ? BLOCK : p.block;
+    uint32_t tail_off = 0u, tx = (uint32_t)p.K * (uint32_t)sizeof(XT) * (NORM && p.residual != 0 ? 2u : 1u);
+    if constexpr (BOXES) {
+        tail_off = p.tail_off;
+        tx = p.tx;
+    }
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t s_full[kMostSlots];
     __shared__ float2 s_part[2][kWarps];
@@ -144,28 +166,47 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
         if (!p.mult) return;
         // a thread's slice as pairs (g[q], g[q + H]), its 16-byte pieces mixed by the slice's number
 #pragma unroll 4
-        for (int i = threadIdx.x; i < p.K / 8; i += kThreads) {
+        for (int i = threadIdx.x; i < (BOXES ? (p.K + E - 1) / E * (H / 4) : p.K / 8); i += kThreads) {
             const uint32_t slice = (uint32_t)i / (H / 4), q = (uint32_t)i % (H / 4) * 4u, key = (slice & 7u) << 4;
-            const float4 lo = ld_global_f4(p.mult + slice * E + q), hi = ld_global_f4(p.mult + slice * E + H + q);
+            const float4 lo = ld_global_f4(p.mult + slice * E + q);
+            const float4 hi = ld_global_f4(p.mult + slice * E + H + q, !BOXES || slice * E + H + q < (uint32_t)p.K);       // (zeros past K)
             const uint32_t to = base + slice * (E * 4u);
             sts128(to + ((q * 8u) ^ key), make_uint4(__float_as_uint(lo.x), __float_as_uint(hi.x), __float_as_uint(lo.y), __float_as_uint(hi.y)));
             sts128(to + ((q * 8u + 16u) ^ key), make_uint4(__float_as_uint(lo.z), __float_as_uint(hi.z), __float_as_uint(lo.w), __float_as_uint(hi.w)));
         }
     };
     if (p.mult_ready) stage_multiplier();
+    if (tail_off) {                                      // what follows a last half line in its thread's slice: zeros, for good
+        const int pieces = ngroups * p.depth * (residual ? 2 : 1) * 4;
+        for (int i = threadIdx.x; i < pieces; i += kThreads)
+            sts128(base + p.mult_bytes + (uint32_t)(i >> 2) * p.row_bytes + tail_off + 64u + (uint32_t)(i & 3) * 16u, make_uint4(0u, 0u, 0u, 0u));
+    }
     __syncthreads();                                       // barriers before any copy
     griddep_wait();
     griddep_launch_dependents();
 
     const int rows = (int)p.rows, first = group * (int)gridDim.x + (int)blockIdx.x, step = (int)gridDim.x * ngroups;
-    const uint32_t tx = (uint32_t)p.K * (uint32_t)sizeof(XT) * (residual ? 2u : 1u);
     const uint32_t slot0 = base + p.mult_bytes + (uint32_t)(group * p.depth) * p.slot_bytes;
     uint64_t* const full0 = &s_full[group * p.depth];
+    // f(line, bytes from the slot's begin) for each box of a row
+    auto each_box = [&](auto&& f) {
+        if constexpr (BOXES)
+            for (int b = 0; b < p.boxes; ++b) f(b * p.box_lines, (uint32_t)(b * p.box_lines) * 128u);
+        else
+            f(0, 0u);
+    };
     auto request = [&](int d, int row) {
         const uint32_t bar = smem_u32(&full0[d]), slot = slot0 + (uint32_t)d * p.slot_bytes;
         mbar_arrive_expect_tx(bar, tx);
-        tma_load_row(slot, &map_x, row, bar);
-        if (residual) tma_load_row(slot + p.row_bytes, &map_r, row, bar);
+        each_box([&](int line, uint32_t at) {
+            tma_load_lines(slot + at, &map_x, line, row, bar);
+            if (residual) tma_load_lines(slot + p.row_bytes + at, &map_r, line, row, bar);
+        });
+        if constexpr (BOXES)
+            if (tail_off) {
+                bulk_load_1d(slot + tail_off, p.x + row * p.pitch_x + p.lines * 128, 64u, bar);
+                if (residual) bulk_load_1d(slot + p.row_bytes + tail_off, p.r + row * p.pitch_r + p.lines * 128, 64u, bar);
+            }
     };
     int issued = 0;
     if (leader) {
@@ -184,7 +225,7 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
                 *reinterpret_cast<uint32_t*>(p.scales + ((row >> 7) * p.scale_tiles + t) * 512 + (row & 31) * 16 + ((row & 127) >> 5) * 4) = 0u;
     if (idle) return;
 
-    const uint32_t xs0 = swz128((uint32_t)col0 * (uint32_t)sizeof(XT)), xs1 = swz128((uint32_t)col0 * (uint32_t)sizeof(XT) + 128u);
+    const uint32_t xs0 = tail_off && col0 == p.K - 32 ? tail_off : swz128((uint32_t)col0 * (uint32_t)sizeof(XT)), xs1 = swz128((uint32_t)col0 * (uint32_t)sizeof(XT) + 128u);
     const uint32_t gkey = (uint32_t)((col0 / E) & 7) << 4;
     const uint32_t g0 = base + (((uint32_t)col0 * 4u) ^ gkey), g1 = base + (((uint32_t)col0 * 4u + 128u) ^ gkey);
     const float2 neg1 = make_float2(-1.0f, -1.0f);
@@ -197,8 +238,10 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
         bool ok = mbar_wait_all(smem_u32(&full0[d]), ph, abort_flag, p.watchdog, 0x100u);
         const uint32_t slot = slot0 + (uint32_t)d * p.slot_bytes;
         if (leader && p.depth == 1 && row + step < rows) {     // the next row has no slot yet: to L2 meanwhile
-            prefetch_row(&map_x, row + step);
-            if (residual) prefetch_row(&map_r, row + step);
+            each_box([&](int line, uint32_t) {
+                prefetch_lines(&map_x, line, row + step);
+                if (residual) prefetch_lines(&map_r, line, row + step);
+            });
         }
         float2 v[H];
         float ss = 0.0f;
@@ -329,7 +372,7 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
         if (NORM && wg == 0) {
             if (m > 0.0f && !sum_in_range(total, p.eps)) {
                 double s = 0.0;                                // the row as it lies in its slot, in binary64
-                for (uint32_t at = (uint32_t)lane * 4u; at < (uint32_t)p.K * (uint32_t)sizeof(XT); at += 128u) {
+                auto square = [&](uint32_t at) {
                     const uint32_t w = *reinterpret_cast<const volatile uint32_t*>(gen + (slot - base) + at);
                     if (sizeof(XT) == 2) {
                         const double a = (double)__uint_as_float(w << 16), b = (double)__uint_as_float(w & 0xffff0000u);
@@ -337,7 +380,10 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
                     } else {
                         s += (double)__uint_as_float(w) * (double)__uint_as_float(w);
                     }
-                }
+                };
+                const uint32_t end = (uint32_t)p.K * (uint32_t)sizeof(XT) - (tail_off ? 64u : 0u);
+                for (uint32_t at = (uint32_t)lane * 4u; at < end; at += 128u) square(at);
+                if (tail_off) square(tail_off + (uint32_t)lane * 4u);        // (zeros behind it)
                 for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
                 rinv = (float)(1.0 / sqrt(s / p.K + (double)p.eps));
             } else {
@@ -349,7 +395,9 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
         // slot of the row before, whose store has had time to read it, is refilled (of a single slot: its own).
         if (leader) {
             if (residual) {
-                tma_store_row(&map_h, row, slot);
+                each_box([&](int line, uint32_t at) { tma_store_lines(&map_h, line, row, slot + at); });
+                if constexpr (BOXES)
+                    if (tail_off) bulk_store_1d(p.h + row * p.pitch_h + p.lines * 128, slot + tail_off, 64u);
                 bulk_commit();
                 if (p.depth == 1) {
                     bulk_wait_read<0>();
@@ -417,7 +465,8 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
             if (col_ok) {
                 uint4* dst = reinterpret_cast<uint4*>(p.codes + (int64_t)row * (p.K / 2) + col0 / 2);
 #pragma unroll
-                for (int j = 0; j < E / 32; ++j) dst[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+                for (int j = 0; j < E / 32; ++j)
+                    if (!BOXES || j == 0 || col0 + 32 * j < p.K) dst[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
             }
         } else {
             constexpr int kPer = FMT == 0 ? 8 : 4, kWords = H / kPer;      // codes of a word, words of a half
@@ -461,7 +510,8 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
             } else if (col_ok) {
                 uint4* dst = reinterpret_cast<uint4*>(p.codes + (int64_t)row * (p.K / 2) + col0 / 2);
 #pragma unroll
-                for (int j = 0; j < E / 32; ++j) dst[j] = make_uint4(w[(4 * j) % (2 * kWords)], w[(4 * j + 1) % (2 * kWords)], w[(4 * j + 2) % (2 * kWords)], w[(4 * j + 3) % (2 * kWords)]);
+                for (int j = 0; j < E / 32; ++j)
+                    if (!BOXES || j == 0 || col0 + 32 * j < p.K) dst[j] = make_uint4(w[(4 * j) % (2 * kWords)], w[(4 * j + 1) % (2 * kWords)], w[(4 * j + 2) % (2 * kWords)], w[(4 * j + 3) % (2 * kWords)]);
             }
         }
         if (leader) p.delta[row] = NORM ? __fmul_rn(dl, rinv) : dl;
@@ -481,32 +531,37 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
 struct RowMaps {
     CUtensorMap x, r, h;
 };
-template <typename XT, int E, int FMT, bool NORM, int BLOCK>
-cudaError_t go(const RowMaps& maps, const RingArgs& p, int grid, size_t smem, cudaStream_t stream) {
-    auto kern = row_quantize_ring_kernel<XT, E, FMT, NORM, BLOCK>;
+template <typename XT, int E, int FMT, bool NORM, int BLOCK, bool BOXES>
+cudaError_t go(const RowMaps& maps, const LongArgs& p, int grid, size_t smem, cudaStream_t stream) {
+    auto kern = row_quantize_ring_kernel<XT, E, FMT, NORM, BLOCK, BOXES>;
     const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void*>(kern), smem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, 1u, maps.x, maps.r, maps.h, p);
+    return launch_pdl(kern, (unsigned)grid, (unsigned)kThreads, smem, stream, 1u, maps.x, maps.r, maps.h, static_cast<const typename ArgsOf<BOXES>::type&>(p));
 }
-template <typename XT, int E, int FMT, bool NORM>
-cudaError_t by_block(const RowMaps& maps, const RingArgs& p, int grid, size_t smem, cudaStream_t stream) {
+template <typename XT, int E, int FMT, bool NORM, bool BOXES>
+cudaError_t by_block(const RowMaps& maps, const LongArgs& p, int grid, size_t smem, cudaStream_t stream) {
     if constexpr (E == 64) {
         switch (p.block) {
-            case 1: return go<XT, E, FMT, NORM, 1>(maps, p, grid, smem, stream);
-            case 64: return go<XT, E, FMT, NORM, 64>(maps, p, grid, smem, stream);
-            case 128: return go<XT, E, FMT, NORM, 128>(maps, p, grid, smem, stream);
-            case 256: return go<XT, E, FMT, NORM, 256>(maps, p, grid, smem, stream);
+            case 1: return go<XT, E, FMT, NORM, 1, BOXES>(maps, p, grid, smem, stream);
+            case 64: return go<XT, E, FMT, NORM, 64, BOXES>(maps, p, grid, smem, stream);
+            case 128: return go<XT, E, FMT, NORM, 128, BOXES>(maps, p, grid, smem, stream);
+            case 256: return go<XT, E, FMT, NORM, 256, BOXES>(maps, p, grid, smem, stream);
         }
     }
-    return go<XT, E, FMT, NORM, 0>(maps, p, grid, smem, stream);
+    return go<XT, E, FMT, NORM, 0, BOXES>(maps, p, grid, smem, stream);
+}
+template <typename XT, int E, int FMT, bool NORM>
+cudaError_t by_boxes(const RowMaps& maps, const LongArgs& p, int grid, size_t smem, cudaStream_t stream) {
+    return p.boxes > 1 || p.tail_off ? by_block<XT, E, FMT, NORM, true>(maps, p, grid, smem, stream)
+                                     : by_block<XT, E, FMT, NORM, false>(maps, p, grid, smem, stream);
 }
 template <typename XT, int E>
-cudaError_t by_format(const RowQuant& q, const RowMaps& maps, const RingArgs& p, int grid, size_t smem, cudaStream_t stream) {
+cudaError_t by_format(const RowQuant& q, const RowMaps& maps, const LongArgs& p, int grid, size_t smem, cudaStream_t stream) {
     switch (q.fmt) {
-        case RowFmt::Int4: return by_block<XT, E, 0, true>(maps, p, grid, smem, stream);
-        case RowFmt::Int8: return by_block<XT, E, 1, true>(maps, p, grid, smem, stream);
-        case RowFmt::Mx: return q.norm ? by_block<XT, E, 3, true>(maps, p, grid, smem, stream) : by_block<XT, E, 3, false>(maps, p, grid, smem, stream);
-        case RowFmt::Nv: return q.norm ? by_block<XT, E, 4, true>(maps, p, grid, smem, stream) : by_block<XT, E, 4, false>(maps, p, grid, smem, stream);
+        case RowFmt::Int4: return by_boxes<XT, E, 0, true>(maps, p, grid, smem, stream);
+        case RowFmt::Int8: return by_boxes<XT, E, 1, true>(maps, p, grid, smem, stream);
+        case RowFmt::Mx: return q.norm ? by_boxes<XT, E, 3, true>(maps, p, grid, smem, stream) : by_boxes<XT, E, 3, false>(maps, p, grid, smem, stream);
+        case RowFmt::Nv: return q.norm ? by_boxes<XT, E, 4, true>(maps, p, grid, smem, stream) : by_boxes<XT, E, 4, false>(maps, p, grid, smem, stream);
     }
     return cudaErrorInvalidValue;
 }
@@ -514,23 +569,51 @@ cudaError_t by_format(const RowQuant& q, const RowMaps& maps, const RingArgs& p,
 }  // namespace
 
 cudaError_t launch_row_quantize_ring(const RowQuant& q, cudaStream_t stream) {
-    const size_t esz = q.xt == FQ_BF16 ? 2 : 4, row = (size_t)q.K * esz;
     if (q.rows < 256) return cudaErrorNotSupported;
+    const size_t esz = q.xt == FQ_BF16 ? 2 : 4, row = (size_t)q.K * esz;
     const int sms = device_sm_count();
-    // whole 128-byte lines, at most 256 of them (a box); rows enough for several a group
-    if (row % 128 != 0 || row > 32768 || q.rows < 2 * sms || q.rows * q.K < (int64_t)sms * 8192 || q.rows > 0x7fff0000) return cudaErrorNotSupported;
-    const int e = q.K % 64 == 0 && q.K >= 1536 ? 64 : 32;
-    const int gw = (int)((q.K + 32 * e - 1) / (32 * e));
-    if (gw > kWarps) return cudaErrorNotSupported;
-    RingArgs p = {};
-    p.row_bytes = (uint32_t)align_up(row, 1024);
+    // rows enough for several a group
+    if (q.rows < 2 * sms || q.rows * q.K < (int64_t)sms * 8192 || q.rows > 0x7fff0000) return cudaErrorNotSupported;
+    // Rows that end in half a line: short ones leave many lanes idle here, which the other kernel spreads over more warps
+    // (13000 x 2080 with norm and residual 60 us against 45; 4000 x 8224 58 against 78).
+    const bool tail = row % 128 != 0;
+    if (tail && q.K <= 8192) return cudaErrorNotSupported;
+    LongArgs p = {};
+    p.lines = (int)(row / 128);
+    p.boxes = (p.lines + 255) / 256;                          // (a box has 256 lines at most; of several, each begins on 1024 bytes)
+    p.box_lines = p.boxes == 1 ? p.lines : ((p.lines + p.boxes - 1) / p.boxes + 7) / 8 * 8;
+    const size_t whole = (size_t)p.boxes * p.box_lines * 128;
+    p.tail_off = tail ? (uint32_t)whole : 0;
+    p.row_bytes = (uint32_t)align_up(whole + (tail ? 128 : 0), 1024);
     p.slot_bytes = p.row_bytes * (q.residual ? 2 : 1);
-    p.mult_bytes = q.mult ? (uint32_t)align_up(sizeof(float) * (size_t)q.K, 1024) : 0;
-    const size_t stage = q.fmt == RowFmt::Int8 ? (size_t)kThreads * e : 0, room = 220 * 1024 - stage - p.mult_bytes;
-    const int slots = (int)(room / p.slot_bytes);
-    p.ngroups = slots < kWarps / gw ? slots : kWarps / gw;    // (rows so long that some warps stay idle)
-    if (p.ngroups < 1) return cudaErrorNotSupported;
-    p.depth = slots / p.ngroups < 4 ? slots / p.ngroups : 4;
+    p.tx = (uint32_t)(whole + (tail ? 64 : 0)) * (q.residual ? 2 : 1);
+    p.x = static_cast<const uint8_t*>(q.x); p.r = static_cast<const uint8_t*>(q.residual); p.h = static_cast<uint8_t*>(q.h);
+    p.pitch_x = q.ldx * (int64_t)esz; p.pitch_r = q.ldr * (int64_t)esz; p.pitch_h = q.ldh * (int64_t)esz;
+    p.mult_bytes = q.mult ? (uint32_t)align_up(sizeof(float) * align_up((size_t)q.K, 64), 1024) : 0;
+    // 64 channels a thread; 32 where rows are short, where 8-bit codes on their way out would take the room of the only slot, and
+    // where the slots of binary32 rows leave half of the warps idle (4000 x 8192 with norm 78 us against 73; bf16, which would pay
+    // the wider rotation more dearly, 114 against 151 at 4000 x 16384)
+    auto shape = [&](int e, int* gw, int* groups, size_t* stage) {
+        *gw = (int)((q.K + 32 * e - 1) / (32 * e));
+        *stage = q.fmt == RowFmt::Int8 ? (size_t)kThreads * e : 0;
+        const int64_t room = 220 * 1024 - (int64_t)*stage - (int64_t)p.mult_bytes;
+        const int slots = room > 0 ? (int)(room / p.slot_bytes) : 0;
+        *groups = *gw > kWarps ? 0 : slots < kWarps / *gw ? slots : kWarps / *gw;
+        p.depth = *groups > 0 ? (slots / *groups < 4 ? slots / *groups : 4) : 0;
+    };
+    int e = (tail || q.K % 64 == 0) && q.K >= 1536 ? 64 : 32, gw, groups;
+    size_t stage;
+    shape(e, &gw, &groups, &stage);
+    if (e == 64 && (groups < 1 || (esz == 4 && groups * gw <= kWarps / 2))) {
+        e = 32;
+        shape(e, &gw, &groups, &stage);
+        if (groups < 1) {
+            e = 64;
+            shape(e, &gw, &groups, &stage);
+        }
+    }
+    if (groups < 1 || p.depth < 1) return cudaErrorNotSupported;
+    p.ngroups = groups;
     const bool fp4 = q.fmt == RowFmt::Mx || q.fmt == RowFmt::Nv;
     p.rows = q.rows;
     p.rows_pad = fp4 ? (q.rows + 127) / 128 * 128 : q.rows;
@@ -544,8 +627,8 @@ cudaError_t launch_row_quantize_ring(const RowQuant& q, cudaStream_t stream) {
     if (!p.watchdog) return cudaErrorUnknown;
     RowMaps maps;
     auto map = [&](CUtensorMap* m, const void* ptr, int64_t ld) {
-        const uint64_t dims[3] = {128 / esz, row / 128, (uint64_t)q.rows}, strides[2] = {128, (uint64_t)ld * esz};
-        const uint32_t box[3] = {(uint32_t)(128 / esz), (uint32_t)(row / 128), 1};
+        const uint64_t dims[3] = {128 / esz, (uint64_t)p.lines, (uint64_t)q.rows}, strides[2] = {128, (uint64_t)ld * esz};
+        const uint32_t box[3] = {(uint32_t)(128 / esz), (uint32_t)p.box_lines, 1};
         return encode_tiled(m, esz == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 3, ptr, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
     };
     if (!map(&maps.x, q.x, q.ldx)) return cudaErrorNotSupported;

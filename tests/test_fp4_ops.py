@@ -420,6 +420,46 @@ def test_norm_extremes(form, K, repeat, residual):
             assert bool((got[2::6] == 0.0).all())
 
 
+# batches whose rows end in half a 128-byte line (bf16), have more than 256 lines, or both
+ODD_ROWS = [(2100, 672, 32, "bf16"), (1300, 1056, 16, "bf16"), (800, 2080, 8, "bf16"), (600, 8224, 32, "bf16"), (330, 16416, 32, "bf16"), (297, 11296, 1, "bf16"),
+            (298, 8224, 32, "f32"), (300, 16384, 256, "f32"), (299, 11296, 2, "f32"), (300, 16448, 64, "bf16"), (296, 32768, 256, "bf16")]
+
+
+@pytest.mark.parametrize("form", ["mx", "nv"])
+@pytest.mark.parametrize("M,K,block,dtype", ODD_ROWS)
+def test_quantize_odd_rows(form, M, K, block, dtype):
+    test_quantize_bits(form, M, K, block, dtype)
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("form", ["int8", "int4", "mx", "nv"])
+@pytest.mark.parametrize("M,K,block,dtype", ODD_ROWS)
+def test_norm_odd_rows(form, M, K, block, dtype, residual):
+    test_norm(form, M, K, block, dtype, residual)
+
+
+@pytest.mark.parametrize("M,K,dtype", [(1400, 1056, "bf16"), (700, 4128, "bf16"), (300, 16416, "bf16"), (300, 11296, "f32")])
+def test_norm_odd_rows_in_place_and_strided(M, K, dtype):
+    test_norm_in_place_and_strided(dtype, M, K)
+
+
+@pytest.mark.parametrize("form", ["int8", "nv"])
+@pytest.mark.parametrize("K,repeat", [(1056, 250), (8224, 55)])
+def test_norm_extremes_of_odd_rows(form, K, repeat):
+    """Rows of bf16 whose squares leave binary32, whose last half line counts as the others do."""
+    rng = np.random.default_rng(8)
+    base = np.tile(rng.standard_normal((6, K)).astype(np.float32), (repeat, 1))
+    base[:, -32:] *= 4.0
+    scale = np.tile(np.array([1e25, 1e-25, 0.0, 1.0, 1e19, 1e-19], np.float32), repeat)[:, None]
+    x = dev(base * scale, "bf16")
+    out = fq.rmsnorm_quantize_act(x, torch.zeros_like(x), None, 1, 8, 0.0) if form == "int8" else fq.rmsnorm_quantize_act_fp4(x, torch.zeros_like(x), None, 1, FORMATS[form], 0.0)
+    d = (fq.quantize_act(x, None, 1, 8) if form == "int8" else fq.quantize_act_fp4(x, None, 1, FORMATS[form]))[-1]
+    live = torch.tensor([i for i in range(6 * repeat) if i % 6 != 2], device="cuda")
+    want = (d.double() / x.double().square().mean(1).sqrt())[live]
+    assert bool(((out[-1].double()[live] - want).abs() <= 27 * 2.0 ** -24 * want + 2.0 ** -149).all())
+    assert bool((out[-1][2::6] == 0.0).all())
+
+
 def test_norm_clip():
     x = dev(tokens(np.random.default_rng(6), 40, 512), "bf16")
     g = torch.ones(512, device="cuda")
