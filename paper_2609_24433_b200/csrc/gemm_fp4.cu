@@ -392,7 +392,7 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
         }
     } else {
         // ------------------------------------------------------------ epilogue
-        // The warps of a quadrant alternate: chunks of 16 tokens: chunk i of set s begins at token (s + kSets i) * 16.
+        // The warps of a quadrant take chunks of 16 tokens in turn: chunk i of set s begins at token (s + kSets i) * 16.
         const int quad = warp & 3, set = (warp - 2) >> 2;
         const uint32_t lanes = (uint32_t)(quad * 32) << 16;
         float* const steps = s_steps[warp - 2];
