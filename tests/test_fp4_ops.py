@@ -289,6 +289,20 @@ def test_product_writes_only_its_rows(M, N, K, dtype):
     assert bool((mem == 3.5).all())
 
 
+@pytest.mark.parametrize("form", ["mx", "nv"])
+@pytest.mark.parametrize("M,N,K", [(513, 10000, 352), (2100, 2600, 1056), (816, 32776, 2048), (700, 9480, 96)])
+def test_product_keeps_outputs_on_their_way(form, M, N, K):
+    """Several tiles to a CTA, the last of them partly past N: what a warp has handed to the copy engine stays until it is read.
+    Many launches one behind the other, each bit for bit the binary32 outputs rounded once (the same sums in the same order)."""
+    a, handle, _, _ = product_case(form, M, N, K)
+    want = fq.gemm_fp4(*a, handle).to(torch.bfloat16)
+    for _ in range(4):
+        got = [fq.gemm_fp4(*a, handle, torch.bfloat16) for _ in range(12)]
+        for y in got:
+            assert torch.equal(y, want)
+    check_status()
+
+
 def test_product_scales_past_the_last_row_do_not_matter():
     for form in ("mx", "nv"):
         a, handle, want, size = product_case(form, 37, 256, 512)
