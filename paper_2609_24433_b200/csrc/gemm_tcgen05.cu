@@ -859,8 +859,8 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                     stmatrix_x4_trans(buf + off_b, wb0, wb1, wb2, wb3);
                     fence_proxy_async_smem();            // the buffer, written through the generic proxy, is read by the copy engine
                     __syncwarp();
-                    if (lane == 0 && any_channel) {
-                        tma_store_2d(&map_y, (int)jq * 2, (int)tc, buf);   // the output map counts bytes along a row
+                    if (lane == 0) {                     // (a group for every buffer taken, past N an empty one: the wait counts them)
+                        if (any_channel) tma_store_2d(&map_y, (int)jq * 2, (int)tc, buf);   // the output map counts bytes along a row
                         bulk_commit();
                     }
                     ++store_use;

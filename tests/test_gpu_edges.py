@@ -321,6 +321,23 @@ def test_w8_epilogues_equal_the_second_witness(M, K, N, warps):
     assert torch.equal(fq.gemm_acc_i32(codes, h), fq.gemm_simt(codes, None, h, raw_acc=True))
 
 
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("M,K,N", [(700, 96, 9480), (513, 352, 10000), (2100, 1056, 2600), (816, 2048, 32776)])
+def test_gemm_keeps_outputs_on_their_way(M, K, N, bits):
+    """Several tiles to a CTA, the last of them partly past N: what a warp has handed to the copy engine stays until it is read.
+    Many launches one behind the other, each with the bits of the second witness."""
+    g = torch.Generator(device="cuda").manual_seed(M + N)
+    h = fq.weights_import(torch.randint(0, 256, (N, K * bits // 8), dtype=torch.uint8, device="cuda", generator=g),
+                          torch.rand(N, device="cuda", generator=g) + 0.1, None, torch.randn(N, device="cuda", generator=g), K, 32, bits)
+    codes = torch.randint(0, 256, (M, K * bits // 8), dtype=torch.uint8, device="cuda", generator=g)
+    delta = torch.rand(M, device="cuda", generator=g) + 0.1
+    want = fq.gemm_simt(codes, delta, h, torch.bfloat16)
+    gemm = fq.gemm_w4a4 if bits == 4 else fq.gemm_w8a8
+    for _ in range(4):
+        for y in [gemm(codes, delta, h, torch.bfloat16) for _ in range(12)]:
+            assert torch.equal(y, want)
+
+
 FEW_UNITS = [
     (9, 1536, 256, 8),         # six units of K for clusters of eight
     (31, 1792, 256, 4),        # seven
