@@ -305,7 +305,8 @@ __global__ void __launch_bounds__(CACHE ? 512 : 1024) row_quantize_kernel(const 
                     t.x = fminf(fmaxf(t.x, -p.qmax), p.qmax);
                     t.y = fminf(fmaxf(t.y, -p.qmax), p.qmax);
                 }
-                t = f2_add(t, make_float2(12582912.0f, 12582912.0f));
+                // (as a packed FMA by 1: a packed multiply ahead of a packed add may be fused, which rounds ties differently)
+                t = f2_fma(t, make_float2(1.0f, 1.0f), make_float2(12582912.0f, 12582912.0f));
                 b[i] = __float_as_uint(t.x);
                 b[i + kHalf] = __float_as_uint(t.y);
             }

@@ -485,6 +485,40 @@ def test_norm_clip():
         assert bool(((steps.double() - want).abs() <= 27 * 2.0 ** -24 * want).all())
 
 
+def next_to_ties(rng, rows, K, bits, clip):
+    """Rows of binary32 whose quotient z * (1/d), rounded to binary32, lies half way between two integers and unrounded beside it: the
+    product's own rounding decides the code.  (Multiplied and rounded to an integer in one operation, they would go the other way.)"""
+    f, q = np.float32, 7 if bits == 4 else 127
+    x = np.zeros((rows, K), f)
+    for r in range(rows):
+        while True:
+            m = f(rng.uniform(0.5, 4.0))
+            d = (f(clip) * m) * (f(1) / f(q))
+            inv = f(1) / d
+            k = np.arange(q)
+            z = ((k + 0.5) * np.float64(d)).astype(f)
+            near = (z.view(np.int32)[:, None] + np.arange(-3, 4)[None]).view(f)
+            exact = near.astype(np.float64) * np.float64(inv)         # (48 bits)
+            fits = ((near * inv).astype(f) == (k + 0.5).astype(f)[:, None]) & (np.rint(exact) != np.rint(k + 0.5)[:, None]) & (near < m)
+            if fits.any():
+                break
+        x[r] = rng.choice(near[fits], K) * rng.choice(np.array([-1, 1], f), K)
+        x[r, rng.integers(K)] = m
+    return x
+
+
+@pytest.mark.parametrize("clip", [1.0, 0.75])
+@pytest.mark.parametrize("bits", [4, 8])
+@pytest.mark.parametrize("K", [64, 4096, 8224, 16416])
+def test_norm_rounds_the_quotient_and_then_the_code(K, bits, clip):
+    """The same rows in a short batch and in one that streams: two operations, each rounded, in every kernel."""
+    x = next_to_ties(np.random.default_rng(K + bits), 8, K, bits, clip)
+    want, _ = integers(x, bits, clip)
+    for repeat in (1, max(40, 160000 // K)):
+        codes = fq.rmsnorm_quantize_act(dev(np.tile(x, (repeat, 1))), None, torch.ones(K, device="cuda"), 1, bits, clip_ratio=clip)[1]
+        assert np.array_equal(host(codes), np.tile(want, (repeat, 1)))
+
+
 # ---------------------------------------------------------------------------- as they are used together
 def test_a_layers_projections():
     """Residual and norm, 8-bit qkv; residual and norm, e2m1 gate/up and down: against the same layer from the plain calls."""
