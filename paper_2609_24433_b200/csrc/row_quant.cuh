@@ -61,11 +61,24 @@ __device__ __forceinline__ uint32_t mx_scale(float m, float* q) {
     *q = __uint_as_float((uint32_t)(254 - e) << 23);
     return (uint32_t)e;
 }
-// 1 / sqrt(sum / K + eps); the sum in binary32, or in binary64 for rows whose squares leave its range.
-__device__ __forceinline__ bool sum_in_range(float total, float eps) { return !(total > 1e37f || (total < 1e-30f && eps < 1e-20f)); }
+// Step of a row with largest magnitude m, ahead of the norm.
+template <int FMT>
+__device__ __forceinline__ float row_step(float m, float clip) {
+    float inv;
+    return FMT == 3 ? 1.0f : FMT == 4 ? nv_step(m, &inv) : int_step(m, clip, 1.0f / (FMT == 0 ? 7.0f : 127.0f), &inv);
+}
+// 1 / sqrt(sum / K + eps); the sum in binary32.
 __device__ __forceinline__ float inverse_rms(float total, int K, float eps) {
     const float ms = __fadd_rn(__fdiv_rn(total, (float)K), eps);
     return ms > 0.0f ? __fdiv_rn(1.0f, __fsqrt_rn(ms)) : 0.0f;
+}
+// Rows whose squares leave binary32 have them added up in binary64, and their step divided there: 1 / rms may leave binary32 where
+// the step does not.  A step of 1 / rms that does (e2m1 with e8m0 scales, whose codes are then all but zeros) makes the zero token.
+__device__ __forceinline__ bool squares_leave_range(float total, float m, float eps) { return m > 0.0f && (total > 1e37f || (total < 1e-30f && eps < 1e-20f)); }
+template <int FMT>
+__device__ __forceinline__ float wide_step(float m, float clip, double sum, int K, float eps) {
+    const double s = (double)row_step<FMT>(m, clip) / sqrt(sum / K + (double)eps);
+    return FMT == 3 && s > (double)FLT_MAX ? 0.0f : (float)s;
 }
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll

@@ -368,9 +368,9 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
             __syncwarp();
         }
         if (!ok) break;
-        float rinv = 1.0f;
+        float rinv = 1.0f;                                     // (-1: the step is written already)
         if (NORM && wg == 0) {
-            if (m > 0.0f && !sum_in_range(total, p.eps)) {
+            if (squares_leave_range(total, m, p.eps)) {
                 double s = 0.0;                                // the row as it lies in its slot, in binary64
                 auto square = [&](uint32_t at) {
                     const uint32_t w = *reinterpret_cast<const volatile uint32_t*>(gen + (slot - base) + at);
@@ -385,7 +385,8 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
                 for (uint32_t at = (uint32_t)lane * 4u; at < end; at += 128u) square(at);
                 if (tail_off) square(tail_off + (uint32_t)lane * 4u);        // (zeros behind it)
                 for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                rinv = (float)(1.0 / sqrt(s / p.K + (double)p.eps));
+                if (lane == 0) p.delta[row] = wide_step<FMT>(m, p.clip_ratio, s, p.K, p.eps);
+                rinv = -1.0f;
             } else {
                 rinv = inverse_rms(total, p.K, p.eps);
             }
@@ -514,7 +515,7 @@ row_quantize_ring_kernel(const __grid_constant__ CUtensorMap map_x, const __grid
                     if (!BOXES || j == 0 || col0 + 32 * j < p.K) dst[j] = make_uint4(w[(4 * j) % (2 * kWords)], w[(4 * j + 1) % (2 * kWords)], w[(4 * j + 2) % (2 * kWords)], w[(4 * j + 3) % (2 * kWords)]);
             }
         }
-        if (leader) p.delta[row] = NORM ? __fmul_rn(dl, rinv) : dl;
+        if (leader && !(NORM && rinv < 0.0f)) p.delta[row] = NORM ? __fmul_rn(dl, rinv) : dl;
         if (++d == p.depth) { d = 0; ph ^= 1u; }
     }
     if (leader && residual) bulk_wait_read<0>();             // the last rows have left shared memory

@@ -519,6 +519,47 @@ def test_norm_rounds_the_quotient_and_then_the_code(K, bits, clip):
         assert np.array_equal(host(codes), np.tile(want, (repeat, 1)))
 
 
+STEP_ROWS = [(1024, "f32"), (1024, "bf16"), (8224, "bf16"), (16416, "f32")]     # short batches of all; the first three stream too
+
+
+@pytest.mark.parametrize("repeat", [1, 240])
+@pytest.mark.parametrize("K,dtype", STEP_ROWS)
+@pytest.mark.parametrize("form", ["int8", "int4", "mx", "nv"])
+def test_norm_steps_of_the_smallest_and_largest_rows(form, K, dtype, repeat):
+    """Subnormal rows and rows at the end of binary32, without eps: d / rms, in 64 bits, rounded once (a half of 2^-149 where it ends
+    below the normal numbers).  For MXFP4 a 1 / rms that binary32 does not have is a step of 0."""
+    rng = np.random.default_rng(K)
+    base = rng.uniform(0.5, 1.0, (8, K)).astype(np.float32) * rng.choice(np.array([-1, 1], np.float32), (8, K))
+    base[7, 1:] = 0.0                                            # a single number
+    scale = np.array([1e-40, 3e-44, 1e-38, 1e-30, 1e-20, 1e-41, 3e38, 1e37], np.float32)[:, None]
+    for gain in (1.0, 2.0 ** 20, 2.0 ** -20):                    # (large: rows below the smallest step without it have one)
+        eight = dev(base * np.where(scale > 1, scale / max(gain, 1.0), scale).astype(np.float32), dtype)
+        x, g = eight.repeat(repeat, 1), torch.full((K,), gain, device="cuda")
+        z = rotate(host(eight), host(g), 1)
+        if form in FORMATS:
+            got = fq.rmsnorm_quantize_act_fp4(x, None, g, 1, FORMATS[form], 0.0)[-1]
+            d = quantize(z, form)[2]
+        else:
+            bits = 8 if form == "int8" else 4
+            got = fq.rmsnorm_quantize_act(x, None, g, 1, bits, 0.0)[-1]
+            d = integers(z, bits)[1]
+        rms = np.sqrt(np.square(host(eight).astype(np.float64)).mean(1))
+        want = d.astype(np.float64) / np.where(rms > 0, rms, np.inf)         # (bf16 does not have the smallest: rows of zeros, steps of 0)
+        if form == "mx":
+            want = np.where(want > float(np.finfo(np.float32).max), 0.0, want)
+        want = np.tile(want, repeat)
+        got = host(got).astype(np.float64)
+        assert np.isfinite(got).all()
+        # (rows in binary32's range: the sum of squares, its mean, root, reciprocal and product, as in the test of the norm)
+        assert (np.abs(got - want) <= 27 * 2.0 ** -24 * want + 2.0 ** -149).all()
+        if form in FORMATS:
+            ones = torch.full((8, K // 2), 0x22, dtype=torch.uint8, device="cuda")
+            scales = torch.full((fq.fp4_scale_bytes(8, K, FORMATS[form]),), 127 if form == "mx" else 56, dtype=torch.uint8, device="cuda")
+            h = fq.weights_import_fp4(ones, scales, None, None, None, K, 1, FORMATS[form])
+            y = fq.gemm_fp4(*fq.rmsnorm_quantize_act_fp4(x[:6], None, g, 1, FORMATS[form], 0.0)[1:], h)
+            assert bool(torch.isfinite(y).all())
+
+
 # ---------------------------------------------------------------------------- as they are used together
 def test_a_layers_projections():
     """Residual and norm, 8-bit qkv; residual and norm, e2m1 gate/up and down: against the same layer from the plain calls."""
