@@ -487,6 +487,7 @@ size_t fq_linear_fp4_workspace_bytes(int64_t M, int64_t K, fq_fp4_format format)
  *     quotient: one unit in the last place at most); codes round(z * (1/d)), delta = d / rms, both 0 where d < 2^-126;
  *   fp4: codes and scales of fq_quantize_act_fp4 of h, delta = its step / rms  (FQ_MXFP4: 1 / rms, or 0, the zero token, where that
  *     passes binary32's largest number: eps 0 and rms below 2.94e-39).
+ * A row of h that is not finite has a step that is NaN, and so has NaN in what is multiplied by it.
  * A learned gain belongs into mult_g (gain_c * (1/s_c) * block^-1/2, see fq_weights_set_multiplier); NULL: the constant block^-1/2.
  * residual device [M, K] of dtype xt, leading dimension ldr, or NULL: the stream is x as it is, and h has to be NULL.  Otherwise h
  * device [M, K] of dtype xt; it may be the very memory of x or of residual (same address and leading dimension), else nothing may

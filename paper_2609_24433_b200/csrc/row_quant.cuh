@@ -67,18 +67,19 @@ __device__ __forceinline__ float row_step(float m, float clip) {
     float inv;
     return FMT == 3 ? 1.0f : FMT == 4 ? nv_step(m, &inv) : int_step(m, clip, 1.0f / (FMT == 0 ? 7.0f : 127.0f), &inv);
 }
-// 1 / sqrt(sum / K + eps); the sum in binary32.
+// 1 / sqrt(sum / K + eps); the sum in binary32.  (0 for a sum of 0 without eps; a sum that is NaN stays it.)
 __device__ __forceinline__ float inverse_rms(float total, int K, float eps) {
     const float ms = __fadd_rn(__fdiv_rn(total, (float)K), eps);
-    return ms > 0.0f ? __fdiv_rn(1.0f, __fsqrt_rn(ms)) : 0.0f;
+    return ms == 0.0f ? 0.0f : __fdiv_rn(1.0f, __fsqrt_rn(ms));
 }
 // Rows whose squares leave binary32 have them added up in binary64, and their step divided there: 1 / rms may leave binary32 where
-// the step does not.  A step of 1 / rms that does (e2m1 with e8m0 scales, whose codes are then all but zeros) makes the zero token.
-__device__ __forceinline__ bool squares_leave_range(float total, float m, float eps) { return m > 0.0f && (total > 1e37f || (total < 1e-30f && eps < 1e-20f)); }
+// the step does not.  A step of 1 / rms that does (e2m1 with e8m0 scales, whose codes are then all but zeros) makes the zero token; an
+// infinite sum, of a row that is not finite, a NaN.
+__device__ __forceinline__ bool squares_leave_range(float total, float m, float eps) { return total > 1e37f || (m > 0.0f && total < 1e-30f && eps < 1e-20f); }
 template <int FMT>
 __device__ __forceinline__ float wide_step(float m, float clip, double sum, int K, float eps) {
     const double s = (double)row_step<FMT>(m, clip) / sqrt(sum / K + (double)eps);
-    return FMT == 3 && s > (double)FLT_MAX ? 0.0f : (float)s;
+    return FMT == 3 && s > (double)FLT_MAX ? 0.0f : (float)(s + (sum - sum));
 }
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll

@@ -560,6 +560,32 @@ def test_norm_steps_of_the_smallest_and_largest_rows(form, K, dtype, repeat):
             assert bool(torch.isfinite(y).all())
 
 
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("repeat", [1, 240])
+@pytest.mark.parametrize("K,dtype", STEP_ROWS)
+@pytest.mark.parametrize("form", ["int8", "int4", "mx", "nv"])
+def test_norm_steps_of_rows_that_are_not_finite(form, K, dtype, repeat, residual):
+    """Such a row's step is NaN; the others' are as they were."""
+    rng = np.random.default_rng(K + 1)
+    a = np.tile(rng.standard_normal((6, K)).astype(np.float32), (repeat, 1))
+    b = a.copy()
+    b[0::6, K - 1] = np.nan
+    b[2::6, 0] = np.inf
+    b[4::6, K // 2] = -np.inf
+    b[4::6, 3] = np.nan
+    g = np.ones(K, np.float32)
+    g[0] = 0.0
+    for eps in (0.0, 1e-6):
+        steps = []
+        for rows in (a, b):
+            x = dev(rows, dtype)
+            r = torch.zeros_like(x) if residual else None
+            out = fq.rmsnorm_quantize_act_fp4(x, r, dev(g), 1, FORMATS[form], eps) if form in FORMATS else fq.rmsnorm_quantize_act(x, r, dev(g), 1, 8 if form == "int8" else 4, eps)
+            steps.append(out[-1])
+        assert bool(torch.isfinite(steps[0]).all())
+        assert torch.equal(steps[0][1::2], steps[1][1::2]) and bool(steps[1][0::2].isnan().all())
+
+
 # ---------------------------------------------------------------------------- as they are used together
 def test_a_layers_projections():
     """Residual and norm, 8-bit qkv; residual and norm, e2m1 gate/up and down: against the same layer from the plain calls."""
