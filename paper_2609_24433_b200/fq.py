@@ -150,6 +150,7 @@ class Weights:
         self.N, self.K, self.block, self.bits = n.value, k.value, blk.value, bits.value
         self._addr = self._h.value
         self.fold_after = bool(lib().fq_weights_fold_after(self._h))
+        self.device = torch.cuda.current_device()            # (where its memory lies)
 
     @property
     def handle(self) -> ctypes.c_void_p:
@@ -483,6 +484,7 @@ class Fp4Weights:
         _check(lib().fq_fp4_weights_info(self._h, ctypes.byref(n), ctypes.byref(k), ctypes.byref(blk), ctypes.byref(fmt)), "fq_fp4_weights_info")
         self.N, self.K, self.block, self.format = n.value, k.value, blk.value, fmt.value
         self._addr = self._h.value
+        self.device = torch.cuda.current_device()            # (where its memory lies)
 
     @property
     def address(self) -> int:
@@ -550,14 +552,19 @@ def weights_import_fp4(codes: torch.Tensor, scales: torch.Tensor, w_scale: Optio
     return Fp4Weights(out.value)
 
 
-def _multiplier(mult_g, x: torch.Tensor):
-    """What the native call takes for a site's multiplier: a float32 tensor or None as they are, a handle's own by its address."""
+def _multiplier(mult_g, x: torch.Tensor, hadamard_block: int):
+    """What the native call takes for a site's multiplier: a float32 tensor or None as they are, a handle's own by its address
+    (which carries the block's norm: another block is another site)."""
     if mult_g is None or mult_g.__class__ is torch.Tensor:
         return mult_g
     if not isinstance(mult_g, (Weights, Fp4Weights)):
         raise TypeError(f"mult_g has to be a tensor, a handle or None, got {type(mult_g).__name__}")
     if mult_g.K != x.shape[-1]:
         raise ValueError(f"the handle has {mult_g.K} channels, the rows {x.shape[-1]}")
+    if mult_g.block != hadamard_block:
+        raise ValueError(f"the handle was folded with blocks of {mult_g.block}, not {hadamard_block}")
+    if mult_g.device != x.device.index:
+        raise ValueError("x has to be on the handle's device")
     if isinstance(mult_g, Weights) and (mult_g.fold_after or lib().fq_weights_composite(mult_g.handle)):
         raise ValueError("the multiplier of a fold-after or composite site does not stand ahead of the butterflies")
     return mult_g.multiplier_ptr()
@@ -565,7 +572,7 @@ def _multiplier(mult_g, x: torch.Tensor):
 
 def quantize_act_fp4(x: torch.Tensor, mult_g, hadamard_block: int, format: int = NVFP4, codes=None, scales=None, delta=None):
     """(codes u8 [M, K/2], block scales u8 in tiles, steps [M]).  ``mult_g``: device float tensor, a handle (its multiplier) or None."""
-    return _result(_native().quantize_act_fp4(x, _multiplier(mult_g, x), hadamard_block, format, codes, scales, delta),
+    return _result(_native().quantize_act_fp4(x, _multiplier(mult_g, x, hadamard_block), hadamard_block, format, codes, scales, delta),
                    "fq_quantize_act_fp4")
 
 
@@ -584,14 +591,14 @@ def rmsnorm_quantize_act(x: torch.Tensor, residual: Optional[torch.Tensor], mult
                          clip_ratio: float = 1.0, h=None, codes=None, delta=None):
     """(h, codes u8 [M, K*bits/8], steps [M]): h = x + residual (x itself without one) and the codes of h / rms(h) for a site whose
     multiplier is ``mult_g`` (device float tensor, a Weights or None)."""
-    return _result(_native().rmsnorm_quantize_act(x, residual, _multiplier(mult_g, x), hadamard_block, bits, eps, clip_ratio, h, codes, delta),
+    return _result(_native().rmsnorm_quantize_act(x, residual, _multiplier(mult_g, x, hadamard_block), hadamard_block, bits, eps, clip_ratio, h, codes, delta),
                    "fq_rmsnorm_quantize_act")
 
 
 def rmsnorm_quantize_act_fp4(x: torch.Tensor, residual: Optional[torch.Tensor], mult_g, hadamard_block: int, format: int = NVFP4,
                              eps: float = 1e-6, h=None, codes=None, scales=None, delta=None):
     """(h, codes u8 [M, K/2], block scales, steps [M]) of the same in e2m1."""
-    return _result(_native().rmsnorm_quantize_act_fp4(x, residual, _multiplier(mult_g, x), hadamard_block, format, eps, h, codes, scales, delta),
+    return _result(_native().rmsnorm_quantize_act_fp4(x, residual, _multiplier(mult_g, x, hadamard_block), hadamard_block, format, eps, h, codes, scales, delta),
                    "fq_rmsnorm_quantize_act_fp4")
 
 

@@ -739,3 +739,15 @@ def test_refusals():
     h.destroy()
     with pytest.raises(RuntimeError):
         fq.linear_fp4(x, h)
+
+
+def test_multiplier_of_a_handle_goes_with_its_block():
+    """A handle's multiplier carries its block's norm: calls with another block are refused."""
+    x = torch.randn(4, 128, device="cuda")
+    for h in (fq.fold_weights_fp4(torch.randn(16, 128, device="cuda"), None, None, 64), fq.fold_weights(torch.randn(16, 128, device="cuda"), None, None, 64, 8)):
+        for call in (lambda block: fq.quantize_act_fp4(x, h, block), lambda block: fq.rmsnorm_quantize_act(x, None, h, block, 8),
+                     lambda block: fq.rmsnorm_quantize_act_fp4(x, None, h, block)):
+            call(64)
+            for block in (1, 32, 128):
+                with pytest.raises(ValueError):
+                    call(block)

@@ -92,3 +92,22 @@ def test_norm_refusals(lib):
         assert norm(lib, **bad) == fq.ERR_ALIGNMENT, bad
     call = lambda fmt, scales: lib.fq_rmsnorm_quantize_act_fp4(ONE, NULL, 1, L(4), L(64), L(64), L(0), F(0.0), NULL, L(0), NULL, 1, fmt, ONE, scales, ONE, NULL)
     assert call(2, ONE) == fq.ERR_INVALID_ARG and call(1, NULL) == fq.ERR_INVALID_ARG and call(0, ODD) == fq.ERR_ALIGNMENT
+
+
+class Rows:
+    """What a handle is compared with: rows of a width, on a device."""
+    def __init__(self, K, device):
+        self.shape, self.device = (4, K), type("Device", (), {"index": device})
+
+
+@pytest.mark.parametrize("cls", [fq.Weights, fq.Fp4Weights])
+def test_multiplier_of_another_site_is_refused(cls, lib, monkeypatch):
+    """A handle's multiplier carries its block's norm and lies on its device."""
+    h = cls.__new__(cls)
+    h.K, h.block, h.device, h.fold_after, h._h, h._addr = 128, 64, 0, False, None, None
+    monkeypatch.setattr(cls, "handle", ctypes.c_void_p(0), raising=False)
+    monkeypatch.setattr(cls, "multiplier_ptr", lambda self: 4096)
+    assert fq._multiplier(h, Rows(128, 0), 64) == 4096
+    for rows, block in ((Rows(96, 0), 64), (Rows(128, 0), 32), (Rows(128, 0), 1), (Rows(128, 1), 64), (Rows(128, None), 64)):
+        with pytest.raises(ValueError):
+            fq._multiplier(h, rows, block)
