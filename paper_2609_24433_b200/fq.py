@@ -555,7 +555,7 @@ def weights_import_fp4(codes: torch.Tensor, scales: torch.Tensor, w_scale: Optio
 def _multiplier(mult_g, x: torch.Tensor, hadamard_block: int):
     """What the native call takes for a site's multiplier: a float32 tensor or None as they are, a handle's own by its address
     (which carries the block's norm: another block is another site)."""
-    if mult_g is None or mult_g.__class__ is torch.Tensor:
+    if mult_g is None or isinstance(mult_g, torch.Tensor):
         return mult_g
     if not isinstance(mult_g, (Weights, Fp4Weights)):
         raise TypeError(f"mult_g has to be a tensor, a handle or None, got {type(mult_g).__name__}")

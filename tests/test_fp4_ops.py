@@ -751,3 +751,16 @@ def test_multiplier_of_a_handle_goes_with_its_block():
             for block in (1, 32, 128):
                 with pytest.raises(ValueError):
                     call(block)
+
+
+def test_parameters_are_tensors():
+    """Multiplier, rows and outputs that a module holds as torch.nn.Parameter."""
+    K = 256
+    x, g = torch.randn(5, K, device="cuda"), torch.rand(K, device="cuda") + 0.5
+    P = lambda t: torch.nn.Parameter(t)
+    for a, b in zip(fq.quantize_act_fp4(P(x), P(g), 64), fq.quantize_act_fp4(x, g, 64)):
+        assert torch.equal(a, b)
+    for a, b in zip(fq.rmsnorm_quantize_act(P(x), P(x), P(g), 64, 8), fq.rmsnorm_quantize_act(x, x, g, 64, 8)):
+        assert torch.equal(a, b)
+    h = fq.fold_weights_fp4(P(torch.ones(16, K, device="cuda")), P(g), P(torch.zeros(16, device="cuda")), 64)
+    assert torch.equal(fq.linear_fp4(P(x), h), fq.linear_fp4(x, h))

@@ -111,3 +111,13 @@ def test_multiplier_of_another_site_is_refused(cls, lib, monkeypatch):
     for rows, block in ((Rows(96, 0), 64), (Rows(128, 0), 32), (Rows(128, 0), 1), (Rows(128, 1), 64), (Rows(128, None), 64)):
         with pytest.raises(ValueError):
             fq._multiplier(h, rows, block)
+
+
+def test_multiplier_may_be_a_parameter():
+    """A torch.nn.Parameter is a tensor like any other."""
+    import torch
+    for g in (None, torch.ones(128), torch.nn.Parameter(torch.ones(128)), torch.nn.Buffer(torch.ones(128))):
+        assert fq._multiplier(g, Rows(128, 0), 64) is g
+    for bad in (4096, 1.0, "g", [1.0]):
+        with pytest.raises(TypeError):
+            fq._multiplier(bad, Rows(128, 0), 64)
