@@ -764,3 +764,62 @@ def test_parameters_are_tensors():
         assert torch.equal(a, b)
     h = fq.fold_weights_fp4(P(torch.ones(16, K, device="cuda")), P(g), P(torch.zeros(16, device="cuda")), 64)
     assert torch.equal(fq.linear_fp4(P(x), h), fq.linear_fp4(x, h))
+
+
+@pytest.mark.parametrize("M,K,F,block", [(77, 512, 1024, 64), (1, 512, 1024, 64), (300, 1056, 2080, 32)])
+def test_a_layers_mlp_against_its_codes(M, K, F, block):
+    """Residual and norm into NVFP4 gate/up, its activation into MXFP4 down, each product against 64 bits from the codes it was given."""
+    rng = np.random.default_rng(M + F)
+    t = lambda *s: dev(rng.standard_normal(s).astype(np.float32))
+    up = fq.fold_weights_fp4(t(2 * F, K) * 0.05, t(K).exp(), t(2 * F), block)
+    down = fq.fold_weights_fp4(t(K, F) * 0.05, t(F).exp(), t(K), block, fq.MXFP4)
+
+    def product(a, handle, form):
+        codes, scales, ws, _, bias = (host(v) for v in handle.export())
+        def plain(c, sc, d, rows):
+            blocks = handle.K // BLOCK[form]
+            flat = sc.reshape(-(-rows // 128), -(-blocks // 4), 32, 4, 4).transpose(0, 3, 2, 1, 4).reshape(-1, -(-blocks // 4) * 4)
+            return dev(values(c, flat[:rows, :blocks], d, form))
+        A, W = plain(*(host(v) for v in a), M), plain(codes, scales, ws, handle.N)
+        return A @ W.T + dev(bias).double(), A.abs() @ W.abs().T + dev(bias).double().abs()
+
+    x, r = t(M, K).to(torch.bfloat16), t(M, K).to(torch.bfloat16)
+    h, *a = fq.rmsnorm_quantize_act_fp4(x, r, up, block)
+    for dtype in (torch.bfloat16, torch.float32):
+        z = fq.gemm_fp4(*a, up, dtype)
+        assert_product(z, *product(a, up, "nv"), K)
+        y = torch.nn.functional.silu(z[:, :F]) * z[:, F:]
+        out = fq.linear_fp4(y, down, dtype)
+        assert_product(out, *product(fq.quantize_act_fp4(y, down, block, fq.MXFP4), down, "mx"), F)
+    check_status()
+
+
+def test_offsets_past_32_bits():
+    """More than 2^32 numbers in rows, codes and outputs: the last rows are those of a short call, the last outputs those of 64 bits."""
+    M, K, N, last, channels = 135000, 32768, 32768, 40, 512
+    x = torch.randn(1000, K, device="cuda", dtype=torch.bfloat16).repeat(M // 1000, 1)
+    x[-last:] = torch.randn(last, K, device="cuda", dtype=torch.bfloat16)
+    tail = x[-last:].clone()
+
+    def rows_of(scales, blocks, first, rows):                        # of the tiles from `first` on
+        at = scales.view(-1, blocks // 4 * 512)[first // 128:(first + rows + 127) // 128]
+        return at.reshape(-1, blocks // 4, 32, 4, 4).permute(0, 3, 2, 1, 4).reshape(-1, blocks)[first % 128:first % 128 + rows]
+
+    for form in ("mx", "nv"):
+        blocks = K // BLOCK[form]
+        codes, scales, steps = fq.quantize_act_fp4(x, None, 64, FORMATS[form])
+        short = fq.quantize_act_fp4(tail, None, 64, FORMATS[form])
+        assert torch.equal(codes[-last:], short[0]) and torch.equal(steps[-last:], short[2])
+        assert torch.equal(rows_of(scales, blocks, M - last, last), rows_of(short[1], blocks, 0, last))
+    h = fq.weights_import_fp4(codes[:N], scales[:fq.fp4_scale_bytes(N, K, fq.NVFP4)], None, None, None, K, 64)
+    y = fq.gemm_fp4(codes, scales, steps, h, torch.bfloat16)
+    A = dev(values(host(short[0]), host(rows_of(short[1], blocks, 0, last)), host(short[2]), "nv"))
+    W = dev(values(host(codes[N - channels:N]), host(rows_of(scales, blocks, N - channels, channels)), np.ones(channels, np.float32), "nv"))
+    assert_product(y[-last:, -channels:], A @ W.T, A.abs() @ W.abs().T, K)
+    check_status()
+    del y, codes, scales, steps
+    want = fq.rmsnorm_quantize_act(tail, tail, None, 64, 8)
+    got = fq.rmsnorm_quantize_act(x, x, None, 64, 8, h=x)
+    assert got[0].data_ptr() == x.data_ptr()
+    assert torch.equal(x[-last:], want[0]) and torch.equal(got[1][-last:], want[1])
+    check_status()
