@@ -423,10 +423,8 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             }
         };
         // Outputs of chunk i, token-major, through one of the warp's buffers, which a bulk store reads; it clips what lies past M or N.
-        // A quadrant past the last channel stores nothing and takes no buffer: the waits count stores, one to a buffer.
         int stores = 0;
         auto emit = [&](const uint32_t* r, int i, int64_t t0, int64_t jq) {
-            if (jq >= p.N) return;                       // (warp-uniform)
             if ((i & 1) == 0 || SPLIT) {
                 float st = step2[0];
 #pragma unroll
@@ -462,8 +460,8 @@ gemm_fp4_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant
             }
             fence_proxy_async_smem();
             __syncwarp();
-            if (elect_one()) {
-                tma_store_2d(&map_y, (int)(jq * (p.bf16 ? 2 : 4)), (int)tc, buf);
+            if (elect_one()) {                               // (a group for every buffer taken, past N an empty one: the waits count them)
+                if (jq < p.N) tma_store_2d(&map_y, (int)(jq * (p.bf16 ? 2 : 4)), (int)tc, buf);
                 bulk_commit();
             }
             __syncwarp();
