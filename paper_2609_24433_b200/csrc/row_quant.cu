@@ -226,8 +226,9 @@ __global__ void __launch_bounds__(CACHE ? 512 : 1024) row_quantize_kernel(const 
                 if (NORM && t_in_row < 32) total = warp_sum(t.y);
             }
         }
-        // 1 / rms of the row, for its first warp (-1: the step is written already)
+        // 1 / rms of the row, for its first warp, or (wide) the step behind the norm
         float rinv = 1.0f;
+        bool wide = false;
         if (NORM && t_in_row < 32) {
             if (row < p.rows && squares_leave_range(total, m, p.eps)) {
                 // squares out of binary32's range: the row once more, in binary64 (the stream was written ahead of the barrier;
@@ -240,8 +241,8 @@ __global__ void __launch_bounds__(CACHE ? 512 : 1024) row_quantize_kernel(const 
                     s += e * e;
                 }
                 for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                if (lane == 0) p.delta[row] = wide_step<FMT>(m, p.clip_ratio, s, p.K, p.eps);
-                rinv = -1.0f;
+                rinv = wide_step<FMT>(m, p.clip_ratio, s, p.K, p.eps);
+                wide = true;
             } else {
                 rinv = inverse_rms(total, p.K, p.eps);
             }
@@ -292,7 +293,7 @@ __global__ void __launch_bounds__(CACHE ? 512 : 1024) row_quantize_kernel(const 
                 uint8_t* dst = p.codes + row * (int64_t)(p.K / 2) + col0 / 2;
                 if (E == 16) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
                 else *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2 % (E / 8)], w[3 % (E / 8)]);
-                if (t_in_row == 0 && !(NORM && rinv < 0.0f)) p.delta[row] = NORM ? __fmul_rn(d, rinv) : d;
+                if (t_in_row == 0) p.delta[row] = NORM ? (wide ? rinv : __fmul_rn(d, rinv)) : d;
             }
         } else {
             float inv;
@@ -323,7 +324,7 @@ __global__ void __launch_bounds__(CACHE ? 512 : 1024) row_quantize_kernel(const 
                     for (int j = 0; j < kWords / 4; ++j)
                         reinterpret_cast<uint4*>(dst)[j] = make_uint4(w[4 * j], w[(4 * j + 1) % kWords], w[(4 * j + 2) % kWords], w[(4 * j + 3) % kWords]);
                 }
-                if (t_in_row == 0 && !(NORM && rinv < 0.0f)) p.delta[row] = NORM ? __fmul_rn(d, rinv) : d;
+                if (t_in_row == 0) p.delta[row] = NORM ? (wide ? rinv : __fmul_rn(d, rinv)) : d;
             }
         }
     }
