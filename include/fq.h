@@ -437,7 +437,7 @@ size_t fq_cross_attention_workspace_bytes(fq_dtype dt, int64_t q_rows, int q_hea
  * A row's value is code * scale * step.
  * Quantiser, for a transformed row z (z = R S^-1 x in binary32 as for fq_quantize_act), each line binary32 operations rounded to nearest:
  *   FQ_MXFP4  m = max |z| of the block, E = max(0, exponent of m - 2) with the exponent field of binary32, code = e2m1(z 2^(127-E)), step 1;
- *   FQ_NVFP4  step d = max |z| of the row * fl(1/2688) (6 * 448; a row with d < 2^-100 is the zero token: step, scales and codes 0), i = 1/d,
+ *   FQ_NVFP4  step d = max |z| of the row * fl(1/2688) (6 * 448; a row with d < 2^-100 is the zero token: step and scales 0, codes zeros), i = 1/d,
  *             S = e4m3((m i) * fl(1/6)), q = i/S (0 where S = 0), code = e2m1(z q);
  * e2m1 and e4m3 round to nearest, ties to even, and saturate; a zero keeps its sign.
  * K a multiple of 32, at most 32768; hadamard_block a power of two in [1, 256] dividing K; N a multiple of 8, at most 2^28; rows of a

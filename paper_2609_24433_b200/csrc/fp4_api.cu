@@ -9,7 +9,7 @@ using namespace fq;
 
 namespace {
 
-constexpr int64_t kMaxRowK = 32768;              // a row lies in the registers of one thread block
+constexpr int64_t kMaxRowK = 32768;              // one thread block works on a row: 1024 threads of 32 channels
 constexpr int64_t kMaxRows = 0x7fff0000;         // rows of one call (indexes of tiles are 32-bit)
 constexpr int64_t kMaxN = 1ll << 28;             // channels of one handle
 

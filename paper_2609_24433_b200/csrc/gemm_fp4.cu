@@ -592,10 +592,12 @@ struct Plan {
 size_t split_bytes(int bt, int split) { return (size_t)(split - 1) * ((bt / 16 + split - 1) / split) * 8192; }
 // Tiles (single CTAs of 128 channels x 64, 128 or 256 tokens, or all of them where there are few; pairs of 256 x 256) and slices of K
 // by the time that they are expected to take, in us: so many waves of (stages of a slice, epilogue), and what the slices' exchange
-// adds.  The constants are those of the launches below; measured, the choice against the next best:
-//   1 x 2048 x 2560 two slices 4.8 (one 5.0, four 5.1), 1 x 16384 x 2048 four 8.7 (two 13.2), 1 x 1024 x 4096 one 3.8 (two 4.1),
-//   333 x 1120 x 1000 tiles of 64 tokens 5.0 (128: 6.0), 816 x 2048 x 2560 128 tokens 7.4 (pairs 9.1), 816 x 16384 x 2048 pairs in two
-//   slices 19.7 (one 28.6), 816 x 2048 x 32768 pairs 37.0 (single CTAs 39.8).
+// adds.  The constants were fitted to the launches below, with an epilogue of eight warps everywhere; with today's, about a tenth faster, the
+// order is the same.  Measured with it, the choice against the next best (M x K x N, us):
+//   1 x 2048 x 2560 two slices 4.4 (four 4.7, one 4.8), 1 x 16384 x 2048 four 8.3 (two 12.8, eight 14.0), 1 x 1024 x 4096 one 3.7 (two 3.8),
+//   333 x 1120 x 1000 tiles of 64 tokens 5.2 (128: 6.1), 512 x 4096 x 4096 128 tokens 9.6 (pairs 10.8), 816 x 2048 x 2560 128 tokens 6.8
+//   (pairs 7.9), 816 x 16384 x 2048 pairs in two slices 18.6 (128 tokens 21.8, pairs in one 24.9), 2048 x 4096 x 4096 pairs 18.9 (single
+//   CTAs of 256 tokens 21.7), 816 x 2048 x 32768 pairs 33.8 (37.2), 16384 x 8192 x 8192 pairs 422 (488).
 Plan plan(int64_t M, int64_t N, int64_t K, int (*held)(int)) {
     const int sms = device_sm_count();
     const int64_t kb = (K + kStageK - 1) / kStageK;
@@ -684,7 +686,9 @@ fq_status launch_planned(const uint8_t* codes, const uint8_t* scales, const floa
         const int most = slots < kMostStages ? slots : kMostStages;
         return (int)(bytes / stage) < most ? (int)(bytes / stage) : most;
     };
-    // received sums beside the stages where at least five are left, else in their place (96 KB of them at most: two stages hold more)
+    // received sums beside the stages where at least five are left, else in their place (112 KB at most, of single CTAs with 256 tokens
+    // in eight slices: their three stages hold more, as do all others')
+    static_assert(7 * 2 * 8192 <= 3 * (kRows * 128 + 256 * 128 + 2 * 512 * 3), "received sums fit where the stages were");
     const size_t sums = split_bytes(r.bt, r.split);
     p.stages = fit(kRingMost);
     p.per = (r.bt / 16 + r.split - 1) / r.split;
@@ -694,7 +698,6 @@ fq_status launch_planned(const uint8_t* codes, const uint8_t* scales, const floa
         if (!p.shared_ring) p.stages = beside;
     }
     p.ring = (uint32_t)(stage * (size_t)p.stages);
-    if (p.shared_ring && p.ring < sums) p.ring = (uint32_t)sums;
     const size_t smem = 1024 + p.ring + kOutBytes + (p.shared_ring ? 0 : sums);
     Maps maps;
     if (!code_map(&maps.x, codes, M, W.K, r.bt / r.ctas) || !scale_map(&maps.xs, scales, M, W.K, W.format, xa)) return FQ_ERR_CUDA;

@@ -571,7 +571,9 @@ def _multiplier(mult_g, x: torch.Tensor, hadamard_block: int):
 
 
 def quantize_act_fp4(x: torch.Tensor, mult_g, hadamard_block: int, format: int = NVFP4, codes=None, scales=None, delta=None):
-    """(codes u8 [M, K/2], block scales u8 in tiles, steps [M]).  ``mult_g``: device float tensor, a handle (its multiplier) or None."""
+    """(codes u8 [M, K/2], block scales u8 in tiles, steps [M]).  ``mult_g``: device float tensor, a handle of this block (its multiplier)
+    or None.  Outputs that are not passed in lie in one allocation, here and in the norms below: a reference to one keeps all of
+    them, and to save one alone takes a clone of it."""
     return _result(_native().quantize_act_fp4(x, _multiplier(mult_g, x, hadamard_block), hadamard_block, format, codes, scales, delta),
                    "fq_quantize_act_fp4")
 
@@ -590,7 +592,7 @@ def linear_fp4(x: torch.Tensor, W: Fp4Weights, out_dtype=torch.float32, y=None, 
 def rmsnorm_quantize_act(x: torch.Tensor, residual: Optional[torch.Tensor], mult_g, hadamard_block: int, bits: int, eps: float = 1e-6,
                          clip_ratio: float = 1.0, h=None, codes=None, delta=None):
     """(h, codes u8 [M, K*bits/8], steps [M]): h = x + residual (x itself without one) and the codes of h / rms(h) for a site whose
-    multiplier is ``mult_g`` (device float tensor, a Weights or None)."""
+    multiplier is ``mult_g`` (device float tensor, a handle of this block or None)."""
     return _result(_native().rmsnorm_quantize_act(x, residual, _multiplier(mult_g, x, hadamard_block), hadamard_block, bits, eps, clip_ratio, h, codes, delta),
                    "fq_rmsnorm_quantize_act")
 
