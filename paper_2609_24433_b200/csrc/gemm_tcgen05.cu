@@ -824,7 +824,7 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 const uint32_t off_a = tok * 64u + ((ch ^ ((tok >> 1) & 3u)) << 4);
                 const uint32_t off_b = tok * 64u + (((ch + 2u) ^ ((tok >> 1) & 3u)) << 4);
                 const uint32_t buf0 = smem_e + (uint32_t)(warp - 2) * kEpiBytes;
-                const bool any_channel = jq < p.N;        // warp-uniform
+                const int64_t rows = jq < p.N ? p.M : 0;  // (warp-uniform: past N nothing is stored and no buffer is taken)
                 if (!ahead) request_constants();
                 // The accumulators and steps of a chunk are requested as soon as the chunk before it has been handed to the copy
                 // engine.
@@ -836,7 +836,7 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 if (half * 16 < p.bt && t0 + half * 16 < p.M) request(half * 16);
                 for (int c = half * 16; c < p.bt; c += 16 * kEpiSets) {
                     const int64_t tc = t0 + c;
-                    if (tc >= p.M) break;                // tokens beyond M: nothing to store (warp-uniform)
+                    if (tc >= rows) break;               // tokens beyond M: nothing to store (warp-uniform)
                     tmem_ld_wait();
                     uint32_t ra[8], rb[8];
 #pragma unroll
@@ -859,8 +859,8 @@ gemm_tcgen05_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                     stmatrix_x4_trans(buf + off_b, wb0, wb1, wb2, wb3);
                     fence_proxy_async_smem();            // the buffer, written through the generic proxy, is read by the copy engine
                     __syncwarp();
-                    if (lane == 0) {                     // (a group for every buffer taken, past N an empty one: the wait counts them)
-                        if (any_channel) tma_store_2d(&map_y, (int)jq * 2, (int)tc, buf);   // the output map counts bytes along a row
+                    if (lane == 0) {
+                        tma_store_2d(&map_y, (int)jq * 2, (int)tc, buf);   // the output map counts bytes along a row
                         bulk_commit();
                     }
                     ++store_use;
